@@ -403,6 +403,67 @@ double lcma_predict_seconds(int scheme_id, int64_t M, int64_t N, int64_t K, lcma
  */
 lcma_status lcma_set_tuning(const char *key, const char *value);
 
+/* ------------------------------------------------------------------ 8-bit integers: a scale for each token and each channel
+ * The linear layer in 8-bit integers: activations quantised row by row when they arrive (dynamic, symmetric), weights held as
+ * codes with a scale for each output channel:
+ *   C[m][n] = Sa[m] * Sw[n] * sum_k Aq[m][k] * Wq[n][k]  (+ bias[n])
+ * The sum is exact (32-bit integers); it is scaled in fp32 and rounded once to the type of C.
+ * Code matrices are int8, row-major and k-contiguous with a row pitch of lcma_i8_code_pitch(K) bytes; columns from K on have to
+ * hold zeros (lcma_i8_quantize writes them).  Scales and bias are fp32.  Code matrices are 16-byte aligned; X and C need the alignment of
+ * their elements only, and any leading dimension that holds a row.  N and the number of rows are free; K is at most 131071 (SHAPE).
+ * Outputs must not overlap inputs (ARG).  All calls run on `stream`, allocate nothing and do not synchronise.
+ *
+ * lcma_i8_code_pitch: K rounded up to 128 (0 for K = 0); -1 for a negative K.
+ * lcma_i8_quantize: row by row amax = max |x|, S = amax / 127, Q = rint(x * (127 / amax)) with ties to even, in fp32.  A row of zeros has
+ * S = 0 and codes 0.  A row that holds an infinity or a NaN has codes 0 and S = infinity or NaN: its products are NaN.
+ * gated != 0: a row of X is 2 K long and x[k] = silu(X[k]) * X[K + k], silu(g) = g / (1 + exp(-g)).
+ * Weights N x K are quantised by the same call (their rows are the channels).
+ */
+int64_t lcma_i8_code_pitch(int64_t K);
+lcma_status lcma_i8_quantize(int64_t rows, int64_t K, const void *X, int64_t ldx, lcma_dtype dtype, int gated, void *Q, float *S, void *stream);
+/* The rows of tokens quantised into expert order: row position[t * top_k + j] of Q and S is token t's, for every j.  Rows of slots
+ * without an expert (position < 0, see lcma_tokens_sort) are not written; the product over experts does not read them. */
+lcma_status lcma_i8_quantize_dispatch(int64_t tokens, int64_t K, const void *X, int64_t ldx, lcma_dtype dtype, int top_k, const int32_t *position,
+                                      void *Q, float *S, void *stream);
+/* bias may be null.  K = 0: C = bias, or zeros. */
+lcma_status lcma_i8_gemm_nt(int64_t M, int64_t N, int64_t K, const void *Aq, const float *Sa, const void *Wq, const float *Sw, const float *bias,
+                            void *C, int64_t ldc, lcma_dtype dtype, void *stream);
+/* The product over experts: rows offsets[e] .. offsets[e + 1] - 1 of A times the weights of expert e.  Wq: experts x N x K codes, Sw and bias
+ * (may be null): experts x N.  offsets: experts + 1 row numbers on the device, ascending from 0, as lcma_tokens_sort writes them.
+ * Rows of C from offsets[experts] on are set to zero.  1 to 1024 experts. */
+lcma_status lcma_i8_gemm_experts(int64_t rows, int64_t N, int64_t K, int experts, const int32_t *offsets, const void *Aq, const float *Sa,
+                                 const void *Wq, const float *Sw, const float *bias, void *C, int64_t ldc, lcma_dtype dtype, void *stream);
+
+/* ------------------------------------------------------------------ tokens sorted by expert and back
+ * A slot is one of the top_k experts of a token, slot t * top_k + j.  lcma_tokens_sort puts the slots in expert order: by expert number, and
+ * by slot number within an expert.  A slot whose number is none of 0 .. experts - 1 has no expert (padding tokens, experts elsewhere);
+ * these follow behind all others, in slot order.
+ *   order[row]       the slot that row `row` of the expert order belongs to              (tokens * top_k)
+ *   position[slot]   its row; -1 - row for a slot without an expert                      (tokens x top_k)
+ *   offsets[e]       first row of expert e; offsets[experts] rows have an expert         (experts + 1)
+ * All are int32 on the device.  1 to 1024 experts, tokens * top_k below 2^31 (SHAPE).  workspace: device memory, 4-byte aligned, of at least
+ * lcma_tokens_sort_workspace_bytes bytes (0 for few slots: it may be null then); -1: sizes out of range.
+ *
+ * The calls that move rows take X, Y in the storage type `dtype` (H elements a row, any H, leading dimension and alignment of an element) and
+ * weights in fp32 (tokens x top_k).  Rows of slots without an expert are written as zeros and never read.  Sums run in fp32, j ascending, and
+ * are rounded once.
+ *   lcma_tokens_dispatch       Y[position[t][j]] = X[t]
+ *   lcma_tokens_combine        X[t] = sum_j weights[t][j] * Y[position[t][j]]; weights null: ones.  Without weights it is the
+ *                              gradient of lcma_tokens_dispatch.
+ *   lcma_tokens_combine_grad   the gradient of lcma_tokens_combine, from that of its result: dY[position[t][j]] = weights[t][j] * dX[t] and
+ *                              dweights[t][j] = sum_h dX[t][h] * Y[position[t][j]][h] (0 for a slot without an expert)
+ */
+int64_t lcma_tokens_sort_workspace_bytes(int64_t tokens, int top_k, int experts);
+lcma_status lcma_tokens_sort(int64_t tokens, int top_k, int experts, const int32_t *ids, int32_t *order, int32_t *position, int32_t *offsets,
+                             void *workspace, int64_t workspace_bytes, void *stream);
+lcma_status lcma_tokens_dispatch(int64_t tokens, int top_k, int64_t H, const void *X, int64_t ldx, lcma_dtype dtype, const int32_t *position,
+                                 void *Y, int64_t ldy, void *stream);
+lcma_status lcma_tokens_combine(int64_t tokens, int top_k, int64_t H, const void *Y, int64_t ldy, lcma_dtype dtype, const int32_t *position,
+                                const float *weights, void *X, int64_t ldx, void *stream);
+lcma_status lcma_tokens_combine_grad(int64_t tokens, int top_k, int64_t H, const void *dX, int64_t lddx, const void *Y, int64_t ldy,
+                                     lcma_dtype dtype, const int32_t *position, const float *weights, void *dY, int64_t lddy, float *dweights,
+                                     void *stream);
+
 /* ------------------------------------------------------------------ tile scheduling (Sec. 3.2, Split-Group Parallelism)
  * Wave counts for `groups` groups of R tile-products on `units` compute units:
  * tile-level scheduling needs ceil(groups*R/units) waves, group-level ceil(groups/units)*R.

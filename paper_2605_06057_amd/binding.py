@@ -33,6 +33,8 @@ EXPORTS = [
     "lcma_static_scratch_bytes", "lcma_gemm_unfused_static", "lcma_split_group_scratch_bytes", "lcma_gemm_nt_ws", "lcma_gemm_ws", "lcma_fp16_range_flags", "lcma_mfma_probe",
     "lcma_fp8_code_pitch", "lcma_fp8_scale_pitch", "lcma_fp8_quantize", "lcma_fp8_gemm_nt", "lcma_fp8_prepared_w_bytes",
     "lcma_fp8_prepare_w", "lcma_fp8_workspace_bytes", "lcma_fp8_gemm_lcma",
+    "lcma_i8_code_pitch", "lcma_i8_quantize", "lcma_i8_quantize_dispatch", "lcma_i8_gemm_nt", "lcma_i8_gemm_experts",
+    "lcma_tokens_sort_workspace_bytes", "lcma_tokens_sort", "lcma_tokens_dispatch", "lcma_tokens_combine", "lcma_tokens_combine_grad",
 ]
 
 
@@ -133,6 +135,18 @@ def lib() -> ctypes.CDLL:
         L.lcma_fp8_workspace_bytes.argtypes = [vp, i64, i64, i64]
         L.lcma_fp8_workspace_bytes.restype = i64
         L.lcma_fp8_gemm_lcma.argtypes = [i64, i64, i64, vp, i64, vp, vp, i64, vp, vp, i64, vp]
+        L.lcma_i8_code_pitch.argtypes = [i64]
+        L.lcma_i8_code_pitch.restype = i64
+        L.lcma_i8_quantize.argtypes = [i64, i64, vp, i64, i32, i32, vp, vp, vp]
+        L.lcma_i8_quantize_dispatch.argtypes = [i64, i64, vp, i64, i32, i32, vp, vp, vp, vp]
+        L.lcma_i8_gemm_nt.argtypes = [i64, i64, i64, vp, vp, vp, vp, vp, vp, i64, i32, vp]
+        L.lcma_i8_gemm_experts.argtypes = [i64, i64, i64, i32, vp, vp, vp, vp, vp, vp, vp, i64, i32, vp]
+        L.lcma_tokens_sort_workspace_bytes.argtypes = [i64, i32, i32]
+        L.lcma_tokens_sort_workspace_bytes.restype = i64
+        L.lcma_tokens_sort.argtypes = [i64, i32, i32, vp, vp, vp, vp, vp, i64, vp]
+        L.lcma_tokens_dispatch.argtypes = [i64, i32, i64, vp, i64, i32, vp, vp, i64, vp]
+        L.lcma_tokens_combine.argtypes = [i64, i32, i64, vp, i64, i32, vp, vp, vp, i64, vp]
+        L.lcma_tokens_combine_grad.argtypes = [i64, i32, i64, vp, i64, vp, i64, i32, vp, vp, vp, i64, vp, vp]
         _lib = L
         # schemes that kernels were generated for beyond the paper's three
         for sid in range(4, int(L.lcma_scheme_id_max()) + 1):
@@ -506,6 +520,158 @@ def lcma_fp8_gemm_lcma(A, Wp, C, scheme: Scheme, workspace):
     _check(lib().lcma_fp8_gemm_lcma(M, N, K, A.data_ptr(), A.stride(0), Wp.data_ptr(), C.data_ptr(), C.stride(0),
                                     scheme.handle, workspace.data_ptr(), workspace.numel(), stream))
     return C
+
+
+# ---------------------------------------------------------------- 8-bit integers (a scale for each row of either operand)
+def _is(t, dtype, *shape) -> bool:
+    """Whether t is a contiguous device tensor of that type and shape."""
+    return t.is_cuda and t.dtype == dtype and t.shape == shape and t.is_contiguous()
+
+
+def _rows_of(t, rows: int, cols: int) -> bool:
+    """Whether t is a rows x cols device tensor with neighbouring elements in a row."""
+    return t.is_cuda and t.shape == (rows, cols) and (cols <= 1 or t.stride(1) == 1)
+
+
+def _ld(t) -> int:
+    """Leading dimension; that of a single row, whose stride says nothing, is the row."""
+    return max(t.stride(0), t.shape[1]) if t.shape[0] <= 1 else t.stride(0)
+
+
+def lcma_i8_code_pitch(K: int) -> int:
+    return int(lib().lcma_i8_code_pitch(K))
+
+
+def lcma_i8_quantize(X, Q=None, S=None, gated: bool = False):
+    """Codes (rows x code pitch, int8) and scales (rows, fp32) of the device tensor X (rows x K; gated: rows x 2 K, of
+    silu(first half) * second half)."""
+    import torch
+    assert X.dim() == 2 and not (gated and X.shape[1] % 2), "expected rows x K (gated: rows x 2 K)"
+    rows, K = X.shape[0], X.shape[1] // 2 if gated else X.shape[1]
+    pitch = lcma_i8_code_pitch(K)
+    if Q is None:
+        Q = torch.empty((rows, pitch), dtype=torch.int8, device=X.device)
+    if S is None:
+        S = torch.empty((rows,), dtype=torch.float32, device=X.device)
+    assert _rows_of(X, *X.shape) and _is(Q, torch.int8, rows, pitch) and _is(S, torch.float32, rows)
+    stream = _stream_of(X)
+    _check(lib().lcma_i8_quantize(rows, K, X.data_ptr(), _ld(X), _dtype_of(X), int(gated), Q.data_ptr(), S.data_ptr(), stream))
+    return Q, S
+
+
+def lcma_i8_quantize_dispatch(X, position, Q=None, S=None):
+    """lcma_i8_quantize of the tokens' rows X (tokens x K) into expert order: Q, S have a row for every slot of position (tokens x top_k)."""
+    import torch
+    tokens, K = X.shape
+    top_k = position.shape[1]
+    pitch = lcma_i8_code_pitch(K)
+    if Q is None:
+        Q = torch.empty((tokens * top_k, pitch), dtype=torch.int8, device=X.device)
+    if S is None:
+        S = torch.empty((tokens * top_k,), dtype=torch.float32, device=X.device)
+    assert _rows_of(X, tokens, K) and _is(position, torch.int32, tokens, top_k)
+    assert _is(Q, torch.int8, tokens * top_k, pitch) and _is(S, torch.float32, tokens * top_k)
+    stream = _stream_of(X)
+    _check(lib().lcma_i8_quantize_dispatch(tokens, K, X.data_ptr(), _ld(X), _dtype_of(X), top_k, position.data_ptr(), Q.data_ptr(), S.data_ptr(), stream))
+    return Q, S
+
+
+def lcma_i8_gemm_nt(Aq, Sa, Wq, Sw, C, K: int, bias=None):
+    """C (M x N) = the product of the codes Aq (M x pitch) and Wq (N x pitch) over K, times the scales of rows and channels, plus bias."""
+    import torch
+    M, N = C.shape
+    pitch = lcma_i8_code_pitch(K)
+    assert _is(Aq, torch.int8, M, pitch) and _is(Wq, torch.int8, N, pitch) and _is(Sa, torch.float32, M) and _is(Sw, torch.float32, N)
+    assert _rows_of(C, M, N) and (bias is None or _is(bias, torch.float32, N))
+    stream = _stream_of(C)
+    _check(lib().lcma_i8_gemm_nt(M, N, K, Aq.data_ptr(), Sa.data_ptr(), Wq.data_ptr(), Sw.data_ptr(), bias.data_ptr() if bias is not None else None,
+                                 C.data_ptr(), _ld(C), _dtype_of(C), stream))
+    return C
+
+
+def lcma_i8_gemm_experts(Aq, Sa, offsets, Wq, Sw, C, K: int, bias=None):
+    """lcma_i8_gemm_nt over experts: rows offsets[e] .. offsets[e + 1] - 1 times the weights Wq[e] (experts x N x pitch), Sw and bias experts x N;
+    rows of C behind the last expert's are set to zero."""
+    import torch
+    rows, N = C.shape
+    experts, pitch = Wq.shape[0], lcma_i8_code_pitch(K)
+    assert _is(Aq, torch.int8, rows, pitch) and _is(Wq, torch.int8, experts, N, pitch) and _is(Sa, torch.float32, rows)
+    assert _is(Sw, torch.float32, experts, N) and _is(offsets, torch.int32, experts + 1)
+    assert _rows_of(C, rows, N) and (bias is None or _is(bias, torch.float32, experts, N))
+    stream = _stream_of(C)
+    _check(lib().lcma_i8_gemm_experts(rows, N, K, experts, offsets.data_ptr(), Aq.data_ptr(), Sa.data_ptr(), Wq.data_ptr(), Sw.data_ptr(),
+                                      bias.data_ptr() if bias is not None else None, C.data_ptr(), _ld(C), _dtype_of(C), stream))
+    return C
+
+
+# ---------------------------------------------------------------- tokens sorted by expert and back
+def lcma_tokens_sort_workspace_bytes(tokens: int, top_k: int, experts: int) -> int:
+    return int(lib().lcma_tokens_sort_workspace_bytes(tokens, top_k, experts))
+
+
+def lcma_tokens_sort(ids, experts: int, order=None, position=None, offsets=None, workspace=None):
+    """order (tokens * top_k), position (tokens x top_k) and offsets (experts + 1), int32, of the slots of ids (tokens x top_k expert numbers,
+    int32); slots with another number than 0 .. experts - 1 come last, with a negative position."""
+    import torch
+    tokens, top_k = ids.shape
+    make = lambda *shape: torch.empty(shape, dtype=torch.int32, device=ids.device)
+    order = make(tokens * top_k) if order is None else order
+    position = make(tokens, top_k) if position is None else position
+    offsets = make(experts + 1) if offsets is None else offsets
+    if workspace is None and (need := lcma_tokens_sort_workspace_bytes(tokens, top_k, experts)) > 0:
+        workspace = torch.empty((need,), dtype=torch.uint8, device=ids.device)
+    assert _is(ids, torch.int32, tokens, top_k) and _is(order, torch.int32, tokens * top_k) and _is(position, torch.int32, tokens, top_k)
+    assert _is(offsets, torch.int32, experts + 1) and (workspace is None or (workspace.is_cuda and workspace.is_contiguous()))
+    stream = _stream_of(ids)
+    _check(lib().lcma_tokens_sort(tokens, top_k, experts, ids.data_ptr(), order.data_ptr(), position.data_ptr(), offsets.data_ptr(),
+                                  workspace.data_ptr() if workspace is not None else None,
+                                  workspace.numel() * workspace.element_size() if workspace is not None else 0, stream))
+    return order, position, offsets
+
+
+def lcma_tokens_dispatch(X, position, Y=None):
+    """Y[position[t, j]] = X[t]: the tokens' rows in expert order (rows of slots without an expert: zeros)."""
+    import torch
+    tokens, H = X.shape
+    top_k = position.shape[1]
+    if Y is None:
+        Y = torch.empty((tokens * top_k, H), dtype=X.dtype, device=X.device)
+    assert _rows_of(X, tokens, H) and _rows_of(Y, tokens * top_k, H) and X.dtype == Y.dtype and _is(position, torch.int32, tokens, top_k)
+    stream = _stream_of(X)
+    _check(lib().lcma_tokens_dispatch(tokens, top_k, H, X.data_ptr(), _ld(X), _dtype_of(X), position.data_ptr(), Y.data_ptr(), _ld(Y), stream))
+    return Y
+
+
+def lcma_tokens_combine(Y, position, weights=None, X=None):
+    """X[t] = sum over j of weights[t, j] * Y[position[t, j]] (weights None: ones, which is the gradient of lcma_tokens_dispatch)."""
+    import torch
+    tokens, top_k = position.shape
+    H = Y.shape[1]
+    if X is None:
+        X = torch.empty((tokens, H), dtype=Y.dtype, device=Y.device)
+    assert _rows_of(Y, tokens * top_k, H) and _rows_of(X, tokens, H) and X.dtype == Y.dtype and _is(position, torch.int32, tokens, top_k)
+    assert weights is None or _is(weights, torch.float32, tokens, top_k)
+    stream = _stream_of(Y)
+    _check(lib().lcma_tokens_combine(tokens, top_k, H, Y.data_ptr(), _ld(Y), _dtype_of(Y), position.data_ptr(),
+                                     weights.data_ptr() if weights is not None else None, X.data_ptr(), _ld(X), stream))
+    return X
+
+
+def lcma_tokens_combine_grad(dX, Y, position, weights, dY=None, dweights=None):
+    """Gradient of lcma_tokens_combine from dX (tokens x H): dY (rows in expert order, in Y's type) and dweights (tokens x top_k, fp32)."""
+    import torch
+    tokens, top_k = position.shape
+    H = Y.shape[1]
+    if dY is None:
+        dY = torch.empty((tokens * top_k, H), dtype=Y.dtype, device=Y.device)
+    if dweights is None:
+        dweights = torch.empty((tokens, top_k), dtype=torch.float32, device=Y.device)
+    assert _rows_of(dX, tokens, H) and _rows_of(Y, tokens * top_k, H) and _rows_of(dY, tokens * top_k, H) and dX.dtype == Y.dtype == dY.dtype
+    assert _is(position, torch.int32, tokens, top_k) and _is(weights, torch.float32, tokens, top_k) and _is(dweights, torch.float32, tokens, top_k)
+    stream = _stream_of(Y)
+    _check(lib().lcma_tokens_combine_grad(tokens, top_k, H, dX.data_ptr(), _ld(dX), Y.data_ptr(), _ld(Y), _dtype_of(Y), position.data_ptr(),
+                                          weights.data_ptr(), dY.data_ptr(), _ld(dY), dweights.data_ptr(), stream))
+    return dY, dweights
 
 
 def lcma_set_tuning(key: str, value: str = ""):

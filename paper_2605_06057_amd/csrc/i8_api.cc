@@ -1,0 +1,121 @@
+// Host side of the 8-bit-integer linear layer, alone and over experts: argument checks, launches.
+#include "experts_host.h"
+
+#include <cstring>
+
+extern "C" int lcma_launch_i8_quantize(const lcma::I8QuantParams *p, int dtype, int gated, void *stream);
+extern "C" int lcma_launch_i8_gemm(const lcma::I8GemmParams *p, int dtype, int grid, void *stream);
+
+using namespace lcma;
+
+namespace {
+
+const int64_t kMostK = 131071; // 128 * 128 * K below 2^31
+
+int64_t pitch_of(int64_t K) { return (K + 127) / 128 * 128; }
+
+lcma_status quantize(const char *who, int64_t rows, int64_t K, const void *X, int64_t ldx, int dtype, bool gated, int top_k, const int32_t *position,
+                     void *Q, float *S, void *stream) {
+    const int es = dtype_size(dtype);
+    if (!es) return fail(LCMA_ERR_DTYPE, "%s: unknown dtype %d", who, dtype);
+    if (rows < 0 || K < 0) return fail(LCMA_ERR_ARG, "%s: negative size", who);
+    if (top_k < 1) return fail(LCMA_ERR_ARG, "%s: top_k = %d must be at least 1", who, top_k);
+    if (K > kMostK) return fail(LCMA_ERR_SHAPE, "%s: K = %lld is more than %lld", who, (long long)K, (long long)kMostK);
+    if (rows >= kRowLimit || rows * top_k >= kRowLimit) return fail(LCMA_ERR_SHAPE, "%s: 2^31 rows or more", who);
+    if (rows * 256 >= kGridLimit) return fail(LCMA_ERR_SHAPE, "%s: too many rows for a launch", who);
+    if (rows == 0) return LCMA_OK;
+    const int64_t width = gated ? 2 * K : K;
+    if (!S || (K && (!X || !Q))) return fail(LCMA_ERR_ARG, "%s: null pointer", who);
+    if (ldx < width) return fail(LCMA_ERR_ARG, "%s: leading dimension smaller than the row", who);
+    if (ldx >= kPitchLimit) return fail(LCMA_ERR_SHAPE, "%s: leading dimension of 2^29 or more", who);
+    if ((uintptr_t)X % es || ((uintptr_t)Q & 15) || ((uintptr_t)S & 3) || ((uintptr_t)position & 3))
+        return fail(LCMA_ERR_ARG, "%s: X must have the alignment of its elements, Q 16-byte and S 4-byte alignment", who);
+    const int64_t to = rows * top_k, x_bytes = ((rows - 1) * ldx + width) * es, q_bytes = to * pitch_of(K);
+    if (touch(Q, q_bytes, X, x_bytes) || touch(S, to * 4, X, x_bytes) || touch(Q, q_bytes, S, to * 4) ||
+        (position && (touch(Q, q_bytes, position, to * 4) || touch(S, to * 4, position, to * 4))))
+        return fail(LCMA_ERR_ARG, "%s: an output overlaps another operand", who);
+    I8QuantParams p;
+    std::memset(&p, 0, sizeof p);
+    p.X = X;
+    p.Q = (int8_t *)Q;
+    p.S = S;
+    p.position = position;
+    p.ldx_b = ldx * es;
+    p.rows = (int32_t)rows;
+    p.K = (int32_t)K;
+    p.pitch = (int32_t)pitch_of(K);
+    p.top_k = top_k;
+    if (const int err = lcma_launch_i8_quantize(&p, dtype, gated, stream)) return fail(LCMA_ERR_HIP, "%s: launch failed with HIP error %d", who, err);
+    return LCMA_OK;
+}
+
+lcma_status gemm(const char *who, int64_t rows, int64_t N, int64_t K, int experts, const int32_t *offsets, const void *Aq, const float *Sa,
+                 const void *Wq, const float *Sw, const float *bias, void *C, int64_t ldc, int dtype, void *stream) {
+    const int es = dtype_size(dtype);
+    if (!es) return fail(LCMA_ERR_DTYPE, "%s: unknown dtype %d", who, dtype);
+    if (rows < 0 || N < 0 || K < 0) return fail(LCMA_ERR_ARG, "%s: negative size", who);
+    if (K > kMostK) return fail(LCMA_ERR_SHAPE, "%s: K = %lld is more than %lld", who, (long long)K, (long long)kMostK);
+    if (rows >= kRowLimit || N >= kRowLimit) return fail(LCMA_ERR_SHAPE, "%s: 2^31 rows or columns or more", who);
+    if (rows == 0 || N == 0) return LCMA_OK;
+    if (!Sa || !Sw || !C || (K && (!Aq || !Wq))) return fail(LCMA_ERR_ARG, "%s: null pointer", who);
+    if (ldc < N) return fail(LCMA_ERR_ARG, "%s: leading dimension smaller than the row", who);
+    if (ldc >= kPitchLimit) return fail(LCMA_ERR_SHAPE, "%s: leading dimension of 2^29 or more", who);
+    if ((((uintptr_t)Aq | (uintptr_t)Wq) & 15) || (((uintptr_t)Sa | (uintptr_t)Sw | (uintptr_t)bias | (uintptr_t)offsets) & 3) || (uintptr_t)C % es)
+        return fail(LCMA_ERR_ARG, "%s: code matrices must be 16-byte aligned, scales, bias and offsets 4-byte aligned, C as its elements", who);
+    const int64_t pitch = pitch_of(K), channels = experts * N, c_bytes = ((rows - 1) * ldc + N) * es;
+    if (touch(C, c_bytes, Aq, rows * pitch) || touch(C, c_bytes, Wq, channels * pitch) || touch(C, c_bytes, Sa, rows * 4) ||
+        touch(C, c_bytes, Sw, channels * 4) || (bias && touch(C, c_bytes, bias, channels * 4)) || (offsets && touch(C, c_bytes, offsets, (experts + 1) * 4)))
+        return fail(LCMA_ERR_ARG, "%s: C overlaps an operand", who);
+    I8GemmParams p;
+    std::memset(&p, 0, sizeof p);
+    p.A = (const int8_t *)Aq;
+    p.W = (const int8_t *)Wq;
+    p.SA = Sa;
+    p.SW = Sw;
+    p.bias = bias;
+    p.C = C;
+    p.offsets = offsets;
+    p.ldc = ldc;
+    p.rows = (int32_t)rows;
+    p.N = (int32_t)N;
+    p.pitch = (int32_t)pitch;
+    p.experts = experts;
+    p.steps = (int32_t)(pitch / 128);
+    const int64_t tile = 64, nz = (N + tile - 1) / tile;
+    // every group, and the rows behind the groups, may end in a tile of its own that is not full
+    const int64_t nx = offsets ? rows / tile + (rows < experts + 1 ? rows : experts + 1) : (rows + tile - 1) / tile;
+    if ((nx * nz + 8) * 256 >= kGridLimit) return fail(LCMA_ERR_SHAPE, "%s: too many tiles for a launch", who);
+    p.nz = (int32_t)nz;
+    p.panel = 8;
+    if (const int err = lcma_launch_i8_gemm(&p, dtype, (int)((nx * nz + 7) / 8 * 8), stream))
+        return fail(LCMA_ERR_HIP, "%s: launch failed with HIP error %d", who, err);
+    return LCMA_OK;
+}
+
+} // namespace
+
+extern "C" int64_t lcma_i8_code_pitch(int64_t K) { return K < 0 ? -1 : pitch_of(K); }
+
+extern "C" lcma_status lcma_i8_quantize(int64_t rows, int64_t K, const void *X, int64_t ldx, lcma_dtype dtype, int gated, void *Q, float *S, void *stream) {
+    return quantize("lcma_i8_quantize", rows, K, X, ldx, dtype, gated != 0, 1, nullptr, Q, S, stream);
+}
+
+extern "C" lcma_status lcma_i8_quantize_dispatch(int64_t tokens, int64_t K, const void *X, int64_t ldx, lcma_dtype dtype, int top_k, const int32_t *position,
+                                                 void *Q, float *S, void *stream) {
+    if (tokens > 0 && !position) return fail(LCMA_ERR_ARG, "lcma_i8_quantize_dispatch: null pointer");
+    return quantize("lcma_i8_quantize_dispatch", tokens, K, X, ldx, dtype, false, top_k, position, Q, S, stream);
+}
+
+extern "C" lcma_status lcma_i8_gemm_nt(int64_t M, int64_t N, int64_t K, const void *Aq, const float *Sa, const void *Wq, const float *Sw, const float *bias,
+                                       void *C, int64_t ldc, lcma_dtype dtype, void *stream) {
+    return gemm("lcma_i8_gemm_nt", M, N, K, 1, nullptr, Aq, Sa, Wq, Sw, bias, C, ldc, dtype, stream);
+}
+
+extern "C" lcma_status lcma_i8_gemm_experts(int64_t rows, int64_t N, int64_t K, int experts, const int32_t *offsets, const void *Aq, const float *Sa,
+                                            const void *Wq, const float *Sw, const float *bias, void *C, int64_t ldc, lcma_dtype dtype, void *stream) {
+    const char *who = "lcma_i8_gemm_experts";
+    if (experts < 1) return fail(LCMA_ERR_ARG, "%s: experts = %d must be at least 1", who, experts);
+    if (experts > kMaxExperts) return fail(LCMA_ERR_SHAPE, "%s: experts = %d is more than %d", who, experts, kMaxExperts);
+    if (rows > 0 && N > 0 && !offsets) return fail(LCMA_ERR_ARG, "%s: null pointer", who);
+    return gemm(who, rows, N, K, experts, offsets, Aq, Sa, Wq, Sw, bias, C, ldc, dtype, stream);
+}
