@@ -400,6 +400,9 @@ double lcma_predict_seconds(int scheme_id, int64_t M, int64_t N, int64_t K, lcma
  *                                                   Combine B, bit 2 the GEMM stage, bit 3 Combine H (default 15, all).  A stage
  *                                                   switched off leaves its output as an earlier call wrote it, so C is only
  *                                                   valid with all four on.
+ *   "i8_kernel"        LCMA_I8_KERNEL=<rows>x<cols> lcma_i8_gemm_nt and lcma_i8_gemm_experts run the kernel with tiles of that size: 16x16,
+ *                                                   32x32, 64x64, 64x128, 128x128, 128x256 or 256x256 (another value: default).  Their
+ *                                                   sums are exact, so this changes no result.
  */
 lcma_status lcma_set_tuning(const char *key, const char *value);
 

@@ -523,19 +523,37 @@ def lcma_fp8_gemm_lcma(A, Wp, C, scheme: Scheme, workspace):
 
 
 # ---------------------------------------------------------------- 8-bit integers (a scale for each row of either operand)
-def _is(t, dtype, *shape) -> bool:
-    """Whether t is a contiguous device tensor of that type and shape."""
-    return t.is_cuda and t.dtype == dtype and t.shape == shape and t.is_contiguous()
+_i8 = _i32 = _f32 = None  # torch's types, from the first use on
 
 
-def _rows_of(t, rows: int, cols: int) -> bool:
-    """Whether t is a rows x cols device tensor with neighbouring elements in a row."""
-    return t.is_cuda and t.shape == (rows, cols) and (cols <= 1 or t.stride(1) == 1)
+def _types():
+    """torch's int8, int32 and float32 (torch is imported with the first tensor, not with this file)."""
+    global _i8, _i32, _f32
+    if _i8 is None:
+        import torch
+        _i8, _i32, _f32 = torch.int8, torch.int32, torch.float32
+    return _i8, _i32, _f32
 
 
-def _ld(t) -> int:
+def _is(t, dtype, shape, device: int) -> bool:
+    """Whether t is a contiguous tensor of that type and shape on that GPU."""
+    return t.dtype is dtype and t.shape == shape and t.is_contiguous() and t.get_device() == device
+
+
+def _has(t, dtype, n: int, device: int) -> bool:
+    """Whether t is n values of that type, one behind the other, on that GPU (a third of the time that a shape takes to compare)."""
+    return t.dtype is dtype and t.numel() == n and t.is_contiguous() and t.get_device() == device
+
+
+def _rows_of(t, shape, device: int) -> bool:
+    """Whether t is a matrix of that shape on that GPU with neighbouring elements in a row."""
+    return t.shape == shape and (t.stride(1) == 1 or shape[1] <= 1) and t.get_device() == device
+
+
+def _ld(t, cols: int) -> int:
     """Leading dimension; that of a single row, whose stride says nothing, is the row."""
-    return max(t.stride(0), t.shape[1]) if t.shape[0] <= 1 else t.stride(0)
+    ld = t.stride(0)
+    return ld if ld >= cols or t.shape[0] > 1 else cols
 
 
 def lcma_i8_code_pitch(K: int) -> int:
@@ -545,62 +563,60 @@ def lcma_i8_code_pitch(K: int) -> int:
 def lcma_i8_quantize(X, Q=None, S=None, gated: bool = False):
     """Codes (rows x code pitch, int8) and scales (rows, fp32) of the device tensor X (rows x K; gated: rows x 2 K, of
     silu(first half) * second half)."""
-    import torch
-    assert X.dim() == 2 and not (gated and X.shape[1] % 2), "expected rows x K (gated: rows x 2 K)"
-    rows, K = X.shape[0], X.shape[1] // 2 if gated else X.shape[1]
-    pitch = lcma_i8_code_pitch(K)
+    i8, _, f32 = _types()
+    rows, width = shape = X.shape
+    assert not (gated and width % 2), "expected rows x 2 K"
+    K, device = width // 2 if gated else width, X.get_device()
+    pitch = (K + 127) // 128 * 128  # lcma_i8_code_pitch
     if Q is None:
-        Q = torch.empty((rows, pitch), dtype=torch.int8, device=X.device)
+        Q = X.new_empty((rows, pitch), dtype=i8)
     if S is None:
-        S = torch.empty((rows,), dtype=torch.float32, device=X.device)
-    assert _rows_of(X, *X.shape) and _is(Q, torch.int8, rows, pitch) and _is(S, torch.float32, rows)
-    stream = _stream_of(X)
-    _check(lib().lcma_i8_quantize(rows, K, X.data_ptr(), _ld(X), _dtype_of(X), int(gated), Q.data_ptr(), S.data_ptr(), stream))
+        S = X.new_empty((rows,), dtype=f32)
+    assert _rows_of(X, shape, device) and _is(Q, i8, (rows, pitch), device) and _has(S, f32, rows, device)
+    _check(lib().lcma_i8_quantize(rows, K, X.data_ptr(), _ld(X, width), _dtype_of(X), gated, Q.data_ptr(), S.data_ptr(), _stream_of(X)))
     return Q, S
 
 
 def lcma_i8_quantize_dispatch(X, position, Q=None, S=None):
     """lcma_i8_quantize of the tokens' rows X (tokens x K) into expert order: Q, S have a row for every slot of position (tokens x top_k)."""
-    import torch
-    tokens, K = X.shape
-    top_k = position.shape[1]
-    pitch = lcma_i8_code_pitch(K)
+    i8, i32, f32 = _types()
+    tokens, K = shape = X.shape
+    top_k, device = position.shape[1], X.get_device()
+    n, pitch = tokens * top_k, (K + 127) // 128 * 128  # lcma_i8_code_pitch
     if Q is None:
-        Q = torch.empty((tokens * top_k, pitch), dtype=torch.int8, device=X.device)
+        Q = X.new_empty((n, pitch), dtype=i8)
     if S is None:
-        S = torch.empty((tokens * top_k,), dtype=torch.float32, device=X.device)
-    assert _rows_of(X, tokens, K) and _is(position, torch.int32, tokens, top_k)
-    assert _is(Q, torch.int8, tokens * top_k, pitch) and _is(S, torch.float32, tokens * top_k)
-    stream = _stream_of(X)
-    _check(lib().lcma_i8_quantize_dispatch(tokens, K, X.data_ptr(), _ld(X), _dtype_of(X), top_k, position.data_ptr(), Q.data_ptr(), S.data_ptr(), stream))
+        S = X.new_empty((n,), dtype=f32)
+    assert _rows_of(X, shape, device) and _is(position, i32, (tokens, top_k), device)
+    assert _is(Q, i8, (n, pitch), device) and _has(S, f32, n, device)
+    _check(lib().lcma_i8_quantize_dispatch(tokens, K, X.data_ptr(), _ld(X, K), _dtype_of(X), top_k, position.data_ptr(), Q.data_ptr(), S.data_ptr(),
+                                           _stream_of(X)))
     return Q, S
 
 
 def lcma_i8_gemm_nt(Aq, Sa, Wq, Sw, C, K: int, bias=None):
     """C (M x N) = the product of the codes Aq (M x pitch) and Wq (N x pitch) over K, times the scales of rows and channels, plus bias."""
-    import torch
-    M, N = C.shape
-    pitch = lcma_i8_code_pitch(K)
-    assert _is(Aq, torch.int8, M, pitch) and _is(Wq, torch.int8, N, pitch) and _is(Sa, torch.float32, M) and _is(Sw, torch.float32, N)
-    assert _rows_of(C, M, N) and (bias is None or _is(bias, torch.float32, N))
-    stream = _stream_of(C)
-    _check(lib().lcma_i8_gemm_nt(M, N, K, Aq.data_ptr(), Sa.data_ptr(), Wq.data_ptr(), Sw.data_ptr(), bias.data_ptr() if bias is not None else None,
-                                 C.data_ptr(), _ld(C), _dtype_of(C), stream))
+    i8, _, f32 = _types()
+    M, N = shape = C.shape
+    pitch, device = (K + 127) // 128 * 128, C.get_device()  # lcma_i8_code_pitch
+    assert _is(Aq, i8, (M, pitch), device) and _is(Wq, i8, (N, pitch), device) and _has(Sa, f32, M, device) and _has(Sw, f32, N, device)
+    assert _rows_of(C, shape, device) and (bias is None or _has(bias, f32, N, device))
+    _check(lib().lcma_i8_gemm_nt(M, N, K, Aq.data_ptr(), Sa.data_ptr(), Wq.data_ptr(), Sw.data_ptr(), None if bias is None else bias.data_ptr(),
+                                 C.data_ptr(), _ld(C, N), _dtype_of(C), _stream_of(C)))
     return C
 
 
 def lcma_i8_gemm_experts(Aq, Sa, offsets, Wq, Sw, C, K: int, bias=None):
     """lcma_i8_gemm_nt over experts: rows offsets[e] .. offsets[e + 1] - 1 times the weights Wq[e] (experts x N x pitch), Sw and bias experts x N;
     rows of C behind the last expert's are set to zero."""
-    import torch
-    rows, N = C.shape
-    experts, pitch = Wq.shape[0], lcma_i8_code_pitch(K)
-    assert _is(Aq, torch.int8, rows, pitch) and _is(Wq, torch.int8, experts, N, pitch) and _is(Sa, torch.float32, rows)
-    assert _is(Sw, torch.float32, experts, N) and _is(offsets, torch.int32, experts + 1)
-    assert _rows_of(C, rows, N) and (bias is None or _is(bias, torch.float32, experts, N))
-    stream = _stream_of(C)
+    i8, i32, f32 = _types()
+    rows, N = shape = C.shape
+    experts, pitch, device = Wq.shape[0], (K + 127) // 128 * 128, C.get_device()  # lcma_i8_code_pitch
+    assert _is(Aq, i8, (rows, pitch), device) and _is(Wq, i8, (experts, N, pitch), device) and _has(Sa, f32, rows, device)
+    assert _is(Sw, f32, (experts, N), device) and _has(offsets, i32, experts + 1, device)
+    assert _rows_of(C, shape, device) and (bias is None or _is(bias, f32, (experts, N), device))
     _check(lib().lcma_i8_gemm_experts(rows, N, K, experts, offsets.data_ptr(), Aq.data_ptr(), Sa.data_ptr(), Wq.data_ptr(), Sw.data_ptr(),
-                                      bias.data_ptr() if bias is not None else None, C.data_ptr(), _ld(C), _dtype_of(C), stream))
+                                      None if bias is None else bias.data_ptr(), C.data_ptr(), _ld(C, N), _dtype_of(C), _stream_of(C)))
     return C
 
 
@@ -612,70 +628,72 @@ def lcma_tokens_sort_workspace_bytes(tokens: int, top_k: int, experts: int) -> i
 def lcma_tokens_sort(ids, experts: int, order=None, position=None, offsets=None, workspace=None):
     """order (tokens * top_k), position (tokens x top_k) and offsets (experts + 1), int32, of the slots of ids (tokens x top_k expert numbers,
     int32); slots with another number than 0 .. experts - 1 come last, with a negative position."""
-    import torch
-    tokens, top_k = ids.shape
-    make = lambda *shape: torch.empty(shape, dtype=torch.int32, device=ids.device)
-    order = make(tokens * top_k) if order is None else order
-    position = make(tokens, top_k) if position is None else position
-    offsets = make(experts + 1) if offsets is None else offsets
+    _, i32, _ = _types()
+    tokens, top_k = shape = ids.shape
+    n, device = tokens * top_k, ids.get_device()
+    if order is None:
+        order = ids.new_empty((n,))
+    if position is None:
+        position = ids.new_empty(shape)
+    if offsets is None:
+        offsets = ids.new_empty((experts + 1,))
     if workspace is None and (need := lcma_tokens_sort_workspace_bytes(tokens, top_k, experts)) > 0:
-        workspace = torch.empty((need,), dtype=torch.uint8, device=ids.device)
-    assert _is(ids, torch.int32, tokens, top_k) and _is(order, torch.int32, tokens * top_k) and _is(position, torch.int32, tokens, top_k)
-    assert _is(offsets, torch.int32, experts + 1) and (workspace is None or (workspace.is_cuda and workspace.is_contiguous()))
-    stream = _stream_of(ids)
-    _check(lib().lcma_tokens_sort(tokens, top_k, experts, ids.data_ptr(), order.data_ptr(), position.data_ptr(), offsets.data_ptr(),
-                                  workspace.data_ptr() if workspace is not None else None,
-                                  workspace.numel() * workspace.element_size() if workspace is not None else 0, stream))
+        workspace = ids.new_empty(((need + 3) // 4,))
+    space, size = None, 0
+    if workspace is not None:
+        assert workspace.is_contiguous() and workspace.get_device() == device
+        space, size = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    assert _is(ids, i32, shape, device) and _has(order, i32, n, device) and _is(position, i32, shape, device) and _has(offsets, i32, experts + 1, device)
+    _check(lib().lcma_tokens_sort(tokens, top_k, experts, ids.data_ptr(), order.data_ptr(), position.data_ptr(), offsets.data_ptr(), space, size,
+                                  _stream_of(ids)))
     return order, position, offsets
 
 
 def lcma_tokens_dispatch(X, position, Y=None):
     """Y[position[t, j]] = X[t]: the tokens' rows in expert order (rows of slots without an expert: zeros)."""
-    import torch
-    tokens, H = X.shape
-    top_k = position.shape[1]
+    _, i32, _ = _types()
+    tokens, H = shape = X.shape
+    top_k, device = position.shape[1], X.get_device()
     if Y is None:
-        Y = torch.empty((tokens * top_k, H), dtype=X.dtype, device=X.device)
-    assert _rows_of(X, tokens, H) and _rows_of(Y, tokens * top_k, H) and X.dtype == Y.dtype and _is(position, torch.int32, tokens, top_k)
-    stream = _stream_of(X)
-    _check(lib().lcma_tokens_dispatch(tokens, top_k, H, X.data_ptr(), _ld(X), _dtype_of(X), position.data_ptr(), Y.data_ptr(), _ld(Y), stream))
+        Y = X.new_empty((tokens * top_k, H))
+    assert _rows_of(X, shape, device) and _rows_of(Y, (tokens * top_k, H), device) and X.dtype is Y.dtype and _is(position, i32, (tokens, top_k), device)
+    _check(lib().lcma_tokens_dispatch(tokens, top_k, H, X.data_ptr(), _ld(X, H), _dtype_of(X), position.data_ptr(), Y.data_ptr(), _ld(Y, H), _stream_of(X)))
     return Y
 
 
 def lcma_tokens_combine(Y, position, weights=None, X=None):
     """X[t] = sum over j of weights[t, j] * Y[position[t, j]] (weights None: ones, which is the gradient of lcma_tokens_dispatch)."""
-    import torch
-    tokens, top_k = position.shape
-    H = Y.shape[1]
+    _, i32, f32 = _types()
+    tokens, top_k = slots = position.shape
+    H, device = Y.shape[1], Y.get_device()
     if X is None:
-        X = torch.empty((tokens, H), dtype=Y.dtype, device=Y.device)
-    assert _rows_of(Y, tokens * top_k, H) and _rows_of(X, tokens, H) and X.dtype == Y.dtype and _is(position, torch.int32, tokens, top_k)
-    assert weights is None or _is(weights, torch.float32, tokens, top_k)
-    stream = _stream_of(Y)
-    _check(lib().lcma_tokens_combine(tokens, top_k, H, Y.data_ptr(), _ld(Y), _dtype_of(Y), position.data_ptr(),
-                                     weights.data_ptr() if weights is not None else None, X.data_ptr(), _ld(X), stream))
+        X = Y.new_empty((tokens, H))
+    assert _rows_of(Y, (tokens * top_k, H), device) and _rows_of(X, (tokens, H), device) and X.dtype is Y.dtype and _is(position, i32, slots, device)
+    assert weights is None or _is(weights, f32, slots, device)
+    _check(lib().lcma_tokens_combine(tokens, top_k, H, Y.data_ptr(), _ld(Y, H), _dtype_of(Y), position.data_ptr(),
+                                     None if weights is None else weights.data_ptr(), X.data_ptr(), _ld(X, H), _stream_of(Y)))
     return X
 
 
 def lcma_tokens_combine_grad(dX, Y, position, weights, dY=None, dweights=None):
     """Gradient of lcma_tokens_combine from dX (tokens x H): dY (rows in expert order, in Y's type) and dweights (tokens x top_k, fp32)."""
-    import torch
-    tokens, top_k = position.shape
-    H = Y.shape[1]
+    _, i32, f32 = _types()
+    tokens, top_k = slots = position.shape
+    H, device = Y.shape[1], Y.get_device()
+    n = tokens * top_k
     if dY is None:
-        dY = torch.empty((tokens * top_k, H), dtype=Y.dtype, device=Y.device)
+        dY = Y.new_empty((n, H))
     if dweights is None:
-        dweights = torch.empty((tokens, top_k), dtype=torch.float32, device=Y.device)
-    assert _rows_of(dX, tokens, H) and _rows_of(Y, tokens * top_k, H) and _rows_of(dY, tokens * top_k, H) and dX.dtype == Y.dtype == dY.dtype
-    assert _is(position, torch.int32, tokens, top_k) and _is(weights, torch.float32, tokens, top_k) and _is(dweights, torch.float32, tokens, top_k)
-    stream = _stream_of(Y)
-    _check(lib().lcma_tokens_combine_grad(tokens, top_k, H, dX.data_ptr(), _ld(dX), Y.data_ptr(), _ld(Y), _dtype_of(Y), position.data_ptr(),
-                                          weights.data_ptr(), dY.data_ptr(), _ld(dY), dweights.data_ptr(), stream))
+        dweights = Y.new_empty(slots, dtype=f32)
+    assert _rows_of(dX, (tokens, H), device) and _rows_of(Y, (n, H), device) and _rows_of(dY, (n, H), device) and dX.dtype is Y.dtype is dY.dtype
+    assert _is(position, i32, slots, device) and _is(weights, f32, slots, device) and _is(dweights, f32, slots, device)
+    _check(lib().lcma_tokens_combine_grad(tokens, top_k, H, dX.data_ptr(), _ld(dX, H), Y.data_ptr(), _ld(Y, H), _dtype_of(Y), position.data_ptr(),
+                                          weights.data_ptr(), dY.data_ptr(), _ld(dY, H), dweights.data_ptr(), _stream_of(Y)))
     return dY, dweights
 
 
 def lcma_set_tuning(key: str, value: str = ""):
-    """Measurement aid: "variant", "unfused_variant", "panel" or "batch_order"; an empty value restores the default."""
+    """Measurement aid: "variant", "unfused_variant", "panel", "batch_order", "schedule", "unfused_stages" or "i8_kernel"; an empty value restores the default."""
     _check(lib().lcma_set_tuning(key.encode(), value.encode()))
 
 

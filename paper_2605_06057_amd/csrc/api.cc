@@ -1,5 +1,5 @@
 // C ABI entry points: argument checks, variant choice, kernel launch.
-#include "host_common.h"
+#include "experts_host.h"
 
 #include <algorithm>
 #include <atomic>
@@ -125,7 +125,7 @@ static const Variant *find_variant(const char *name) {
 // Measurement aids (see lcma_set_tuning): process-wide, initialised once from the environment, never read from it again.
 namespace {
 std::atomic<const Variant *> g_forced{nullptr}, g_forced_unfused{nullptr};
-std::atomic<int> g_panel{8}, g_batch_order{0}, g_schedule{0}, g_stages{15};
+std::atomic<int> g_panel{8}, g_batch_order{0}, g_schedule{0}, g_stages{15}, g_i8_kernel{-1};
 std::once_flag g_tuning_once;
 bool set_tuning(const char *key, const char *value) {
     const char *v = value ? value : "";
@@ -135,7 +135,11 @@ bool set_tuning(const char *key, const char *value) {
     else if (!std::strcmp(key, "batch_order")) g_batch_order = *v ? std::atoi(v) != 0 : 0;
     else if (!std::strcmp(key, "schedule")) g_schedule = !std::strcmp(v, "static") ? 1 : !std::strcmp(v, "split") ? 2 : !std::strcmp(v, "persist") ? 3 : !std::strcmp(v, "slices") ? 4 : 0;
     else if (!std::strcmp(key, "unfused_stages")) g_stages = *v ? (std::atoi(v) & 15) : 15;
-    else return false;
+    else if (!std::strcmp(key, "i8_kernel")) {
+        g_i8_kernel = -1;
+        for (int k = 0; k < kI8Kernels; ++k)
+            if (!std::strcmp(v, kI8KernelNames[k])) g_i8_kernel = k;
+    } else return false;
     return true;
 }
 void init_tuning() {
@@ -146,6 +150,7 @@ void init_tuning() {
         if (const char *e = std::getenv("LCMA_BATCH_ORDER")) set_tuning("batch_order", e);
         if (const char *e = std::getenv("LCMA_SCHEDULE")) set_tuning("schedule", e);
         if (const char *e = std::getenv("LCMA_UNFUSED_STAGES")) set_tuning("unfused_stages", e);
+        if (const char *e = std::getenv("LCMA_I8_KERNEL")) set_tuning("i8_kernel", e);
     });
 }
 } // namespace
@@ -155,6 +160,7 @@ int tuning_panel() { init_tuning(); return g_panel.load(); }
 int tuning_batch_order() { init_tuning(); return g_batch_order.load(); }
 int tuning_schedule() { init_tuning(); return g_schedule.load(); }
 int tuning_unfused_stages() { init_tuning(); return g_stages.load(); }
+int tuning_i8_kernel() { init_tuning(); return g_i8_kernel.load(); }
 
 // [p, p + bytes) and [q, q + qbytes) share a byte
 static bool overlap(const void *p, int64_t bytes, const void *q, int64_t qbytes) {

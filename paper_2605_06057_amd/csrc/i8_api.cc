@@ -4,7 +4,7 @@
 #include <cstring>
 
 extern "C" int lcma_launch_i8_quantize(const lcma::I8QuantParams *p, int dtype, int gated, void *stream);
-extern "C" int lcma_launch_i8_gemm(const lcma::I8GemmParams *p, int dtype, int grid, void *stream);
+extern "C" int lcma_launch_i8_gemm(const lcma::I8GemmParams *p, int kernel, int dtype, int grid, void *stream);
 
 using namespace lcma;
 
@@ -49,6 +49,19 @@ lcma_status quantize(const char *who, int64_t rows, int64_t K, const void *X, in
     return LCMA_OK;
 }
 
+// The kernel for rows x N over `experts` groups.  Few rows for each: the weights are read once, K is split between waves; then the larger the
+// tile, the fewer bytes travel into LDS, and the fewer work-groups there are.
+const struct { int rows, cols; } kTile[] = {{16, 16}, {32, 32}, {64, 64}, {64, 128}, {128, 128}, {128, 256}, {256, 256}};
+int pick(int64_t rows, int64_t N, int experts) {
+    const int64_t r = (rows + experts - 1) / experts;
+    auto tiles = [&](int k) { return (r + kTile[k].rows - 1) / kTile[k].rows * experts * ((N + kTile[k].cols - 1) / kTile[k].cols); };
+    if (r <= 16) return kI8Few16;
+    if (tiles(kI8Ring64) < 192) return kI8Few32;
+    if (tiles(kI8Ring64) < 768) return kI8Ring64;
+    if (tiles(kI8PingPong) >= 128 && r >= 80) return kI8PingPong;
+    return tiles(kI8Ring128) >= 192 && r > 64 ? kI8Ring128 : kI8Ring64x128;
+}
+
 lcma_status gemm(const char *who, int64_t rows, int64_t N, int64_t K, int experts, const int32_t *offsets, const void *Aq, const float *Sa,
                  const void *Wq, const float *Sw, const float *bias, void *C, int64_t ldc, int dtype, void *stream) {
     const int es = dtype_size(dtype);
@@ -81,13 +94,15 @@ lcma_status gemm(const char *who, int64_t rows, int64_t N, int64_t K, int expert
     p.pitch = (int32_t)pitch;
     p.experts = experts;
     p.steps = (int32_t)(pitch / 128);
-    const int64_t tile = 64, nz = (N + tile - 1) / tile;
-    // every group, and the rows behind the groups, may end in a tile of its own that is not full
-    const int64_t nx = offsets ? rows / tile + (rows < experts + 1 ? rows : experts + 1) : (rows + tile - 1) / tile;
-    if ((nx * nz + 8) * 256 >= kGridLimit) return fail(LCMA_ERR_SHAPE, "%s: too many tiles for a launch", who);
+    const int forced = tuning_i8_kernel(), kernel = K == 0 ? kI8Ring64 : forced >= 0 ? forced : pick(rows, N, experts);
+    const int64_t tm = kTile[kernel].rows, tn = kTile[kernel].cols;
+    // tiles along M, at most: every group may end in one of its own that is not full
+    const int64_t nx = offsets ? rows / tm + (rows < experts ? rows : experts) : (rows + tm - 1) / tm, nz = (N + tn - 1) / tn, jobs = nx * nz;
+    if ((jobs + 8) * (kernel == kI8PingPong ? 1 : 512) >= kGridLimit / 2) return fail(LCMA_ERR_SHAPE, "%s: too many tiles for a launch", who);
     p.nz = (int32_t)nz;
-    p.panel = 8;
-    if (const int err = lcma_launch_i8_gemm(&p, dtype, (int)((nx * nz + 7) / 8 * 8), stream))
+    p.panel = kernel <= kI8Few32 ? 1 : 8;
+    const int grid = kernel == kI8PingPong ? (int)(jobs < 256 ? jobs : 256) : (int)((jobs + 7) / 8 * 8);
+    if (const int err = lcma_launch_i8_gemm(&p, kernel, dtype, grid, stream))
         return fail(LCMA_ERR_HIP, "%s: launch failed with HIP error %d", who, err);
     return LCMA_OK;
 }

@@ -1,5 +1,6 @@
 // Rows quantised to 8-bit integers, and the instances of the 8-bit-integer product (csrc/lcma_i8.hpp).
-#include "lcma_i8.hpp"
+#include "lcma_i8_few_rows.hpp"
+#include "lcma_i8_pingpong.hpp"
 #include "lcma_prepare_b.hpp"
 
 using namespace lcma;
@@ -109,10 +110,28 @@ template <class T, bool GATED> __global__ __launch_bounds__(256) void i8_quantiz
     }
 }
 
-template <class OUT> __global__ __launch_bounds__(256) void i8_gemm_64(const I8GemmParams p) {
-    using G = I8Tile<64, 64, 2, 2, OUT>;
+#define LCMA_I8_RING(TM, TN, WGM, WGN, S)                                                                           \
+    template <class OUT> __global__ __launch_bounds__(64 * WGM * WGN, 2) void i8_ring_##TM##_##TN(const I8GemmParams p) { \
+        using G = I8Ring<TM, TN, WGM, WGN, S, OUT>;                                                                 \
+        __shared__ __attribute__((aligned(16))) char smem[G::LDS_BYTES];                                            \
+        G::run(p, (LCMA_LDS char *)smem);                                                                           \
+    }
+LCMA_I8_RING(64, 64, 2, 2, 4)
+LCMA_I8_RING(64, 128, 2, 2, 3)
+LCMA_I8_RING(128, 128, 2, 4, 4)
+LCMA_I8_RING(128, 256, 2, 4, 3)
+#define LCMA_I8_FEW(T, WK, S)                                                                               \
+    template <class OUT> __global__ __launch_bounds__(64 * WK) void i8_few_##T(const I8GemmParams p) {      \
+        using G = I8FewRows<T, WK, S, OUT>;                                                                 \
+        __shared__ __attribute__((aligned(16))) char smem[G::LDS_BYTES];                                    \
+        G::run(p, (LCMA_LDS char *)smem);                                                                   \
+    }
+LCMA_I8_FEW(16, 4, 2)
+LCMA_I8_FEW(32, 4, 2)
+template <class OUT> __global__ __launch_bounds__(512, 2) void i8_gemm_256(const I8GemmParams) {
+    using G = I8PingPong<OUT>;
     __shared__ __attribute__((aligned(16))) char smem[G::LDS_BYTES];
-    G::run(p, (LCMA_LDS char *)smem);
+    G::run((LCMA_LDS char *)smem);
 }
 
 } // namespace
@@ -130,10 +149,22 @@ extern "C" int lcma_launch_i8_quantize(const lcma::I8QuantParams *p, int dtype, 
     return (int)hipGetLastError();
 }
 
-extern "C" int lcma_launch_i8_gemm(const lcma::I8GemmParams *p, int dtype, int grid, void *stream) {
+extern "C" int lcma_launch_i8_gemm(const lcma::I8GemmParams *p, int kernel, int dtype, int grid, void *stream) {
     const hipStream_t s = (hipStream_t)stream;
-    if (dtype == 0) i8_gemm_64<F32><<<dim3(grid), dim3(256), 0, s>>>(*p);
-    else if (dtype == 1) i8_gemm_64<BF16><<<dim3(grid), dim3(256), 0, s>>>(*p);
-    else i8_gemm_64<F16><<<dim3(grid), dim3(256), 0, s>>>(*p);
+#define LCMA_I8(KERNEL, THREADS)                                                \
+    if (dtype == 0) KERNEL<F32><<<dim3(grid), dim3(THREADS), 0, s>>>(*p);       \
+    else if (dtype == 1) KERNEL<BF16><<<dim3(grid), dim3(THREADS), 0, s>>>(*p); \
+    else KERNEL<F16><<<dim3(grid), dim3(THREADS), 0, s>>>(*p);                  \
+    break;
+    switch (kernel) {
+    case kI8Few16: LCMA_I8(i8_few_16, 256)
+    case kI8Few32: LCMA_I8(i8_few_32, 256)
+    case kI8Ring64: LCMA_I8(i8_ring_64_64, 256)
+    case kI8Ring64x128: LCMA_I8(i8_ring_64_128, 256)
+    case kI8Ring128: LCMA_I8(i8_ring_128_128, 512)
+    case kI8Ring128x256: LCMA_I8(i8_ring_128_256, 512)
+    default: LCMA_I8(i8_gemm_256, 512)
+    }
+#undef LCMA_I8
     return (int)hipGetLastError();
 }

@@ -10,6 +10,7 @@
 #include <stdint.h>
 
 #include "lcma_device.hpp"
+#include "lcma_few_rows.hpp" // wait_loads
 #include "lcma_experts_params.h"
 
 namespace lcma {
@@ -17,28 +18,28 @@ namespace lcma {
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x16 __attribute__((ext_vector_type(16)));
 
-// A tile of C: rows row0 .. row0 + rows - 1 of A, all of expert `expert` (experts: the rows behind the groups), columns col0 .. of C.
+// A tile of C: rows row0 .. row0 + rows - 1 of A, all of expert `expert`, columns col0 .. of C.
 struct I8Place {
     int row0, rows, col0, expert;
 };
 
 // First row of group e (experts: of the rows behind the groups), inside A whatever the offsets say; tiles of TM rows that a group takes.
 LCMA_DEV int i8_row(const I8GemmParams &p, int e) {
-    const int row = e <= p.experts ? p.offsets[e] : p.rows;
+    const int row = p.offsets[e];
     return row < 0 ? 0 : row > p.rows ? p.rows : row;
 }
 template <int TM> LCMA_DEV int i8_tiles(int begin, int end) { return end > begin ? (end - begin + TM - 1) / TM : 0; }
 
-// Tile `x` of TM rows among those of all groups (in expert order, every group in tiles of its own, the rows behind the groups last): its
-// place along the rows; false past the last one.  total: how many there are.  Every wave by itself, a lane per expert.
+// The tiles of TM rows of all groups, in expert order, every group in tiles of its own: how many there are, and the rows of tile x.  Every wave
+// by itself, a lane per expert.
 template <int TM> LCMA_DEV int i8_row_tiles(const I8GemmParams &p) {
     if (!p.offsets) return (p.rows + TM - 1) / TM;
     const int lane = threadIdx.x & 63;
     int total = 0;
-    for (int e0 = 0; e0 <= p.experts; e0 += 64) {
+    for (int e0 = 0; e0 < p.experts; e0 += 64) {
         const int e = e0 + lane;
         int tiles = 0;
-        if (e <= p.experts) tiles = i8_tiles<TM>(i8_row(p, e), i8_row(p, e + 1));
+        if (e < p.experts) tiles = i8_tiles<TM>(i8_row(p, e), i8_row(p, e + 1));
 #pragma unroll
         for (int d = 32; d; d >>= 1) tiles += __shfl_xor(tiles, d);
         total += tiles;
@@ -50,10 +51,10 @@ template <int TM> LCMA_DEV I8Place i8_row_place(const I8GemmParams &p, int x) {
     if (p.offsets) {
         const int lane = threadIdx.x & 63;
         int before = 0;
-        for (int e0 = 0; e0 <= p.experts; e0 += 64) {
+        for (int e0 = 0; e0 < p.experts; e0 += 64) {
             const int e = e0 + lane;
             int begin = 0, end = 0;
-            if (e <= p.experts) {
+            if (e < p.experts) {
                 begin = i8_row(p, e);
                 end = i8_row(p, e + 1);
             }
@@ -83,48 +84,94 @@ template <int TM> LCMA_DEV I8Place i8_row_place(const I8GemmParams &p, int x) {
     return at;
 }
 
+// Tile j of nx x nz: they run down the rows inside column panels of `panel` tiles.
+LCMA_DEV void i8_tile_of_job(int nx, int nz, int panel, int j, int &x, int &z) {
+    const int whole = nz / panel * panel, full = whole * nx;
+    const int width = j < full ? panel : nz - whole, id = j < full ? j % (panel * nx) : j - full;
+    x = id / width;
+    z = (j < full ? j / (panel * nx) * panel : whole) + id % width;
+}
+
+// Rows of C behind the groups are zero: the work-groups of the launch share them.
+template <class OUT> LCMA_DEV void i8_zero_behind(const I8GemmParams &p, int groups, int threads) {
+    if (!p.offsets) return;
+    for (int row = i8_row(p, p.experts) + (int)blockIdx.x; row < p.rows; row += groups)
+        for (int n = threadIdx.x; n < p.N; n += threads) {
+            char *c = (char *)p.C + ((int64_t)row * p.ldc + n) * OUT::ES;
+            if constexpr (OUT::ES == 4) *(float *)c = 0.f;
+            else *(uint16_t *)c = 0;
+        }
+}
+
+// Scales (or biases) of columns n .. n + 3, zeros from N on.
+LCMA_DEV f32x4 i8_four(const float *at, int n, int N) {
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+    if (n + 4 <= N) __builtin_memcpy(&v, at + n, 16);
+    else
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (n + i < N) v[i] = at[n + i];
+    return v;
+}
+
+// 16 bytes of a row of C, `cols` columns of which are inside it.
+template <class OUT> LCMA_DEV void i8_store16(char *at, u32x4 v, int cols) {
+    if (cols >= 16 / OUT::ES) __builtin_memcpy(at, &v, 16);
+    else
+#pragma unroll
+        for (int i = 0; i < 16 / OUT::ES; ++i)
+            if (i < cols) {
+                if constexpr (OUT::ES == 4) ((uint32_t *)at)[i] = v[i];
+                else ((uint16_t *)at)[i] = (uint16_t)(v[i / 2] >> (i & 1) * 16);
+            }
+}
+
 // Four neighbouring columns of a row of C, the last ones of which may be past N.
-template <class OUT> LCMA_DEV void i8_store4(char *at, const float (&v)[4], int cols) {
+template <class OUT> LCMA_DEV void i8_store4(char *at, f32x4 v, int cols) {
     if constexpr (OUT::ES == 4) {
         if (cols >= 4) {
-            const u32x4 raw = {Round<OUT>::run(v[0]), Round<OUT>::run(v[1]), Round<OUT>::run(v[2]), Round<OUT>::run(v[3])};
-            __builtin_memcpy(at, &raw, 16);
+            __builtin_memcpy(at, &v, 16);
         } else {
-            for (int i = 0; i < cols; ++i) ((float *)at)[i] = v[i];
+            #pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (i < cols) ((float *)at)[i] = v[i];
         }
     } else {
         if (cols >= 4) {
             const uint32_t raw[2] = {Round<OUT>::run(v[0]) | (Round<OUT>::run(v[1]) << 16), Round<OUT>::run(v[2]) | (Round<OUT>::run(v[3]) << 16)};
             __builtin_memcpy(at, raw, 8);
         } else {
-            for (int i = 0; i < cols; ++i) ((uint16_t *)at)[i] = (uint16_t)Round<OUT>::run(v[i]);
+            #pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (i < cols) ((uint16_t *)at)[i] = (uint16_t)Round<OUT>::run(v[i]);
         }
     }
 }
 
-// One tile of TM x TN per work-group of WGM x WGN waves, two LDS stages of 128 bytes of K.  The weights are the left operand of the matrix
-// instruction, so a lane holds four neighbouring columns of one row of C.
-template <int TM, int TN, int WGM, int WGN, class OUT> struct I8Tile {
+// One tile of TM x TN per work-group of WGM x WGN waves.  A step is 128 bytes of K; S stages of LDS hold the steps in flight, the loads (straight into LDS)
+// run S - 1 steps ahead and are waited for by count, and one barrier a step says that all waves' parts of it have landed and that all
+// have read the stage that is loaded anew.  What the depth is for: with two stages a step takes as long as a load does, about 0.8 us,
+// whatever the tile.
+// The weights are the left operand of the matrix instruction, so a lane holds four neighbouring columns of one row of C.
+template <int TM, int TN, int WGM, int WGN, int S, class OUT> struct I8Ring {
     static constexpr int NT = 64 * WGM * WGN, NMI = TM / WGM / 32, NNI = TN / WGN / 32;
-    static constexpr int A_STAGE = TM * 128, STAGE = (TM + TN) * 128, LDS_BYTES = 2 * STAGE;
+    static constexpr int A_STAGE = TM * 128, STAGE = (TM + TN) * 128, LDS_BYTES = S * STAGE;
     static constexpr int QA = TM * 8 / NT, QB = TN * 8 / NT;
-    static_assert(TM * 8 % NT == 0 && TN * 8 % NT == 0 && LDS_BYTES <= 160 * 1024, "tile and wave grid");
+    static_assert(TM * 8 % NT == 0 && TN * 8 % NT == 0 && LDS_BYTES <= 160 * 1024 && (S == 3 || S == 4) && (S - 1) * (QA + QB) <= 63, "tile and wave grid");
 
     // 16-byte chunk c of a row sits at position c ^ (row / 2 % 8)
     static LCMA_DEV constexpr int swz(int row, int c) { return c ^ ((row >> 1) & 7); }
 
     static LCMA_DEV void run(const I8GemmParams &p, LCMA_LDS char *lds) {
-        const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), wm = w / WGN, wn = w % WGN;
+        const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = w / WGN, wn = w % WGN;
+        i8_zero_behind<OUT>(p, gridDim.x, NT);
         const int nx = i8_row_tiles<TM>(p), jobs = nx * p.nz, per = (jobs + 7) / 8;
         const int job = (blockIdx.x & 7) * per + (blockIdx.x >> 3); // an eighth of the tiles to every XCD
         if ((int)(blockIdx.x >> 3) >= per || job >= jobs) return;
-        const int whole = p.nz / p.panel * p.panel, full = whole * nx, width = job < full ? p.panel : p.nz - whole, id = job < full ? job : job - full;
-        const int x = job < full ? id % (p.panel * nx) / p.panel : id / width, z = job < full ? id / (p.panel * nx) * p.panel + id % p.panel : whole + id % width;
-        const I8Place at = i8_row_place<TM>(p, x);
-        const int col0 = z * TN, cols = p.N - col0 < TN ? p.N - col0 : TN, steps = at.expert < p.experts ? p.steps : 0;
-        const auto ra = __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t *>(p.A) + (int64_t)at.row0 * p.pitch, 0, at.rows * p.pitch, 0x00020000);
-        const auto rb = __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t *>(p.W) + ((int64_t)at.expert * p.N + col0) * p.pitch, 0, cols * p.pitch, 0x00020000);
-        const uint32_t voff = (uint32_t)(tid >> 3) * p.pitch + swz(tid >> 3, tid & 7) * 16;
+        int x, z;
+        i8_tile_of_job(nx, p.nz, p.panel, job, x, z);
+        I8Place at = i8_row_place<TM>(p, x);
+        at.col0 = z * TN;
         i32x16 acc[NMI][NNI];
 #pragma unroll
         for (int i = 0; i < NMI; ++i)
@@ -132,63 +179,89 @@ template <int TM, int TN, int WGM, int WGN, class OUT> struct I8Tile {
             for (int j = 0; j < NNI; ++j)
 #pragma unroll
                 for (int v = 0; v < 16; ++v) acc[i][j][v] = 0;
-        auto load = [&](LCMA_LDS char *st, int y) {
-#pragma unroll
-            for (int q = 0; q < QA; ++q)
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (LCMA_LDS void *)(st + (q * NT + w * 64) * 16), 16, (int)voff, y * 128 + q * (NT / 8) * p.pitch, 0, 0);
-#pragma unroll
-            for (int q = 0; q < QB; ++q)
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (LCMA_LDS void *)(st + A_STAGE + (q * NT + w * 64) * 16), 16, (int)voff, y * 128 + q * (NT / 8) * p.pitch, 0, 0);
-        };
-        if (steps) load(lds, 0);
-        for (int y = 0; y < steps; ++y) {
-            __syncthreads(); // step y has landed, and all waves have read the stage of step y - 1
-            LCMA_LDS char *st = lds + (y & 1) * STAGE;
-            if (y + 1 < steps) load(lds + (~y & 1) * STAGE, y + 1);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                i32x4 a[NMI], b[NNI];
-#pragma unroll
-                for (int i = 0; i < NMI; ++i) {
-                    const int row = (wm * NMI + i) * 32 + (lane & 31);
-                    a[i] = *(const LCMA_LDS i32x4 *)(st + row * 128 + swz(row, k * 2 + (lane >> 5)) * 16);
-                }
-#pragma unroll
-                for (int j = 0; j < NNI; ++j) {
-                    const int row = (wn * NNI + j) * 32 + (lane & 31);
-                    b[j] = *(const LCMA_LDS i32x4 *)(st + A_STAGE + row * 128 + swz(row, k * 2 + (lane >> 5)) * 16);
-                }
-#pragma unroll
-                for (int i = 0; i < NMI; ++i)
-#pragma unroll
-                    for (int j = 0; j < NNI; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(b[j], a[i], acc[i][j], 0, 0, 0);
-            }
-        }
+        multiply(p, at, w, wm, wn, acc, lds, lds + STAGE, lds + 2 * STAGE, lds + (S == 4 ? 3 * STAGE : 0));
 #pragma unroll
         for (int i = 0; i < NMI; ++i) {
             const int row = (wm * NMI + i) * 32 + (lane & 31);
             if (row >= at.rows) continue;
-            const bool some = at.expert < p.experts; // rows behind the groups are zero
-            const float sa = some ? p.SA[at.row0 + row] : 0.f;
+            const float sa = p.SA[at.row0 + row];
             char *c = (char *)p.C + (int64_t)(at.row0 + row) * p.ldc * OUT::ES;
 #pragma unroll
             for (int j = 0; j < NNI; ++j)
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {
-                    const int col = col0 + (wn * NNI + j) * 32 + g * 8 + (lane >> 5) * 4, left = p.N - col;
-                    float v[4];
+                    const int col = at.col0 + (wn * NNI + j) * 32 + g * 8 + (lane >> 5) * 4, left = p.N - col;
+                    if (left <= 0) continue;
+                    const f32x4 sw = i8_four(p.SW + (int64_t)at.expert * p.N, col, p.N);
+                    f32x4 v;
 #pragma unroll
-                    for (int i4 = 0; i4 < 4; ++i4) {
-                        const int64_t n = (int64_t)at.expert * p.N + col + i4;
-                        v[i4] = 0.f;
-                        if (some && i4 < left) {
-                            v[i4] = (float)acc[i][j][g * 4 + i4] * sa * p.SW[n];
-                            if (p.bias) v[i4] += p.bias[n];
-                        }
-                    }
-                    if (left > 0) i8_store4<OUT>(c + (int64_t)col * OUT::ES, v, left);
+                    for (int k = 0; k < 4; ++k) v[k] = (float)acc[i][j][g * 4 + k] * sa * sw[k];
+                    if (p.bias) v += i8_four(p.bias + (int64_t)at.expert * p.N, col, p.N);
+                    i8_store4<OUT>(c + (int64_t)col * OUT::ES, v, left);
                 }
         }
+    }
+    // restrict: the loads in flight towards one stage do not touch what is read from another (the compiler would otherwise wait for all of them in
+    // front of every read)
+    static LCMA_DEV void multiply(const I8GemmParams &p, const I8Place &at, int w, int wm, int wn, i32x16 (&acc)[NMI][NNI], LCMA_LDS char *__restrict__ s0,
+                                  LCMA_LDS char *__restrict__ s1, LCMA_LDS char *__restrict__ s2, LCMA_LDS char *__restrict__ s3) {
+        const int tid = threadIdx.x, lane = tid & 63, cols = p.N - at.col0 < TN ? p.N - at.col0 : TN, steps = p.steps;
+        const auto ra = __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t *>(p.A) + (int64_t)at.row0 * p.pitch, 0, at.rows * p.pitch, 0x00020000);
+        const auto rb = __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t *>(p.W) + ((int64_t)at.expert * p.N + at.col0) * p.pitch, 0, cols * p.pitch, 0x00020000);
+        const uint32_t voff = (uint32_t)(tid >> 3) * p.pitch + swz(tid >> 3, tid & 7) * 16;
+        auto load = [&](LCMA_LDS char *st, int y) { // a step past the end: zeros, from past the extents
+            const int k = y < steps ? y * 128 : 1 << 30;
+#pragma unroll
+            for (int q = 0; q < QB; ++q)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (LCMA_LDS void *)(st + A_STAGE + (q * NT + w * 64) * 16), 16, (int)voff, k + q * (NT / 8) * p.pitch, 0, 0);
+#pragma unroll
+            for (int q = 0; q < QA; ++q)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (LCMA_LDS void *)(st + (q * NT + w * 64) * 16), 16, (int)voff, k + q * (NT / 8) * p.pitch, 0, 0);
+        };
+        uint32_t fa[4], fb[4]; // of this lane's 16 bytes in the first 32 rows of the wave
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int c = k * 2 + (lane >> 5), ra0 = wm * NMI * 32 + (lane & 31), rb0 = wn * NNI * 32 + (lane & 31);
+            fa[k] = ra0 * 128 + swz(ra0, c) * 16;
+            fb[k] = A_STAGE + rb0 * 128 + swz(rb0, c) * 16;
+        }
+        auto step = [&](LCMA_LDS char *st, LCMA_LDS char *before, int y) {
+            wait_loads<(S - 2) * (QA + QB)>();
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_sched_barrier(0);
+            load(before, y + S - 1);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                i32x4 a[NMI], b[NNI];
+#pragma unroll
+                for (int i = 0; i < NMI; ++i) a[i] = *(const LCMA_LDS i32x4 *)(st + fa[k] + i * 32 * 128);
+#pragma unroll
+                for (int j = 0; j < NNI; ++j) b[j] = *(const LCMA_LDS i32x4 *)(st + fb[k] + j * 32 * 128);
+#pragma unroll
+                for (int i = 0; i < NMI; ++i)
+#pragma unroll
+                    for (int j = 0; j < NNI; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(b[j], a[i], acc[i][j], 0, 0, 0);
+            }
+            __builtin_amdgcn_sched_barrier(0); // (the multiplications stay in front of the next wait; what they read has left LDS)
+        };
+        load(s0, 0);
+        load(s1, 1);
+        if constexpr (S == 4) load(s2, 2);
+        for (int y = 0; y < steps;) {
+            step(s0, S == 4 ? s3 : s2, y);
+            if (++y >= steps) break;
+            step(s1, s0, y);
+            if (++y >= steps) break;
+            step(s2, s1, y);
+            ++y;
+            if constexpr (S == 4) {
+                if (y >= steps) break;
+                step(s3, s2, y);
+                ++y;
+            }
+        }
+        wait_loads<0>(); // the loads past the end land before the LDS is another work-group's
     }
 };
 

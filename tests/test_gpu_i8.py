@@ -290,3 +290,36 @@ def test_weights_that_pass_32_bits():
     want = torch.full((N,), 2.0 * 384, device="cuda")
     want[65500:] = 3 * 16000 + 2 * 384
     assert (c[0] == 0).all().item() and (c[1:] == want.bfloat16()).all().item()
+
+
+KERNELS = ["16x16", "32x32", "64x64", "64x128", "128x128", "128x256", "256x256"]
+
+
+@pytest.fixture
+def kernel(request):
+    from paper_2605_06057_amd import binding as B
+    B.lcma_set_tuning("i8_kernel", request.param)
+    yield request.param
+    B.lcma_set_tuning("i8_kernel", "")
+
+
+@pytest.mark.parametrize("kernel", KERNELS, indirect=True)
+@pytest.mark.parametrize("M,N,K", [(1, 1, 1), (17, 65, 128), (64, 256, 257), (129, 255, 130), (300, 520, 1000), (257, 1025, 384), (1025, 1536, 640)], ids=lambda v: str(v))
+def test_product_on_every_kernel(kernel, M, N, K):
+    for dt in ("f32", "bf16", "f16"):
+        test_product(dt, M, N, K)
+
+
+@pytest.mark.parametrize("kernel", KERNELS, indirect=True)
+@pytest.mark.parametrize("counts,behind", [([3, 0, 5, 1], 2), ([65, 0, 0, 200, 7, 0, 31], 0), ([2] * 130, 1), ([256, 255, 300, 1, 700], 300)], ids=lambda v: str(v).replace(" ", "")[:30])
+def test_experts_on_every_kernel(kernel, counts, behind):
+    test_experts("bf16", counts, behind)
+
+
+def test_an_unknown_kernel_is_the_default():
+    from paper_2605_06057_amd import binding as B
+    B.lcma_set_tuning("i8_kernel", "7x9")
+    try:
+        test_product("bf16", 33, 127, 256)
+    finally:
+        B.lcma_set_tuning("i8_kernel", "")
