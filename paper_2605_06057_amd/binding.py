@@ -147,6 +147,8 @@ def lib() -> ctypes.CDLL:
         L.lcma_tokens_dispatch.argtypes = [i64, i32, i64, vp, i64, i32, vp, vp, i64, vp]
         L.lcma_tokens_combine.argtypes = [i64, i32, i64, vp, i64, i32, vp, vp, vp, i64, vp]
         L.lcma_tokens_combine_grad.argtypes = [i64, i32, i64, vp, i64, vp, i64, i32, vp, vp, vp, i64, vp, vp]
+        global _i8, _i32, _f32
+        _i8, _i32, _f32 = torch.int8, torch.int32, torch.float32
         _lib = L
         # schemes that kernels were generated for beyond the paper's three
         for sid in range(4, int(L.lcma_scheme_id_max()) + 1):
@@ -220,16 +222,21 @@ def _dtype_of(t) -> int:
     return _dtypes[t.dtype]
 
 
-def _stream_of(t) -> int:
-    """Handle of the current stream on the tensor's device."""
+def _stream_on(device: int) -> int:
+    """Handle of the current stream on that device."""
     global _raw_stream
     if _raw_stream is None:
         import torch
         _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+    return _raw_stream(device)
+
+
+def _stream_of(t) -> int:
+    """Handle of the current stream on the tensor's device."""
     device = t.get_device()
     if device < 0:
         raise ValueError(f"expected a tensor on the GPU, got one on {t.device}")
-    return _raw_stream(device)
+    return _stream_on(device)
 
 
 def _marshal(A, B, C, b_nk: bool = False):
@@ -523,16 +530,9 @@ def lcma_fp8_gemm_lcma(A, Wp, C, scheme: Scheme, workspace):
 
 
 # ---------------------------------------------------------------- 8-bit integers (a scale for each row of either operand)
-_i8 = _i32 = _f32 = None  # torch's types, from the first use on
-
-
-def _types():
-    """torch's int8, int32 and float32 (torch is imported with the first tensor, not with this file)."""
-    global _i8, _i32, _f32
-    if _i8 is None:
-        import torch
-        _i8, _i32, _f32 = torch.int8, torch.int32, torch.float32
-    return _i8, _i32, _f32
+# As for the products above, what a call does here before the C entry point counts for small sizes (a launch takes 2.9 us, the call 0.5): every tensor is
+# asked for its type, shape, layout and device once, and nothing is looked up twice.
+_i8 = _i32 = _f32 = None  # torch's types, from the library's loading on
 
 
 def _is(t, dtype, shape, device: int) -> bool:
@@ -563,60 +563,64 @@ def lcma_i8_code_pitch(K: int) -> int:
 def lcma_i8_quantize(X, Q=None, S=None, gated: bool = False):
     """Codes (rows x code pitch, int8) and scales (rows, fp32) of the device tensor X (rows x K; gated: rows x 2 K, of
     silu(first half) * second half)."""
-    i8, _, f32 = _types()
+    L = _lib or lib()
     rows, width = shape = X.shape
     assert not (gated and width % 2), "expected rows x 2 K"
     K, device = width // 2 if gated else width, X.get_device()
     pitch = (K + 127) // 128 * 128  # lcma_i8_code_pitch
     if Q is None:
-        Q = X.new_empty((rows, pitch), dtype=i8)
+        Q = X.new_empty((rows, pitch), dtype=_i8)
     if S is None:
-        S = X.new_empty((rows,), dtype=f32)
-    assert _rows_of(X, shape, device) and _is(Q, i8, (rows, pitch), device) and _has(S, f32, rows, device)
-    _check(lib().lcma_i8_quantize(rows, K, X.data_ptr(), _ld(X, width), _dtype_of(X), gated, Q.data_ptr(), S.data_ptr(), _stream_of(X)))
+        S = X.new_empty((rows,), dtype=_f32)
+    assert device >= 0 and _rows_of(X, shape, device) and _is(Q, _i8, (rows, pitch), device) and _has(S, _f32, rows, device)
+    if status := L.lcma_i8_quantize(rows, K, X.data_ptr(), _ld(X, width), _dtype_of(X), gated, Q.data_ptr(), S.data_ptr(), _stream_on(device)):
+        _check(status)
     return Q, S
 
 
 def lcma_i8_quantize_dispatch(X, position, Q=None, S=None):
     """lcma_i8_quantize of the tokens' rows X (tokens x K) into expert order: Q, S have a row for every slot of position (tokens x top_k)."""
-    i8, i32, f32 = _types()
+    L = _lib or lib()
     tokens, K = shape = X.shape
     top_k, device = position.shape[1], X.get_device()
     n, pitch = tokens * top_k, (K + 127) // 128 * 128  # lcma_i8_code_pitch
     if Q is None:
-        Q = X.new_empty((n, pitch), dtype=i8)
+        Q = X.new_empty((n, pitch), dtype=_i8)
     if S is None:
-        S = X.new_empty((n,), dtype=f32)
-    assert _rows_of(X, shape, device) and _is(position, i32, (tokens, top_k), device)
-    assert _is(Q, i8, (n, pitch), device) and _has(S, f32, n, device)
-    _check(lib().lcma_i8_quantize_dispatch(tokens, K, X.data_ptr(), _ld(X, K), _dtype_of(X), top_k, position.data_ptr(), Q.data_ptr(), S.data_ptr(),
-                                           _stream_of(X)))
+        S = X.new_empty((n,), dtype=_f32)
+    assert device >= 0 and _rows_of(X, shape, device) and _is(position, _i32, (tokens, top_k), device)
+    assert _is(Q, _i8, (n, pitch), device) and _has(S, _f32, n, device)
+    if status := L.lcma_i8_quantize_dispatch(tokens, K, X.data_ptr(), _ld(X, K), _dtype_of(X), top_k, position.data_ptr(), Q.data_ptr(), S.data_ptr(),
+                                           _stream_on(device)):
+        _check(status)
     return Q, S
 
 
 def lcma_i8_gemm_nt(Aq, Sa, Wq, Sw, C, K: int, bias=None):
     """C (M x N) = the product of the codes Aq (M x pitch) and Wq (N x pitch) over K, times the scales of rows and channels, plus bias."""
-    i8, _, f32 = _types()
+    L = _lib or lib()
     M, N = shape = C.shape
     pitch, device = (K + 127) // 128 * 128, C.get_device()  # lcma_i8_code_pitch
-    assert _is(Aq, i8, (M, pitch), device) and _is(Wq, i8, (N, pitch), device) and _has(Sa, f32, M, device) and _has(Sw, f32, N, device)
-    assert _rows_of(C, shape, device) and (bias is None or _has(bias, f32, N, device))
-    _check(lib().lcma_i8_gemm_nt(M, N, K, Aq.data_ptr(), Sa.data_ptr(), Wq.data_ptr(), Sw.data_ptr(), None if bias is None else bias.data_ptr(),
-                                 C.data_ptr(), _ld(C, N), _dtype_of(C), _stream_of(C)))
+    assert device >= 0 and _is(Aq, _i8, (M, pitch), device) and _is(Wq, _i8, (N, pitch), device) and _has(Sa, _f32, M, device) and _has(Sw, _f32, N, device)
+    assert _rows_of(C, shape, device) and (bias is None or _has(bias, _f32, N, device))
+    if status := L.lcma_i8_gemm_nt(M, N, K, Aq.data_ptr(), Sa.data_ptr(), Wq.data_ptr(), Sw.data_ptr(), None if bias is None else bias.data_ptr(),
+                                 C.data_ptr(), _ld(C, N), _dtype_of(C), _stream_on(device)):
+        _check(status)
     return C
 
 
 def lcma_i8_gemm_experts(Aq, Sa, offsets, Wq, Sw, C, K: int, bias=None):
     """lcma_i8_gemm_nt over experts: rows offsets[e] .. offsets[e + 1] - 1 times the weights Wq[e] (experts x N x pitch), Sw and bias experts x N;
     rows of C behind the last expert's are set to zero."""
-    i8, i32, f32 = _types()
+    L = _lib or lib()
     rows, N = shape = C.shape
     experts, pitch, device = Wq.shape[0], (K + 127) // 128 * 128, C.get_device()  # lcma_i8_code_pitch
-    assert _is(Aq, i8, (rows, pitch), device) and _is(Wq, i8, (experts, N, pitch), device) and _has(Sa, f32, rows, device)
-    assert _is(Sw, f32, (experts, N), device) and _has(offsets, i32, experts + 1, device)
-    assert _rows_of(C, shape, device) and (bias is None or _is(bias, f32, (experts, N), device))
-    _check(lib().lcma_i8_gemm_experts(rows, N, K, experts, offsets.data_ptr(), Aq.data_ptr(), Sa.data_ptr(), Wq.data_ptr(), Sw.data_ptr(),
-                                      None if bias is None else bias.data_ptr(), C.data_ptr(), _ld(C, N), _dtype_of(C), _stream_of(C)))
+    assert device >= 0 and _is(Aq, _i8, (rows, pitch), device) and _is(Wq, _i8, (experts, N, pitch), device) and _has(Sa, _f32, rows, device)
+    assert _is(Sw, _f32, (experts, N), device) and _has(offsets, _i32, experts + 1, device)
+    assert _rows_of(C, shape, device) and (bias is None or _is(bias, _f32, (experts, N), device))
+    if status := L.lcma_i8_gemm_experts(rows, N, K, experts, offsets.data_ptr(), Aq.data_ptr(), Sa.data_ptr(), Wq.data_ptr(), Sw.data_ptr(),
+                                      None if bias is None else bias.data_ptr(), C.data_ptr(), _ld(C, N), _dtype_of(C), _stream_on(device)):
+        _check(status)
     return C
 
 
@@ -628,7 +632,7 @@ def lcma_tokens_sort_workspace_bytes(tokens: int, top_k: int, experts: int) -> i
 def lcma_tokens_sort(ids, experts: int, order=None, position=None, offsets=None, workspace=None):
     """order (tokens * top_k), position (tokens x top_k) and offsets (experts + 1), int32, of the slots of ids (tokens x top_k expert numbers,
     int32); slots with another number than 0 .. experts - 1 come last, with a negative position."""
-    _, i32, _ = _types()
+    L = _lib or lib()
     tokens, top_k = shape = ids.shape
     n, device = tokens * top_k, ids.get_device()
     if order is None:
@@ -643,52 +647,56 @@ def lcma_tokens_sort(ids, experts: int, order=None, position=None, offsets=None,
     if workspace is not None:
         assert workspace.is_contiguous() and workspace.get_device() == device
         space, size = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-    assert _is(ids, i32, shape, device) and _has(order, i32, n, device) and _is(position, i32, shape, device) and _has(offsets, i32, experts + 1, device)
-    _check(lib().lcma_tokens_sort(tokens, top_k, experts, ids.data_ptr(), order.data_ptr(), position.data_ptr(), offsets.data_ptr(), space, size,
-                                  _stream_of(ids)))
+    assert device >= 0 and _is(ids, _i32, shape, device) and _has(order, _i32, n, device) and _is(position, _i32, shape, device) and _has(offsets, _i32, experts + 1, device)
+    if status := L.lcma_tokens_sort(tokens, top_k, experts, ids.data_ptr(), order.data_ptr(), position.data_ptr(), offsets.data_ptr(), space, size,
+                                  _stream_on(device)):
+        _check(status)
     return order, position, offsets
 
 
 def lcma_tokens_dispatch(X, position, Y=None):
     """Y[position[t, j]] = X[t]: the tokens' rows in expert order (rows of slots without an expert: zeros)."""
-    _, i32, _ = _types()
+    L = _lib or lib()
     tokens, H = shape = X.shape
     top_k, device = position.shape[1], X.get_device()
     if Y is None:
         Y = X.new_empty((tokens * top_k, H))
-    assert _rows_of(X, shape, device) and _rows_of(Y, (tokens * top_k, H), device) and X.dtype is Y.dtype and _is(position, i32, (tokens, top_k), device)
-    _check(lib().lcma_tokens_dispatch(tokens, top_k, H, X.data_ptr(), _ld(X, H), _dtype_of(X), position.data_ptr(), Y.data_ptr(), _ld(Y, H), _stream_of(X)))
+    assert device >= 0 and _rows_of(X, shape, device) and _rows_of(Y, (tokens * top_k, H), device) and X.dtype is Y.dtype and _is(position, _i32, (tokens, top_k), device)
+    if status := L.lcma_tokens_dispatch(tokens, top_k, H, X.data_ptr(), _ld(X, H), _dtype_of(X), position.data_ptr(), Y.data_ptr(), _ld(Y, H), _stream_on(device)):
+        _check(status)
     return Y
 
 
 def lcma_tokens_combine(Y, position, weights=None, X=None):
     """X[t] = sum over j of weights[t, j] * Y[position[t, j]] (weights None: ones, which is the gradient of lcma_tokens_dispatch)."""
-    _, i32, f32 = _types()
+    L = _lib or lib()
     tokens, top_k = slots = position.shape
     H, device = Y.shape[1], Y.get_device()
     if X is None:
         X = Y.new_empty((tokens, H))
-    assert _rows_of(Y, (tokens * top_k, H), device) and _rows_of(X, (tokens, H), device) and X.dtype is Y.dtype and _is(position, i32, slots, device)
-    assert weights is None or _is(weights, f32, slots, device)
-    _check(lib().lcma_tokens_combine(tokens, top_k, H, Y.data_ptr(), _ld(Y, H), _dtype_of(Y), position.data_ptr(),
-                                     None if weights is None else weights.data_ptr(), X.data_ptr(), _ld(X, H), _stream_of(Y)))
+    assert device >= 0 and _rows_of(Y, (tokens * top_k, H), device) and _rows_of(X, (tokens, H), device) and X.dtype is Y.dtype and _is(position, _i32, slots, device)
+    assert weights is None or _is(weights, _f32, slots, device)
+    if status := L.lcma_tokens_combine(tokens, top_k, H, Y.data_ptr(), _ld(Y, H), _dtype_of(Y), position.data_ptr(),
+                                     None if weights is None else weights.data_ptr(), X.data_ptr(), _ld(X, H), _stream_on(device)):
+        _check(status)
     return X
 
 
 def lcma_tokens_combine_grad(dX, Y, position, weights, dY=None, dweights=None):
     """Gradient of lcma_tokens_combine from dX (tokens x H): dY (rows in expert order, in Y's type) and dweights (tokens x top_k, fp32)."""
-    _, i32, f32 = _types()
+    L = _lib or lib()
     tokens, top_k = slots = position.shape
     H, device = Y.shape[1], Y.get_device()
     n = tokens * top_k
     if dY is None:
         dY = Y.new_empty((n, H))
     if dweights is None:
-        dweights = Y.new_empty(slots, dtype=f32)
-    assert _rows_of(dX, (tokens, H), device) and _rows_of(Y, (n, H), device) and _rows_of(dY, (n, H), device) and dX.dtype is Y.dtype is dY.dtype
-    assert _is(position, i32, slots, device) and _is(weights, f32, slots, device) and _is(dweights, f32, slots, device)
-    _check(lib().lcma_tokens_combine_grad(tokens, top_k, H, dX.data_ptr(), _ld(dX, H), Y.data_ptr(), _ld(Y, H), _dtype_of(Y), position.data_ptr(),
-                                          weights.data_ptr(), dY.data_ptr(), _ld(dY, H), dweights.data_ptr(), _stream_of(Y)))
+        dweights = Y.new_empty(slots, dtype=_f32)
+    assert device >= 0 and _rows_of(dX, (tokens, H), device) and _rows_of(Y, (n, H), device) and _rows_of(dY, (n, H), device) and dX.dtype is Y.dtype is dY.dtype
+    assert _is(position, _i32, slots, device) and _is(weights, _f32, slots, device) and _is(dweights, _f32, slots, device)
+    if status := L.lcma_tokens_combine_grad(tokens, top_k, H, dX.data_ptr(), _ld(dX, H), Y.data_ptr(), _ld(Y, H), _dtype_of(Y), position.data_ptr(),
+                                          weights.data_ptr(), dY.data_ptr(), _ld(dY, H), dweights.data_ptr(), _stream_on(device)):
+        _check(status)
     return dY, dweights
 
 

@@ -3,7 +3,7 @@
 
 #include <cstring>
 
-extern "C" int lcma_launch_i8_quantize(const lcma::I8QuantParams *p, int dtype, int gated, void *stream);
+extern "C" int lcma_launch_i8_quantize(const lcma::I8QuantParams *p, int dtype, int gated, int threads, void *stream);
 extern "C" int lcma_launch_i8_gemm(const lcma::I8GemmParams *p, int kernel, int dtype, int grid, void *stream);
 
 using namespace lcma;
@@ -22,7 +22,6 @@ lcma_status quantize(const char *who, int64_t rows, int64_t K, const void *X, in
     if (top_k < 1) return fail(LCMA_ERR_ARG, "%s: top_k = %d must be at least 1", who, top_k);
     if (K > kMostK) return fail(LCMA_ERR_SHAPE, "%s: K = %lld is more than %lld", who, (long long)K, (long long)kMostK);
     if (rows >= kRowLimit || rows * top_k >= kRowLimit) return fail(LCMA_ERR_SHAPE, "%s: 2^31 rows or more", who);
-    if (rows * 256 >= kGridLimit) return fail(LCMA_ERR_SHAPE, "%s: too many rows for a launch", who);
     if (rows == 0) return LCMA_OK;
     const int64_t width = gated ? 2 * K : K;
     if (!S || (K && (!X || !Q))) return fail(LCMA_ERR_ARG, "%s: null pointer", who);
@@ -45,7 +44,10 @@ lcma_status quantize(const char *who, int64_t rows, int64_t K, const void *X, in
     p.K = (int32_t)K;
     p.pitch = (int32_t)pitch_of(K);
     p.top_k = top_k;
-    if (const int err = lcma_launch_i8_quantize(&p, dtype, gated, stream)) return fail(LCMA_ERR_HIP, "%s: launch failed with HIP error %d", who, err);
+    // as many threads as keep the row in registers
+    const int threads = K <= 1024 ? 64 : K <= 4096 ? 256 : 1024;
+    if (rows * threads >= kGridLimit) return fail(LCMA_ERR_SHAPE, "%s: too many rows for a launch", who);
+    if (const int err = lcma_launch_i8_quantize(&p, dtype, gated, threads, stream)) return fail(LCMA_ERR_HIP, "%s: launch failed with HIP error %d", who, err);
     return LCMA_OK;
 }
 

@@ -5,8 +5,9 @@
 
 namespace lcma {
 
-// lcma_tokens_sort (csrc/lcma_tokens.hip): n = tokens * top_k slots, cut into blocks of kSortSlots.
-constexpr int kSortSlots = 4096, kMaxExperts = 1024;
+// lcma_tokens_sort (csrc/lcma_tokens.hip): n = tokens * top_k slots, up to kSortOnce in one launch, above in blocks of kSortSlots (more than
+// kSortBlocks blocks: their counts are summed by a launch of its own).
+constexpr int kSortSlots = 2048, kSortOnce = 4096, kSortBlocks = 128, kMaxExperts = 1024;
 struct TokensSortParams {
     const int32_t *ids;
     int32_t *order, *position, *offsets;
@@ -25,6 +26,7 @@ struct TokensRowsParams {
     int64_t ldx_b, lddx_b, ldy_b;
     int32_t tokens, top_k, H;
     int32_t lane_shift; // 2^lane_shift neighbouring threads along a row
+    int32_t stream;     // bit 0: what is written, bit 1: the rows in expert order that are read, pass the caches by
 };
 
 // lcma_i8_quantize, lcma_i8_quantize_dispatch (csrc/lcma_i8.hip).

@@ -11,7 +11,8 @@ namespace {
 // codes zero; one with an infinity or a NaN has codes zero and amax / 127 (infinity, NaN) for its scale, so that its products are NaN.
 // Magnitudes are compared as bits: NaN is above infinity there.  Rows below 2^-100 are scaled up first (127 / amax has to be finite).
 // GATED: the row is 2 K long and x = silu(row[k]) row[K + k].
-// A work-group of 256 per row; a thread takes eight values at a time.
+// L threads per row (a wave, four or sixteen), eight values at a time: a thread keeps its first two eights in registers and reads others again.  Bound by
+// the bytes it moves; the quotient is a product with 127 / amax and the rounding an addition of 1.5 * 2^23 (whose low byte is the code).
 template <class T> LCMA_DEV void eight(const char *at, int k, int K, float (&v)[8]) { // values k .. k + 7 of a row, zeros from K on
     if (k + 8 <= K) {
         if constexpr (T::ES == 4) {
@@ -45,7 +46,7 @@ template <class T, bool GATED> LCMA_DEV void values(const char *row, int k, int 
         float u[8];
         eight<T>(row + (int64_t)K * T::ES, k, K, u);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = v[i] / (1.f + __expf(-v[i])) * u[i];
+        for (int i = 0; i < 8; ++i) v[i] = v[i] * __builtin_amdgcn_rcpf(1.f + __expf(-v[i])) * u[i];
     }
 }
 LCMA_DEV uint32_t magnitude(float x) { return __builtin_bit_cast(uint32_t, x) & 0x7fffffffu; }
@@ -64,20 +65,44 @@ LCMA_DEV RowScale row_scale(uint32_t bits) {
     s.scale = amax / 127.f;
     return s;
 }
-LCMA_DEV uint64_t codes(const float (&v)[8], const RowScale &s) {
+LCMA_DEV uint64_t codes(float (&v)[8], const RowScale &s) {
 #pragma clang fp contract(off)
     uint32_t c[8];
+    if (s.up != 1.f)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) c[i] = s.finite ? (uint32_t)(int)__builtin_rintf(v[i] * s.up * s.inv) & 255u : 0u;
-    return (uint64_t)(c[0] | c[1] << 8 | c[2] << 16 | c[3] << 24) | (uint64_t)(c[4] | c[5] << 8 | c[6] << 16 | c[7] << 24) << 32;
+        for (int i = 0; i < 8; ++i) v[i] *= s.up;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float q = v[i] * s.inv; // (rounded on its own, as the definition says)
+        c[i] = __builtin_bit_cast(uint32_t, q + 12582912.f);
+    }
+    const uint32_t lo = __builtin_amdgcn_perm(__builtin_amdgcn_perm(c[3], c[2], 0x0c0c0400), __builtin_amdgcn_perm(c[1], c[0], 0x0c0c0400), 0x05040100),
+                   hi = __builtin_amdgcn_perm(__builtin_amdgcn_perm(c[7], c[6], 0x0c0c0400), __builtin_amdgcn_perm(c[5], c[4], 0x0c0c0400), 0x05040100);
+    return s.finite ? (uint64_t)hi << 32 | lo : 0;
 }
 
-template <class T, bool GATED> __global__ __launch_bounds__(256) void i8_quantize(const I8QuantParams p) {
-    __shared__ uint32_t part[4];
-    const int64_t r = blockIdx.x;
+template <class T, bool GATED, int L> __global__ __launch_bounds__(L < 256 ? 256 : L) void i8_quantize(const I8QuantParams p) {
+    constexpr int KEPT = 2, ROWS = L < 256 ? 256 / L : 1;
+    __shared__ uint32_t part[L / 64];
+    const int64_t r = (int64_t)blockIdx.x * ROWS + threadIdx.x / L;
+    const int lane = threadIdx.x % L;
+    if (r >= p.rows) return; // (L >= 256: a work-group is a row)
     const char *row = (const char *)p.X + r * p.ldx_b;
     uint32_t most = 0;
-    for (int k = threadIdx.x * 8; k < p.K; k += 2048) {
+    float kept[KEPT][8];
+#pragma unroll
+    for (int n = 0; n < KEPT; ++n) {
+        const int k = (n * L + lane) * 8;
+        if (k < p.K) values<T, GATED>(row, k, p.K, kept[n]);
+        else
+#pragma unroll
+            for (int i = 0; i < 8; ++i) kept[n][i] = 0.f;
+    }
+#pragma unroll
+    for (int n = 0; n < KEPT; ++n)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) most = max(most, magnitude(kept[n][i]));
+    for (int k = (KEPT * L + lane) * 8; k < p.K; k += L * 8) {
         float v[8];
         values<T, GATED>(row, k, p.K, v);
 #pragma unroll
@@ -85,28 +110,35 @@ template <class T, bool GATED> __global__ __launch_bounds__(256) void i8_quantiz
     }
 #pragma unroll
     for (int d = 32; d; d >>= 1) most = max(most, (uint32_t)__shfl_xor((int)most, d));
-    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = most;
-    __syncthreads();
-    const RowScale s = row_scale(max(max(part[0], part[1]), max(part[2], part[3])));
-    for (int k = threadIdx.x * 8; k < p.pitch; k += 2048) {
-        uint64_t c = 0;
-        if (k < p.K) {
-            float v[8];
-            values<T, GATED>(row, k, p.K, v);
-            c = codes(v, s);
-        }
-        if (!p.position) *(uint64_t *)(p.Q + r * p.pitch + k) = c;
-        else
-            for (int j = 0; j < p.top_k; ++j) {
-                const int to = p.position[r * p.top_k + j];
-                if (to >= 0) *(uint64_t *)(p.Q + (int64_t)to * p.pitch + k) = c;
-            }
+    if constexpr (L > 64) {
+        if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = most;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < L / 64; ++w) most = max(most, part[w]);
     }
-    if (!p.position) {
-        if (threadIdx.x == 0) p.S[r] = s.scale;
+    const RowScale s = row_scale(most);
+    const int32_t *position = p.position ? p.position + r * p.top_k : nullptr;
+    auto put = [&](int k, uint64_t c) {
+        if (!position) *(uint64_t *)(p.Q + r * p.pitch + k) = c;
+        else
+            for (int j = 0; j < p.top_k; ++j)
+                if (const int to = position[j]; to >= 0) *(uint64_t *)(p.Q + (int64_t)to * p.pitch + k) = c;
+    };
+#pragma unroll
+    for (int n = 0; n < KEPT; ++n) {
+        const int k = (n * L + lane) * 8;
+        if (k < p.pitch) put(k, codes(kept[n], s)); // (columns behind K: values 0, codes 0)
+    }
+    for (int k = (KEPT * L + lane) * 8; k < p.pitch; k += L * 8) {
+        float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        if (k < p.K) values<T, GATED>(row, k, p.K, v);
+        put(k, codes(v, s));
+    }
+    if (!position) {
+        if (lane == 0) p.S[r] = s.scale;
     } else {
-        for (int j = threadIdx.x; j < p.top_k; j += 256)
-            if (const int to = p.position[r * p.top_k + j]; to >= 0) p.S[to] = s.scale;
+        for (int j = lane; j < p.top_k; j += L)
+            if (const int to = position[j]; to >= 0) p.S[to] = s.scale;
     }
 }
 
@@ -136,16 +168,21 @@ template <class OUT> __global__ __launch_bounds__(512, 2) void i8_gemm_256(const
 
 } // namespace
 
-extern "C" int lcma_launch_i8_quantize(const lcma::I8QuantParams *p, int dtype, int gated, void *stream) {
-    const dim3 grid(p->rows), block(256);
+// threads: of a row
+extern "C" int lcma_launch_i8_quantize(const lcma::I8QuantParams *p, int dtype, int gated, int threads, void *stream) {
     const hipStream_t s = (hipStream_t)stream;
-#define LCMA_QUANTIZE(T)                                       \
-    if (gated) i8_quantize<T, true><<<grid, block, 0, s>>>(*p); \
-    else i8_quantize<T, false><<<grid, block, 0, s>>>(*p);
+#define LCMA_QUANTIZE_L(T, G)                                                                          \
+    if (threads == 64) i8_quantize<T, G, 64><<<dim3((p->rows + 3) / 4), dim3(256), 0, s>>>(*p);         \
+    else if (threads == 256) i8_quantize<T, G, 256><<<dim3(p->rows), dim3(256), 0, s>>>(*p);            \
+    else i8_quantize<T, G, 1024><<<dim3(p->rows), dim3(1024), 0, s>>>(*p);
+#define LCMA_QUANTIZE(T)                    \
+    if (gated) { LCMA_QUANTIZE_L(T, true) } \
+    else { LCMA_QUANTIZE_L(T, false) }
     if (dtype == 0) { LCMA_QUANTIZE(F32) }
     else if (dtype == 1) { LCMA_QUANTIZE(BF16) }
     else { LCMA_QUANTIZE(F16) }
 #undef LCMA_QUANTIZE
+#undef LCMA_QUANTIZE_L
     return (int)hipGetLastError();
 }
 

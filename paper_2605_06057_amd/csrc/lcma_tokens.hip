@@ -17,10 +17,11 @@ namespace {
 using namespace lcma;
 
 // ------------------------------------------------------------------ sort
-// A stable counting sort.  Eight waves own kSortSlots neighbouring slots, a wave the 512 from its first on; the slots of a round of 64 that
-// name the same expert are found with one ballot per bit of the expert number, so a wave's counts need no atomics and the rank of a slot
-// is the count before the round plus the lanes below with the same number.
-constexpr int kSortWaves = 8, kSortRounds = kSortSlots / (64 * kSortWaves);
+// A stable counting sort.  A wave owns 64 R neighbouring slots; the slots of a round of 64 that name the same expert are found with one ballot per bit
+// of the expert number, so a wave's counts need no atomics and the rank of a slot is the count before the round plus the lanes below with the
+// same number.  What bounds it is latency: up to kSortOnce slots are one work-group's, 16 waves; above, a launch counts blocks of kSortSlots and
+// another one places them, every block adding up the counts of those before it (more than kSortBlocks of them: a third launch in between does).
+// Measured, us: see the table of the tokens' calls.
 
 // What a wave's lanes wrote to LDS is there for the reads of its other lanes behind this (for the compiler: the LDS works in order).
 LCMA_DEV void lanes_meet() {
@@ -38,74 +39,89 @@ LCMA_DEV uint64_t same_expert(int e, int bits, bool in) {
     return m;
 }
 
+// Inclusive prefix sum over the lanes of a wave.
+LCMA_DEV int lanes_upto(int v, int lane) {
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int below = __shfl_up(v, d);
+        if (lane >= d) v += below;
+    }
+    return v;
+}
 // Exclusive prefix sums of v[0 .. n) in LDS, by one wave.
 LCMA_DEV void prefix_sums(LCMA_LDS int32_t *v, int n, int lane) {
     int carry = 0;
     for (int i = 0; i < n; i += 64) {
-        const int mine = i + lane < n ? v[i + lane] : 0;
-        int sum = mine;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int below = __shfl_up(sum, d);
-            if (lane >= d) sum += below;
-        }
+        const int mine = i + lane < n ? v[i + lane] : 0, sum = lanes_upto(mine, lane);
         if (i + lane < n) v[i + lane] = carry + sum - mine;
         carry += __shfl(sum, 63);
     }
 }
 
-// STAGE 0: all slots are one block's.  1: counts of every block.  2: rows, from the counts of the blocks before (made by block_prefix).
-template <int STAGE> __global__ __launch_bounds__(64 * kSortWaves) void tokens_sort(const TokensSortParams p) {
+// STAGE 0: all slots are one block's.  1: counts of every block.  2: rows, from the counts of all blocks.  3: rows, from what block_prefix made of
+// them.  W waves of R rounds each; a wave's counts fit 16 bits.
+template <int STAGE, int W, int R> __global__ __launch_bounds__(64 * W) void tokens_sort(const TokensSortParams p) {
     extern __shared__ __attribute__((aligned(16))) char smem[];
     const int B = p.experts + 1, lane = threadIdx.x & 63, w = threadIdx.x >> 6, bits = 32 - __builtin_clz(p.experts);
-    LCMA_LDS int32_t *counts = (LCMA_LDS int32_t *)smem, *first = counts + kSortWaves * B; // first row of every expert (and of the rest)
-    LCMA_LDS int32_t *mine = counts + w * B;
-    for (int i = threadIdx.x; i < kSortWaves * B; i += 64 * kSortWaves) counts[i] = 0;
-    const int64_t slot0 = (int64_t)blockIdx.x * kSortSlots + w * 64 * kSortRounds + lane;
-    int e[kSortRounds];
+    LCMA_LDS int32_t *first = (LCMA_LDS int32_t *)smem, *base = first + B; // first row of every expert (and of the rest); rows of it before this block
+    LCMA_LDS uint16_t *counts = (LCMA_LDS uint16_t *)(base + B), *mine = counts + w * B;
+    for (int i = threadIdx.x; i < W * B; i += 64 * W) counts[i] = 0;
+    for (int i = threadIdx.x; i < 2 * B; i += 64 * W) first[i] = 0;
+    const int64_t slot0 = (int64_t)blockIdx.x * (64 * W * R) + w * 64 * R + lane;
+    int e[R];
 #pragma unroll
-    for (int r = 0; r < kSortRounds; ++r) {
+    for (int r = 0; r < R; ++r) {
         const int64_t slot = slot0 + r * 64;
         const int id = slot < p.n ? p.ids[slot] : 0;
         e[r] = (uint32_t)id < (uint32_t)p.experts ? id : p.experts;
     }
     __syncthreads();
-    uint64_t same[kSortRounds];
+    if (STAGE == 2) // (additions of whole numbers: in any order)
+        for (int i = threadIdx.x; i < p.blocks * B; i += 64 * W) {
+            const int c = p.counts[i], b = i / B, x = i - b * B;
+            if (c) __hip_atomic_fetch_add(first + x, c, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+            if (c && b < (int)blockIdx.x) __hip_atomic_fetch_add(base + x, c, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+        }
+    if (STAGE == 3)
+        for (int x = threadIdx.x; x < B; x += 64 * W) {
+            first[x] = p.counts[(int64_t)p.blocks * B + x];
+            base[x] = p.counts[(int64_t)blockIdx.x * B + x];
+        }
+    uint64_t same[R];
 #pragma unroll
-    for (int r = 0; r < kSortRounds; ++r) {
+    for (int r = 0; r < R; ++r) {
         same[r] = same_expert(e[r], bits, slot0 + r * 64 < p.n);
-        if (slot0 + r * 64 < p.n && (same[r] & ((1ull << lane) - 1)) == 0) mine[e[r]] += __popcll(same[r]);
+        if (slot0 + r * 64 < p.n && (same[r] & ((1ull << lane) - 1)) == 0) mine[e[r]] += (uint16_t)__popcll(same[r]);
         lanes_meet();
     }
     __syncthreads();
-    // counts become, for every wave, the rows of the expert before its own; first: all of the block (the launch)
-    const int32_t *before = p.counts + (int64_t)blockIdx.x * B, *totals = p.counts + (int64_t)p.blocks * B;
-    for (int x = threadIdx.x; x < B; x += 64 * kSortWaves) {
-        int sum = STAGE == 2 ? before[x] : 0;
+    // counts become, for every wave, the rows of the expert that the waves before it have in this block
+    for (int x = threadIdx.x; x < B; x += 64 * W) {
+        int sum = 0;
 #pragma unroll
-        for (int k = 0; k < kSortWaves; ++k) {
+        for (int k = 0; k < W; ++k) {
             const int c = counts[k * B + x];
-            counts[k * B + x] = sum;
+            counts[k * B + x] = (uint16_t)sum;
             sum += c;
         }
         if (STAGE == 1) p.counts[(int64_t)blockIdx.x * B + x] = sum;
-        else first[x] = STAGE == 2 ? totals[x] : sum;
+        else if (STAGE == 0) first[x] = sum;
     }
     if (STAGE == 1) return;
     __syncthreads();
     if (w == 0) prefix_sums(first, B, lane);
     __syncthreads();
     if (blockIdx.x == 0)
-        for (int x = threadIdx.x; x < B; x += 64 * kSortWaves) p.offsets[x] = first[x];
+        for (int x = threadIdx.x; x < B; x += 64 * W) p.offsets[x] = first[x];
 #pragma unroll
-    for (int r = 0; r < kSortRounds; ++r) {
+    for (int r = 0; r < R; ++r) {
         const int64_t slot = slot0 + r * 64;
         if (slot < p.n) {
-            const int below = __popcll(same[r] & ((1ull << lane) - 1)), row = first[e[r]] + mine[e[r]] + below;
+            const int below = __popcll(same[r] & ((1ull << lane) - 1)), row = first[e[r]] + base[e[r]] + mine[e[r]] + below;
             p.order[row] = (int32_t)slot;
             p.position[slot] = e[r] < p.experts ? row : -1 - row;
             lanes_meet();
-            if (below == 0) mine[e[r]] += __popcll(same[r]);
+            if (below == 0) mine[e[r]] += (uint16_t)__popcll(same[r]);
         }
         lanes_meet();
     }
@@ -117,13 +133,7 @@ __global__ __launch_bounds__(64) void block_prefix(const TokensSortParams p) {
     int carry = 0;
     for (int b = 0; b < p.blocks; b += 64) {
         int32_t *at = p.counts + (int64_t)(b + lane) * B + x;
-        const int mine = b + lane < p.blocks ? *at : 0;
-        int sum = mine;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int below = __shfl_up(sum, d);
-            if (lane >= d) sum += below;
-        }
+        const int mine = b + lane < p.blocks ? *at : 0, sum = lanes_upto(mine, lane);
         if (b + lane < p.blocks) *at = carry + sum - mine;
         carry += __shfl(sum, 63);
     }
@@ -132,12 +142,18 @@ __global__ __launch_bounds__(64) void block_prefix(const TokensSortParams p) {
 
 // ------------------------------------------------------------------ rows
 // 16 bytes at any address that is aligned to an element: rows need not be whole vectors, nor start on one.
-LCMA_DEV u32x4 load16(const char *at) {
-    u32x4 v;
-    __builtin_memcpy(&v, at, 16);
-    return v;
+// STREAM, bit 0: rows that are written, bit 1: rows in expert order that are read pass the caches by (kept there they would push each other out, and
+// be written back under the next call's reads).  Measured on dispatch, combine and both gradients: 16384 tokens x 4 x 4096 bf16 646 us, stores alone 610, both
+// 589; 4099 x 6 x 1543 fp32 198, 175, 184 (its rows, 152 MB, fit the Infinity Cache: the loads gain nothing by it).
+typedef u32x4 u32x4_any __attribute__((aligned(2)));
+template <int STREAM> LCMA_DEV u32x4 load16(const char *at) {
+    if constexpr (STREAM & 2) return __builtin_nontemporal_load((const u32x4_any *)at);
+    else return *(const u32x4_any *)at;
 }
-LCMA_DEV void store16(char *at, u32x4 v) { __builtin_memcpy(at, &v, 16); }
+template <int STREAM> LCMA_DEV void store16(char *at, u32x4 v) {
+    if constexpr (STREAM & 1) __builtin_nontemporal_store(v, (u32x4_any *)at);
+    else *(u32x4_any *)at = v;
+}
 
 template <class T> LCMA_DEV u32x4 packed(const float (&v)[16 / T::ES]) {
     u32x4 out;
@@ -165,7 +181,7 @@ template <class T> LCMA_DEV int64_t vector_at(int c, int H) {
     return (int64_t)(c * V + V <= H ? c * V : H - V) * T::ES;
 }
 
-template <class T> __global__ __launch_bounds__(256) void tokens_dispatch(const TokensRowsParams p) {
+template <class T, int STREAM> __global__ __launch_bounds__(256) void tokens_dispatch(const TokensRowsParams p) {
     constexpr int V = 16 / T::ES;
     const int64_t t = (int64_t)blockIdx.x * (256 >> p.lane_shift) + (threadIdx.x >> p.lane_shift);
     const int c = blockIdx.y * (1 << p.lane_shift) + (threadIdx.x & ((1 << p.lane_shift) - 1));
@@ -174,10 +190,10 @@ template <class T> __global__ __launch_bounds__(256) void tokens_dispatch(const 
     const int32_t *position = p.position + t * p.top_k;
     if (p.H >= V) {
         const int64_t at = vector_at<T>(c, p.H);
-        const u32x4 v = load16(x + at);
+        const u32x4 v = load16<0>(x + at);
         for (int j = 0; j < p.top_k; ++j) {
             const int row = position[j];
-            store16((char *)p.Y + (int64_t)(row < 0 ? -1 - row : row) * p.ldy_b + at, row < 0 ? u32x4{0, 0, 0, 0} : v);
+            store16<STREAM>((char *)p.Y + (int64_t)(row < 0 ? -1 - row : row) * p.ldy_b + at, row < 0 ? u32x4{0, 0, 0, 0} : v);
         }
     } else {
         for (int j = 0; j < p.top_k; ++j) {
@@ -188,29 +204,58 @@ template <class T> __global__ __launch_bounds__(256) void tokens_dispatch(const 
     }
 }
 
-template <class T> __global__ __launch_bounds__(256) void tokens_combine(const TokensRowsParams p) {
-    constexpr int V = 16 / T::ES;
+// The rows of up to four slots of a token from j on: which they are (-1: none), and their weights.
+struct Four {
+    int row[4];
+    float w[4];
+};
+LCMA_DEV Four four_slots(const int32_t *position, const float *weights, int j, int top_k) {
+    Four s;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        s.row[q] = j + q < top_k ? position[j + q] : -1;
+        s.w[q] = s.row[q] < 0 ? 0.f : weights ? weights[j + q] : 1.f;
+    }
+    return s;
+}
+
+// A thread: two vectors of a token's row, those of four slots in flight together.
+template <class T, int STREAM> __global__ __launch_bounds__(256) void tokens_combine(const TokensRowsParams p) {
+    constexpr int V = 16 / T::ES, N = 2;
     const int64_t t = (int64_t)blockIdx.x * (256 >> p.lane_shift) + (threadIdx.x >> p.lane_shift);
-    const int c = blockIdx.y * (1 << p.lane_shift) + (threadIdx.x & ((1 << p.lane_shift) - 1));
-    if (t >= p.tokens || c * V >= p.H) return;
+    const int lanes = 1 << p.lane_shift, c0 = blockIdx.y * (N * lanes) + (threadIdx.x & (lanes - 1));
+    if (t >= p.tokens || c0 * V >= p.H) return;
     char *y = (char *)p.Y + t * p.ldy_b;
     const int32_t *position = p.position + t * p.top_k;
     const float *weights = p.weights ? p.weights + t * p.top_k : nullptr;
     if (p.H >= V) {
-        const int64_t at = vector_at<T>(c, p.H);
-        float sum[V];
+        // (a second vector past the row is the first one again: the same values to the same place)
+        const int64_t at[N] = {vector_at<T>(c0, p.H), vector_at<T>((c0 + lanes) * V < p.H ? c0 + lanes : c0, p.H)};
+        float sum[N][V];
 #pragma unroll
-        for (int i = 0; i < V; ++i) sum[i] = 0.f;
-        for (int j = 0; j < p.top_k; ++j) {
-            const int row = position[j];
-            if (row < 0) continue;
-            const float w = weights ? weights[j] : 1.f;
-            float v[V];
-            Widen<T>::run(load16((const char *)p.X + (int64_t)row * p.ldx_b + at), v);
+        for (int n = 0; n < N; ++n)
 #pragma unroll
-            for (int i = 0; i < V; ++i) sum[i] += w * v[i];
+            for (int i = 0; i < V; ++i) sum[n][i] = 0.f;
+        for (int j = 0; j < p.top_k; j += 4) {
+            const Four s = four_slots(position, weights, j, p.top_k);
+            u32x4 raw[4][N];
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+#pragma unroll
+                for (int n = 0; n < N; ++n)
+                    raw[q][n] = s.row[q] >= 0 ? load16<STREAM>((const char *)p.X + (int64_t)s.row[q] * p.ldx_b + at[n]) : u32x4{0, 0, 0, 0};
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+#pragma unroll
+                for (int n = 0; n < N; ++n) {
+                    float v[V];
+                    Widen<T>::run(raw[q][n], v);
+#pragma unroll
+                    for (int i = 0; i < V; ++i) sum[n][i] += s.w[q] * v[i];
+                }
         }
-        store16(y + at, packed<T>(sum));
+#pragma unroll
+        for (int n = 0; n < N; ++n) store16<STREAM>(y + at[n], packed<T>(sum[n]));
     } else {
         for (int i = 0; i < p.H; ++i) {
             float sum = 0.f;
@@ -221,73 +266,139 @@ template <class T> __global__ __launch_bounds__(256) void tokens_combine(const T
     }
 }
 
-// A work-group per token: its four waves walk along the row, once for every slot.
-template <class T> __global__ __launch_bounds__(256) void tokens_combine_grad(const TokensRowsParams p) {
+// L threads per token, walking along the rows of four of its slots at a time.
+template <class T, int L, int STREAM> __global__ __launch_bounds__(256) void tokens_combine_grad(const TokensRowsParams p) {
     constexpr int V = 16 / T::ES;
-    __shared__ float part[4];
-    const int64_t t = blockIdx.x;
+    __shared__ float part[4][4];
+    const int64_t t = (int64_t)blockIdx.x * (256 / L) + threadIdx.x / L;
+    const int lane = threadIdx.x % L;
+    if (t >= p.tokens) return; // (L = 256: a work-group is a token)
     const char *dx = (const char *)p.dX + t * p.lddx_b;
-    for (int j = 0; j < p.top_k; ++j) {
-        const int pos = p.position[t * p.top_k + j];
-        const int64_t row = pos < 0 ? -1 - pos : pos;
-        const float w = pos < 0 ? 0.f : p.weights[t * p.top_k + j];
-        const char *x = (const char *)p.X + row * p.ldx_b;
-        char *y = (char *)p.Y + row * p.ldy_b;
-        float dot = 0.f;
-        if (pos < 0) {
-            for (int c = threadIdx.x; c < p.H; c += 256) put_element<T>(y + c * T::ES, 0.f);
-        } else if (p.H >= V) {
-            for (int c = threadIdx.x; c * V < p.H; c += 256) {
+    for (int j = 0; j < p.top_k; j += 4) {
+        const Four s = four_slots(p.position + t * p.top_k, p.weights + t * p.top_k, j, p.top_k);
+        const char *x[4];
+        char *y[4];
+        float dot[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int64_t row = j + q < p.top_k && s.row[q] < 0 ? -1 - (int64_t)s.row[q] : s.row[q]; // (zeros are written for a slot without an expert)
+            x[q] = (const char *)p.X + row * p.ldx_b;
+            y[q] = (char *)p.Y + row * p.ldy_b;
+        }
+        if (p.H >= V) {
+            for (int c = lane; c * V < p.H; c += L) {
                 const int64_t at = vector_at<T>(c, p.H);
                 const int again = c * V - (int)(at / T::ES); // elements that the vector before has counted
-                float g[V], v[V], out[V];
-                Widen<T>::run(load16(dx + at), g);
-                Widen<T>::run(load16(x + at), v);
+                float g[V];
+                u32x4 raw[4];
+                const u32x4 mine = load16<0>(dx + at);
 #pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    out[i] = w * g[i];
-                    if (i >= again) dot += g[i] * v[i];
-                }
-                store16(y + at, packed<T>(out));
+                for (int q = 0; q < 4; ++q) raw[q] = s.row[q] >= 0 ? load16<STREAM>(x[q] + at) : u32x4{0, 0, 0, 0};
+                Widen<T>::run(mine, g);
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    if (j + q < p.top_k) {
+                        float v[V], out[V];
+                        Widen<T>::run(raw[q], v);
+#pragma unroll
+                        for (int i = 0; i < V; ++i) {
+                            out[i] = s.row[q] >= 0 ? s.w[q] * g[i] : 0.f;
+                            if (i >= again && s.row[q] >= 0) dot[q] += g[i] * v[i];
+                        }
+                        store16<STREAM>(y[q] + at, packed<T>(out));
+                    }
             }
-        } else if ((int)threadIdx.x < p.H) {
-            const float g = element<T>(dx + threadIdx.x * T::ES);
-            dot = g * element<T>(x + threadIdx.x * T::ES);
-            put_element<T>(y + threadIdx.x * T::ES, w * g);
+        } else if (lane < p.H) {
+            const float g = element<T>(dx + lane * T::ES);
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                if (j + q < p.top_k) {
+                    if (s.row[q] >= 0) dot[q] = g * element<T>(x[q] + lane * T::ES);
+                    put_element<T>(y[q] + lane * T::ES, s.row[q] >= 0 ? s.w[q] * g : 0.f);
+                }
         }
 #pragma unroll
-        for (int d = 32; d; d >>= 1) dot += __shfl_xor(dot, d);
-        if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = dot;
-        __syncthreads();
-        if (threadIdx.x == 0) p.dW[t * p.top_k + j] = (part[0] + part[1]) + (part[2] + part[3]);
-        __syncthreads();
+        for (int q = 0; q < 4; ++q)
+#pragma unroll
+            for (int d = 32; d; d >>= 1) dot[q] += __shfl_xor(dot[q], d);
+        if constexpr (L > 64) {
+            if ((threadIdx.x & 63) == 0)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) part[q][threadIdx.x >> 6] = dot[q];
+            __syncthreads();
+            if (lane < 4 && j + lane < p.top_k) p.dW[t * p.top_k + j + lane] = (part[lane][0] + part[lane][1]) + (part[lane][2] + part[lane][3]);
+            __syncthreads();
+        } else {
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                if (lane == q && j + q < p.top_k) p.dW[t * p.top_k + j + q] = dot[q];
+        }
     }
 }
 
 } // namespace
 
 extern "C" int lcma_launch_tokens_sort(const lcma::TokensSortParams *p, void *stream) {
-    const size_t lds = (size_t)(kSortWaves + 1) * (p->experts + 1) * 4;
-    const dim3 block(64 * kSortWaves);
-    if (p->blocks == 1) {
-        tokens_sort<0><<<dim3(1), block, lds, (hipStream_t)stream>>>(*p);
+    const hipStream_t s = (hipStream_t)stream;
+    const int B = p->experts + 1;
+    constexpr int W = 8, R = kSortSlots / (64 * W);
+    const size_t lds = (size_t)B * (8 + 2 * W), lds_once = (size_t)B * (8 + 2 * 2 * W);
+    if (p->n <= kSortOnce) { // (few slots: half the waves, which start and meet sooner)
+        if (p->n <= kSortSlots) tokens_sort<0, W, R><<<dim3(1), dim3(64 * W), lds, s>>>(*p);
+        else tokens_sort<0, 2 * W, R><<<dim3(1), dim3(128 * W), lds_once, s>>>(*p);
         return (int)hipGetLastError();
     }
-    tokens_sort<1><<<dim3(p->blocks), block, lds, (hipStream_t)stream>>>(*p);
+    tokens_sort<1, W, R><<<dim3(p->blocks), dim3(64 * W), lds, s>>>(*p);
     if (const hipError_t e = hipGetLastError()) return (int)e;
-    block_prefix<<<dim3(p->experts + 1), dim3(64), 0, (hipStream_t)stream>>>(*p);
-    if (const hipError_t e = hipGetLastError()) return (int)e;
-    tokens_sort<2><<<dim3(p->blocks), block, lds, (hipStream_t)stream>>>(*p);
+    if (p->blocks > kSortBlocks) {
+        block_prefix<<<dim3(B), dim3(64), 0, s>>>(*p);
+        if (const hipError_t e = hipGetLastError()) return (int)e;
+        tokens_sort<3, W, R><<<dim3(p->blocks), dim3(64 * W), lds, s>>>(*p);
+    } else {
+        tokens_sort<2, W, R><<<dim3(p->blocks), dim3(64 * W), lds, s>>>(*p);
+    }
     return (int)hipGetLastError();
 }
 
-#define LCMA_TOKENS_ROWS(NAME, KERNEL, GRID)                                                                             \
-    extern "C" int lcma_launch_tokens_##NAME(const lcma::TokensRowsParams *p, int dtype, int gx, int gy, void *stream) { \
-        if (dtype == 0) KERNEL<F32><<<GRID, dim3(256), 0, (hipStream_t)stream>>>(*p);                                    \
-        else if (dtype == 1) KERNEL<BF16><<<GRID, dim3(256), 0, (hipStream_t)stream>>>(*p);                              \
-        else KERNEL<F16><<<GRID, dim3(256), 0, (hipStream_t)stream>>>(*p);                                               \
-        return (int)hipGetLastError();                                                                                   \
+#define LCMA_TYPES(LAUNCH)         \
+    if (dtype == 0) { LAUNCH(F32) } \
+    else if (dtype == 1) { LAUNCH(BF16) } \
+    else { LAUNCH(F16) }               \
+    return (int)hipGetLastError();
+
+extern "C" int lcma_launch_tokens_dispatch(const lcma::TokensRowsParams *p, int dtype, int gx, int gy, void *stream) {
+    const dim3 grid(gx, gy), block(256);
+    const hipStream_t s = (hipStream_t)stream;
+#define LCMA_DISPATCH(T)                                            \
+    if (p->stream) tokens_dispatch<T, 1><<<grid, block, 0, s>>>(*p); \
+    else tokens_dispatch<T, 0><<<grid, block, 0, s>>>(*p);
+    LCMA_TYPES(LCMA_DISPATCH)
+}
+
+extern "C" int lcma_launch_tokens_combine(const lcma::TokensRowsParams *p, int dtype, int gx, int gy, void *stream) {
+    const dim3 grid(gx, gy), block(256);
+    const hipStream_t s = (hipStream_t)stream;
+#define LCMA_COMBINE(T)                                                     \
+    if (p->stream == 3) tokens_combine<T, 3><<<grid, block, 0, s>>>(*p);     \
+    else if (p->stream == 2) tokens_combine<T, 2><<<grid, block, 0, s>>>(*p); \
+    else if (p->stream == 1) tokens_combine<T, 1><<<grid, block, 0, s>>>(*p); \
+    else tokens_combine<T, 0><<<grid, block, 0, s>>>(*p);
+    LCMA_TYPES(LCMA_COMBINE)
+}
+
+// a wave per token where its row is no more than 128 vectors, else a work-group; as many rows in expert order are written as are read
+extern "C" int lcma_launch_tokens_combine_grad(const lcma::TokensRowsParams *p, int dtype, int wave, void *stream) {
+    const hipStream_t s = (hipStream_t)stream;
+    const dim3 block(256), tokens(p->tokens), fours((p->tokens + 3) / 4);
+#define LCMA_GRAD(T)                                                                        \
+    if (wave) {                                                                             \
+        if (p->stream == 3) tokens_combine_grad<T, 64, 3><<<fours, block, 0, s>>>(*p);      \
+        else if (p->stream) tokens_combine_grad<T, 64, 1><<<fours, block, 0, s>>>(*p);      \
+        else tokens_combine_grad<T, 64, 0><<<fours, block, 0, s>>>(*p);                     \
+    } else {                                                                                \
+        if (p->stream == 3) tokens_combine_grad<T, 256, 3><<<tokens, block, 0, s>>>(*p);    \
+        else if (p->stream) tokens_combine_grad<T, 256, 1><<<tokens, block, 0, s>>>(*p);    \
+        else tokens_combine_grad<T, 256, 0><<<tokens, block, 0, s>>>(*p);                   \
     }
-LCMA_TOKENS_ROWS(dispatch, tokens_dispatch, dim3(gx, gy))
-LCMA_TOKENS_ROWS(combine, tokens_combine, dim3(gx, gy))
-LCMA_TOKENS_ROWS(combine_grad, tokens_combine_grad, dim3(gx, gy))
+    LCMA_TYPES(LCMA_GRAD)
+}

@@ -6,7 +6,7 @@
 extern "C" int lcma_launch_tokens_sort(const lcma::TokensSortParams *p, void *stream);
 extern "C" int lcma_launch_tokens_dispatch(const lcma::TokensRowsParams *p, int dtype, int gx, int gy, void *stream);
 extern "C" int lcma_launch_tokens_combine(const lcma::TokensRowsParams *p, int dtype, int gx, int gy, void *stream);
-extern "C" int lcma_launch_tokens_combine_grad(const lcma::TokensRowsParams *p, int dtype, int gx, int gy, void *stream);
+extern "C" int lcma_launch_tokens_combine_grad(const lcma::TokensRowsParams *p, int dtype, int wave, void *stream);
 
 using namespace lcma;
 
@@ -35,6 +35,9 @@ lcma_status check_rows(const char *who, int64_t tokens, int top_k, int64_t H, co
 }
 int64_t span(int64_t rows, int64_t ld, int64_t H, int dtype) { return rows > 0 ? ((rows - 1) * ld + H) * dtype_size(dtype) : 0; }
 
+// Which rows pass the caches by (csrc/lcma_tokens.hip): those that are written from a quarter of the Infinity Cache on, those that are read from all of it on.
+int streamed(int64_t written, int64_t read) { return (written >= ((int64_t)64 << 20) ? 1 : 0) | (read >= ((int64_t)256 << 20) ? 2 : 0); }
+
 // Threads along a row: as many as it has 16-byte vectors, up to a work-group.
 int lanes_of(int64_t vectors) {
     int s = 0;
@@ -46,8 +49,8 @@ int lanes_of(int64_t vectors) {
 
 extern "C" int64_t lcma_tokens_sort_workspace_bytes(int64_t tokens, int top_k, int experts) {
     if (!sort_range(tokens, top_k, experts)) return -1;
-    const int64_t blocks = (tokens * top_k + kSortSlots - 1) / kSortSlots;
-    return blocks > 1 ? (blocks + 1) * (experts + 1) * 4 : 0;
+    const int64_t n = tokens * top_k, blocks = (n + kSortSlots - 1) / kSortSlots;
+    return n > kSortOnce ? (blocks + 1) * (experts + 1) * 4 : 0;
 }
 
 extern "C" lcma_status lcma_tokens_sort(int64_t tokens, int top_k, int experts, const int32_t *ids, int32_t *order, int32_t *position, int32_t *offsets,
@@ -77,7 +80,7 @@ extern "C" lcma_status lcma_tokens_sort(int64_t tokens, int top_k, int experts, 
     p.counts = (int32_t *)workspace;
     p.n = (int32_t)n;
     p.experts = experts;
-    p.blocks = n ? (int32_t)((n + kSortSlots - 1) / kSortSlots) : 1;
+    p.blocks = (int32_t)((n + kSortSlots - 1) / kSortSlots);
     if (const int err = lcma_launch_tokens_sort(&p, stream)) return fail(LCMA_ERR_HIP, "%s: launch failed with HIP error %d", who, err);
     return LCMA_OK;
 }
@@ -102,6 +105,7 @@ extern "C" lcma_status lcma_tokens_dispatch(int64_t tokens, int top_k, int64_t H
     p.top_k = top_k;
     p.H = (int32_t)H;
     p.lane_shift = lanes_of(vectors);
+    p.stream = streamed(n * H * es, 0);
     const int64_t per = 256 >> p.lane_shift, gy = (vectors + (1 << p.lane_shift) - 1) >> p.lane_shift;
     if (gy > 65535) return fail(LCMA_ERR_SHAPE, "%s: a row is too long", who);
     if (const int err = lcma_launch_tokens_dispatch(&p, dtype, (int)((tokens + per - 1) / per), (int)gy, stream))
@@ -131,8 +135,9 @@ extern "C" lcma_status lcma_tokens_combine(int64_t tokens, int top_k, int64_t H,
     p.tokens = (int32_t)tokens;
     p.top_k = top_k;
     p.H = (int32_t)H;
-    p.lane_shift = lanes_of(vectors);
-    const int64_t per = 256 >> p.lane_shift, gy = (vectors + (1 << p.lane_shift) - 1) >> p.lane_shift;
+    p.lane_shift = lanes_of((vectors + 1) / 2); // (a thread takes two)
+    p.stream = streamed(tokens * H * es, n * H * es);
+    const int64_t per = 256 >> p.lane_shift, gy = (vectors + (2 << p.lane_shift) - 1) >> (p.lane_shift + 1);
     if (gy > 65535) return fail(LCMA_ERR_SHAPE, "%s: a row is too long", who);
     if (const int err = lcma_launch_tokens_combine(&p, dtype, (int)((tokens + per - 1) / per), (int)gy, stream))
         return fail(LCMA_ERR_HIP, "%s: launch failed with HIP error %d", who, err);
@@ -169,7 +174,8 @@ extern "C" lcma_status lcma_tokens_combine_grad(int64_t tokens, int top_k, int64
     p.tokens = (int32_t)tokens;
     p.top_k = top_k;
     p.H = (int32_t)H;
-    if (const int err = lcma_launch_tokens_combine_grad(&p, dtype, (int)tokens, 1, stream))
+    p.stream = streamed(n * H * es, n * H * es);
+    if (const int err = lcma_launch_tokens_combine_grad(&p, dtype, H * es <= 128 * 16, stream))
         return fail(LCMA_ERR_HIP, "%s: launch failed with HIP error %d", who, err);
     return LCMA_OK;
 }

@@ -25,7 +25,7 @@ CALLS = {
     "lcma_i8_gemm_experts": dict(rows=4, N=50, K=100, experts=3, offsets=AT["offsets"], Aq=AT["q"], Sa=AT["s"], Wq=AT["w"], Sw=AT["sw"], bias=AT["bias"], C=AT["c"], ldc=50,
                                  dtype=1, stream=None),
     "lcma_tokens_sort": dict(tokens=3000, top_k=2, experts=3, ids=AT["ids"], order=AT["order"], position=AT["position"], offsets=AT["offsets"], workspace=AT["space"],
-                             workspace_bytes=48, stream=None),
+                             workspace_bytes=64, stream=None),
     "lcma_tokens_dispatch": dict(tokens=4, top_k=2, H=100, X=AT["x"], ldx=100, dtype=1, position=AT["position"], Y=AT["c"], ldy=100, stream=None),
     "lcma_tokens_combine": dict(tokens=4, top_k=2, H=100, Y=AT["x"], ldy=100, dtype=1, position=AT["position"], weights=AT["weights"], X=AT["c"], ldx=100, stream=None),
     "lcma_tokens_combine_grad": dict(tokens=4, top_k=2, H=100, dX=AT["x"], lddx=100, Y=AT["c"], ldy=100, dtype=1, position=AT["position"], weights=AT["weights"], dY=AT["dy"],
@@ -43,8 +43,8 @@ BAD = {
                         ("SHAPE", dict(M=1 << 31)), ("SHAPE", dict(M=(1 << 31) - 1, N=1 << 20, ldc=1 << 20, C=1 << 60))],
     "lcma_i8_gemm_experts": [("ARG", dict(experts=0)), ("SHAPE", dict(experts=1025)), ("ARG", dict(offsets=None)), ("ARG", dict(offsets=AT["offsets"] + 2)), ("ARG", dict(C=AT["offsets"] + 14)),
                              ("ARG", dict(C=AT["w"] + 128 * 149))],
-    "lcma_tokens_sort": [("ARG", dict(tokens=-1)), ("ARG", dict(top_k=0)), ("ARG", dict(experts=0)), ("SHAPE", dict(experts=1025)), ("SHAPE", dict(tokens=1 << 30)), ("ARG", dict(workspace_bytes=47)),
-                         ("ARG", dict(workspace=None)), ("ARG", dict(order=AT["ids"] + 23996)), ("ARG", dict(offsets=AT["space"] + 44)), ("ARG", dict(position=AT["position"] + 1))] +
+    "lcma_tokens_sort": [("ARG", dict(tokens=-1)), ("ARG", dict(top_k=0)), ("ARG", dict(experts=0)), ("SHAPE", dict(experts=1025)), ("SHAPE", dict(tokens=1 << 30)), ("ARG", dict(workspace_bytes=63)),
+                         ("ARG", dict(workspace=None)), ("ARG", dict(order=AT["ids"] + 23996)), ("ARG", dict(offsets=AT["space"] + 60)), ("ARG", dict(position=AT["position"] + 1))] +
                         [("ARG", {k: None}) for k in ("ids", "order", "position", "offsets")],
     "lcma_tokens_dispatch": [("DTYPE", dict(dtype=9)), ("ARG", dict(tokens=-1)), ("ARG", dict(H=-1)), ("ARG", dict(top_k=0)), ("ARG", dict(X=None)), ("ARG", dict(Y=None)), ("ARG", dict(position=None)),
                              ("ARG", dict(ldx=99)), ("ARG", dict(ldy=99)), ("ARG", dict(Y=AT["x"] + 798)), ("ARG", dict(X=AT["x"] + 1)), ("SHAPE", dict(tokens=1 << 30)),
