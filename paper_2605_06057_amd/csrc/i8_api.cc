@@ -100,10 +100,10 @@ lcma_status gemm(const char *who, int64_t rows, int64_t N, int64_t K, int expert
     const int64_t tm = kTile[kernel].rows, tn = kTile[kernel].cols;
     // tiles along M, at most: every group may end in one of its own that is not full
     const int64_t nx = offsets ? rows / tm + (rows < experts ? rows : experts) : (rows + tm - 1) / tm, nz = (N + tn - 1) / tn, jobs = nx * nz;
-    if ((jobs + 8) * (kernel == kI8PingPong ? 1 : 512) >= kGridLimit / 2) return fail(LCMA_ERR_SHAPE, "%s: too many tiles for a launch", who);
+    if ((jobs + 8) * (kernel >= kI8Narrow ? 1 : 512) >= kGridLimit / 2) return fail(LCMA_ERR_SHAPE, "%s: too many tiles for a launch", who);
     p.nz = (int32_t)nz;
     p.panel = kernel <= kI8Few32 ? 1 : 8;
-    const int grid = kernel == kI8PingPong ? (int)(jobs < 256 ? jobs : 256) : (int)((jobs + 7) / 8 * 8);
+    const int grid = kernel >= kI8Narrow ? (int)(jobs < 256 ? jobs : 256) : (int)((jobs + 7) / 8 * 8);
     if (const int err = lcma_launch_i8_gemm(&p, kernel, dtype, grid, stream))
         return fail(LCMA_ERR_HIP, "%s: launch failed with HIP error %d", who, err);
     return LCMA_OK;

@@ -40,7 +40,7 @@ struct I8QuantParams {
 };
 
 // Kernels of the product: tiles of 16 x 16 and 32 x 32 (csrc/lcma_i8_few_rows.hpp), of the sizes named (csrc/lcma_i8.hpp), of 256 x 256 (csrc/lcma_i8_pingpong.hpp).
-enum { kI8Few16 = 0, kI8Few32, kI8Ring64, kI8Ring64x128, kI8Ring128, kI8Ring128x256, kI8PingPong, kI8Kernels };
+enum { kI8Few16 = 0, kI8Few32, kI8Ring64, kI8Ring64x128, kI8Ring128, kI8Narrow, kI8PingPong, kI8Kernels };
 
 // lcma_i8_gemm_nt, lcma_i8_gemm_experts (csrc/lcma_i8.hpp): rows of A in groups, group e times the weights of expert e.
 struct I8GemmParams {

@@ -1,6 +1,6 @@
 // Rows quantised to 8-bit integers, and the instances of the 8-bit-integer product (csrc/lcma_i8.hpp).
 #include "lcma_i8_few_rows.hpp"
-#include "lcma_i8_pingpong.hpp"
+#include "lcma_i8_narrow.hpp"
 #include "lcma_prepare_b.hpp"
 
 using namespace lcma;
@@ -150,8 +150,7 @@ template <class T, bool GATED, int L> __global__ __launch_bounds__(L < 256 ? 256
     }
 LCMA_I8_RING(64, 64, 2, 2, 4)
 LCMA_I8_RING(64, 128, 2, 2, 3)
-LCMA_I8_RING(128, 128, 2, 4, 4)
-LCMA_I8_RING(128, 256, 2, 4, 3)
+LCMA_I8_RING(128, 128, 4, 2, 4)
 #define LCMA_I8_FEW(T, WK, S)                                                                               \
     template <class OUT> __global__ __launch_bounds__(64 * WK) void i8_few_##T(const I8GemmParams p) {      \
         using G = I8FewRows<T, WK, S, OUT>;                                                                 \
@@ -160,6 +159,11 @@ LCMA_I8_RING(128, 256, 2, 4, 3)
     }
 LCMA_I8_FEW(16, 4, 2)
 LCMA_I8_FEW(32, 4, 2)
+template <class OUT> __global__ __launch_bounds__(512, 2) void i8_narrow(const I8GemmParams) {
+    using G = I8Narrow<128, 256, OUT>;
+    __shared__ __attribute__((aligned(16))) char smem[G::LDS_BYTES];
+    G::run((LCMA_LDS char *)smem);
+}
 template <class OUT> __global__ __launch_bounds__(512, 2) void i8_gemm_256(const I8GemmParams) {
     using G = I8PingPong<OUT>;
     __shared__ __attribute__((aligned(16))) char smem[G::LDS_BYTES];
@@ -199,7 +203,7 @@ extern "C" int lcma_launch_i8_gemm(const lcma::I8GemmParams *p, int kernel, int 
     case kI8Ring64: LCMA_I8(i8_ring_64_64, 256)
     case kI8Ring64x128: LCMA_I8(i8_ring_64_128, 256)
     case kI8Ring128: LCMA_I8(i8_ring_128_128, 512)
-    case kI8Ring128x256: LCMA_I8(i8_ring_128_256, 512)
+    case kI8Narrow: LCMA_I8(i8_narrow, 512)
     default: LCMA_I8(i8_gemm_256, 512)
     }
 #undef LCMA_I8

@@ -18,6 +18,13 @@ namespace lcma {
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x16 __attribute__((ext_vector_type(16)));
 
+// What a wave's lanes wrote to LDS is there for the reads of its other lanes behind this.  For the compiler: the LDS works in order, but without the barrier (which may
+// not be moved into a branch) a lane's reads can end up in front of what lanes on the other side of a branch write.
+LCMA_DEV void lanes_meet() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
 // A tile of C: rows row0 .. row0 + rows - 1 of A, all of expert `expert`, columns col0 .. of C.
 struct I8Place {
     int row0, rows, col0, expert;
@@ -148,6 +155,98 @@ template <class OUT> LCMA_DEV void i8_store4(char *at, f32x4 v, int cols) {
     }
 }
 
+// A wave's part of a tile (NMI x 2 blocks of 32 x 32 from (row, col) of the tile on) scaled, rounded and stored: through a strip of LDS that is the wave's own, SR
+// rows of 128 bytes, so that it leaves as whole lines, 16 bytes a lane.  FULL: all of it lies inside C.
+template <class OUT, int NMI, int SR, bool FULL>
+LCMA_DEV void i8_store_rows(const I8GemmParams &p, LCMA_LDS char *strip, const I8Place &at, int row, int col, const i32x16 (&acc)[NMI][2]) {
+    constexpr int ES = OUT::ES, BLOCKS = ES == 2 ? 2 : 1; // 32-column blocks in a strip's 128 bytes
+    // (the lane number anew, hidden: what derives from it would otherwise be kept in registers through the steps)
+    int lane = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));
+    asm volatile("" : "+v"(lane));
+    const int l32 = lane & 31, lh = lane >> 5, cols = p.N - at.col0 - col, left = at.rows - row;
+    if (!FULL && (cols <= 0 || left <= 0)) return;
+    const int64_t channel = (int64_t)at.expert * p.N + at.col0 + col;
+    auto vector = [&](const float *of) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<float *>(of + channel), 0, cols * 4, 0x00020000); };
+    const auto rsw = vector(p.SW), rbias = vector(p.bias ? p.bias : p.SW);
+    auto four = [&](__amdgpu_buffer_rsrc_t of, int n) { // (past the last column: zeros)
+        if constexpr (FULL) {
+            return __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(of, lh * 16, n * 4, 0));
+        } else {
+            f32x4 v;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(of, lh * 16 + i * 4, n * 4, 0));
+            return v;
+        }
+    };
+    f32x4 sw[2][4];
+    float sa[NMI];
+#pragma unroll
+    for (int mi = 0; mi < NMI; ++mi) {
+        const int m = mi * 32 + l32;
+        sa[mi] = p.SA[at.row0 + row + (FULL || m < left ? m : left - 1)];
+    }
+#pragma unroll
+    for (int ni = 0; ni < 2; ++ni)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) sw[ni][g] = four(rsw, ni * 32 + g * 8);
+    const int row8 = lane >> 3, ch = lane & 7; // a store: eight rows, eight lanes along each
+    char *c = (char *)p.C + ((int64_t)(at.row0 + row + row8) * p.ldc + at.col0 + col) * ES + ch * 16;
+    const int64_t down = 8 * p.ldc * ES;
+#pragma unroll
+    for (int mi = 0; mi < NMI; ++mi) {
+#pragma unroll
+        for (int n0 = 0; n0 < 2; n0 += BLOCKS) {
+            u32x4 out[2][4]; // (16 bit: the first two words)
+#pragma unroll
+            for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const int ni = n0 + b;
+                    f32x4 v;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) v[i] = (float)acc[mi][ni][g * 4 + i] * sa[mi] * sw[ni][g][i];
+                    if (p.bias) v += four(rbias, ni * 32 + g * 8);
+                    if constexpr (ES == 2) {
+                        out[b][g][0] = Round<OUT>::run(v[0]) | (Round<OUT>::run(v[1]) << 16);
+                        out[b][g][1] = Round<OUT>::run(v[2]) | (Round<OUT>::run(v[3]) << 16);
+                    } else {
+                        out[b][g] = __builtin_bit_cast(u32x4, v);
+                    }
+                }
+#pragma unroll
+            for (int h = 0; h < 32 / SR; ++h) {
+                if (SR == 32 || l32 / SR == h) {
+#pragma unroll
+                    for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+                        for (int g = 0; g < 4; ++g) {
+                            const int byte = (b * 32 + g * 8 + lh * 4) * ES;
+                            LCMA_LDS char *to = strip + l32 % SR * 128 + ((byte >> 4) ^ (l32 & 7)) * 16 + (byte & 15);
+                            if constexpr (ES == 2) *(LCMA_LDS uint64_t *)to = (uint64_t)out[b][g][1] << 32 | out[b][g][0];
+                            else *(LCMA_LDS u32x4 *)to = out[b][g];
+                        }
+                }
+                lanes_meet();
+#pragma unroll
+                for (int it = 0; it < SR / 8; ++it) {
+                    const u32x4 v = *(const LCMA_LDS u32x4 *)(strip + (it * 8 + row8) * 128 + (ch ^ row8) * 16);
+                    char *to = c + (h * (SR / 8) + it) * down + n0 * 32 * ES;
+                    const int n = n0 * 32 + ch * (16 / ES);
+                    if constexpr (FULL) __builtin_memcpy(to, &v, 16);
+                    else if (mi * 32 + h * SR + it * 8 + row8 < left && n < cols) i8_store16<OUT>(to, v, cols - n);
+                }
+                lanes_meet();
+            }
+        }
+        c += 4 * down;
+    }
+}
+template <class OUT, int NMI, int SR>
+LCMA_DEV void i8_store_part(const I8GemmParams &p, LCMA_LDS char *strip, const I8Place &at, int row, int col, const i32x16 (&acc)[NMI][2]) {
+    if (at.rows >= row + NMI * 32 && at.col0 + col + 64 <= p.N) i8_store_rows<OUT, NMI, SR, true>(p, strip, at, row, col, acc);
+    else i8_store_rows<OUT, NMI, SR, false>(p, strip, at, row, col, acc);
+}
+
 // One tile of TM x TN per work-group of WGM x WGN waves.  A step is 128 bytes of K; S stages of LDS hold the steps in flight, the loads (straight into LDS)
 // run S - 1 steps ahead and are waited for by count, and one barrier a step says that all waves' parts of it have landed and that all
 // have read the stage that is loaded anew.  What the depth is for: with two stages a step takes as long as a load does, about 0.8 us,
@@ -157,6 +256,7 @@ template <int TM, int TN, int WGM, int WGN, int S, class OUT> struct I8Ring {
     static constexpr int NT = 64 * WGM * WGN, NMI = TM / WGM / 32, NNI = TN / WGN / 32;
     static constexpr int A_STAGE = TM * 128, STAGE = (TM + TN) * 128, LDS_BYTES = S * STAGE;
     static constexpr int QA = TM * 8 / NT, QB = TN * 8 / NT;
+    static_assert(NNI != 2 || NT * 64 <= LDS_BYTES, "strips");
     static_assert(TM * 8 % NT == 0 && TN * 8 % NT == 0 && LDS_BYTES <= 160 * 1024 && (S == 3 || S == 4) && (S - 1) * (QA + QB) <= 63, "tile and wave grid");
 
     // 16-byte chunk c of a row sits at position c ^ (row / 2 % 8)
@@ -180,6 +280,11 @@ template <int TM, int TN, int WGM, int WGN, int S, class OUT> struct I8Ring {
 #pragma unroll
                 for (int v = 0; v < 16; ++v) acc[i][j][v] = 0;
         multiply(p, at, w, wm, wn, acc, lds, lds + STAGE, lds + 2 * STAGE, lds + (S == 4 ? 3 * STAGE : 0));
+        if constexpr (NNI == 2) {
+            __syncthreads(); // no load is in flight and every wave has read its last step: the strips take the place of the stages
+            i8_store_part<OUT, NMI, 32>(p, lds + w * 4096, at, wm * NMI * 32, wn * 64, acc);
+            return;
+        }
 #pragma unroll
         for (int i = 0; i < NMI; ++i) {
             const int row = (wm * NMI + i) * 32 + (lane & 31);

@@ -12,12 +12,13 @@
 
 namespace lcma {
 
-template <class OUT> struct I8PingPong {
-    static constexpr int TM = 256, TN = 256, NT = 512, WM = 128, WN = 64, NMI = 4, NNI = 2, ROW = 128, NK = 4;
-    static constexpr int HALF = 128 * ROW, STRIP = 32 * 128, LDS_BYTES = 8 * HALF + 8 * STRIP;
-    static_assert(LDS_BYTES <= 160 * 1024, "LDS budget of one CU");
-    static LCMA_DEV constexpr int swz(int row, int c) { return c ^ ((row >> 1) & 7); }
+// What the kernels have in common in which work-groups walk through tiles and two groups of waves take turns.
+struct I8Turns {
+    static constexpr int NT = 512, ROW = 128, NK = 4;
+    static LCMA_DEV constexpr int swz(int row, int c) { return c ^ ((row >> 1) & 7); } // position of 16-byte chunk c of a row in LDS
 
+    // The end of a slot.  (Not __syncthreads(): its fences would wait for the loads in flight.  The scheduling barriers keep matrix instructions, which
+    // touch no memory, in their slot.)
     static LCMA_DEV void slot_end() {
         __builtin_amdgcn_sched_barrier(0);
         asm volatile("" ::: "memory");
@@ -25,25 +26,13 @@ template <class OUT> struct I8PingPong {
         asm volatile("" ::: "memory");
         __builtin_amdgcn_sched_barrier(0);
     }
-    // lgkmcnt(0), vmcnt(12): the fragments are read, and all but the six youngest pairs of loads have landed
-    static LCMA_DEV void memory_slot_end() {
-        __builtin_amdgcn_sched_barrier(0);
-        __builtin_amdgcn_s_waitcnt(0x007C);
-        slot_end();
-    }
-
-    typedef const __attribute__((address_space(4))) I8GemmParams *Args;
 
     // The argument block is read where it is needed: kept in scalar registers through the steps, its fields would push the offsets of the loads out
     // of them (and the compiler then loops over the lanes of each load).
+    typedef const __attribute__((address_space(4))) I8GemmParams *Args;
     static LCMA_DEV I8GemmParams arguments(Args at) {
         asm volatile("" : "+s"(at));
         return I8GemmParams{at->A, at->W, at->SA, at->SW, at->bias, at->C, at->offsets, at->ldc, at->rows, at->N, at->pitch, at->experts, at->steps, at->nz, at->panel};
-    }
-
-    static LCMA_DEV const int8_t *uniform(const int8_t *at) {
-        const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)at), hi = __builtin_amdgcn_readfirstlane((uint32_t)((uintptr_t)at >> 32));
-        return (const int8_t *)((uint64_t)hi << 32 | lo);
     }
 
     // Where the operands of a tile are: bases, and extents in bytes (0: no tile, all reads are past the end).
@@ -51,6 +40,48 @@ template <class OUT> struct I8PingPong {
         const int8_t *a, *b;
         int a_bytes, b_bytes;
     };
+    static LCMA_DEV const int8_t *uniform(const int8_t *at) {
+        const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)at), hi = __builtin_amdgcn_readfirstlane((uint32_t)((uintptr_t)at >> 32));
+        return (const int8_t *)((uint64_t)hi << 32 | lo);
+    }
+    static LCMA_DEV __amdgpu_buffer_rsrc_t rsrc(const int8_t *base, int bytes) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t *>(base), 0, bytes, 0x00020000); }
+    template <int TM, int TN> static LCMA_DEV Source source(Args args, int nx, int jobs, int job, I8Place &at) {
+        Source s = {nullptr, nullptr, 0, 0};
+        at = I8Place{0, 0, 0, 0};
+        if (job < jobs) {
+            const I8GemmParams p = arguments(args);
+            int x, z;
+            i8_tile_of_job(nx, p.nz, p.panel, job, x, z);
+            at = i8_row_place<TM>(p, x);
+            at.col0 = z * TN;
+            const int cols = p.N - at.col0 < TN ? p.N - at.col0 : TN;
+            s.a = p.A + (int64_t)at.row0 * p.pitch;
+            s.a_bytes = at.rows * p.pitch;
+            s.b = p.W + ((int64_t)at.expert * p.N + at.col0) * p.pitch;
+            s.b_bytes = cols * p.pitch;
+        }
+        // (uniform anyway; said here so that the descriptors stay in scalar registers)
+        s.a = uniform(s.a);
+        s.b = uniform(s.b);
+        s.a_bytes = __builtin_amdgcn_readfirstlane(s.a_bytes);
+        s.b_bytes = __builtin_amdgcn_readfirstlane(s.b_bytes);
+        return s;
+    }
+    static constexpr uint32_t NONE = 1u << 30; // an offset past any extent
+};
+
+template <class OUT> struct I8PingPong : I8Turns {
+    static constexpr int TM = 256, TN = 256, WM = 128, WN = 64, NMI = 4, NNI = 2;
+    static constexpr int HALF = 128 * ROW, STRIP = 32 * 128;
+    static constexpr int LDS_BYTES = 8 * HALF + 8 * STRIP;
+    static_assert(LDS_BYTES <= 160 * 1024, "LDS budget of one CU");
+
+    // lgkmcnt(0), vmcnt(12): the fragments are read, and all but the six youngest pairs of loads have landed
+    static LCMA_DEV void memory_slot_end() {
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_waitcnt(0x007C);
+        slot_end();
+    }
 
     static LCMA_DEV void load_half(__amdgpu_buffer_rsrc_t r, LCMA_LDS char *dst, int wave_chunk, uint32_t voff, uint32_t off, uint32_t rows) {
 #pragma unroll
@@ -103,35 +134,13 @@ template <class OUT> struct I8PingPong {
         int job = unit < whole ? unit : (int)blockIdx.x;
         if (job >= jobs) return;
         const int pitch = args->pitch, ny = args->steps, n2 = (ny + 1) & ~1;
-        auto source = [&](int j, I8Place &at) {
-            Source s = {nullptr, nullptr, 0, 0};
-            at = I8Place{0, 0, 0, 0};
-            if (j < jobs) {
-                const I8GemmParams p = arguments(args);
-                int x, z;
-                i8_tile_of_job(nx, p.nz, p.panel, j, x, z);
-                at = i8_row_place<TM>(p, x);
-                at.col0 = z * TN;
-                const int cols = p.N - at.col0 < TN ? p.N - at.col0 : TN;
-                s.a = p.A + (int64_t)at.row0 * p.pitch;
-                s.a_bytes = at.rows * p.pitch;
-                s.b = p.W + ((int64_t)at.expert * p.N + at.col0) * p.pitch;
-                s.b_bytes = cols * p.pitch;
-            }
-            // (uniform anyway; said here so that the descriptors stay in scalar registers)
-            s.a = uniform(s.a);
-            s.b = uniform(s.b);
-            s.a_bytes = __builtin_amdgcn_readfirstlane(s.a_bytes);
-            s.b_bytes = __builtin_amdgcn_readfirstlane(s.b_bytes);
-            return s;
-        };
         uint32_t a_voff, b_voff;
         {
             const int row = tid >> 3, c = swz(row, tid & 7) * 16;
             a_voff = (uint32_t)row * pitch + c;
             b_voff = (uint32_t)((row >> 5) * 64 + (row & 31)) * pitch + c;
         }
-        const uint32_t rows = 128 * pitch, a_half = 64 * pitch, b_half = 32 * pitch, none = 1u << 30; // none: past any extent
+        const uint32_t rows = 128 * pitch, a_half = 64 * pitch, b_half = 32 * pitch;
         uint32_t a_frag[NK], b_frag[NK];
         {
             const int ar = wm * 64 + l32, br = wn * 32 + l32;
@@ -141,9 +150,8 @@ template <class OUT> struct I8PingPong {
                 b_frag[k] = br * ROW + swz(br, k * 2 + lh) * 16;
             }
         }
-        auto rsrc = [](const int8_t *base, int bytes) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t *>(base), 0, bytes, 0x00020000); };
         I8Place at, at_next;
-        Source cur = source(job, at), nxt;
+        Source cur = source<TM, TN>(args, nx, jobs, job, at), nxt;
         i32x4 fa0[2][NK], fa1[2][NK], fb0[NK], fb1[NK];
         i32x16 acc[NMI][NNI];
         {
@@ -155,7 +163,7 @@ template <class OUT> struct I8PingPong {
                 load_half(rb, B1, wave_chunk, b_voff, off + b_half, rows);
             };
             load_step(A00, A10, B00, B10, 0);
-            load_step(A01, A11, B01, B11, ny > 1 ? ROW : none);
+            load_step(A01, A11, B01, B11, ny > 1 ? ROW : NONE);
         }
         memory_slot_end();
         read_b(B00, b_frag, fb0);
@@ -164,7 +172,7 @@ template <class OUT> struct I8PingPong {
         while (true) {
             int next = job + units;
             if (next >= whole && job < whole && whole < jobs) next = whole + (int)blockIdx.x;
-            nxt = source(next, at_next);
+            nxt = source<TM, TN>(args, nx, jobs, next, at_next);
 #pragma unroll
             for (int mi = 0; mi < NMI; ++mi)
 #pragma unroll
@@ -199,7 +207,7 @@ template <class OUT> struct I8PingPong {
                 };
                 step(A00, A10, B00, B10, B01, off);
                 slot_end();
-                step(A01, A11, B01, B11, B00, (in ? y + 3 == ny : ny == 1) ? none : off + ROW); // (an odd number of steps: one of zeros behind)
+                step(A01, A11, B01, B11, B00, (in ? y + 3 == ny : ny == 1) ? NONE : off + ROW); // (an odd number of steps: one of zeros behind)
                 y += 2;
                 if (y >= n2) break;
                 slot_end();
@@ -218,81 +226,7 @@ template <class OUT> struct I8PingPong {
 
     static LCMA_DEV void store_tile(Args args, LCMA_LDS char *strip, const I8Place &at, int wm, int wn, const i32x16 (&acc)[NMI][NNI]) {
         const I8GemmParams p = arguments(args);
-        const bool full = at.rows >= wm * WM + WM && at.col0 + wn * WN + WN <= p.N;
-        if (full) store_rows<true>(p, strip, at, wm, wn, acc);
-        else store_rows<false>(p, strip, at, wm, wn, acc);
-    }
-
-    // FULL: all of the wave's part of the tile lies inside C.  (Else columns past N take the scale of the last one, and are not stored.)
-    template <bool FULL>
-    static LCMA_DEV void store_rows(const I8GemmParams &p, LCMA_LDS char *strip, const I8Place &at, int wm, int wn, const i32x16 (&acc)[NMI][NNI]) {
-        constexpr int ES = OUT::ES, BLOCKS = ES == 2 ? NNI : 1; // 32-column blocks in a strip's 128 bytes
-        // (the lane number anew, hidden: what derives from it would otherwise be kept in registers through the steps)
-        int lane = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));
-        asm volatile("" : "+v"(lane));
-        const int l32 = lane & 31, lh = lane >> 5, col = at.col0 + wn * WN, cols = p.N - col, left = at.rows - wm * WM;
-        if (!FULL && (cols <= 0 || left <= 0)) return;
-        const int64_t channel = (int64_t)at.expert * p.N + col;
-        auto vector = [&](const float *of) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<float *>(of + channel), 0, cols * 4, 0x00020000); };
-        const auto rsw = vector(p.SW), rbias = vector(p.bias ? p.bias : p.SW);
-        auto four = [&](__amdgpu_buffer_rsrc_t of, int n) { // (past the last column: zeros)
-            if constexpr (FULL) {
-                return __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(of, lh * 16, n * 4, 0));
-            } else {
-                f32x4 v;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) v[i] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(of, lh * 16 + i * 4, n * 4, 0));
-                return v;
-            }
-        };
-        f32x4 sw[NNI][4];
-        float sa[NMI];
-#pragma unroll
-        for (int mi = 0; mi < NMI; ++mi) {
-            const int row = mi * 32 + l32;
-            sa[mi] = p.SA[at.row0 + wm * WM + (FULL || row < left ? row : left - 1)];
-        }
-#pragma unroll
-        for (int ni = 0; ni < NNI; ++ni)
-#pragma unroll
-            for (int g = 0; g < 4; ++g) sw[ni][g] = four(rsw, ni * 32 + g * 8);
-        const int row8 = lane >> 3, ch = lane & 7; // a store: eight rows, eight lanes along each
-        char *c = (char *)p.C + ((int64_t)(at.row0 + wm * WM + row8) * p.ldc + col) * ES + ch * 16;
-        const int64_t down = 8 * p.ldc * ES;
-#pragma unroll
-        for (int mi = 0; mi < NMI; ++mi) {
-#pragma unroll
-            for (int n0 = 0; n0 < NNI; n0 += BLOCKS) {
-#pragma unroll
-                for (int ni = n0; ni < n0 + BLOCKS; ++ni)
-#pragma unroll
-                    for (int g = 0; g < 4; ++g) {
-                        f32x4 v;
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) v[i] = (float)acc[mi][ni][g * 4 + i] * sa[mi] * sw[ni][g][i];
-                        if (p.bias) v += four(rbias, ni * 32 + g * 8);
-                        const int byte = ((ni - n0) * 32 + g * 8 + lh * 4) * ES;
-                        LCMA_LDS char *to = strip + l32 * 128 + ((byte >> 4) ^ (l32 & 7)) * 16 + (byte & 15);
-                        if constexpr (ES == 2) {
-                            const uint32_t lo = Round<OUT>::run(v[0]) | (Round<OUT>::run(v[1]) << 16), hi = Round<OUT>::run(v[2]) | (Round<OUT>::run(v[3]) << 16);
-                            *(LCMA_LDS uint64_t *)to = (uint64_t)hi << 32 | lo;
-                        } else {
-                            *(LCMA_LDS f32x4 *)to = v;
-                        }
-                    }
-                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); // (for the compiler: the reads stay behind the writes)
-#pragma unroll
-                for (int it = 0; it < 4; ++it) {
-                    const u32x4 v = *(const LCMA_LDS u32x4 *)(strip + (it * 8 + row8) * 128 + (ch ^ row8) * 16);
-                    char *to = c + it * down + n0 * 32 * ES;
-                    const int n = n0 * 32 + ch * (16 / ES);
-                    if constexpr (FULL) __builtin_memcpy(to, &v, 16);
-                    else if (mi * 32 + it * 8 + row8 < left && n < cols) i8_store16<OUT>(to, v, cols - n);
-                }
-                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            }
-            c += 4 * down;
-        }
+        i8_store_part<OUT, NMI, 32>(p, strip, at, wm * WM, wn * WN, acc);
     }
 };
 
