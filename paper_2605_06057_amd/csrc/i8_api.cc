@@ -1,6 +1,7 @@
 // Host side of the 8-bit-integer linear layer, alone and over experts: argument checks, launches.
 #include "experts_host.h"
 
+#include <cmath>
 #include <cstring>
 
 extern "C" int lcma_launch_i8_quantize(const lcma::I8QuantParams *p, int dtype, int gated, int threads, void *stream);
@@ -51,17 +52,37 @@ lcma_status quantize(const char *who, int64_t rows, int64_t K, const void *X, in
     return LCMA_OK;
 }
 
-// The kernel for rows x N over `experts` groups.  Few rows for each: the weights are read once, K is split between waves; then the larger the
-// tile, the fewer bytes travel into LDS, and the fewer work-groups there are.
-const struct { int rows, cols; } kTile[] = {{16, 16}, {32, 32}, {64, 64}, {64, 128}, {128, 128}, {128, 256}, {256, 256}};
-int pick(int64_t rows, int64_t N, int experts) {
-    const int64_t r = (rows + experts - 1) / experts;
-    auto tiles = [&](int k) { return (r + kTile[k].rows - 1) / kTile[k].rows * experts * ((N + kTile[k].cols - 1) / kTile[k].cols); };
-    if (r <= 16) return kI8Few16;
-    if (tiles(kI8Ring64) < 192) return kI8Few32;
-    if (tiles(kI8Ring64) < 768) return kI8Ring64;
-    if (tiles(kI8PingPong) >= 128 && r >= 80) return kI8PingPong;
-    return tiles(kI8Ring128) >= 192 && r > 64 ? kI8Ring128 : kI8Ring64x128;
+// What a kernel takes, in us: `start` once; for every round of one tile per compute unit `end` and, for every step of 128 k, `step` with all units at work (the
+// chip's power and what the units share bound it then), `alone` with few; and no less than the bytes at `rate` GB/us take.  Fitted to 110 products and 90 over experts of
+// random sizes (1 to 8192 rows, 8 to 128 experts, 64 to 28672 columns, K 64 to 14336) timed on every kernel: a single time is predicted within 9 to
+// 15 % (root mean square), the kernel with the smallest prediction is on average 2.5 % slower than the fastest one, 36 % at worst.
+const struct Cost {
+    int rows, cols;
+    double start, alone, step, end, rate;
+    bool in_turn; // one work-group per compute unit: rounds count; else several, which share it
+} kCost[kI8Kernels] = {{16, 16, 3.3, 0.026, 0.051, 0.40, 9.5, false},  {32, 32, 2.8, 0.041, 0.107, 1.07, 8.3, false},   {64, 64, 2.7, 0.165, 0.215, 1.49, 7.2, false},
+                       {64, 128, 2.5, 0.292, 0.362, 1.50, 7.1, false}, {128, 128, 1.1, 0.387, 0.586, 3.29, 9.8, true},   {128, 256, 1.3, 0.506, 0.961, 4.88, 7.8, true},
+                       {256, 256, 2.0, 0.861, 1.41, 5.82, 6.5, true}};
+double predicted_us(const Cost &k, int64_t rows, int64_t N, int64_t K, int experts) {
+    // (the rows of each expert are known on the device alone: half a tile left over for each that can have any)
+    const double hit = experts < rows ? experts : (double)rows, nz = (double)((N + k.cols - 1) / k.cols);
+    double nx = (double)((rows + k.rows - 1) / k.rows);
+    if (experts > 1) nx = (double)rows / k.rows + 0.5 * hit > hit ? (double)rows / k.rows + 0.5 * hit : hit;
+    const double n = nx * nz / 256, steps = (double)((K + 127) / 128);
+    const double bytes = hit * N * K + (double)rows * K + 2.0 * rows * N, memory = k.start + bytes / (k.rate * 1e6);
+    const double whole = k.in_turn ? (double)(int64_t)n : n >= 1 ? n : 0, part = n - whole;
+    const double t = k.start + whole * (steps * k.step + k.end) + (part > 0 ? steps * (k.alone + (k.step - k.alone) * part) + k.end : 0);
+    return std::sqrt(std::sqrt(t * t * t * t + memory * memory * memory * memory));
+}
+int pick(int64_t rows, int64_t N, int64_t K, int experts) {
+    int best = 0;
+    double least = 0;
+    for (int k = 0; k < kI8Kernels; ++k)
+        if (const double t = predicted_us(kCost[k], rows, N, K, experts); k == 0 || t < least) {
+            least = t;
+            best = k;
+        }
+    return best;
 }
 
 lcma_status gemm(const char *who, int64_t rows, int64_t N, int64_t K, int experts, const int32_t *offsets, const void *Aq, const float *Sa,
@@ -96,14 +117,15 @@ lcma_status gemm(const char *who, int64_t rows, int64_t N, int64_t K, int expert
     p.pitch = (int32_t)pitch;
     p.experts = experts;
     p.steps = (int32_t)(pitch / 128);
-    const int forced = tuning_i8_kernel(), kernel = K == 0 ? kI8Ring64 : forced >= 0 ? forced : pick(rows, N, experts);
-    const int64_t tm = kTile[kernel].rows, tn = kTile[kernel].cols;
+    const int forced = tuning_i8_kernel(), kernel = K == 0 ? kI8Ring64 : forced >= 0 ? forced : pick(rows, N, K, experts);
+    const bool in_turn = kernel >= kI8Narrow; // (a work-group walks through tiles)
+    const int64_t tm = kCost[kernel].rows, tn = kCost[kernel].cols;
     // tiles along M, at most: every group may end in one of its own that is not full
     const int64_t nx = offsets ? rows / tm + (rows < experts ? rows : experts) : (rows + tm - 1) / tm, nz = (N + tn - 1) / tn, jobs = nx * nz;
-    if ((jobs + 8) * (kernel >= kI8Narrow ? 1 : 512) >= kGridLimit / 2) return fail(LCMA_ERR_SHAPE, "%s: too many tiles for a launch", who);
+    if ((jobs + 8) * (in_turn ? 1 : 512) >= kGridLimit / 2) return fail(LCMA_ERR_SHAPE, "%s: too many tiles for a launch", who);
     p.nz = (int32_t)nz;
     p.panel = kernel <= kI8Few32 ? 1 : 8;
-    const int grid = kernel >= kI8Narrow ? (int)(jobs < 256 ? jobs : 256) : (int)((jobs + 7) / 8 * 8);
+    const int grid = in_turn ? (int)(jobs < 256 ? jobs : 256) : (int)((jobs + 7) / 8 * 8);
     if (const int err = lcma_launch_i8_gemm(&p, kernel, dtype, grid, stream))
         return fail(LCMA_ERR_HIP, "%s: launch failed with HIP error %d", who, err);
     return LCMA_OK;

@@ -37,59 +37,62 @@ LCMA_DEV int i8_row(const I8GemmParams &p, int e) {
 }
 template <int TM> LCMA_DEV int i8_tiles(int begin, int end) { return end > begin ? (end - begin + TM - 1) / TM : 0; }
 
-// The tiles of TM rows of all groups, in expert order, every group in tiles of its own: how many there are, and the rows of tile x.  Every wave
-// by itself, a lane per expert.
-template <int TM> LCMA_DEV int i8_row_tiles(const I8GemmParams &p) {
-    if (!p.offsets) return (p.rows + TM - 1) / TM;
-    const int lane = threadIdx.x & 63;
-    int total = 0;
-    for (int e0 = 0; e0 < p.experts; e0 += 64) {
-        const int e = e0 + lane;
-        int tiles = 0;
-        if (e < p.experts) tiles = i8_tiles<TM>(i8_row(p, e), i8_row(p, e + 1));
-#pragma unroll
-        for (int d = 32; d; d >>= 1) tiles += __shfl_xor(tiles, d);
-        total += tiles;
-    }
-    return __builtin_amdgcn_readfirstlane(total);
+// Sum over the lanes up to and with this one.
+LCMA_DEV int lanes_upto(int v) {
+#define LCMA_FROM_LANES(CTRL, ROWS) v += __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 15, false)
+    LCMA_FROM_LANES(0x111, 15); // 1, 2, 4, 8 lanes below, inside the rows of 16
+    LCMA_FROM_LANES(0x112, 15);
+    LCMA_FROM_LANES(0x114, 15);
+    LCMA_FROM_LANES(0x118, 15);
+    LCMA_FROM_LANES(0x142, 10); // the last lane of the row below, in rows 1 and 3; of the half below, in the upper half
+    LCMA_FROM_LANES(0x143, 12);
+#undef LCMA_FROM_LANES
+    return v;
 }
-template <int TM> LCMA_DEV I8Place i8_row_place(const I8GemmParams &p, int x) {
-    I8Place at = {x * TM, p.rows - x * TM, 0, 0};
-    if (p.offsets) {
-        const int lane = threadIdx.x & 63;
-        int before = 0;
-        for (int e0 = 0; e0 < p.experts; e0 += 64) {
-            const int e = e0 + lane;
-            int begin = 0, end = 0;
-            if (e < p.experts) {
-                begin = i8_row(p, e);
-                end = i8_row(p, e + 1);
-            }
-            const int tiles = i8_tiles<TM>(begin, end);
-            int upto = tiles;
-#pragma unroll
-            for (int d = 1; d < 64; d <<= 1) {
-                const int below = __shfl_up(upto, d);
-                if (lane >= d) upto += below;
-            }
-            upto += before;
-            const uint64_t past = __ballot(x < upto);
-            if (past) {
-                const int l = __builtin_ctzll(past);
-                const int skip = (x - (__shfl(upto, l) - __shfl(tiles, l))) * TM;
-                at.expert = e0 + l;
-                at.row0 = __shfl(begin, l) + skip;
-                at.rows = __shfl(end, l) - at.row0;
-                break;
-            }
-            before = __shfl(upto, 63);
+
+// The tiles of TM rows of all groups, in expert order, every group in tiles of its own: how many there are, and the rows of tile x.  Every wave
+// by itself, a lane per expert; the first 64 experts are kept, which are mostly all.
+template <int TM> struct I8Rows {
+    int begin, end, upto; // rows of this lane's expert, tiles up to and with it
+    int tiles;
+
+    LCMA_DEV void experts_from(const I8GemmParams &p, int e0, int before) {
+        const int e = e0 + (int)(threadIdx.x & 63);
+        begin = end = 0;
+        if (e < p.experts) {
+            begin = i8_row(p, e);
+            end = i8_row(p, e + 1);
+        }
+        upto = before + lanes_upto(i8_tiles<TM>(begin, end));
+    }
+    LCMA_DEV I8Rows(const I8GemmParams &p) {
+        if (!p.offsets) {
+            tiles = (p.rows + TM - 1) / TM;
+            return;
+        }
+        experts_from(p, 0, 0);
+        tiles = __builtin_amdgcn_readlane(upto, 63);
+        for (int e0 = 64; e0 < p.experts; e0 += 64) {
+            I8Rows more = *this;
+            more.experts_from(p, e0, tiles);
+            tiles = __builtin_amdgcn_readlane(more.upto, 63);
         }
     }
-    at.row0 = __builtin_amdgcn_readfirstlane(at.row0);
-    at.rows = __builtin_amdgcn_readfirstlane(at.rows < TM ? at.rows : TM);
-    at.expert = __builtin_amdgcn_readfirstlane(at.expert);
-    return at;
-}
+    LCMA_DEV I8Place place(const I8GemmParams &p, int x) const {
+        if (!p.offsets) return {x * TM, p.rows - x * TM < TM ? p.rows - x * TM : TM, 0, 0};
+        I8Rows at = *this;
+        int e0 = 0;
+        uint64_t past;
+        while (!(past = __ballot(x < at.upto)) && e0 + 64 < p.experts) {
+            e0 += 64;
+            at.experts_from(p, e0, __builtin_amdgcn_readlane(at.upto, 63));
+        }
+        const int l = past ? __builtin_ctzll(past) : 63;
+        const int begin = __builtin_amdgcn_readlane(at.begin, l), end = __builtin_amdgcn_readlane(at.end, l);
+        const int row0 = begin + (x - (__builtin_amdgcn_readlane(at.upto, l) - i8_tiles<TM>(begin, end))) * TM;
+        return {row0, end - row0 < TM ? end - row0 : TM, 0, e0 + l};
+    }
+};
 
 // Tile j of nx x nz: they run down the rows inside column panels of `panel` tiles.
 LCMA_DEV void i8_tile_of_job(int nx, int nz, int panel, int j, int &x, int &z) {
@@ -265,12 +268,13 @@ template <int TM, int TN, int WGM, int WGN, int S, class OUT> struct I8Ring {
     static LCMA_DEV void run(const I8GemmParams &p, LCMA_LDS char *lds) {
         const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = w / WGN, wn = w % WGN;
         i8_zero_behind<OUT>(p, gridDim.x, NT);
-        const int nx = i8_row_tiles<TM>(p), jobs = nx * p.nz, per = (jobs + 7) / 8;
+        const I8Rows<TM> groups(p);
+        const int nx = groups.tiles, jobs = nx * p.nz, per = (jobs + 7) / 8;
         const int job = (blockIdx.x & 7) * per + (blockIdx.x >> 3); // an eighth of the tiles to every XCD
         if ((int)(blockIdx.x >> 3) >= per || job >= jobs) return;
         int x, z;
         i8_tile_of_job(nx, p.nz, p.panel, job, x, z);
-        I8Place at = i8_row_place<TM>(p, x);
+        I8Place at = groups.place(p, x);
         at.col0 = z * TN;
         i32x16 acc[NMI][NNI];
 #pragma unroll

@@ -39,7 +39,7 @@ template <int TM, int TN, class OUT> struct I8Narrow : I8Turns {
         {
             const I8GemmParams p = arguments(args);
             i8_zero_behind<OUT>(p, gridDim.x, NT);
-            nx = i8_row_tiles<TM>(p);
+            nx = I8Rows<TM>(p).tiles;
             jobs = nx * p.nz;
         }
         const int units = gridDim.x, per = units >> 3; // rounds of one tile per work-group, as in I8PingPong

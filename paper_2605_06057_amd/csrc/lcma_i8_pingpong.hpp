@@ -52,7 +52,7 @@ struct I8Turns {
             const I8GemmParams p = arguments(args);
             int x, z;
             i8_tile_of_job(nx, p.nz, p.panel, job, x, z);
-            at = i8_row_place<TM>(p, x);
+            at = I8Rows<TM>(p).place(p, x);
             at.col0 = z * TN;
             const int cols = p.N - at.col0 < TN ? p.N - at.col0 : TN;
             s.a = p.A + (int64_t)at.row0 * p.pitch;
@@ -123,7 +123,7 @@ template <class OUT> struct I8PingPong : I8Turns {
         {
             const I8GemmParams p = arguments(args);
             i8_zero_behind<OUT>(p, gridDim.x, NT);
-            nx = i8_row_tiles<TM>(p);
+            nx = I8Rows<TM>(p).tiles;
             jobs = nx * p.nz;
         }
         const int units = gridDim.x;
