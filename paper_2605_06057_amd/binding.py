@@ -1,4 +1,4 @@
-"""Thin ctypes binding of liblcma.so: argument marshalling only, same names as include/lcma.h.
+"""Thin binding of liblcma.so: argument marshalling only (ctypes; the 8-bit-integer calls and the tokens' through _calls.so), same names as include/lcma.h.
 
 Every step of the GEMM runs in the library's HIP kernels.  There is no CPU or PyTorch
 fallback: if the shared library is missing, loading raises.
@@ -10,6 +10,7 @@ import os
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "liblcma.so")
+CALLS_PATH = os.path.join(_HERE, "_calls.so")
 
 LCMA_OK = 0
 STATUS_NAMES = ["OK", "ERR_ARG", "ERR_IO", "ERR_PARSE", "ERR_BRENT", "ERR_SHAPE", "ERR_DTYPE",
@@ -147,8 +148,6 @@ def lib() -> ctypes.CDLL:
         L.lcma_tokens_dispatch.argtypes = [i64, i32, i64, vp, i64, i32, vp, vp, i64, vp]
         L.lcma_tokens_combine.argtypes = [i64, i32, i64, vp, i64, i32, vp, vp, vp, i64, vp]
         L.lcma_tokens_combine_grad.argtypes = [i64, i32, i64, vp, i64, vp, i64, i32, vp, vp, vp, i64, vp, vp]
-        global _i8, _i32, _f32
-        _i8, _i32, _f32 = torch.int8, torch.int32, torch.float32
         _lib = L
         # schemes that kernels were generated for beyond the paper's three
         for sid in range(4, int(L.lcma_scheme_id_max()) + 1):
@@ -222,21 +221,16 @@ def _dtype_of(t) -> int:
     return _dtypes[t.dtype]
 
 
-def _stream_on(device: int) -> int:
-    """Handle of the current stream on that device."""
+def _stream_of(t) -> int:
+    """Handle of the current stream on the tensor's device."""
     global _raw_stream
     if _raw_stream is None:
         import torch
         _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
-    return _raw_stream(device)
-
-
-def _stream_of(t) -> int:
-    """Handle of the current stream on the tensor's device."""
     device = t.get_device()
     if device < 0:
         raise ValueError(f"expected a tensor on the GPU, got one on {t.device}")
-    return _stream_on(device)
+    return _raw_stream(device)
 
 
 def _marshal(A, B, C, b_nk: bool = False):
@@ -530,30 +524,28 @@ def lcma_fp8_gemm_lcma(A, Wp, C, scheme: Scheme, workspace):
 
 
 # ---------------------------------------------------------------- 8-bit integers (a scale for each row of either operand)
-# As for the products above, what a call does here before the C entry point counts for small sizes (a launch takes 2.9 us, the call 0.5): every tensor is
-# asked for its type, shape, layout and device once, and nothing is looked up twice.
-_i8 = _i32 = _f32 = None  # torch's types, from the library's loading on
+# These calls and the tokens' below are marshalled by _calls.so (csrc/calls.cc): in Python the checks of five to seven tensors took 2 to 3 us of a call, as long as
+# its launch.  What is left out of the arguments is allocated here.
+_calls = None
 
 
-def _is(t, dtype, shape, device: int) -> bool:
-    """Whether t is a contiguous tensor of that type and shape on that GPU."""
-    return t.dtype is dtype and t.shape == shape and t.is_contiguous() and t.get_device() == device
+def _native():
+    """The loaded _calls.so (raises if it has not been built: run `python -m paper_2605_06057_amd.build`)."""
+    global _calls
+    if _calls is None:
+        lib()
+        if not os.path.exists(CALLS_PATH):
+            raise FileNotFoundError(f"{CALLS_PATH} is missing: build it with `python -m paper_2605_06057_amd.build`")
+        import importlib.util
+        spec = importlib.util.spec_from_file_location(__package__ + "._calls", CALLS_PATH)
+        _calls = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(_calls)
+    return _calls
 
 
-def _has(t, dtype, n: int, device: int) -> bool:
-    """Whether t is n values of that type, one behind the other, on that GPU (a third of the time that a shape takes to compare)."""
-    return t.dtype is dtype and t.numel() == n and t.is_contiguous() and t.get_device() == device
-
-
-def _rows_of(t, shape, device: int) -> bool:
-    """Whether t is a matrix of that shape on that GPU with neighbouring elements in a row."""
-    return t.shape == shape and (t.stride(1) == 1 or shape[1] <= 1) and t.get_device() == device
-
-
-def _ld(t, cols: int) -> int:
-    """Leading dimension; that of a single row, whose stride says nothing, is the row."""
-    ld = t.stride(0)
-    return ld if ld >= cols or t.shape[0] > 1 else cols
+def _empty(like, *shape, dtype=None):
+    import torch
+    return torch.empty(shape, dtype=dtype and getattr(torch, dtype) or like.dtype, device=like.device)
 
 
 def lcma_i8_code_pitch(K: int) -> int:
@@ -563,48 +555,29 @@ def lcma_i8_code_pitch(K: int) -> int:
 def lcma_i8_quantize(X, Q=None, S=None, gated: bool = False):
     """Codes (rows x code pitch, int8) and scales (rows, fp32) of the device tensor X (rows x K; gated: rows x 2 K, of
     silu(first half) * second half)."""
-    L = _lib or lib()
-    rows, width = shape = X.shape
-    assert not (gated and width % 2), "expected rows x 2 K"
-    K, device = width // 2 if gated else width, X.get_device()
-    pitch = (K + 127) // 128 * 128  # lcma_i8_code_pitch
     if Q is None:
-        Q = X.new_empty((rows, pitch), dtype=_i8)
+        Q = _empty(X, X.shape[0], lcma_i8_code_pitch(X.shape[1] // 2 if gated else X.shape[1]), dtype="int8")
     if S is None:
-        S = X.new_empty((rows,), dtype=_f32)
-    assert device >= 0 and _rows_of(X, shape, device) and _is(Q, _i8, (rows, pitch), device) and _has(S, _f32, rows, device)
-    if status := L.lcma_i8_quantize(rows, K, X.data_ptr(), _ld(X, width), _dtype_of(X), gated, Q.data_ptr(), S.data_ptr(), _stream_on(device)):
+        S = _empty(X, X.shape[0], dtype="float32")
+    if status := (_calls or _native()).i8_quantize(X, Q, S, gated):
         _check(status)
     return Q, S
 
 
 def lcma_i8_quantize_dispatch(X, position, Q=None, S=None):
     """lcma_i8_quantize of the tokens' rows X (tokens x K) into expert order: Q, S have a row for every slot of position (tokens x top_k)."""
-    L = _lib or lib()
-    tokens, K = shape = X.shape
-    top_k, device = position.shape[1], X.get_device()
-    n, pitch = tokens * top_k, (K + 127) // 128 * 128  # lcma_i8_code_pitch
     if Q is None:
-        Q = X.new_empty((n, pitch), dtype=_i8)
+        Q = _empty(X, position.numel(), lcma_i8_code_pitch(X.shape[1]), dtype="int8")
     if S is None:
-        S = X.new_empty((n,), dtype=_f32)
-    assert device >= 0 and _rows_of(X, shape, device) and _is(position, _i32, (tokens, top_k), device)
-    assert _is(Q, _i8, (n, pitch), device) and _has(S, _f32, n, device)
-    if status := L.lcma_i8_quantize_dispatch(tokens, K, X.data_ptr(), _ld(X, K), _dtype_of(X), top_k, position.data_ptr(), Q.data_ptr(), S.data_ptr(),
-                                           _stream_on(device)):
+        S = _empty(X, position.numel(), dtype="float32")
+    if status := (_calls or _native()).i8_quantize_dispatch(X, position, Q, S):
         _check(status)
     return Q, S
 
 
 def lcma_i8_gemm_nt(Aq, Sa, Wq, Sw, C, K: int, bias=None):
     """C (M x N) = the product of the codes Aq (M x pitch) and Wq (N x pitch) over K, times the scales of rows and channels, plus bias."""
-    L = _lib or lib()
-    M, N = shape = C.shape
-    pitch, device = (K + 127) // 128 * 128, C.get_device()  # lcma_i8_code_pitch
-    assert device >= 0 and _is(Aq, _i8, (M, pitch), device) and _is(Wq, _i8, (N, pitch), device) and _has(Sa, _f32, M, device) and _has(Sw, _f32, N, device)
-    assert _rows_of(C, shape, device) and (bias is None or _has(bias, _f32, N, device))
-    if status := L.lcma_i8_gemm_nt(M, N, K, Aq.data_ptr(), Sa.data_ptr(), Wq.data_ptr(), Sw.data_ptr(), None if bias is None else bias.data_ptr(),
-                                 C.data_ptr(), _ld(C, N), _dtype_of(C), _stream_on(device)):
+    if status := (_calls or _native()).i8_gemm_nt(Aq, Sa, Wq, Sw, C, K, bias):
         _check(status)
     return C
 
@@ -612,14 +585,7 @@ def lcma_i8_gemm_nt(Aq, Sa, Wq, Sw, C, K: int, bias=None):
 def lcma_i8_gemm_experts(Aq, Sa, offsets, Wq, Sw, C, K: int, bias=None):
     """lcma_i8_gemm_nt over experts: rows offsets[e] .. offsets[e + 1] - 1 times the weights Wq[e] (experts x N x pitch), Sw and bias experts x N;
     rows of C behind the last expert's are set to zero."""
-    L = _lib or lib()
-    rows, N = shape = C.shape
-    experts, pitch, device = Wq.shape[0], (K + 127) // 128 * 128, C.get_device()  # lcma_i8_code_pitch
-    assert device >= 0 and _is(Aq, _i8, (rows, pitch), device) and _is(Wq, _i8, (experts, N, pitch), device) and _has(Sa, _f32, rows, device)
-    assert _is(Sw, _f32, (experts, N), device) and _has(offsets, _i32, experts + 1, device)
-    assert _rows_of(C, shape, device) and (bias is None or _is(bias, _f32, (experts, N), device))
-    if status := L.lcma_i8_gemm_experts(rows, N, K, experts, offsets.data_ptr(), Aq.data_ptr(), Sa.data_ptr(), Wq.data_ptr(), Sw.data_ptr(),
-                                      None if bias is None else bias.data_ptr(), C.data_ptr(), _ld(C, N), _dtype_of(C), _stream_on(device)):
+    if status := (_calls or _native()).i8_gemm_experts(Aq, Sa, offsets, Wq, Sw, C, K, bias):
         _check(status)
     return C
 
@@ -632,70 +598,44 @@ def lcma_tokens_sort_workspace_bytes(tokens: int, top_k: int, experts: int) -> i
 def lcma_tokens_sort(ids, experts: int, order=None, position=None, offsets=None, workspace=None):
     """order (tokens * top_k), position (tokens x top_k) and offsets (experts + 1), int32, of the slots of ids (tokens x top_k expert numbers,
     int32); slots with another number than 0 .. experts - 1 come last, with a negative position."""
-    L = _lib or lib()
-    tokens, top_k = shape = ids.shape
-    n, device = tokens * top_k, ids.get_device()
     if order is None:
-        order = ids.new_empty((n,))
+        order = _empty(ids, ids.numel(), dtype="int32")
     if position is None:
-        position = ids.new_empty(shape)
+        position = _empty(ids, *ids.shape, dtype="int32")
     if offsets is None:
-        offsets = ids.new_empty((experts + 1,))
-    if workspace is None and (need := lcma_tokens_sort_workspace_bytes(tokens, top_k, experts)) > 0:
-        workspace = ids.new_empty(((need + 3) // 4,))
-    space, size = None, 0
-    if workspace is not None:
-        assert workspace.is_contiguous() and workspace.get_device() == device
-        space, size = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-    assert device >= 0 and _is(ids, _i32, shape, device) and _has(order, _i32, n, device) and _is(position, _i32, shape, device) and _has(offsets, _i32, experts + 1, device)
-    if status := L.lcma_tokens_sort(tokens, top_k, experts, ids.data_ptr(), order.data_ptr(), position.data_ptr(), offsets.data_ptr(), space, size,
-                                  _stream_on(device)):
+        offsets = _empty(ids, max(experts, 0) + 1, dtype="int32")
+    if workspace is None and (need := lcma_tokens_sort_workspace_bytes(*ids.shape, experts)) > 0:
+        workspace = _empty(ids, (need + 3) // 4, dtype="int32")
+    if status := (_calls or _native()).tokens_sort(ids, experts, order, position, offsets, workspace):
         _check(status)
     return order, position, offsets
 
 
 def lcma_tokens_dispatch(X, position, Y=None):
     """Y[position[t, j]] = X[t]: the tokens' rows in expert order (rows of slots without an expert: zeros)."""
-    L = _lib or lib()
-    tokens, H = shape = X.shape
-    top_k, device = position.shape[1], X.get_device()
     if Y is None:
-        Y = X.new_empty((tokens * top_k, H))
-    assert device >= 0 and _rows_of(X, shape, device) and _rows_of(Y, (tokens * top_k, H), device) and X.dtype is Y.dtype and _is(position, _i32, (tokens, top_k), device)
-    if status := L.lcma_tokens_dispatch(tokens, top_k, H, X.data_ptr(), _ld(X, H), _dtype_of(X), position.data_ptr(), Y.data_ptr(), _ld(Y, H), _stream_on(device)):
+        Y = _empty(X, position.numel(), X.shape[1])
+    if status := (_calls or _native()).tokens_dispatch(X, position, Y):
         _check(status)
     return Y
 
 
 def lcma_tokens_combine(Y, position, weights=None, X=None):
     """X[t] = sum over j of weights[t, j] * Y[position[t, j]] (weights None: ones, which is the gradient of lcma_tokens_dispatch)."""
-    L = _lib or lib()
-    tokens, top_k = slots = position.shape
-    H, device = Y.shape[1], Y.get_device()
     if X is None:
-        X = Y.new_empty((tokens, H))
-    assert device >= 0 and _rows_of(Y, (tokens * top_k, H), device) and _rows_of(X, (tokens, H), device) and X.dtype is Y.dtype and _is(position, _i32, slots, device)
-    assert weights is None or _is(weights, _f32, slots, device)
-    if status := L.lcma_tokens_combine(tokens, top_k, H, Y.data_ptr(), _ld(Y, H), _dtype_of(Y), position.data_ptr(),
-                                     None if weights is None else weights.data_ptr(), X.data_ptr(), _ld(X, H), _stream_on(device)):
+        X = _empty(Y, position.shape[0], Y.shape[1])
+    if status := (_calls or _native()).tokens_combine(Y, position, weights, X):
         _check(status)
     return X
 
 
 def lcma_tokens_combine_grad(dX, Y, position, weights, dY=None, dweights=None):
     """Gradient of lcma_tokens_combine from dX (tokens x H): dY (rows in expert order, in Y's type) and dweights (tokens x top_k, fp32)."""
-    L = _lib or lib()
-    tokens, top_k = slots = position.shape
-    H, device = Y.shape[1], Y.get_device()
-    n = tokens * top_k
     if dY is None:
-        dY = Y.new_empty((n, H))
+        dY = _empty(Y, *Y.shape)
     if dweights is None:
-        dweights = Y.new_empty(slots, dtype=_f32)
-    assert device >= 0 and _rows_of(dX, (tokens, H), device) and _rows_of(Y, (n, H), device) and _rows_of(dY, (n, H), device) and dX.dtype is Y.dtype is dY.dtype
-    assert _is(position, _i32, slots, device) and _is(weights, _f32, slots, device) and _is(dweights, _f32, slots, device)
-    if status := L.lcma_tokens_combine_grad(tokens, top_k, H, dX.data_ptr(), _ld(dX, H), Y.data_ptr(), _ld(Y, H), _dtype_of(Y), position.data_ptr(),
-                                          weights.data_ptr(), dY.data_ptr(), _ld(dY, H), dweights.data_ptr(), _stream_on(device)):
+        dweights = _empty(Y, *position.shape, dtype="float32")
+    if status := (_calls or _native()).tokens_combine_grad(dX, Y, position, weights, dY, dweights):
         _check(status)
     return dY, dweights
 

@@ -12,6 +12,7 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(PKG, "csrc")
 GEN = os.path.join(CSRC, "generated")
 LIB = os.path.join(PKG, "liblcma.so")
+CALLS = os.path.join(PKG, "_calls.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 DEVICE_FLAGS = ["--offload-arch=gfx950", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 COMMON = ["-O3", "-std=c++17", "-fPIC", "-I", CSRC, "-I", GEN, "-Wno-unused-command-line-argument"]
@@ -38,6 +39,29 @@ def _compile(src: str, obj: str, deps: list[str], force: bool) -> str:
     return f"compiled {time.time() - t0:5.1f}s  {os.path.basename(src)}" + (("\n" + err) if err.strip() else "")
 
 
+def _build_calls(force: bool) -> str:
+    """_calls.so, the Python side of the calls in csrc/calls.cc, against the torch that is installed and liblcma.so beside it."""
+    src = os.path.join(CSRC, "calls.cc")
+    if not force and _newer(CALLS, [src, os.path.join(PKG, "..", "include", "lcma.h")]):
+        return "up to date  calls.cc"
+    import sysconfig
+
+    import torch
+    from torch.utils.cpp_extension import include_paths
+    t0 = time.time()
+    libs = os.path.join(os.path.dirname(torch.__file__), "lib")
+    rocm = os.path.dirname(os.path.dirname(HIPCC))
+    tmp = CALLS + f".tmp{os.getpid()}"
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wno-attributes", "-D__HIP_PLATFORM_AMD__=1", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}"]
+    cmd += [f"-I{d}" for d in include_paths() + [sysconfig.get_paths()["include"], os.path.join(rocm, "include")]]
+    cmd += [src, "-o", tmp, f"-L{libs}", "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_hip", f"-L{PKG}", "-l:liblcma.so", "-Wl,-rpath,$ORIGIN"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode:
+        raise RuntimeError(f"{' '.join(cmd)}\n{r.stderr}")
+    os.replace(tmp, CALLS)
+    return f"compiled {time.time() - t0:5.1f}s  calls.cc"
+
+
 def build(force: bool = False, jobs: int | None = None, verbose: bool = True) -> str:
     from .gen.generate import generate
 
@@ -61,6 +85,9 @@ def build(force: bool = False, jobs: int | None = None, verbose: bool = True) ->
         os.replace(tmp, LIB)
         if verbose:
             print(f"linked {LIB}", flush=True)
+    msg = _build_calls(force)
+    if verbose:
+        print(msg, flush=True)
     return LIB
 
 

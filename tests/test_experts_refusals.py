@@ -88,3 +88,19 @@ def test_the_binding_refuses_what_it_cannot_pass_on(B):
         B.lcma_i8_quantize(x)  # not on the GPU
     with pytest.raises((AssertionError, ValueError)):
         B.lcma_tokens_sort(torch.zeros((4, 2), dtype=torch.int32), 8)
+
+
+def test_the_binding_names_the_argument_it_refuses(B):
+    import torch
+    calls = B._native()
+    x, ids = torch.zeros((4, 8)), torch.zeros((4, 2), dtype=torch.int32)
+    for f, args, what in [(calls.i8_quantize, (x, x, x, False), "X: expected a tensor on the GPU"), (calls.i8_quantize, (7, x, x, False), "X: expected a tensor"),
+                          (calls.i8_quantize, (torch.zeros(4), x, x, False), "X: expected two dimensions"), (calls.tokens_sort, (ids, 0, ids, ids, ids, None), "experts: expected"),
+                          (calls.tokens_dispatch, (x, ids, x), "X: expected a tensor on the GPU"), (calls.tokens_combine, (x, ids, None, x), "Y: expected a tensor on the GPU"),
+                          (calls.i8_gemm_nt, (x, x, x, x, x, 8, None), "C: expected a tensor on the GPU")]:
+        with pytest.raises(AssertionError, match=what):
+            f(*args)
+    with pytest.raises(TypeError):
+        calls.i8_quantize(x)
+    with pytest.raises(TypeError):
+        calls.tokens_sort(ids, "three", ids, ids, ids, None)
