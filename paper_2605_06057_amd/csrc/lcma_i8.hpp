@@ -289,25 +289,37 @@ template <int TM, int TN, int WGM, int WGN, int S, class OUT> struct I8Ring {
             i8_store_part<OUT, NMI, 32>(p, lds + w * 4096, at, wm * NMI * 32, wn * 64, acc);
             return;
         }
+// (wave parts of 32 columns: the tile meets in LDS, rows of TN columns)
+        constexpr int ES = OUT::ES, PITCH = TN * ES, CHUNKS = PITCH / 16;
+        static_assert(NNI == 2 || TM * PITCH <= LDS_BYTES, "the tile of C fits the stages");
+        __syncthreads();
 #pragma unroll
         for (int i = 0; i < NMI; ++i) {
             const int row = (wm * NMI + i) * 32 + (lane & 31);
-            if (row >= at.rows) continue;
-            const float sa = p.SA[at.row0 + row];
-            char *c = (char *)p.C + (int64_t)(at.row0 + row) * p.ldc * OUT::ES;
+            const float sa = row < at.rows ? p.SA[at.row0 + row] : 0.f;
 #pragma unroll
-            for (int j = 0; j < NNI; ++j)
+            for (int g = 0; g < 4; ++g) {
+                const int n = wn * 32 + g * 8 + (lane >> 5) * 4, byte = n * ES;
+                const f32x4 sw = i8_four(p.SW + (int64_t)at.expert * p.N, at.col0 + n, p.N);
+                f32x4 v;
 #pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    const int col = at.col0 + (wn * NNI + j) * 32 + g * 8 + (lane >> 5) * 4, left = p.N - col;
-                    if (left <= 0) continue;
-                    const f32x4 sw = i8_four(p.SW + (int64_t)at.expert * p.N, col, p.N);
-                    f32x4 v;
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) v[k] = (float)acc[i][j][g * 4 + k] * sa * sw[k];
-                    if (p.bias) v += i8_four(p.bias + (int64_t)at.expert * p.N, col, p.N);
-                    i8_store4<OUT>(c + (int64_t)col * OUT::ES, v, left);
+                for (int k = 0; k < 4; ++k) v[k] = (float)acc[i][0][g * 4 + k] * sa * sw[k];
+                if (p.bias) v += i8_four(p.bias + (int64_t)at.expert * p.N, at.col0 + n, p.N);
+                LCMA_LDS char *to = lds + row * PITCH + ((byte >> 4) ^ (row & 7)) * 16 + (byte & 15);
+                if constexpr (ES == 2) {
+                    const uint32_t lo = Round<OUT>::run(v[0]) | (Round<OUT>::run(v[1]) << 16), hi = Round<OUT>::run(v[2]) | (Round<OUT>::run(v[3]) << 16);
+                    *(LCMA_LDS uint64_t *)to = (uint64_t)hi << 32 | lo;
+                } else {
+                    *(LCMA_LDS f32x4 *)to = v;
                 }
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int t = 0; t < TM * CHUNKS / NT; ++t) {
+            const int row = (t * NT + (int)threadIdx.x) / CHUNKS, ch = threadIdx.x % CHUNKS, col = at.col0 + ch * (16 / ES);
+            const u32x4 v = *(const LCMA_LDS u32x4 *)(lds + row * PITCH + (ch ^ (row & 7)) * 16);
+            if (row < at.rows && col < p.N) i8_store16<OUT>((char *)p.C + ((int64_t)(at.row0 + row) * p.ldc + col) * ES, v, p.N - col);
         }
     }
     // restrict: the loads in flight towards one stage do not touch what is read from another (the compiler would otherwise wait for all of them in

@@ -87,6 +87,14 @@ template <int STAGE, int W, int R> __global__ __launch_bounds__(64 * W) void tok
             first[x] = p.counts[(int64_t)p.blocks * B + x];
             base[x] = p.counts[(int64_t)blockIdx.x * B + x];
         }
+    if (STAGE == 1) {
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+            if (slot0 + r * 64 < p.n) __hip_atomic_fetch_add(first + e[r], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+        __syncthreads();
+        for (int x = threadIdx.x; x < B; x += 64 * W) p.counts[(int64_t)blockIdx.x * B + x] = first[x];
+        return;
+    }
     uint64_t same[R];
 #pragma unroll
     for (int r = 0; r < R; ++r) {
@@ -104,10 +112,8 @@ template <int STAGE, int W, int R> __global__ __launch_bounds__(64 * W) void tok
             counts[k * B + x] = (uint16_t)sum;
             sum += c;
         }
-        if (STAGE == 1) p.counts[(int64_t)blockIdx.x * B + x] = sum;
-        else if (STAGE == 0) first[x] = sum;
+        if (STAGE == 0) first[x] = sum;
     }
-    if (STAGE == 1) return;
     __syncthreads();
     if (w == 0) prefix_sums(first, B, lane);
     __syncthreads();
