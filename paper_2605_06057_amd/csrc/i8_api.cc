@@ -125,7 +125,7 @@ lcma_status gemm(const char *who, int64_t rows, int64_t N, int64_t K, int expert
     if ((jobs + 8) * (in_turn ? 1 : 512) >= kGridLimit / 2) return fail(LCMA_ERR_SHAPE, "%s: too many tiles for a launch", who);
     p.nz = (int32_t)nz;
     p.panel = kernel <= kI8Few32 ? 1 : 8;
-    const int grid = in_turn ? (int)(jobs < 256 ? jobs : 256) : (int)((jobs + 7) / 8 * 8);
+    const int grid = in_turn ? 256 : (int)((jobs + 7) / 8 * 8);
     if (const int err = lcma_launch_i8_gemm(&p, kernel, dtype, grid, stream))
         return fail(LCMA_ERR_HIP, "%s: launch failed with HIP error %d", who, err);
     return LCMA_OK;

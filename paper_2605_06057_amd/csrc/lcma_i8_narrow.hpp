@@ -57,7 +57,7 @@ template <int TM, int TN, class OUT> struct I8Narrow : I8Turns {
             fb[k] = A_STAGE + br * ROW + swz(br, k * 2 + lh) * 16;
         }
         I8Place at, at_next;
-        Source cur = source<TM, TN>(args, nx, jobs, job, at), nxt;
+        Source cur = source<TM, TN>(args, nx, jobs, jobs, job, at), nxt;
         // loads FROM .. TO of a step: first those of A, then those of B
         auto load = [&](auto from, auto to, const Source &s, LCMA_LDS char *st, int y) {
             const auto ra = rsrc(s.a, s.a_bytes), rb = rsrc(s.b, s.b_bytes);
@@ -107,7 +107,7 @@ template <int TM, int TN, class OUT> struct I8Narrow : I8Turns {
         while (true) {
             int next = job + units;
             if (next >= whole && job < whole && whole < jobs) next = whole + (int)blockIdx.x;
-            nxt = source<TM, TN>(args, nx, jobs, next, at_next);
+            nxt = source<TM, TN>(args, nx, jobs, jobs, next, at_next);
 #pragma unroll
             for (int i = 0; i < 2; ++i)
 #pragma unroll
