@@ -55,12 +55,12 @@ lcma_status quantize(const char *who, int64_t rows, int64_t K, const void *X, in
 // What a kernel takes, in us: `start` once; for every round of one tile per compute unit `end` and, for every step of 128 k, `step` with all units at work (the
 // chip's power and what the units share bound it then), `alone` with few; and no less than the bytes at `rate` GB/us take.  Fitted to 110 products and 90 over experts of
 // random sizes (1 to 8192 rows, 8 to 128 experts, 64 to 28672 columns, K 64 to 14336) timed on every kernel: a single time is predicted within 9 to
-// 15 % (root mean square), the kernel with the smallest prediction is on average 2.5 % slower than the fastest one, 36 % at worst.
+// 15 % (root mean square).  On 400 other sizes the kernel with the smallest prediction is 1.8 % slower than the fastest one on average, 20 % at worst.
 const struct Cost {
     int rows, cols;
     double start, alone, step, end, rate;
     bool in_turn; // one work-group per compute unit: rounds count; else several, which share it
-} kCost[kI8Kernels] = {{16, 16, 3.3, 0.026, 0.051, 0.40, 9.5, false},  {32, 32, 2.8, 0.041, 0.107, 1.07, 8.3, false},   {64, 64, 2.7, 0.165, 0.215, 1.49, 7.2, false},
+} kCost[kI8Kernels] = {{16, 16, 3.3, 0.026, 0.051, 0.40, 9.5, false},  {32, 32, 2.8, 0.041, 0.107, 1.07, 8.3, false},   {64, 64, 2.55, 0.168, 0.195, 1.44, 7.0, false},
                        {64, 128, 2.5, 0.292, 0.362, 1.50, 7.1, false}, {128, 128, 1.1, 0.387, 0.586, 3.29, 9.8, true},   {128, 256, 1.3, 0.506, 0.961, 4.88, 7.8, true},
                        {256, 256, 2.0, 0.861, 1.41, 5.82, 6.5, true}};
 double predicted_us(const Cost &k, int64_t rows, int64_t N, int64_t K, int experts) {
