@@ -54,7 +54,7 @@ LCMA_DEV int lanes_upto(int v) {
 // by itself, a lane per expert; the first 64 experts are kept, which are mostly all.
 template <int TM> struct I8Rows {
     int begin, end, upto; // rows of this lane's expert, tiles up to and with it
-    int tiles;
+    int tiles, behind;    // all tiles, and the first row behind the groups
 
     LCMA_DEV void experts_from(const I8GemmParams &p, int e0, int before) {
         const int e = e0 + (int)(threadIdx.x & 63);
@@ -68,14 +68,17 @@ template <int TM> struct I8Rows {
     LCMA_DEV I8Rows(const I8GemmParams &p) {
         if (!p.offsets) {
             tiles = (p.rows + TM - 1) / TM;
+            behind = p.rows;
             return;
         }
         experts_from(p, 0, 0);
         tiles = __builtin_amdgcn_readlane(upto, 63);
+        behind = __builtin_amdgcn_readlane(end, (p.experts - 1) & 63);
         for (int e0 = 64; e0 < p.experts; e0 += 64) {
             I8Rows more = *this;
             more.experts_from(p, e0, tiles);
             tiles = __builtin_amdgcn_readlane(more.upto, 63);
+            behind = __builtin_amdgcn_readlane(more.end, (p.experts - 1) & 63);
         }
     }
     LCMA_DEV I8Place place(const I8GemmParams &p, int x) const {
@@ -102,17 +105,6 @@ LCMA_DEV void i8_tile_of_job(int nx, int nz, int panel, int j, int &x, int &z) {
     z = (j < full ? j / (panel * nx) * panel : whole) + id % width;
 }
 
-// Rows of C behind the groups are zero: the work-groups of the launch share them.
-template <class OUT> LCMA_DEV void i8_zero_behind(const I8GemmParams &p, int groups, int threads) {
-    if (!p.offsets) return;
-    for (int row = i8_row(p, p.experts) + (int)blockIdx.x; row < p.rows; row += groups)
-        for (int n = threadIdx.x; n < p.N; n += threads) {
-            char *c = (char *)p.C + ((int64_t)row * p.ldc + n) * OUT::ES;
-            if constexpr (OUT::ES == 4) *(float *)c = 0.f;
-            else *(uint16_t *)c = 0;
-        }
-}
-
 // Scales (or biases) of columns n .. n + 3, zeros from N on.
 LCMA_DEV f32x4 i8_four(const float *at, int n, int N) {
     f32x4 v = {0.f, 0.f, 0.f, 0.f};
@@ -134,6 +126,13 @@ template <class OUT> LCMA_DEV void i8_store16(char *at, u32x4 v, int cols) {
                 if constexpr (OUT::ES == 4) ((uint32_t *)at)[i] = v[i];
                 else ((uint16_t *)at)[i] = (uint16_t)(v[i / 2] >> (i & 1) * 16);
             }
+}
+
+// Rows of C behind the groups are zero: the work-groups of the launch share them.
+template <class OUT> LCMA_DEV void i8_zero_behind(const I8GemmParams &p, int behind, int groups, int threads) {
+    constexpr int V = 16 / OUT::ES;
+    for (int row = behind + (int)blockIdx.x; row < p.rows; row += groups)
+        for (int n = threadIdx.x * V; n < p.N; n += threads * V) i8_store16<OUT>((char *)p.C + ((int64_t)row * p.ldc + n) * OUT::ES, u32x4{0, 0, 0, 0}, p.N - n);
 }
 
 // Four neighbouring columns of a row of C, the last ones of which may be past N.
@@ -271,8 +270,8 @@ template <int TM, int TN, int WGM, int WGN, int S, class OUT> struct I8Ring {
 
     static LCMA_DEV void run(const I8GemmParams &p, LCMA_LDS char *lds) {
         const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = w / WGN, wn = w % WGN;
-        i8_zero_behind<OUT>(p, gridDim.x, NT);
         const I8Rows<TM> groups(p);
+        i8_zero_behind<OUT>(p, groups.behind, gridDim.x, NT);
         const int nx = groups.tiles, jobs = nx * p.nz, per = (jobs + 7) / 8;
         const int job = (blockIdx.x & 7) * per + (blockIdx.x >> 3); // an eighth of the tiles to every XCD
         if ((int)(blockIdx.x >> 3) >= per || job >= jobs) return;

@@ -21,8 +21,8 @@ template <int T, int WK, int S, class OUT> struct I8FewRows {
 
     static LCMA_DEV void run(const I8GemmParams &p, LCMA_LDS char *lds) {
         const int lane = threadIdx.x & 63, fr = lane & (F - 1), fk = lane / F, wk = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-        i8_zero_behind<OUT>(p, gridDim.x, 64 * WK);
         const I8Rows<T> groups(p);
+        i8_zero_behind<OUT>(p, groups.behind, gridDim.x, 64 * WK);
         const int nx = groups.tiles, jobs = nx * p.nz, per = (jobs + 7) / 8;
         const int job = (blockIdx.x & 7) * per + (blockIdx.x >> 3); // an eighth of the tiles to every XCD, row tiles that share weights next to each other
         if ((int)(blockIdx.x >> 3) >= per || job >= jobs) return;

@@ -40,8 +40,9 @@ template <int TM, int TN, class OUT> struct I8Narrow : I8Turns {
         int nx, jobs;
         {
             const I8GemmParams p = arguments(args);
-            i8_zero_behind<OUT>(p, gridDim.x, NT);
-            nx = I8Rows<TM>(p).tiles;
+            const I8Rows<TM> groups(p);
+            i8_zero_behind<OUT>(p, groups.behind, gridDim.x, NT);
+            nx = groups.tiles;
             jobs = nx * p.nz;
         }
         const int units = gridDim.x, per = units >> 3; // rounds of one tile per work-group, as in I8PingPong

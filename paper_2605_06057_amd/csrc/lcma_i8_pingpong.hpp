@@ -133,8 +133,9 @@ template <class OUT> struct I8PingPong : I8Turns {
         int nx, jobs;
         {
             const I8GemmParams p = arguments(args);
-            i8_zero_behind<OUT>(p, gridDim.x, NT);
-            nx = I8Rows<TM>(p).tiles;
+            const I8Rows<TM> groups(p);
+            i8_zero_behind<OUT>(p, groups.behind, gridDim.x, NT);
+            nx = groups.tiles;
             jobs = nx * p.nz;
         }
         const int units = gridDim.x;
