@@ -323,3 +323,30 @@ def test_an_unknown_kernel_is_the_default():
         test_product("bf16", 33, 127, 256)
     finally:
         B.lcma_set_tuning("i8_kernel", "")
+
+
+def test_many_rows():
+    """More rows than a grid has in its second dimension, quantised and multiplied; sums below 2^24 are exact in fp32."""
+    import torch
+    from paper_2605_06057_amd import binding as B
+    gen = torch.Generator(device="cuda").manual_seed(8)
+    M, N, K = 70001, 40, 72
+    x = torch.randint(-127, 128, (M, K), device="cuda", generator=gen).float()
+    x[:, 0] = 127  # scale 1: the codes are the values
+    Q, S = B.lcma_i8_quantize(x)
+    assert torch.equal(Q[:, :K].float(), x) and (Q[:, K:] == 0).all().item() and (S == 1).all().item()
+    Wq = torch.zeros((N, 128), dtype=torch.int8, device="cuda")
+    Wq[:, :K] = torch.randint(-127, 128, (N, K), device="cuda", generator=gen)
+    c = B.lcma_i8_gemm_nt(Q, S, Wq, torch.ones((N,), device="cuda"), torch.empty((M, N), device="cuda"), K)
+    assert torch.equal(c.double(), x.double() @ Wq[:, :K].double().t())
+
+
+def test_nothing_to_multiply():
+    import torch
+    from paper_2605_06057_amd import binding as B
+    q, s = B.lcma_i8_quantize(torch.empty((0, 30), device="cuda"))
+    w, sw = torch.ones((5, 128), dtype=torch.int8, device="cuda"), torch.ones((5,), device="cuda")
+    assert B.lcma_i8_gemm_nt(q, s, w, sw, torch.empty((0, 5), device="cuda"), 30).shape == (0, 5)
+    zeros = torch.zeros((3,), dtype=torch.int32, device="cuda")  # no rows for either of two experts
+    c = B.lcma_i8_gemm_experts(w[:4], sw[:4], zeros, w.expand(2, 5, 128).contiguous(), sw.expand(2, 5).contiguous(), torch.full((4, 5), float("nan"), device="cuda"), 128)
+    assert (c == 0).all().item()

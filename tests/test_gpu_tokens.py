@@ -214,3 +214,41 @@ def test_on_a_stream_of_its_own_and_in_a_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(buffers["out"], want), f"replay {k}"
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_many_tokens(dt):
+    """More tokens than a grid has in its second dimension; the plain forms by torch's indexing."""
+    import torch
+    from paper_2605_06057_amd import binding as B
+    td = {"f32": torch.float32, "bf16": torch.bfloat16}[dt]
+    gen = torch.Generator(device="cuda").manual_seed(6)
+    T, top_k, H = 70001, 3, 24
+    ids = torch.randint(-1, 40, (T, top_k), device="cuda", generator=gen).int()
+    x, w = torch.randn((T, H), device="cuda", generator=gen).to(td), torch.rand((T, top_k), device="cuda", generator=gen)
+    order, position, offsets = B.lcma_tokens_sort(ids, 40)
+    kept = int(offsets[-1])
+    rows = B.lcma_tokens_dispatch(x, position)
+    assert torch.equal(rows[:kept], x[order[:kept].long() // top_k]) and (rows[kept:] == 0).all().item()
+    picked = torch.where((position >= 0)[:, :, None], rows.double()[position.clamp(min=0).long()], 0.0)
+    got, want = B.lcma_tokens_combine(rows, position, w).double(), (picked * w.double()[:, :, None]).sum(1)
+    assert ((got - want).abs() <= picked.abs().sum(1) * 4 * 2.0 ** -24 + want.abs() * 1.001 * HALF_ULP[dt] + 2.0 ** -25).all().item()
+    dy, dw = B.lcma_tokens_combine_grad(x, rows, position, w)
+    assert ((dw.double() - (picked * x.double()[:, None]).sum(2)).abs() <= (picked * x.double()[:, None]).abs().sum(2) * (H + 1) * 2.0 ** -24).all().item()
+    want = (x.double()[:, None] * w.double()[:, :, None])[position >= 0]
+    assert ((dy.double()[position[position >= 0].long()] - want).abs() <= want.abs() * (2.0 ** -24 + 1.001 * HALF_ULP[dt]) + 2.0 ** -25).all().item() and (dy[kept:] == 0).all().item()
+
+
+def test_no_tokens_and_no_columns():
+    import torch
+    from paper_2605_06057_amd import binding as B
+    none = torch.empty((0, 2), dtype=torch.int32, device="cuda")
+    x, w = torch.empty((0, 16), device="cuda"), torch.empty((0, 2), device="cuda")
+    assert B.lcma_tokens_dispatch(x, none).shape == (0, 16) and B.lcma_tokens_combine(x, none, w).shape == (0, 16)
+    assert [t.shape for t in B.lcma_tokens_combine_grad(x, x, none, w)] == [(0, 16), (0, 2)]
+    assert [t.shape for t in B.lcma_i8_quantize_dispatch(x, none)] == [(0, 128), (0,)]
+    _, position, _ = B.lcma_tokens_sort(torch.zeros((3, 2), dtype=torch.int32, device="cuda"), 2)
+    empty, w = torch.empty((3, 0), device="cuda"), torch.ones((3, 2), device="cuda")
+    assert B.lcma_tokens_dispatch(empty, position).shape == (6, 0)
+    _, dw = B.lcma_tokens_combine_grad(empty, torch.empty((6, 0), device="cuda"), position, w)
+    assert (dw == 0).all().item()
