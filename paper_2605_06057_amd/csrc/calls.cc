@@ -63,6 +63,8 @@ Rows rows(const at::Tensor &t, const char *name, int64_t n, int64_t cols, int gp
 }
 Rows rows(PyObject *o, const char *name, int64_t n, int64_t cols, int gpu, at::ScalarType type) { return rows(tensor(o, name), name, n, cols, gpu, type); }
 void *stream_of(int gpu) { return (void *)c10::hip::getCurrentHIPStream((c10::DeviceIndex)gpu).stream(); }
+// (a number that the C entry points refuse in place of one that an int does not hold)
+int as_int(int64_t v) { return v > INT32_MAX ? INT32_MAX : (int)v; }
 const at::Tensor &matrix(PyObject *o, const char *name) {
     const at::Tensor &t = tensor(o, name);
     if (t.dim() != 2) refuse(name, "two dimensions");
@@ -89,7 +91,8 @@ template <int N, class F> PyObject *call(PyObject *const *, Py_ssize_t n, F &&f)
 PyObject *i8_quantize(PyObject *, PyObject *const *a, Py_ssize_t n) { // X, Q, S, gated
     return call<4>(a, n, [&] {
         const at::Tensor &x = matrix(a[0], "X");
-        const bool gated = PyObject_IsTrue(a[3]);
+        const int gated = PyObject_IsTrue(a[3]);
+        if (gated < 0) throw std::exception();
         const int64_t r = x.size(0), width = x.size(1), K = gated ? width / 2 : width;
         if (gated && width % 2) refuse("X", "rows x 2 K");
         const int gpu = gpu_of(x, "X");
@@ -106,7 +109,7 @@ PyObject *i8_quantize_dispatch(PyObject *, PyObject *const *a, Py_ssize_t n) { /
         const Rows in = rows(x, "X", tokens, K, gpu, x.scalar_type());
         void *to = whole(position, "position", at::kInt, {tokens, top}, gpu);
         void *q = whole(a[2], "Q", at::kChar, {tokens * top, lcma_i8_code_pitch(K)}, gpu), *s = whole(a[3], "S", at::kFloat, {tokens * top}, gpu);
-        return lcma_i8_quantize_dispatch(tokens, K, in.at, in.ld, storage(x, "X"), (int)top, (const int32_t *)to, q, (float *)s, stream_of(gpu));
+        return lcma_i8_quantize_dispatch(tokens, K, in.at, in.ld, storage(x, "X"), as_int(top), (const int32_t *)to, q, (float *)s, stream_of(gpu));
     });
 }
 PyObject *i8_gemm_nt(PyObject *, PyObject *const *a, Py_ssize_t n) { // Aq, Sa, Wq, Sw, C, K, bias
@@ -131,7 +134,7 @@ PyObject *i8_gemm_experts(PyObject *, PyObject *const *a, Py_ssize_t n) { // Aq,
         const void *wq = whole(w, "Wq", at::kChar, {E, N, pitch}, gpu), *sw = whole(a[4], "Sw", at::kFloat, {E, N}, gpu);
         const void *bias = a[7] == Py_None ? nullptr : whole(a[7], "bias", at::kFloat, {E, N}, gpu);
         const Rows out = rows(c, "C", r, N, gpu, c.scalar_type());
-        return lcma_i8_gemm_experts(r, N, K, (int)E, (const int32_t *)offsets, aq, (const float *)sa, wq, (const float *)sw, (const float *)bias, out.at, out.ld,
+        return lcma_i8_gemm_experts(r, N, K, as_int(E), (const int32_t *)offsets, aq, (const float *)sa, wq, (const float *)sw, (const float *)bias, out.at, out.ld,
                                     storage(c, "C"), stream_of(gpu));
     });
 }
@@ -151,7 +154,7 @@ PyObject *tokens_sort(PyObject *, PyObject *const *a, Py_ssize_t n) { // ids, ex
             space = w.data_ptr();
             size = (int64_t)w.nbytes();
         }
-        return lcma_tokens_sort(tokens, (int)top, (int)E, (const int32_t *)in, (int32_t *)order, (int32_t *)position, (int32_t *)offsets, space, size, stream_of(gpu));
+        return lcma_tokens_sort(tokens, as_int(top), (int)E, (const int32_t *)in, (int32_t *)order, (int32_t *)position, (int32_t *)offsets, space, size, stream_of(gpu));
     });
 }
 PyObject *tokens_dispatch(PyObject *, PyObject *const *a, Py_ssize_t n) { // X, position, Y
@@ -161,7 +164,7 @@ PyObject *tokens_dispatch(PyObject *, PyObject *const *a, Py_ssize_t n) { // X, 
         const int gpu = gpu_of(x, "X");
         const Rows in = rows(x, "X", tokens, H, gpu, x.scalar_type()), out = rows(a[2], "Y", tokens * top, H, gpu, x.scalar_type());
         const void *to = whole(position, "position", at::kInt, {tokens, top}, gpu);
-        return lcma_tokens_dispatch(tokens, (int)top, H, in.at, in.ld, storage(x, "X"), (const int32_t *)to, out.at, out.ld, stream_of(gpu));
+        return lcma_tokens_dispatch(tokens, as_int(top), H, in.at, in.ld, storage(x, "X"), (const int32_t *)to, out.at, out.ld, stream_of(gpu));
     });
 }
 PyObject *tokens_combine(PyObject *, PyObject *const *a, Py_ssize_t n) { // Y, position, weights, X
@@ -172,7 +175,7 @@ PyObject *tokens_combine(PyObject *, PyObject *const *a, Py_ssize_t n) { // Y, p
         const Rows in = rows(y, "Y", tokens * top, H, gpu, y.scalar_type()), out = rows(a[3], "X", tokens, H, gpu, y.scalar_type());
         const void *to = whole(position, "position", at::kInt, {tokens, top}, gpu);
         const void *w = a[2] == Py_None ? nullptr : whole(a[2], "weights", at::kFloat, {tokens, top}, gpu);
-        return lcma_tokens_combine(tokens, (int)top, H, in.at, in.ld, storage(y, "Y"), (const int32_t *)to, (const float *)w, out.at, out.ld, stream_of(gpu));
+        return lcma_tokens_combine(tokens, as_int(top), H, in.at, in.ld, storage(y, "Y"), (const int32_t *)to, (const float *)w, out.at, out.ld, stream_of(gpu));
     });
 }
 PyObject *tokens_combine_grad(PyObject *, PyObject *const *a, Py_ssize_t n) { // dX, Y, position, weights, dY, dweights
@@ -184,7 +187,7 @@ PyObject *tokens_combine_grad(PyObject *, PyObject *const *a, Py_ssize_t n) { //
         const Rows dx = rows(a[0], "dX", tokens, H, gpu, type), in = rows(y, "Y", tokens * top, H, gpu, type), dy = rows(a[4], "dY", tokens * top, H, gpu, type);
         const void *to = whole(position, "position", at::kInt, {tokens, top}, gpu), *w = whole(a[3], "weights", at::kFloat, {tokens, top}, gpu);
         void *dw = whole(a[5], "dweights", at::kFloat, {tokens, top}, gpu);
-        return lcma_tokens_combine_grad(tokens, (int)top, H, dx.at, dx.ld, in.at, in.ld, storage(y, "Y"), (const int32_t *)to, (const float *)w, dy.at, dy.ld, (float *)dw,
+        return lcma_tokens_combine_grad(tokens, as_int(top), H, dx.at, dx.ld, in.at, in.ld, storage(y, "Y"), (const int32_t *)to, (const float *)w, dy.at, dy.ld, (float *)dw,
                                         stream_of(gpu));
     });
 }

@@ -104,3 +104,14 @@ def test_the_binding_names_the_argument_it_refuses(B):
         calls.i8_quantize(x)
     with pytest.raises(TypeError):
         calls.tokens_sort(ids, "three", ids, ids, ids, None)
+
+
+def test_an_error_of_an_argument_is_passed_on(B):
+    import torch
+
+    class Neither:
+        def __bool__(self):
+            raise KeyError("neither")
+    x = torch.zeros((4, 8))
+    with pytest.raises(KeyError, match="neither"):
+        B._native().i8_quantize(x, x, x, Neither())
