@@ -425,7 +425,8 @@ lcma_status lcma_set_tuning(const char *key, const char *value);
 int64_t lcma_i8_code_pitch(int64_t K);
 lcma_status lcma_i8_quantize(int64_t rows, int64_t K, const void *X, int64_t ldx, lcma_dtype dtype, int gated, void *Q, float *S, void *stream);
 /* The rows of tokens quantised into expert order: row position[t * top_k + j] of Q and S is token t's, for every j.  Rows of slots
- * without an expert (position < 0, see lcma_tokens_sort) are not written; the product over experts does not read them. */
+ * without an expert (position < 0, see lcma_tokens_sort) are not written; the product over experts does not read them.  Nor is
+ * anything written for a position of tokens * top_k or more. */
 lcma_status lcma_i8_quantize_dispatch(int64_t tokens, int64_t K, const void *X, int64_t ldx, lcma_dtype dtype, int top_k, const int32_t *position,
                                       void *Q, float *S, void *stream);
 /* bias may be null.  K = 0: C = bias, or zeros. */
@@ -449,7 +450,7 @@ lcma_status lcma_i8_gemm_experts(int64_t rows, int64_t N, int64_t K, int experts
  *
  * The calls that move rows take X, Y in the storage type `dtype` (H elements a row, any H, leading dimension and alignment of an element) and
  * weights in fp32 (tokens x top_k).  Rows of slots without an expert are written as zeros and never read.  Sums run in fp32, j ascending, and
- * are rounded once.
+ * are rounded once.  A slot whose position names no row (lcma_tokens_sort writes none such) counts as without an expert, and no row is written for it.
  *   lcma_tokens_dispatch       Y[position[t][j]] = X[t]
  *   lcma_tokens_combine        X[t] = sum_j weights[t][j] * Y[position[t][j]]; weights null: ones.  Without weights it is the
  *                              gradient of lcma_tokens_dispatch.

@@ -120,11 +120,12 @@ template <class T, bool GATED, int L> __global__ __launch_bounds__(L < 256 ? 256
     }
     const RowScale s = row_scale(most);
     const int32_t *position = p.position ? p.position + r * p.top_k : nullptr;
+    const uint32_t slots = (uint32_t)p.rows * p.top_k; // (a position that names none of them is left out, as a negative one)
     auto put = [&](int k, uint64_t c) {
         if (!position) *(uint64_t *)(p.Q + r * p.pitch + k) = c;
         else
             for (int j = 0; j < p.top_k; ++j)
-                if (const int to = position[j]; to >= 0) *(uint64_t *)(p.Q + (int64_t)to * p.pitch + k) = c;
+                if (const uint32_t to = position[j]; to < slots) *(uint64_t *)(p.Q + (int64_t)to * p.pitch + k) = c;
     };
 #pragma unroll
     for (int n = 0; n < KEPT; ++n) {
@@ -140,7 +141,7 @@ template <class T, bool GATED, int L> __global__ __launch_bounds__(L < 256 ? 256
         if (lane == 0) p.S[r] = s.scale;
     } else {
         for (int j = lane; j < p.top_k; j += L)
-            if (const int to = position[j]; to >= 0) p.S[to] = s.scale;
+            if (const uint32_t to = position[j]; to < slots) p.S[to] = s.scale;
     }
 }
 

@@ -191,6 +191,12 @@ template <class T> LCMA_DEV int64_t vector_at(int c, int H) {
     return (int64_t)(c * V + V <= H ? c * V : H - V) * T::ES;
 }
 
+// The row that a slot has, of `rows` of them; -1 for a position that names none (which is then neither read nor written).
+LCMA_DEV int row_of(int position, int rows) {
+    const int row = position < 0 ? -1 - position : position;
+    return row < rows ? row : -1;
+}
+
 template <class T, int STREAM> __global__ __launch_bounds__(256) void tokens_dispatch(const TokensRowsParams p) {
     constexpr int V = 16 / T::ES;
     const int64_t t = (int64_t)blockIdx.x * (256 >> p.lane_shift) + (threadIdx.x >> p.lane_shift);
@@ -198,32 +204,36 @@ template <class T, int STREAM> __global__ __launch_bounds__(256) void tokens_dis
     if (t >= p.tokens || c * V >= p.H) return;
     const char *x = (const char *)p.X + t * p.ldx_b;
     const int32_t *position = p.position + t * p.top_k;
+    const int rows = p.tokens * p.top_k;
     if (p.H >= V) {
         const int64_t at = vector_at<T>(c, p.H);
         const u32x4 v = load16<0>(x + at);
         for (int j = 0; j < p.top_k; ++j) {
-            const int row = position[j];
-            store16<STREAM>((char *)p.Y + (int64_t)(row < 0 ? -1 - row : row) * p.ldy_b + at, row < 0 ? u32x4{0, 0, 0, 0} : v);
+            const int to = position[j], row = row_of(to, rows);
+            if (row >= 0) store16<STREAM>((char *)p.Y + (int64_t)row * p.ldy_b + at, to < 0 ? u32x4{0, 0, 0, 0} : v);
         }
     } else {
         for (int j = 0; j < p.top_k; ++j) {
-            const int row = position[j];
-            char *y = (char *)p.Y + (int64_t)(row < 0 ? -1 - row : row) * p.ldy_b;
-            for (int i = 0; i < p.H; ++i) put_element<T>(y + i * T::ES, row < 0 ? 0.f : element<T>(x + i * T::ES));
+            const int to = position[j], row = row_of(to, rows);
+            char *y = (char *)p.Y + (int64_t)row * p.ldy_b;
+            if (row >= 0)
+                for (int i = 0; i < p.H; ++i) put_element<T>(y + i * T::ES, to < 0 ? 0.f : element<T>(x + i * T::ES));
         }
     }
 }
 
-// The rows of up to four slots of a token from j on: which they are (-1: none), and their weights.
+// Up to four slots of a token from j on: the rows that they have and, of those with an expert, that they read (-1: none), and their weights.
 struct Four {
-    int row[4];
+    int has[4], row[4];
     float w[4];
 };
-LCMA_DEV Four four_slots(const int32_t *position, const float *weights, int j, int top_k) {
+LCMA_DEV Four four_slots(const int32_t *position, const float *weights, int j, int top_k, int rows) {
     Four s;
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-        s.row[q] = j + q < top_k ? position[j + q] : -1;
+        const int at = j + q < top_k ? position[j + q] : -1;
+        s.has[q] = j + q < top_k ? row_of(at, rows) : -1;
+        s.row[q] = at < 0 ? -1 : s.has[q];
         s.w[q] = s.row[q] < 0 ? 0.f : weights ? weights[j + q] : 1.f;
     }
     return s;
@@ -238,6 +248,7 @@ template <class T, int STREAM> __global__ __launch_bounds__(256) void tokens_com
     char *y = (char *)p.Y + t * p.ldy_b;
     const int32_t *position = p.position + t * p.top_k;
     const float *weights = p.weights ? p.weights + t * p.top_k : nullptr;
+    const int rows = p.tokens * p.top_k;
     if (p.H >= V) {
         // (a second vector past the row is the first one again: the same values to the same place)
         const int64_t at[N] = {vector_at<T>(c0, p.H), vector_at<T>((c0 + lanes) * V < p.H ? c0 + lanes : c0, p.H)};
@@ -247,7 +258,7 @@ template <class T, int STREAM> __global__ __launch_bounds__(256) void tokens_com
 #pragma unroll
             for (int i = 0; i < V; ++i) sum[n][i] = 0.f;
         for (int j = 0; j < p.top_k; j += 4) {
-            const Four s = four_slots(position, weights, j, p.top_k);
+            const Four s = four_slots(position, weights, j, p.top_k, rows);
             u32x4 raw[4][N];
 #pragma unroll
             for (int q = 0; q < 4; ++q)
@@ -270,7 +281,7 @@ template <class T, int STREAM> __global__ __launch_bounds__(256) void tokens_com
         for (int i = 0; i < p.H; ++i) {
             float sum = 0.f;
             for (int j = 0; j < p.top_k; ++j)
-                if (position[j] >= 0) sum += (weights ? weights[j] : 1.f) * element<T>((const char *)p.X + (int64_t)position[j] * p.ldx_b + i * T::ES);
+                if (position[j] >= 0 && position[j] < rows) sum += (weights ? weights[j] : 1.f) * element<T>((const char *)p.X + (int64_t)position[j] * p.ldx_b + i * T::ES);
             put_element<T>(y + i * T::ES, sum);
         }
     }
@@ -285,15 +296,14 @@ template <class T, int L, int STREAM> __global__ __launch_bounds__(256) void tok
     if (t >= p.tokens) return; // (L = 256: a work-group is a token)
     const char *dx = (const char *)p.dX + t * p.lddx_b;
     for (int j = 0; j < p.top_k; j += 4) {
-        const Four s = four_slots(p.position + t * p.top_k, p.weights + t * p.top_k, j, p.top_k);
+        const Four s = four_slots(p.position + t * p.top_k, p.weights + t * p.top_k, j, p.top_k, p.tokens * p.top_k);
         const char *x[4];
         char *y[4];
         float dot[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-            const int64_t row = j + q < p.top_k && s.row[q] < 0 ? -1 - (int64_t)s.row[q] : s.row[q]; // (zeros are written for a slot without an expert)
-            x[q] = (const char *)p.X + row * p.ldx_b;
-            y[q] = (char *)p.Y + row * p.ldy_b;
+            x[q] = (const char *)p.X + (int64_t)s.row[q] * p.ldx_b;
+            y[q] = (char *)p.Y + (int64_t)s.has[q] * p.ldy_b; // (zeros are written for a slot without an expert)
         }
         if (p.H >= V) {
             for (int c = lane; c * V < p.H; c += L) {
@@ -307,7 +317,7 @@ template <class T, int L, int STREAM> __global__ __launch_bounds__(256) void tok
                 Widen<T>::run(mine, g);
 #pragma unroll
                 for (int q = 0; q < 4; ++q)
-                    if (j + q < p.top_k) {
+                    if (s.has[q] >= 0) {
                         float v[V], out[V];
                         Widen<T>::run(raw[q], v);
 #pragma unroll
@@ -322,7 +332,7 @@ template <class T, int L, int STREAM> __global__ __launch_bounds__(256) void tok
             const float g = element<T>(dx + lane * T::ES);
 #pragma unroll
             for (int q = 0; q < 4; ++q)
-                if (j + q < p.top_k) {
+                if (s.has[q] >= 0) {
                     if (s.row[q] >= 0) dot[q] = g * element<T>(x[q] + lane * T::ES);
                     put_element<T>(y[q] + lane * T::ES, s.row[q] >= 0 ? s.w[q] * g : 0.f);
                 }

@@ -350,3 +350,20 @@ def test_nothing_to_multiply():
     zeros = torch.zeros((3,), dtype=torch.int32, device="cuda")  # no rows for either of two experts
     c = B.lcma_i8_gemm_experts(w[:4], sw[:4], zeros, w.expand(2, 5, 128).contiguous(), sw.expand(2, 5).contiguous(), torch.full((4, 5), float("nan"), device="cuda"), 128)
     assert (c == 0).all().item()
+
+
+@pytest.mark.parametrize("K", [100, 5000])
+def test_quantised_to_rows_that_are_not_there(K):
+    """A position of the row behind the last one is left out, as a negative one."""
+    import torch
+    from paper_2605_06057_amd import binding as B
+    rng = np.random.default_rng(K)
+    stored, x = _values(rng, (3, K), "bf16")
+    n, pitch = 6, B.lcma_i8_code_pitch(K)
+    Q, S = torch.full((n + 1, pitch), 99, dtype=torch.int8, device="cuda"), torch.full((n + 1,), -1.0, device="cuda")
+    B.lcma_i8_quantize_dispatch(_device(stored, "bf16"), torch.tensor([[4, n], [0, 1], [-1 - n, 5]], dtype=torch.int32, device="cuda"), Q[:n], S[:n])
+    q, s = X.i8_quantize(x)
+    Q, S = Q.cpu().numpy(), S.cpu().numpy()
+    written, token = [4, 0, 1, 5], [0, 1, 1, 2]
+    assert np.array_equal(Q[written, :K], q[token]) and (Q[written, K:] == 0).all() and np.array_equal(S[written], s[token])
+    assert (Q[[2, 3, n]] == 99).all() and (S[[2, 3, n]] == -1).all()

@@ -252,3 +252,43 @@ def test_no_tokens_and_no_columns():
     assert B.lcma_tokens_dispatch(empty, position).shape == (6, 0)
     _, dw = B.lcma_tokens_combine_grad(empty, torch.empty((6, 0), device="cuda"), position, w)
     assert (dw == 0).all().item()
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("tokens,top_k,H", [(5, 3, 2), (6, 5, 40), (4, 2, 4100)])
+def test_positions_that_name_no_row(dt, tokens, top_k, H):
+    """The row behind the last one, as a slot's own and as that of a slot without an expert: neither read nor written."""
+    import torch
+    from paper_2605_06057_amd import binding as B
+    rng = np.random.default_rng(H)
+    n = tokens * top_k
+    pos = rng.permutation(n).astype(np.int32).reshape(tokens, top_k)
+    gone = pos[[0, -1], [top_k - 1, 0]]  # (the rows that no slot has any more)
+    pos[0, top_k - 1], pos[-1, 0] = n, -1 - n
+    none = np.where((pos < 0) | (pos >= n), -1, pos)
+    position = torch.from_numpy(pos).cuda()
+    x, x64 = _store(rng, (tokens, H), dt)
+    w = rng.uniform(-1, 1, (tokens, top_k)).astype(np.float32)
+    weights, named = torch.from_numpy(w).cuda(), np.setdiff1d(np.arange(n), gone)
+    rows, rows64 = _store(rng, (n, H), dt)
+    whole_r, rv = _view(n, H, dt, 0)
+    rv.copy_(rows)
+    whole, y = _view(n, H, dt, 0)
+    B.lcma_tokens_dispatch(x, position, y)
+    want = np.full((n, H), np.nan)
+    want[none[none >= 0]] = x64[np.nonzero(none >= 0)[0]]
+    assert np.array_equal(_host(y, dt), want, equal_nan=True) and _untouched(whole, n, H, 0)
+    out = B.lcma_tokens_combine(rv, position, weights)
+    wz = np.where(none < 0, 0, w).astype(np.float64)
+    taken = rows64[np.maximum(none, 0)]
+    want, size = (wz[..., None] * taken).sum(1), np.abs(wz[..., None] * taken).sum(1)
+    assert np.all(np.abs(_host(out, dt) - want) <= size * (top_k + 1) * 2.0 ** -24 + np.abs(want) * 1.001 * HALF_ULP[dt] + 2.0 ** -25)
+    whole, dy = _view(n, H, dt, 0)
+    _, dw = B.lcma_tokens_combine_grad(x, rv, position, weights, dy)
+    got, product = _host(dy, dt), w[..., None].astype(np.float64) * x64[:, None]
+    assert np.isnan(got[gone]).all() and np.isfinite(got[named]).all() and _untouched(whole, n, H, 0)
+    room = np.abs(product) * (2.0 ** -24 + 1.001 * HALF_ULP[dt]) + 2.0 ** -25
+    assert np.all((np.abs(got[np.maximum(none, 0)] - product) <= room)[none >= 0])
+    want, size = (taken * x64[:, None]).sum(-1), np.abs(taken * x64[:, None]).sum(-1)
+    got = dw.cpu().numpy()
+    assert np.all(got[none < 0] == 0) and np.all((np.abs(got - want) <= size * (H + 1) * 2.0 ** -24)[none >= 0])
