@@ -419,7 +419,8 @@ lcma_status lcma_set_tuning(const char *key, const char *value);
  * lcma_i8_code_pitch: K rounded up to 128 (0 for K = 0); -1 for a negative K.
  * lcma_i8_quantize: row by row amax = max |x|, S = amax / 127, Q = rint(x * (127 / amax)) with ties to even, in fp32.  A row of zeros has
  * S = 0 and codes 0.  A row that holds an infinity or a NaN has codes 0 and S = infinity or NaN: its products are NaN.
- * gated != 0: a row of X is 2 K long and x[k] = silu(X[k]) * X[K + k], silu(g) = g / (1 + exp(-g)).
+ * gated != 0: a row of X is 2 K long and x[k] = silu(X[k]) * X[K + k], silu(g) = g / (1 + exp(-g)), formed in fp32 to within 2^-18 of its
+ * value (gates below -174 may give zero).
  * Weights N x K are quantised by the same call (their rows are the channels).
  */
 int64_t lcma_i8_code_pitch(int64_t K);

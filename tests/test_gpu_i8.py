@@ -144,6 +144,25 @@ def test_gate_at_the_ends():
 
 
 @pytest.mark.parametrize("dt", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("gate", [-80.0, -86.0, -88.0, -89.0, -92.0, -100.0, -150.0, -170.0])
+def test_gates_far_below_zero(dt, gate):
+    """silu(g) there is |g| exp(g), a small number and not zero, up to where exp(-g) has left fp32 (88.7) and beyond: rows in which all gates are of that size, times
+    large linear parts.  The gate is off by at most 2^-18 of the value (test_gated); below 2^-126 a value has an error of 2^-149 besides."""
+    from paper_2605_06057_amd import binding as B
+    rng = np.random.default_rng(int(-gate))
+    K, up = 777, {"f32": 2.0 ** 120, "bf16": 2.0 ** 120, "f16": 2.0 ** 14}[dt]
+    stored = inp.store(np.concatenate([gate + rng.uniform(-2, 2, (3, K)), rng.uniform(-3, 3, (3, K)) * up], axis=1), dt)
+    v = X.silu_gate(inp.widen(stored, dt).astype(np.float64))
+    if np.abs(v).max(axis=1).min() < 2.0 ** -120:
+        return  # (fp16: nothing that fp32 can tell from zero)
+    Q, S = B.lcma_i8_quantize(_device(stored, dt), gated=True)
+    s, q, amax, off = S.cpu().numpy().astype(np.float64), Q.cpu().numpy(), np.abs(v).max(axis=1), 2.0 ** -18
+    assert np.all(np.abs(s - amax / 127) <= amax / 127 * off + 2.0 ** -149)
+    room = 0.5 + 127 * 2 * off + 2.0 ** -148 / (amax / 127)
+    assert np.all(np.abs(q[:, :K] - v / (amax[:, None] / 127)) <= room[:, None]) and (np.abs(q).max(axis=1) == 127).all()
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16", "f16"])
 @pytest.mark.parametrize("tokens,top_k,K", [(1, 1, 1), (5, 2, 129), (33, 8, 520), (70, 3, 2051)])
 def test_quantised_while_dispatching(dt, tokens, top_k, K):
     import torch
