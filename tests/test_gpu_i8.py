@@ -386,3 +386,66 @@ def test_quantised_to_rows_that_are_not_there(K):
     written, token = [4, 0, 1, 5], [0, 1, 1, 2]
     assert np.array_equal(Q[written, :K], q[token]) and (Q[written, K:] == 0).all() and np.array_equal(S[written], s[token])
     assert (Q[[2, 3, n]] == 99).all() and (S[[2, 3, n]] == -1).all()
+
+
+# ------------------------------------------------------------------ work-groups that walk through several tiles
+def _whole_numbers(gen, *shape):
+    """Codes of -100 .. 100 on the device, rows padded with zeros to the code pitch."""
+    import torch
+    out = torch.zeros((*shape[:-1], (shape[-1] + 127) // 128 * 128), dtype=torch.int8, device="cuda")
+    out[..., :shape[-1]] = torch.randint(-100, 101, shape, device="cuda", generator=gen)
+    return out
+
+
+WALKS = [(tiles, K) for tiles in (256 + 40, 256 + 200, 512 + 40, 512 + 200) for K in (100, 256, 384, 500, 640, 768)]
+
+
+@pytest.mark.parametrize("kernel", ["128x256", "256x256"], indirect=True)
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("tiles,K", WALKS)
+def test_product_of_more_tiles_than_work_groups(kernel, dt, tiles, K):
+    """256 work-groups walk through the tiles: a second and a third one, a last round that at most half of them have a tile in and one that more have, 1 to 6
+    steps of K, the last tiles along M and N not full.  Whole numbers: sums below 2^24 are exact in fp32, and a rounding to bf16 is the same one."""
+    import torch
+    from paper_2605_06057_amd import binding as B
+    rows, cols = map(int, kernel.split("x"))
+    gen = torch.Generator(device="cuda").manual_seed(tiles + K)
+    M, N = tiles // 8 * rows - 37, 8 * cols - 61
+    Aq, Wq = _whole_numbers(gen, M, K), _whole_numbers(gen, N, K)
+    whole, c = _strided(M, N, dt, 3, float("nan"))
+    B.lcma_i8_gemm_nt(Aq, torch.ones((M,), device="cuda"), Wq, torch.ones((N,), device="cuda"), c, K)
+    assert torch.equal(c, (Aq.float() @ Wq.float().t()).to(c.dtype)) and _untouched(whole, M, N, 3)
+
+
+@pytest.mark.parametrize("kernel", ["128x256", "256x256"], indirect=True)
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("counts", [[130, 0, 4000, 1, 2200, 255, 257, 2500], [5000, 17, 5003, 0, 0, 6000, 300, 129]], ids=["more than 256", "more than 512"])
+@pytest.mark.parametrize("K", [100, 256, 384, 500, 640])
+def test_experts_of_more_tiles_than_work_groups(kernel, dt, counts, K):
+    """The same with groups that end inside tiles and rows behind them."""
+    import torch
+    from paper_2605_06057_amd import binding as B
+    cols, behind, E = int(kernel.split("x")[1]), 301, len(counts)
+    gen = torch.Generator(device="cuda").manual_seed(len(counts) + K)
+    rows, N = sum(counts) + behind, 8 * cols - 61
+    ends = np.cumsum([0] + counts).astype(np.int32)
+    Aq, Wq, bias = _whole_numbers(gen, rows, K), _whole_numbers(gen, E, N, K), torch.randint(-50, 51, (E, N), device="cuda", generator=gen).float()
+    whole, c = _strided(rows, N, dt, 3, float("nan"))
+    one = torch.ones((rows + E * N,), device="cuda")
+    B.lcma_i8_gemm_experts(Aq, one[:rows], torch.from_numpy(ends).cuda(), Wq, one[rows:].view(E, N), c, K, bias)
+    for e in range(E):
+        a, b = int(ends[e]), int(ends[e + 1])
+        assert torch.equal(c[a:b], (Aq[a:b].float() @ Wq[e].float().t() + bias[e]).to(c.dtype)), f"expert {e}"
+    assert (c[ends[-1]:] == 0).all().item() and _untouched(whole, rows, N, 3)
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("M,N,K", [(8192, 14336, 640), (8191, 14335, 777), (2048, 4096, 1000)])
+def test_large_product_by_the_rule(dt, M, N, K):
+    import torch
+    from paper_2605_06057_amd import binding as B
+    gen = torch.Generator(device="cuda").manual_seed(M + K)
+    Aq, Wq = _whole_numbers(gen, M, K), _whole_numbers(gen, N, K)
+    c = torch.full((M, N), float("nan"), device="cuda", dtype={"f32": torch.float32, "bf16": torch.bfloat16}[dt])
+    B.lcma_i8_gemm_nt(Aq, torch.ones((M,), device="cuda"), Wq, torch.ones((N,), device="cuda"), c, K)
+    assert torch.equal(c, (Aq.float() @ Wq.float().t()).to(c.dtype))
