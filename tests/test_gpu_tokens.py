@@ -292,3 +292,60 @@ def test_positions_that_name_no_row(dt, tokens, top_k, H):
     want, size = (taken * x64[:, None]).sum(-1), np.abs(taken * x64[:, None]).sum(-1)
     got = dw.cpu().numpy()
     assert np.all(got[none < 0] == 0) and np.all((np.abs(got - want) <= size * (H + 1) * 2.0 ** -24)[none >= 0])
+
+
+# ------------------------------------------------------------------ rows that pass the caches by
+def _large(dt, T, top_k, H, pad):
+    """Dispatch, combine with weights and without, and the gradient of it, against torch's indexing in 64 bits; slots without an expert, NaN in the rows behind
+    and around every output."""
+    import torch
+    from paper_2605_06057_amd import binding as B
+    gen = torch.Generator(device="cuda").manual_seed(T + H)
+    n = T * top_k
+    ids = torch.randint(-1, 7, (T, top_k), device="cuda", generator=gen).int()
+    order, position, offsets = B.lcma_tokens_sort(ids, 7)
+    kept = int(offsets[-1])
+    w = torch.rand((T, top_k), device="cuda", generator=gen) * 2 - 1
+
+    def filled(rows):
+        whole, view = _view(rows, H, dt, pad)
+        view.copy_(torch.randn((rows, H), device="cuda", generator=gen))
+        return view
+
+    x, rows = filled(T), filled(n)
+    rows[kept:] = float("nan")
+    token, has = order.long() // top_k, (position >= 0)[:, :, None]
+    whole, y = _view(n, H, dt, pad)
+    B.lcma_tokens_dispatch(x, position, y)
+    assert torch.equal(y[:kept], x[token[:kept]]) and (y[kept:] == 0).all().item() and _untouched(whole, n, H, pad)
+    picked = torch.where(has, rows[position.clamp(min=0).long()].double(), 0.0)
+    for weights in (w, None):
+        whole, out = _view(T, H, dt, pad)
+        B.lcma_tokens_combine(rows, position, weights, out)
+        each = picked if weights is None else picked * w.double()[:, :, None]
+        want = each.sum(1)
+        assert ((out.double() - want).abs() <= each.abs().sum(1) * (top_k + 1) * 2.0 ** -24 + want.abs() * 1.001 * HALF_ULP[dt] + 2.0 ** -25).all().item()
+        assert _untouched(whole, T, H, pad)
+        del each
+    whole, dy = _view(n, H, dt, pad)
+    _, dw = B.lcma_tokens_combine_grad(x, rows, position, w, dy)
+    picked *= x.double()[:, None]
+    assert ((dw.double() - picked.sum(2)).abs() <= picked.abs().sum(2) * (H + 1) * 2.0 ** -24).all().item()
+    want = x.double()[token[:kept]] * w.double().flatten()[order[:kept].long()][:, None]
+    assert ((dy[:kept].double() - want).abs() <= want.abs() * (2.0 ** -24 + 1.001 * HALF_ULP[dt]) + 2.0 ** -25).all().item()
+    assert (dy[kept:] == 0).all().item() and _untouched(whole, n, H, pad)
+
+
+# Written rows pass the caches by from 64 MiB on, read ones in expert order from 256 MiB on: 3 slots a token: the writes alone, 4: both, 8: the reads alone (combine).
+# Rows of more than 128 vectors (odd and whole ones) and of fewer, which the gradient gives to a wave.
+@pytest.mark.parametrize("dt", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("row,pad", [(6172, 3), (6176, 0), (2036, 1), (2048, 8)])
+@pytest.mark.parametrize("top_k", [3, 4, 8])
+def test_rows_past_the_caches(dt, row, pad, top_k):
+    es = 4 if dt == "f32" else 2
+    H = (row // es) if row % 16 == 0 else row // es - (row // es + 1) % 2  # (an odd number of elements)
+    mib = 65 if top_k < 8 else 33
+    T = (mib << 20) // (H * es) + 1
+    written, read = T * H * es >> 20, T * top_k * H * es >> 20
+    assert (written >= 64, read >= 256) == {3: (True, False), 4: (True, True), 8: (False, True)}[top_k] and (H * es > 2048) == (row > 2048)
+    _large(dt, T, top_k, H, pad)
