@@ -401,7 +401,8 @@ double lcma_predict_seconds(int scheme_id, int64_t M, int64_t N, int64_t K, lcma
  *                                                   switched off leaves its output as an earlier call wrote it, so C is only
  *                                                   valid with all four on.
  *   "i8_kernel"        LCMA_I8_KERNEL=<rows>x<cols> lcma_i8_gemm_nt and lcma_i8_gemm_experts run the kernel with tiles of that size: 16x16,
- *                                                   32x32, 64x64, 64x128, 128x128, 128x256 or 256x256 (another value: default).  Their
+ *                                                   32x32, 64x64, 64x128, 128x128, 128x256 or 256x256 (another value, or more tiles than its
+ *                                                   launch holds: default).  Their
  *                                                   sums are exact, so this changes no result.
  */
 lcma_status lcma_set_tuning(const char *key, const char *value);
@@ -413,7 +414,8 @@ lcma_status lcma_set_tuning(const char *key, const char *value);
  * The sum is exact (32-bit integers); it is scaled in fp32 and rounded once to the type of C.
  * Code matrices are int8, row-major and k-contiguous with a row pitch of lcma_i8_code_pitch(K) bytes; columns from K on have to
  * hold zeros (lcma_i8_quantize writes them).  Scales and bias are fp32.  Code matrices are 16-byte aligned; X and C need the alignment of
- * their elements only, and any leading dimension that holds a row.  N and the number of rows are free; K is at most 131071 (SHAPE).
+ * their elements only, and a leading dimension that holds a row.  Up to 2^31 - 1 rows, leading dimensions (and so N) below 2^29, K at most
+ * 131071 (SHAPE).
  * Outputs must not overlap inputs (ARG).  All calls run on `stream`, allocate nothing and do not synchronise.
  *
  * lcma_i8_code_pitch: K rounded up to 128 (0 for K = 0); -1 for a negative K.

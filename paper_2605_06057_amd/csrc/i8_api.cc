@@ -74,11 +74,26 @@ double predicted_us(const Cost &k, int64_t rows, int64_t N, int64_t K, int exper
     const double t = k.start + whole * (steps * k.step + k.end) + (part > 0 ? steps * (k.alone + (k.step - k.alone) * part) + k.end : 0);
     return std::sqrt(std::sqrt(t * t * t * t + memory * memory * memory * memory));
 }
-int pick(int64_t rows, int64_t N, int64_t K, int experts) {
-    int best = 0;
+bool walks(int kernel) { return kernel >= kI8Narrow; } // 256 work-groups walk through the tiles; the other kernels have one for every tile
+// Tiles, at most: every group of rows may end in one of its own that is not full.
+int64_t tiles_along_rows(int kernel, int64_t rows, int experts, bool grouped) {
+    const int64_t tm = kCost[kernel].rows;
+    return grouped ? rows / tm + (rows < experts ? rows : experts) : (rows + tm - 1) / tm;
+}
+int64_t tiles_along_columns(int kernel, int64_t N) { return (N + kCost[kernel].cols - 1) / kCost[kernel].cols; }
+bool launches(int kernel, int64_t rows, int64_t N, int experts, bool grouped) {
+    const int64_t jobs = tiles_along_rows(kernel, rows, experts, grouped) * tiles_along_columns(kernel, N);
+    return walks(kernel) ? jobs < kRowLimit - 1024 : (jobs + 8) * 512 < kGridLimit / 2; // (numbers of tiles are 32-bit on the device)
+}
+// Of the kernels whose launch holds the tiles; -1: none does.
+int pick(int64_t rows, int64_t N, int64_t K, int experts, bool grouped) {
+    if (K == 0) // (nothing to multiply: the smallest tiles that any number of steps suits, as long as they are not too many)
+        return launches(kI8Ring64, rows, N, experts, grouped) ? kI8Ring64 : launches(kI8PingPong, rows, N, experts, grouped) ? kI8PingPong : -1;
+    if (const int forced = tuning_i8_kernel(); forced >= 0 && launches(forced, rows, N, experts, grouped)) return forced;
+    int best = -1;
     double least = 0;
     for (int k = 0; k < kI8Kernels; ++k)
-        if (const double t = predicted_us(kCost[k], rows, N, K, experts); k == 0 || t < least) {
+        if (const double t = predicted_us(kCost[k], rows, N, K, experts); launches(k, rows, N, experts, grouped) && (best < 0 || t < least)) {
             least = t;
             best = k;
         }
@@ -117,15 +132,12 @@ lcma_status gemm(const char *who, int64_t rows, int64_t N, int64_t K, int expert
     p.pitch = (int32_t)pitch;
     p.experts = experts;
     p.steps = (int32_t)(pitch / 128);
-    const int forced = tuning_i8_kernel(), kernel = K == 0 ? kI8Ring64 : forced >= 0 ? forced : pick(rows, N, K, experts);
-    const bool in_turn = kernel >= kI8Narrow; // (a work-group walks through tiles)
-    const int64_t tm = kCost[kernel].rows, tn = kCost[kernel].cols;
-    // tiles along M, at most: every group may end in one of its own that is not full
-    const int64_t nx = offsets ? rows / tm + (rows < experts ? rows : experts) : (rows + tm - 1) / tm, nz = (N + tn - 1) / tn, jobs = nx * nz;
-    if ((jobs + 8) * (in_turn ? 1 : 512) >= kGridLimit / 2) return fail(LCMA_ERR_SHAPE, "%s: too many tiles for a launch", who);
+    const int kernel = pick(rows, N, K, experts, offsets != nullptr);
+    if (kernel < 0) return fail(LCMA_ERR_SHAPE, "%s: too many tiles for a launch", who);
+    const int64_t nz = tiles_along_columns(kernel, N), jobs = tiles_along_rows(kernel, rows, experts, offsets != nullptr) * nz;
     p.nz = (int32_t)nz;
     p.panel = kernel <= kI8Few32 ? 1 : 8;
-    const int grid = in_turn ? 256 : (int)((jobs + 7) / 8 * 8);
+    const int grid = walks(kernel) ? 256 : (int)((jobs + 7) / 8 * 8);
     if (const int err = lcma_launch_i8_gemm(&p, kernel, dtype, grid, stream))
         return fail(LCMA_ERR_HIP, "%s: launch failed with HIP error %d", who, err);
     return LCMA_OK;

@@ -35,7 +35,7 @@ LCMA_DEV int i8_row(const I8GemmParams &p, int e) {
     const int row = p.offsets[e];
     return row < 0 ? 0 : row > p.rows ? p.rows : row;
 }
-template <int TM> LCMA_DEV int i8_tiles(int begin, int end) { return end > begin ? (end - begin + TM - 1) / TM : 0; }
+template <int TM> LCMA_DEV int i8_tiles(int begin, int end) { return end > begin ? (int)(((uint32_t)(end - begin) + (TM - 1)) / TM) : 0; } // (up to 2^31 - 1 rows)
 
 // Sum over the lanes up to and with this one.
 LCMA_DEV int lanes_upto(int v) {
@@ -67,7 +67,7 @@ template <int TM> struct I8Rows {
     }
     LCMA_DEV I8Rows(const I8GemmParams &p) {
         if (!p.offsets) {
-            tiles = (p.rows + TM - 1) / TM;
+            tiles = i8_tiles<TM>(0, p.rows);
             behind = p.rows;
             return;
         }
@@ -131,7 +131,7 @@ template <class OUT> LCMA_DEV void i8_store16(char *at, u32x4 v, int cols) {
 // Rows of C behind the groups are zero: the work-groups of the launch share them.
 template <class OUT> LCMA_DEV void i8_zero_behind(const I8GemmParams &p, int behind, int groups, int threads) {
     constexpr int V = 16 / OUT::ES;
-    for (int row = behind + (int)blockIdx.x; row < p.rows; row += groups)
+    for (uint32_t row = behind + blockIdx.x; row < (uint32_t)p.rows; row += groups) // (past 2^31 before it ends)
         for (int n = threadIdx.x * V; n < p.N; n += threads * V) i8_store16<OUT>((char *)p.C + ((int64_t)row * p.ldc + n) * OUT::ES, u32x4{0, 0, 0, 0}, p.N - n);
 }
 

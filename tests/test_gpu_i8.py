@@ -449,3 +449,39 @@ def test_large_product_by_the_rule(dt, M, N, K):
     c = torch.full((M, N), float("nan"), device="cuda", dtype={"f32": torch.float32, "bf16": torch.bfloat16}[dt])
     B.lcma_i8_gemm_nt(Aq, torch.ones((M,), device="cuda"), Wq, torch.ones((N,), device="cuda"), c, K)
     assert torch.equal(c, (Aq.float() @ Wq.float().t()).to(c.dtype))
+
+
+# ------------------------------------------------------------------ more rows than some kernel's launch holds
+@pytest.mark.parametrize("K", [8, 0])
+def test_product_of_very_many_rows(K):
+    """2^28 rows: more tiles of 64 x 64 than a launch holds."""
+    import torch
+    from paper_2605_06057_amd import binding as B
+    M, N = (1 << 28) + 5, 3
+    Aq, sa = torch.zeros((M, 128 if K else 0), dtype=torch.int8, device="cuda"), torch.ones((M,), device="cuda")
+    Wq, bias = torch.zeros((N, 128 if K else 0), dtype=torch.int8, device="cuda"), torch.tensor([0.0, 1.0, 2.0], device="cuda")
+    number = torch.arange(M, device="cuda", dtype=torch.int32) % 101
+    if K:
+        Aq[:, K - 1] = number
+        Wq[:, K - 1] = 1
+    c = torch.full((M, N), float("nan"), device="cuda", dtype=torch.bfloat16)
+    B.lcma_i8_gemm_nt(Aq, sa, Wq, torch.ones((N,), device="cuda"), c, K, bias)
+    for n in range(N):
+        assert ((c[:, n] == number + n) if K else (c[:, n] == n)).all().item()
+
+
+def test_the_last_row_number():
+    """2^31 - 1 rows (of nothing: K = 0), whose tiles and rows behind the groups end at the last number that 32 bits hold."""
+    import torch
+    from paper_2605_06057_amd import binding as B
+    M = (1 << 31) - 1
+    Aq, sa, one = torch.empty((M, 0), dtype=torch.int8, device="cuda"), torch.zeros((M,), device="cuda"), torch.ones((2, 1), device="cuda")
+    Wq, bias = torch.empty((2, 1, 0), dtype=torch.int8, device="cuda"), torch.tensor([[3.0], [5.0]], device="cuda")
+    c = torch.full((M, 1), float("nan"), device="cuda", dtype=torch.bfloat16)
+    B.lcma_i8_gemm_nt(Aq, sa, Wq[0], one[0], c, 0, bias[0])
+    assert (c == 3).all().item()
+    for offsets in ([0, 7, 1000], [0, 1000, M - 3], [0, 1, M]):
+        c.fill_(float("nan"))
+        B.lcma_i8_gemm_experts(Aq, sa, torch.tensor(offsets, dtype=torch.int32, device="cuda"), Wq, one, c, 0, bias)
+        a, b = offsets[1:]
+        assert (c[:a] == 3).all().item() and (c[a:b] == 5).all().item() and (c[b:] == 0).all().item()
