@@ -47,7 +47,6 @@ lcma_status quantize(const char *who, int64_t rows, int64_t K, const void *X, in
     p.top_k = top_k;
     // as many threads as keep the row in registers
     const int threads = K <= 1024 ? 64 : K <= 4096 ? 256 : 1024;
-    if (rows * threads >= kGridLimit) return fail(LCMA_ERR_SHAPE, "%s: too many rows for a launch", who);
     if (const int err = lcma_launch_i8_quantize(&p, dtype, gated, threads, stream)) return fail(LCMA_ERR_HIP, "%s: launch failed with HIP error %d", who, err);
     return LCMA_OK;
 }

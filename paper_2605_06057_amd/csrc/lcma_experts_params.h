@@ -5,6 +5,15 @@
 
 namespace lcma {
 
+// n work-groups as `along` x `across`: a dimension of a launch holds fewer than 2^32 threads.  Group number: across * along's extent + along.
+struct Groups {
+    uint32_t along, across;
+};
+inline Groups groups_of(int64_t n) {
+    const int64_t most = 1 << 20; // (times 1024 threads: 2^30)
+    return n <= most ? Groups{(uint32_t)n, 1} : Groups{(uint32_t)most, (uint32_t)((n + most - 1) / most)};
+}
+
 // lcma_tokens_sort (csrc/lcma_tokens.hip): n = tokens * top_k slots, up to kSortOnce in one launch, above in blocks of kSortSlots (more than
 // kSortBlocks blocks: their counts are summed by a launch of its own).
 constexpr int kSortSlots = 2048, kSortOnce = 4096, kSortBlocks = 128, kMaxExperts = 1024;

@@ -107,7 +107,7 @@ LCMA_DEV uint64_t codes(float (&v)[8], const RowScale &s) {
 template <class T, bool GATED, int L> __global__ __launch_bounds__(L < 256 ? 256 : L) void i8_quantize(const I8QuantParams p) {
     constexpr int KEPT = 2, ROWS = L < 256 ? 256 / L : 1;
     __shared__ uint32_t part[L / 64];
-    const int64_t r = (int64_t)blockIdx.x * ROWS + threadIdx.x / L;
+    const int64_t r = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * ROWS + threadIdx.x / L;
     const int lane = threadIdx.x % L;
     if (r >= p.rows) return; // (L >= 256: a work-group is a row)
     const char *row = (const char *)p.X + r * p.ldx_b;
@@ -199,10 +199,12 @@ template <class OUT> __global__ __launch_bounds__(512, 2) void i8_gemm_256(const
 // threads: of a row
 extern "C" int lcma_launch_i8_quantize(const lcma::I8QuantParams *p, int dtype, int gated, int threads, void *stream) {
     const hipStream_t s = (hipStream_t)stream;
-#define LCMA_QUANTIZE_L(T, G)                                                                          \
-    if (threads == 64) i8_quantize<T, G, 64><<<dim3((p->rows + 3) / 4), dim3(256), 0, s>>>(*p);         \
-    else if (threads == 256) i8_quantize<T, G, 256><<<dim3(p->rows), dim3(256), 0, s>>>(*p);            \
-    else i8_quantize<T, G, 1024><<<dim3(p->rows), dim3(1024), 0, s>>>(*p);
+    const Groups g = groups_of(threads == 64 ? ((int64_t)p->rows + 3) / 4 : p->rows);
+    const dim3 grid(g.along, g.across);
+#define LCMA_QUANTIZE_L(T, G)                                                        \
+    if (threads == 64) i8_quantize<T, G, 64><<<grid, dim3(256), 0, s>>>(*p);         \
+    else if (threads == 256) i8_quantize<T, G, 256><<<grid, dim3(256), 0, s>>>(*p);  \
+    else i8_quantize<T, G, 1024><<<grid, dim3(1024), 0, s>>>(*p);
 #define LCMA_QUANTIZE(T)                    \
     if (gated) { LCMA_QUANTIZE_L(T, true) } \
     else { LCMA_QUANTIZE_L(T, false) }

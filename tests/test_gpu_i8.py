@@ -485,3 +485,18 @@ def test_the_last_row_number():
         B.lcma_i8_gemm_experts(Aq, sa, torch.tensor(offsets, dtype=torch.int32, device="cuda"), Wq, one, c, 0, bias)
         a, b = offsets[1:]
         assert (c[:a] == 3).all().item() and (c[a:b] == 5).all().item() and (c[b:] == 0).all().item()
+
+
+def test_very_many_long_rows_quantised():
+    """2^22 rows of more than 4096 values: more threads than a launch holds along one dimension."""
+    import torch
+    from paper_2605_06057_amd import binding as B
+    rows, K = (1 << 22) + 5, 4104
+    x = torch.zeros((rows, K), dtype=torch.bfloat16, device="cuda")
+    number = torch.arange(rows, device="cuda") % 100 + 27
+    x[:, 1], x[:, K - 1] = number, -number
+    Q, S = B.lcma_i8_quantize(x)
+    del x
+    assert torch.equal(S.cpu(), number.cpu().float() / torch.tensor(127.0))  # (a division; torch multiplies by 1 / 127 on the GPU)
+    for k, code in ((1, 127), (K - 1, -127), (0, 0), (K, 0)):
+        assert (Q[:, k] == code).all().item()

@@ -95,3 +95,16 @@ def test_kernels_by_name(lib):
     lib.lcma_set_tuning(b"i8_kernel", b"16x16")  # (2^26 tiles: more than its launch holds)
     assert _dense(lib, 1 << 30, 1, 64)[0] in ("128x256", "256x256")
     lib.lcma_set_tuning(b"i8_kernel", b"")
+
+
+def test_work_groups_of_a_launch(tmp_path):
+    """Two dimensions hold any number of work-groups of up to 1024 threads, and few more than that."""
+    src = tmp_path / "groups.cc"
+    src.write_text('#include "lcma_experts_params.h"\nextern "C" long groups(long n, int which) { return which ? lcma::groups_of(n).across : lcma::groups_of(n).along; }\n')
+    so = str(tmp_path / "groups.so")
+    subprocess.check_call(["g++", "-std=c++17", "-O1", "-shared", "-fPIC", "-I", CSRC, str(src), "-o", so])
+    f = ctypes.CDLL(so).groups
+    f.argtypes, f.restype = [ctypes.c_long, ctypes.c_int], ctypes.c_long
+    for n in (1, 255, (1 << 20) - 1, 1 << 20, (1 << 20) + 1, (1 << 22) + 5, (1 << 24) + 1, (1 << 31) - 1):
+        along, across = f(n, 0), f(n, 1)
+        assert along * across >= n > along * (across - 1) and along * 1024 < 1 << 32 and across <= 65535 and (across == 1 or n > 1 << 20)
