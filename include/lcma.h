@@ -451,8 +451,8 @@ lcma_status lcma_i8_gemm_experts(int64_t rows, int64_t N, int64_t K, int experts
  * All are int32 on the device.  1 to 1024 experts, tokens * top_k below 2^31 (SHAPE).  workspace: device memory, 4-byte aligned, of at least
  * lcma_tokens_sort_workspace_bytes bytes (0 for few slots: it may be null then); -1: sizes out of range.
  *
- * The calls that move rows take X, Y in the storage type `dtype` (H elements a row, any H, leading dimension and alignment of an element) and
- * weights in fp32 (tokens x top_k).  Rows of slots without an expert are written as zeros and never read.  Sums run in fp32, j ascending, and
+ * The calls that move rows take X, Y in the storage type `dtype` (H elements a row below 2^26, alignment of an element, any leading dimension below 2^29 that holds
+ * a row; longer: SHAPE) and weights in fp32 (tokens x top_k).  Rows of slots without an expert are written as zeros and never read.  Sums run in fp32, j ascending, and
  * are rounded once.  A slot whose position names no row (lcma_tokens_sort writes none such) counts as without an expert, and no row is written for it.
  *   lcma_tokens_dispatch       Y[position[t][j]] = X[t]
  *   lcma_tokens_combine        X[t] = sum_j weights[t][j] * Y[position[t][j]]; weights null: ones.  Without weights it is the

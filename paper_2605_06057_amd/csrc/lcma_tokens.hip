@@ -185,6 +185,9 @@ template <class T> LCMA_DEV void put_element(char *at, float v) {
     else *(uint16_t *)at = (uint16_t)Round<T>::run(v);
 }
 
+// Tokens are dealt out along x, and along z where they are more than x holds (y runs along the rows).
+LCMA_DEV int64_t group_number() { return (int64_t)blockIdx.z * gridDim.x + blockIdx.x; }
+
 // Vector c of a row of H elements: the last one ends with the row, so it may repeat elements of the one before (which get the same values).
 template <class T> LCMA_DEV int64_t vector_at(int c, int H) {
     constexpr int V = 16 / T::ES;
@@ -199,7 +202,7 @@ LCMA_DEV int row_of(int position, int rows) {
 
 template <class T, int STREAM> __global__ __launch_bounds__(256) void tokens_dispatch(const TokensRowsParams p) {
     constexpr int V = 16 / T::ES;
-    const int64_t t = (int64_t)blockIdx.x * (256 >> p.lane_shift) + (threadIdx.x >> p.lane_shift);
+    const int64_t t = group_number() * (256 >> p.lane_shift) + (threadIdx.x >> p.lane_shift);
     const int c = blockIdx.y * (1 << p.lane_shift) + (threadIdx.x & ((1 << p.lane_shift) - 1));
     if (t >= p.tokens || c * V >= p.H) return;
     const char *x = (const char *)p.X + t * p.ldx_b;
@@ -242,7 +245,7 @@ LCMA_DEV Four four_slots(const int32_t *position, const float *weights, int j, i
 // A thread: two vectors of a token's row, those of four slots in flight together.
 template <class T, int STREAM> __global__ __launch_bounds__(256) void tokens_combine(const TokensRowsParams p) {
     constexpr int V = 16 / T::ES, N = 2;
-    const int64_t t = (int64_t)blockIdx.x * (256 >> p.lane_shift) + (threadIdx.x >> p.lane_shift);
+    const int64_t t = group_number() * (256 >> p.lane_shift) + (threadIdx.x >> p.lane_shift);
     const int lanes = 1 << p.lane_shift, c0 = blockIdx.y * (N * lanes) + (threadIdx.x & (lanes - 1));
     if (t >= p.tokens || c0 * V >= p.H) return;
     char *y = (char *)p.Y + t * p.ldy_b;
@@ -291,7 +294,7 @@ template <class T, int STREAM> __global__ __launch_bounds__(256) void tokens_com
 template <class T, int L, int STREAM> __global__ __launch_bounds__(256) void tokens_combine_grad(const TokensRowsParams p) {
     constexpr int V = 16 / T::ES;
     __shared__ float part[4][4];
-    const int64_t t = (int64_t)blockIdx.x * (256 / L) + threadIdx.x / L;
+    const int64_t t = group_number() * (256 / L) + threadIdx.x / L;
     const int lane = threadIdx.x % L;
     if (t >= p.tokens) return; // (L = 256: a work-group is a token)
     const char *dx = (const char *)p.dX + t * p.lddx_b;
@@ -386,8 +389,13 @@ extern "C" int lcma_launch_tokens_sort(const lcma::TokensSortParams *p, void *st
     else { LAUNCH(F16) }               \
     return (int)hipGetLastError();
 
+static dim3 grid_of(int64_t groups, int gy) {
+    const Groups g = groups_of(groups);
+    return dim3(g.along, gy, g.across);
+}
+
 extern "C" int lcma_launch_tokens_dispatch(const lcma::TokensRowsParams *p, int dtype, int gx, int gy, void *stream) {
-    const dim3 grid(gx, gy), block(256);
+    const dim3 grid = grid_of(gx, gy), block(256);
     const hipStream_t s = (hipStream_t)stream;
 #define LCMA_DISPATCH(T)                                            \
     if (p->stream) tokens_dispatch<T, 1><<<grid, block, 0, s>>>(*p); \
@@ -396,7 +404,7 @@ extern "C" int lcma_launch_tokens_dispatch(const lcma::TokensRowsParams *p, int 
 }
 
 extern "C" int lcma_launch_tokens_combine(const lcma::TokensRowsParams *p, int dtype, int gx, int gy, void *stream) {
-    const dim3 grid(gx, gy), block(256);
+    const dim3 grid = grid_of(gx, gy), block(256);
     const hipStream_t s = (hipStream_t)stream;
 #define LCMA_COMBINE(T)                                                     \
     if (p->stream == 3) tokens_combine<T, 3><<<grid, block, 0, s>>>(*p);     \
@@ -409,7 +417,7 @@ extern "C" int lcma_launch_tokens_combine(const lcma::TokensRowsParams *p, int d
 // a wave per token where its row is no more than 128 vectors, else a work-group; as many rows in expert order are written as are read
 extern "C" int lcma_launch_tokens_combine_grad(const lcma::TokensRowsParams *p, int dtype, int wave, void *stream) {
     const hipStream_t s = (hipStream_t)stream;
-    const dim3 block(256), tokens(p->tokens), fours((p->tokens + 3) / 4);
+    const dim3 block(256), tokens = grid_of(p->tokens, 1), fours = grid_of(((int64_t)p->tokens + 3) / 4, 1);
 #define LCMA_GRAD(T)                                                                        \
     if (wave) {                                                                             \
         if (p->stream == 3) tokens_combine_grad<T, 64, 3><<<fours, block, 0, s>>>(*p);      \

@@ -24,7 +24,6 @@ lcma_status check_rows(const char *who, int64_t tokens, int top_k, int64_t H, co
     if (tokens < 0 || H < 0) return fail(LCMA_ERR_ARG, "%s: negative size", who);
     if (top_k < 1) return fail(LCMA_ERR_ARG, "%s: top_k = %d must be at least 1", who, top_k);
     if (tokens >= kRowLimit || tokens * top_k >= kRowLimit) return fail(LCMA_ERR_SHAPE, "%s: 2^31 slots or more", who);
-    if (tokens * 256 >= kGridLimit) return fail(LCMA_ERR_SHAPE, "%s: too many tokens for a launch", who);
     if (tokens == 0) return LCMA_OK;
     if (!position || (H && (!wide || !tall))) return fail(LCMA_ERR_ARG, "%s: null pointer", who);
     if (ldw < H || ldt < H) return fail(LCMA_ERR_ARG, "%s: leading dimension smaller than the row", who);

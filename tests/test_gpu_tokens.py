@@ -349,3 +349,36 @@ def test_rows_past_the_caches(dt, row, pad, top_k):
     written, read = T * H * es >> 20, T * top_k * H * es >> 20
     assert (written >= 64, read >= 256) == {3: (True, False), 4: (True, True), 8: (False, True)}[top_k] and (H * es > 2048) == (row > 2048)
     _large(dt, T, top_k, H, pad)
+
+
+# ------------------------------------------------------------------ more tokens than a launch holds along one dimension
+def test_very_many_tokens():
+    """2^24 tokens of short rows."""
+    import torch
+    from paper_2605_06057_amd import binding as B
+    T, H = (1 << 24) + 5, 9
+    x = (torch.arange(T * H, device="cuda", dtype=torch.int32) % 251).bfloat16().view(T, H)
+    position = torch.flip(torch.arange(T, device="cuda", dtype=torch.int32), (0,)).view(T, 1)
+    y = B.lcma_tokens_dispatch(x, position)
+    assert torch.equal(y, x.flip(0))
+    assert torch.equal(B.lcma_tokens_combine(y, position), x)
+    w = torch.full((T, 1), 0.5, device="cuda")
+    dy, dw = B.lcma_tokens_combine_grad(x, y, position, w)
+    assert torch.equal(dy, (x * 0.5).flip(0)) and torch.equal(dw[:, 0], (x.double() ** 2).sum(1).float())
+
+
+def test_very_many_long_tokens():
+    """More tokens of long rows than 2^20 work-groups, which a launch spreads over two dimensions."""
+    import torch
+    from paper_2605_06057_amd import binding as B
+    T, H = (1 << 20) + 3, 4089
+    x = torch.zeros((T, H), dtype=torch.bfloat16, device="cuda")
+    number = (torch.arange(T, device="cuda") % 100 + 1).bfloat16()
+    x[:, 0], x[:, 2051], x[:, H - 1] = number, 2, -number
+    position = torch.flip(torch.arange(T, device="cuda", dtype=torch.int32), (0,)).view(T, 1)
+    y = B.lcma_tokens_dispatch(x, position)
+    assert torch.equal(y, x.flip(0))
+    assert torch.equal(B.lcma_tokens_combine(y, position), x)
+    w = torch.full((T, 1), 0.5, device="cuda")
+    dy, dw = B.lcma_tokens_combine_grad(x, y, position, w)
+    assert torch.equal(dy, (y * 0.5)) and torch.equal(dw[:, 0], 2 * number.float() ** 2 + 4)
