@@ -48,7 +48,7 @@ void *whole(const at::Tensor &t, const char *name, at::ScalarType type, c10::Int
     return t.data_ptr();
 }
 void *whole(PyObject *o, const char *name, at::ScalarType type, c10::IntArrayRef shape, int gpu) { return whole(tensor(o, name), name, type, shape, gpu); }
-// A matrix whose rows are contiguous; its leading dimension (of a single row, whose stride says nothing: at least the row).
+// A matrix whose rows are contiguous; its leading dimension (of a single row, whose stride says nothing: the row).
 struct Rows {
     char *at;
     int64_t ld;
@@ -58,8 +58,7 @@ Rows rows(const at::Tensor &t, const char *name, int64_t n, int64_t cols, int gp
     if (t.scalar_type() != type) refuse(name, "the other rows' type");
     if (cols > 1 && t.stride(1) != 1) refuse(name, "neighbouring elements in a row");
     if (!t.is_cuda() || t.get_device() != gpu) refuse(name, "a tensor on the same GPU");
-    const int64_t ld = t.stride(0);
-    return {(char *)t.data_ptr(), n <= 1 && ld < cols ? cols : ld};
+    return {(char *)t.data_ptr(), n <= 1 ? cols : t.stride(0)};
 }
 Rows rows(PyObject *o, const char *name, int64_t n, int64_t cols, int gpu, at::ScalarType type) { return rows(tensor(o, name), name, n, cols, gpu, type); }
 void *stream_of(int gpu) { return (void *)c10::hip::getCurrentHIPStream((c10::DeviceIndex)gpu).stream(); }

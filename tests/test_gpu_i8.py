@@ -500,3 +500,19 @@ def test_very_many_long_rows_quantised():
     assert torch.equal(S.cpu(), number.cpu().float() / torch.tensor(127.0))  # (a division; torch multiplies by 1 / 127 on the GPU)
     for k, code in ((1, 127), (K - 1, -127), (0, 0), (K, 0)):
         assert (Q[:, k] == code).all().item()
+
+
+def test_one_row_whose_stride_says_nothing():
+    """A single row of a tensor with rows of 2^30 elements, which no row that is there is apart from another."""
+    import torch
+    from paper_2605_06057_amd import binding as B
+    rng = np.random.default_rng(1)
+    stored, x = _values(rng, (1, 200), "bf16")
+    dev = _device(stored, "bf16")
+    Q, S = B.lcma_i8_quantize(dev.as_strided((1, 200), (1 << 30, 1)))
+    q, s = X.i8_quantize(x)
+    assert np.array_equal(Q.cpu().numpy()[:, :200], q) and np.array_equal(S.cpu().numpy(), s)
+    Wq, w = _codes(rng, (), 33, 200)
+    c = torch.empty((33,), device="cuda")
+    B.lcma_i8_gemm_nt(Q, S, Wq, torch.ones((33,), device="cuda"), c.as_strided((1, 33), (1 << 30, 1)), 200)
+    _check(c.cpu().numpy().astype(np.float64)[None], X.i8_gemm(q, s, w, np.ones(33, np.float32)), "f32", None)
