@@ -39,11 +39,41 @@ def _compile(src: str, obj: str, deps: list[str], force: bool) -> str:
     return f"compiled {time.time() - t0:5.1f}s  {os.path.basename(src)}" + (("\n" + err) if err.strip() else "")
 
 
+def _calls_built_for() -> str:
+    """What _calls.so depends on beside its sources: the interpreter and the torch that it is compiled against ("" without torch)."""
+    import importlib.metadata
+    import sysconfig
+    try:
+        return f"{sysconfig.get_config_var('SOABI')} {sys.version_info[:3]} torch {importlib.metadata.version('torch')}"
+    except importlib.metadata.PackageNotFoundError:
+        return ""
+
+
+def _calls_missing() -> str:
+    """What is not there of the headers that calls.cc needs ("": nothing)."""
+    import importlib.util
+    import sysconfig
+    torch = importlib.util.find_spec("torch")
+    if torch is None:
+        return "torch"
+    if not os.path.exists(os.path.join(os.path.dirname(torch.origin), "include", "torch", "csrc", "autograd", "python_variable.h")):
+        return "torch's C++ headers"
+    if not os.path.exists(os.path.join(sysconfig.get_paths()["include"], "Python.h")):
+        return "Python.h"
+    return ""
+
+
 def _build_calls(force: bool) -> str:
-    """_calls.so, the Python side of the calls in csrc/calls.cc, against the torch that is installed and liblcma.so beside it."""
+    """_calls.so, the Python side of the calls in csrc/calls.cc, against the torch that is installed and liblcma.so beside it.  liblcma.so needs neither Python nor
+    torch: without their headers it is all that is built, and an older _calls.so, which may be another torch's, does not stay."""
     src = os.path.join(CSRC, "calls.cc")
-    if not force and _newer(CALLS, [src, os.path.join(PKG, "..", "include", "lcma.h")]):
+    stamp, built_for = os.path.join(GEN, "calls.built_for"), _calls_built_for()
+    if not force and _newer(CALLS, [src, os.path.join(PKG, "..", "include", "lcma.h")]) and os.path.exists(stamp) and open(stamp).read() == built_for:
         return "up to date  calls.cc"
+    if os.path.exists(CALLS):
+        os.remove(CALLS)
+    if missing := _calls_missing():
+        return f"not built  calls.cc: {missing} not found; the 8-bit-integer calls and the tokens' are left out of the Python binding"
     import sysconfig
 
     import torch
@@ -52,13 +82,15 @@ def _build_calls(force: bool) -> str:
     libs = os.path.join(os.path.dirname(torch.__file__), "lib")
     rocm = os.path.dirname(os.path.dirname(HIPCC))
     tmp = CALLS + f".tmp{os.getpid()}"
-    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wno-attributes", "-D__HIP_PLATFORM_AMD__=1", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}"]
+    cmd = [HIPCC, "-x", "c++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wno-unused-command-line-argument", "-D__HIP_PLATFORM_AMD__=1", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}"]
     cmd += [f"-I{d}" for d in include_paths() + [sysconfig.get_paths()["include"], os.path.join(rocm, "include")]]
     cmd += [src, "-o", tmp, f"-L{libs}", "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_hip", f"-L{PKG}", "-l:liblcma.so", "-Wl,-rpath,$ORIGIN"]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode:
         raise RuntimeError(f"{' '.join(cmd)}\n{r.stderr}")
     os.replace(tmp, CALLS)
+    with open(stamp, "w") as f:
+        f.write(built_for)
     return f"compiled {time.time() - t0:5.1f}s  calls.cc"
 
 
