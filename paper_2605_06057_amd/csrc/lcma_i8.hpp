@@ -12,18 +12,12 @@
 #include "lcma_device.hpp"
 #include "lcma_few_rows.hpp" // wait_loads
 #include "lcma_experts_params.h"
+#include "lcma_lanes.hpp"
 
 namespace lcma {
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x16 __attribute__((ext_vector_type(16)));
-
-// What a wave's lanes wrote to LDS is there for the reads of its other lanes behind this.  For the compiler: the LDS works in order, but without the barrier (which may
-// not be moved into a branch) a lane's reads can end up in front of what lanes on the other side of a branch write.
-LCMA_DEV void lanes_meet() {
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-}
 
 // A tile of C: rows row0 .. row0 + rows - 1 of A, all of expert `expert`, columns col0 .. of C.
 struct I8Place {
@@ -36,19 +30,6 @@ LCMA_DEV int i8_row(const I8GemmParams &p, int e) {
     return row < 0 ? 0 : row > p.rows ? p.rows : row;
 }
 template <int TM> LCMA_DEV int i8_tiles(int begin, int end) { return end > begin ? (int)(((uint32_t)(end - begin) + (TM - 1)) / TM) : 0; } // (up to 2^31 - 1 rows)
-
-// Sum over the lanes up to and with this one.
-LCMA_DEV int lanes_upto(int v) {
-#define LCMA_FROM_LANES(CTRL, ROWS) v += __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 15, false)
-    LCMA_FROM_LANES(0x111, 15); // 1, 2, 4, 8 lanes below, inside the rows of 16
-    LCMA_FROM_LANES(0x112, 15);
-    LCMA_FROM_LANES(0x114, 15);
-    LCMA_FROM_LANES(0x118, 15);
-    LCMA_FROM_LANES(0x142, 10); // the last lane of the row below, in rows 1 and 3; of the half below, in the upper half
-    LCMA_FROM_LANES(0x143, 12);
-#undef LCMA_FROM_LANES
-    return v;
-}
 
 // The tiles of TM rows of all groups, in expert order, every group in tiles of its own: how many there are, and the rows of tile x.  Every wave
 // by itself, a lane per expert; the first 64 experts are kept, which are mostly all.

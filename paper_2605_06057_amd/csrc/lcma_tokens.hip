@@ -15,6 +15,7 @@
 #include <stdint.h>
 
 #include "lcma_experts_params.h"
+#include "lcma_lanes.hpp"
 #include "lcma_prepare_b.hpp"
 
 namespace {
@@ -25,13 +26,7 @@ using namespace lcma;
 // of the expert number, so a wave's counts need no atomics and the rank of a slot is the count before the round plus the lanes below with the
 // same number.  What bounds it is latency: up to kSortOnce slots are one work-group's, 16 waves; above, a launch counts blocks of kSortSlots and
 // another one places them, every block adding up the counts of those before it (more than kSortBlocks of them: a third launch in between does).
-// Measured (us, launches included): 2000 slots of 64 experts 4.7, 4096 6.1, 6126 7.6, 65536 9.4, 131072 of 128 14.4.
-
-// What a wave's lanes wrote to LDS is there for the reads of its other lanes behind this (for the compiler: the LDS works in order).
-LCMA_DEV void lanes_meet() {
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-}
+// Measured (us, launches included): 2000 slots of 64 experts 4.6, 4096 5.8, 6126 7.2, 65536 9.1, 131072 of 128 13.9.
 
 LCMA_DEV uint64_t same_expert(int e, int bits, bool in) {
     uint64_t m = __ballot(in);
@@ -43,20 +38,11 @@ LCMA_DEV uint64_t same_expert(int e, int bits, bool in) {
     return m;
 }
 
-// Inclusive prefix sum over the lanes of a wave.
-LCMA_DEV int lanes_upto(int v, int lane) {
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const int below = __shfl_up(v, d);
-        if (lane >= d) v += below;
-    }
-    return v;
-}
 // Exclusive prefix sums of v[0 .. n) in LDS, by one wave.
 LCMA_DEV void prefix_sums(LCMA_LDS int32_t *v, int n, int lane) {
     int carry = 0;
     for (int i = 0; i < n; i += 64) {
-        const int mine = i + lane < n ? v[i + lane] : 0, sum = lanes_upto(mine, lane);
+        const int mine = i + lane < n ? v[i + lane] : 0, sum = lanes_upto(mine);
         if (i + lane < n) v[i + lane] = carry + sum - mine;
         carry += __shfl(sum, 63);
     }
@@ -143,7 +129,7 @@ __global__ __launch_bounds__(64) void block_prefix(const TokensSortParams p) {
     int carry = 0;
     for (int b = 0; b < p.blocks; b += 64) {
         int32_t *at = p.counts + (int64_t)(b + lane) * B + x;
-        const int mine = b + lane < p.blocks ? *at : 0, sum = lanes_upto(mine, lane);
+        const int mine = b + lane < p.blocks ? *at : 0, sum = lanes_upto(mine);
         if (b + lane < p.blocks) *at = carry + sum - mine;
         carry += __shfl(sum, 63);
     }
