@@ -175,16 +175,16 @@ template <class T, bool GATED, int L> __global__ __launch_bounds__(L < 256 ? 256
 LCMA_I8_RING(64, 64, 2, 2, 4)
 LCMA_I8_RING(64, 128, 2, 2, 3)
 LCMA_I8_RING(128, 128, 4, 2, 4)
-#define LCMA_I8_FEW(T, WK, S)                                                                               \
+#define LCMA_I8_FEW(T, WK)                                                                                  \
     template <class OUT> __global__ __launch_bounds__(64 * WK) void i8_few_##T(const I8GemmParams p) {      \
-        using G = I8FewRows<T, WK, S, OUT>;                                                                 \
+        using G = I8FewRows<T, WK, OUT>;                                                                    \
         __shared__ __attribute__((aligned(16))) char smem[G::LDS_BYTES];                                    \
         G::run(p, (LCMA_LDS char *)smem);                                                                   \
     }
-LCMA_I8_FEW(16, 4, 2)
-LCMA_I8_FEW(32, 4, 2)
+LCMA_I8_FEW(16, 4)
+LCMA_I8_FEW(32, 4)
 template <class OUT> __global__ __launch_bounds__(512, 2) void i8_narrow(const I8GemmParams) {
-    using G = I8Narrow<128, 256, OUT>;
+    using G = I8Narrow<OUT>;
     __shared__ __attribute__((aligned(16))) char smem[G::LDS_BYTES];
     G::run((LCMA_LDS char *)smem);
 }

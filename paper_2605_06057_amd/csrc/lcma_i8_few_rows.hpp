@@ -12,11 +12,11 @@
 
 namespace lcma {
 
-template <int T, int WK, int S, class OUT> struct I8FewRows {
+template <int T, int WK, class OUT> struct I8FewRows {
     static constexpr int F = T == 16 ? 16 : 32, NF = T / F, KF = 128 / (1024 / F); // 16x16x64 or 32x32x32 instructions; fragments of a line along K
     static constexpr int LOADS = T / 8, HALF = T * 128, STAGE = 2 * HALF;
-    static constexpr int PITCH = T + 4, SUMS = WK * T * PITCH * 4, STAGES = WK * S * STAGE, LDS_BYTES = SUMS > STAGES ? SUMS : STAGES;
-    static_assert(LDS_BYTES <= 160 * 1024 && (S == 2 || S == 4) && 2 * LOADS * S <= 63, "LDS budget of one CU; counter of loads");
+    static constexpr int PITCH = T + 4, SUMS = WK * T * PITCH * 4, STAGES = WK * 2 * STAGE, LDS_BYTES = SUMS > STAGES ? SUMS : STAGES;
+    static_assert(LDS_BYTES <= 160 * 1024 && 2 * LOADS * 2 <= 63, "LDS budget of one CU; counter of loads");
     using Acc = std::conditional_t<F == 16, i32x4, i32x16>;
 
     static LCMA_DEV void run(const I8GemmParams &p, LCMA_LDS char *lds) {
@@ -37,8 +37,8 @@ template <int T, int WK, int S, class OUT> struct I8FewRows {
             for (int j = 0; j < NF; ++j)
 #pragma unroll
                 for (int v = 0; v < F * F / 64; ++v) acc[i][j][v] = 0;
-        LCMA_LDS char *st = lds + wk * (S * STAGE);
-        lines_of_wave(p, at, wk, acc, st, st + STAGE, st + (S == 4 ? 2 * STAGE : 0), st + (S == 4 ? 3 * STAGE : 0));
+        LCMA_LDS char *st = lds + wk * (2 * STAGE);
+        lines_of_wave(p, at, wk, acc, st, st + STAGE);
         __syncthreads(); // no load is in flight and every wave has read its last line: the sums take the place of the stages
         LCMA_LDS int *mine = (LCMA_LDS int *)lds + wk * (T * PITCH);
 #pragma unroll
@@ -67,10 +67,10 @@ template <int T, int WK, int S, class OUT> struct I8FewRows {
             i8_store4<OUT>((char *)p.C + ((int64_t)(at.row0 + row) * p.ldc + col) * OUT::ES, v, p.N - col);
         }
     }
-    // Lines `line`, line + WK, ... of a tile.  s0 .. s3: the stages of the wave.  restrict: the loads in flight towards one do not touch what is read
+    // Lines `line`, line + WK, ... of a tile.  s0, s1: the stages of the wave.  restrict: the loads in flight towards one do not touch what is read
     // from another (the compiler would otherwise wait for all of them in front of every read).
     static LCMA_DEV void lines_of_wave(const I8GemmParams &p, const I8Place &tile, int line, Acc (&acc)[NF][NF], LCMA_LDS char *__restrict__ s0,
-                                       LCMA_LDS char *__restrict__ s1, LCMA_LDS char *__restrict__ s2, LCMA_LDS char *__restrict__ s3) {
+                                       LCMA_LDS char *__restrict__ s1) {
         const int lane = threadIdx.x & 63, fr = lane & (F - 1), fk = lane / F, end = p.steps;
         const int cols = p.N - tile.col0 < T ? p.N - tile.col0 : T;
         const auto ra = __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t *>(p.A) + (int64_t)tile.row0 * p.pitch, 0, tile.rows * p.pitch, 0x00020000);
@@ -90,7 +90,7 @@ template <int T, int WK, int S, class OUT> struct I8FewRows {
         for (int k = 0; k < KF; ++k) frag[k] = fr * 128 + ((k * (64 / F) + fk) ^ (fr >> 1 & 7)) * 16;
         auto step = [&](LCMA_LDS char *st, int line) {
             i32x4 a[KF][NF], b[KF][NF];
-            wait_loads<2 * LOADS *(S - 1)>();
+            wait_loads<2 * LOADS>();
 #pragma unroll
             for (int k = 0; k < KF; ++k)
 #pragma unroll
@@ -102,7 +102,7 @@ template <int T, int WK, int S, class OUT> struct I8FewRows {
             __builtin_amdgcn_s_waitcnt(0xC07F); // lgkmcnt(0): what was read has left LDS, so its place may be loaded anew
             asm volatile("" ::: "memory");
             __builtin_amdgcn_sched_barrier(0);
-            load(st, line + S * WK);
+            load(st, line + 2 * WK);
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int k = 0; k < KF; ++k)
@@ -116,20 +116,10 @@ template <int T, int WK, int S, class OUT> struct I8FewRows {
         };
         load(s0, line);
         load(s1, line + WK);
-        if constexpr (S == 4) {
-            load(s2, line + 2 * WK);
-            load(s3, line + 3 * WK);
-        }
         while (line < end) {
             step(s0, line);
             if ((line += WK) >= end) break;
             step(s1, line);
-            if constexpr (S == 4) {
-                if ((line += WK) >= end) break;
-                step(s2, line);
-                if ((line += WK) >= end) break;
-                step(s3, line);
-            }
             line += WK;
         }
         wait_loads<0>();

@@ -1,4 +1,4 @@
-// The 8-bit-integer product on tiles of 128 x 256 (256 x 128), two groups of waves in turn: for fewer rows (of an expert) than a 256 x 256 tile has, and
+// The 8-bit-integer product on tiles of 128 x 256, two groups of waves in turn: for fewer rows (of an expert) than a 256 x 256 tile has, and
 // where there are too few of those to fill the chip or to end its last round.  Wave tiles of 64 x 64, the two groups one beside the other; a step of 128 k is
 // two phases (the upper and the lower 32 rows of the wave tile) of eight matrix instructions.  What bounds it is what a CU can take in, 48 KB a step, and
 // the LDS (48 KB written, 128 KB read for 1024 cycles of matrix instructions): so loads go two whole steps ahead into one of three stages (144 KB), and
@@ -12,10 +12,10 @@
 
 namespace lcma {
 
-template <int TM, int TN, class OUT> struct I8Narrow : I8Turns {
-    static constexpr int A_STAGE = TM * ROW, STAGE = (TM + TN) * ROW, STRIP = 16 * 128, LDS_BYTES = 3 * STAGE + 8 * STRIP;
+template <class OUT> struct I8Narrow : I8Turns {
+    static constexpr int TM = 128, TN = 256, A_STAGE = TM * ROW, STAGE = (TM + TN) * ROW, STRIP = 16 * 128, LDS_BYTES = 3 * STAGE + 8 * STRIP;
     static constexpr int LA = TM / 64, LB = TN / 64; // direct loads of a thread for a step
-    static_assert(LA * LB == 8 && LA + LB == 6 && LDS_BYTES <= 160 * 1024, "eight waves of 64 x 64; LDS budget of one CU");
+    static_assert(LDS_BYTES <= 160 * 1024, "LDS budget of one CU");
 
     static LCMA_DEV void multiply(const i32x4 (&a)[NK], const i32x4 (&b)[2][NK], i32x16 (&c)[2]) {
         __builtin_amdgcn_sched_barrier(0);
@@ -35,8 +35,8 @@ template <int TM, int TN, class OUT> struct I8Narrow : I8Turns {
     // front of every read)
     static LCMA_DEV void pipeline(Args args, LCMA_LDS char *__restrict__ s0, LCMA_LDS char *__restrict__ s1, LCMA_LDS char *__restrict__ s2,
                                   LCMA_LDS char *__restrict__ strips) {
-        const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = tid & 31, lh = (tid >> 5) & 1, g = w >> 2; // waves w and w + 4 share a SIMD
-        const int wm = LA == 2 ? g : w & 3, wn = LA == 2 ? w & 3 : g;
+        const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = tid & 31, lh = (tid >> 5) & 1;
+        const int wm = w >> 2, wn = w & 3, g = wm; // the wave's place among 2 x 4 wave tiles, its group; waves w and w + 4 share a SIMD
         int nx, jobs;
         {
             const I8GemmParams p = arguments(args);
