@@ -87,12 +87,12 @@ class TrainedLinearExperts(torch.autograd.Function):
 
 
 def train(x, target, w, router, top, steps):
-    """Gradient descent on the experts' matrices (bf16, updated from fp32 copies) and on the router, for tokens x of independent N(0, 1); the loss of
-    every step."""
-    master, losses = w.float(), []
+    """Gradient descent on copies of the experts' matrices (in the type of x, updated in fp32) and of the router, for tokens x of independent N(0, 1); the loss
+    of every step."""
+    master, router, losses = w.float().clone(), router.clone(), []
     rate = 0.5 / (1 + (x.shape[1] / x.shape[0]) ** 0.5) ** 2  # half of what the largest eigenvalue of x^T x / tokens allows
     for _ in range(steps):
-        wb, r = master.to(x.dtype).requires_grad_(), router.clone().requires_grad_()
+        wb, r = master.to(x.dtype, copy=True).requires_grad_(), router.clone().requires_grad_()
         ids, weights = route(x, r, top)
         out = TrainedLinearExperts.apply(x, wb, ids, weights)
         loss = 0.5 * (out.float() - target.float()).square().sum(dim=1).mean()
@@ -135,7 +135,7 @@ def main():
     print(f"{a.tokens} tokens, {a.top} of {a.experts} experts, {a.hidden} x {a.ffn}: {ms * 1e3:.0f} us, {ops / ms / 1e9:.0f} TOP/s")
 
     w = normal(a.experts, 512, a.hidden, spread=a.hidden ** -0.5)
-    losses = train(x, normal(a.tokens, 512, spread=0.1), w, router.clone(), a.top, 8)
+    losses = train(x, normal(a.tokens, 512, spread=0.1), w, router, a.top, 8)
     print("training, loss of every step: " + " ".join(f"{v:.4f}" for v in losses))
 
 

@@ -68,3 +68,14 @@ def test_training_reduces_the_loss(layer):
     x, target, w = normal(512, 128).bfloat16(), (normal(512, 64) * 0.1).bfloat16(), (normal(4, 64, 128) * 0.09).bfloat16()
     losses = layer.train(x, target, w, normal(4, 128) * 0.1, 2, 6)
     assert all(b < a for a, b in zip(losses, losses[1:])), losses
+
+
+def test_training_leaves_its_arguments_alone(layer):
+    """In fp32, where the weights could be their own fp32 copies."""
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    normal = lambda *s: torch.randn(s, device="cuda", generator=gen)
+    args = [normal(256, 64), normal(256, 64) * 0.1, normal(4, 64, 64) * 0.09, normal(4, 64) * 0.1]
+    before = [t.clone() for t in args]
+    losses = layer.train(*args, 2, 4)
+    assert all(torch.equal(a, b) and not a.requires_grad for a, b in zip(args, before)) and all(b < a for a, b in zip(losses, losses[1:])), losses
