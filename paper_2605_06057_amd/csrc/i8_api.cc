@@ -53,8 +53,10 @@ lcma_status quantize(const char *who, int64_t rows, int64_t K, const void *X, in
 
 // What a kernel takes, in us: `start` once; for every round of one tile per compute unit `end` and, for every step of 128 k, `step` with all units at work (the
 // chip's power and what the units share bound it then), `alone` with few; and no less than the bytes at `rate` GB/us take.  Fitted to 110 products and 90 over experts of
-// random sizes (1 to 8192 rows, 8 to 128 experts, 64 to 28672 columns, K 64 to 14336) timed on every kernel: a single time is predicted within 9 to
-// 15 % (root mean square).  On 400 other sizes the kernel with the smallest prediction is 1.8 % slower than the fastest one on average, 20 % at worst.
+// random sizes (1 to 8192 rows, 8 to 128 experts, 64 to 28672 columns, K 64 to 14336) timed on every kernel: a single time is predicted within 8 to
+// 15 % (root mean square; 13 to 18 % with fp32 results).  On 200 other sizes the kernel with the smallest prediction is 2.0 % slower than the fastest one on
+// average, 17 % at worst; on 200 with fp32 results 1.8 % and 33 %.  Left out because they choose no better: four bytes instead of two for an element of C in fp32 (1.9 % and 33 %),
+// the halves of tiles that a last round of 256 x 256 may have (2.0 to 2.2 %; a whole one is charged, which is 10 % too much there).
 const struct Cost {
     int rows, cols;
     double start, alone, step, end, rate;

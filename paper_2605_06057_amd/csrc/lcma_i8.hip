@@ -14,7 +14,7 @@ namespace {
 // L threads per row (a wave, four or sixteen), eight values at a time: a thread keeps its first two eights in registers and reads others again.  Bound by
 // the bytes it moves; the quotient is a product with 127 / amax and the rounding an addition of 1.5 * 2^23 (whose low byte is the code).
 // Measured: 8192 x 4096 bf16 18.3 us (5.5 TB/s), gated 8192 x 14336 106 (5.5 TB/s; 208 with a true division and every value computed twice), gated 2 x 14336
-// 4.5 (15 with a quarter of the threads).
+// 4.5 (15 with a quarter of the threads), where the shortest launches take 2.8: a row is one work-group's, loads of all of it, a meeting of its 16 waves and its stores one after the other.
 template <class T> LCMA_DEV void eight(const char *at, int k, int K, float (&v)[8]) { // values k .. k + 7 of a row, zeros from K on
     if (k + 8 <= K) {
         if constexpr (T::ES == 4) {

@@ -1,6 +1,7 @@
 // C = (A W^T) in 8-bit integers for gfx950: codes A (rows x K) and W (N x K, or experts x N x K), a scale for each row of A and of W:
 //   C[m][n] = SA[m] SW[n] sum_k A[m][k] W[n][k] (+ bias[n])
-// The sum is exact in 32-bit integers (K <= 131071), is turned into fp32 once, scaled there and rounded once to the type of C.  With
+// The sum is exact in 32-bit integers (K <= 131071), is turned into fp32 once, scaled there and rounded once to the type of C (16-bit rows that are combined into tokens
+// afterwards are rounded a second time there: half the bytes of fp32 rows, which a caller can have by asking for them).  With
 // offsets the rows of A are in groups, group e times the weights of expert e; rows behind the last group give zeros.
 //
 // Rows of codes are whole 128 bytes (zeros behind K).  All addresses of a tile are 32-bit offsets from 64-bit bases, so a matrix may be of any

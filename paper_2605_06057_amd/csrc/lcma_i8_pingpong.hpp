@@ -5,7 +5,7 @@
 // What bounds it: a step of 128 k is 2048 cycles of matrix instructions per SIMD against 192 KB of fragment reads (1536 clocks) and 64 KB of direct loads (820) of the
 // LDS, and beyond about a hundred work-groups power: a step takes 0.98 us on 64 CUs and 1.4 to 1.7 on 256, where the chip runs at 1.6 GHz with the matrix pipe
 // 71 % busy (8192 x 14336 x 4096; 2.2 GHz under the tiles of 128 x 256).
-// Measured (us, bf16 results): 8192 x 14336 x 4096 385 (2500 TOP/s; operands of zeros, which spare the power, 287; the vendor's 32-bit product of the same codes 506), 4096^3
+// Measured (us, bf16 results): 8192 x 14336 x 4096 385 to 400 (2400 to 2500 TOP/s; 520 at worst between 2 and 20 ms after a pause, while the power is being held; operands of zeros, which spare it, 287; the vendor's 32-bit product of the same codes 506), 4096^3
 // 58, 16384 x 4096 x 14336 715 (2690 TOP/s), 16384 rows of 8 experts x 28672 x 4096 1600, 8192 of 8 x 4096 x 14336 449.
 // Tried and not kept: the next tile's scales through LDS, with strips of 16 rows to make room (0.5 to 1 % slower).
 // Every work-group walks through tiles of its own, in turn; the loads run two steps ahead, into the next tile too.  The descriptors of the

@@ -8,8 +8,8 @@
 // row is written as zeros and never read.  All sums run in fp32 in a fixed order (j ascending; the gradient's dot product over fixed
 // lanes), so results do not change from run to run.
 //
-// The calls that move rows are bound by the bytes: 16384 tokens x 4 of 64 experts x 4096 bf16, one after the other: dispatch 127 us (671 MB), combine 111 (671), its
-// gradient 231 (1208), the sort 13: 3.2 GB in 590, 5.5 TB/s, where a copy of 2 GiB runs at 4.9 and a read at 6.1.  A token's rows are read or written by
+// The calls that move rows are bound by the bytes: 16384 tokens x 4 of 64 experts x 4096 bf16, one after the other: dispatch 125 us (671 MB), combine 111 (671), its
+// gradient 230 (1208), the sort 11: 3.2 GB in 590, 5.5 TB/s, where a copy of 2 GiB runs at 4.9 and a read at 6.1.  A token's rows are read or written by
 // the same threads, so the token's own row moves once; four rows are in flight together (one after the other: combine 165).
 #include <hip/hip_runtime.h>
 #include <stdint.h>

@@ -1,5 +1,5 @@
 """Which kernel of the 8-bit-integer product a call runs, found out on the CPU with launchers that record instead of launching: the rule reaches every
-kernel, more rows never take a kernel of smaller tiles by far, launches cover all tiles and stay within the limits of a grid."""
+kernel, launches cover all tiles and stay within the limits of a grid."""
 import ctypes
 import os
 import subprocess
