@@ -473,6 +473,56 @@ lcma_status lcma_tokens_combine_grad(int64_t tokens, int top_k, int64_t H, const
                                      lcma_dtype dtype, const int32_t *position, const float *weights, void *dY, int64_t lddy, float *dweights,
                                      void *stream);
 
+/* ------------------------------------------------------------------ products of experts in their own type, with both gradients
+ * Rows in expert order (lcma_tokens_dispatch writes them, lcma_tokens_sort the offsets) times a matrix of each expert's, as a training step runs them and as a layer that
+ * is not quantised is served: one call for all experts, the host never learns how many rows one has.  F32, BF16 and F16; sums in fp32, one rounding; BF16 is multiplied as
+ * it is.  offsets: experts + 1 row numbers on the device, ascending from 0.  Any sizes: N and K below 2^29, N * K up to 2^44, rows below 2^31, 1 to 1024 experts
+ * (SHAPE), alignment of an element; leading dimensions that hold a row, below 2^29 (SHAPE).  Fastest with 16-byte aligned pointers and N, K and leading dimensions of whole 16 bytes.  Outputs must not
+ * overlap inputs (ARG).  Calls run on `stream`, allocate nothing and do not synchronise.  Results do not depend on what runs beside them: no sum is formed by atomics.
+ *
+ * lcma_gemm_experts       C[r] = A[r] x W_e^T for the rows r = offsets[e] .. offsets[e + 1] - 1, for every expert e.  A: rows x K, C: rows x N.  b_layout 2: B holds
+ *                         W_e, experts x N x K; 0: B holds experts x K x N and C[r] = A[r] x B_e.  The gradient of A is the product of the gradient of C with the same
+ *                         weights in the other layout.  Rows of C from offsets[experts] on are set to zero.  K = 0: zeros.
+ * lcma_gemm_experts_grad  the gradient of W: dW_e[n][k] = sum over the rows r of expert e of dC[r][n] * A[r][k]; experts without rows get zeros.  dW: experts x N x K
+ *                         (for weights given K x N: dC and A, N and K change places).  Rows from offsets[experts] on are not read.
+ */
+lcma_status lcma_gemm_experts(int b_layout, int64_t rows, int64_t N, int64_t K, int experts, const int32_t *offsets, const void *A, int64_t lda, const void *B,
+                              void *C, int64_t ldc, lcma_dtype dtype, void *stream);
+lcma_status lcma_gemm_experts_grad(int64_t rows, int64_t N, int64_t K, int experts, const int32_t *offsets, const void *dC, int64_t lddc, const void *A, int64_t lda,
+                                   void *dW, lcma_dtype dtype, void *stream);
+
+/* The gate between an experts' layer's products, and its gradient.  A row of X is 2 F long, gates and then the linear part:
+ *   lcma_gated_silu       Y[f] = silu(X[f]) * X[F + f],  silu(g) = g s(g),  s(g) = 1 / (1 + exp(-g))
+ *   lcma_gated_silu_grad  dX[f] = dY[f] * X[F + f] * s(g) (1 + g (1 - s(g))),  dX[F + f] = dY[f] * silu(g),  g = X[f]
+ * All in fp32 (gates below -174 may give zero, an infinite one NaN), one rounding.  F32, BF16 and F16, alignment of an element, F below 2^26, rows below 2^31, leading
+ * dimensions that hold a row, below 2^29 (SHAPE).  Outputs must not overlap inputs (ARG). */
+lcma_status lcma_gated_silu(int64_t rows, int64_t F, const void *X, int64_t ldx, void *Y, int64_t ldy, lcma_dtype dtype, void *stream);
+lcma_status lcma_gated_silu_grad(int64_t rows, int64_t F, const void *dY, int64_t lddy, const void *X, int64_t ldx, void *dX, int64_t lddx, lcma_dtype dtype,
+                                 void *stream);
+
+/* ------------------------------------------------------------------ weights of 4 bits: a scale for each group of columns
+ * The linear layer with weights of 4-bit integers and activations as they are (F32, BF16 or F16), for the few rows of single tokens, where reading the weights is all:
+ *   C[m][n] = sum_k X[m][k] * q[n][k] * S[n][k / group]  (+ bias[n]),   q = -8 .. 7
+ * group: 32, 64 or 128; the last group of a row may be short.  Every activation is multiplied exactly, sums run in fp32 (the terms of a group first, which are then
+ * multiplied with its scale; their roundings count up to 2^-20 of sum |X| 8 S), one rounding.  An infinity or a NaN in a row of X, or a bf16 or fp32 value above 2^125, may give NaN in all of that
+ * row of C; scales have to be below 2^123.
+ * Weights are laid out once, into Wp (device memory, 16-byte aligned, lcma_i4_prepared_bytes() bytes for each expert; -1: bad sizes):
+ *   lcma_i4_quantize   from values W (experts x N x K, rows ldw elements apart, experts N * ldw; experts = 1: one matrix): S = max |w| / 7 over a group, q = rint(w / S) with ties to
+ *                      even, in fp32.  A group of zeros has S = 0; one that holds an infinity or a NaN has q = 0 and S = infinity or NaN: its products are NaN.
+ *   lcma_i4_prepare    from codes (int8, experts x N x K, -8 .. 7; others count as the nearest of these) and scales (fp32, experts x N x ceil(K / group))
+ * Any sizes: N and K below 2^29, N * K (N * ldw) up to 2^44, rows below 2^31 (SHAPE), alignment of an element; leading dimensions that hold a row, below 2^29 (SHAPE).  bias (fp32, N, or experts x N) may be null.
+ * K = 0: C = bias, or zeros.  Outputs must not overlap inputs (ARG).  Calls run on `stream`, allocate nothing and do not synchronise.
+ *   lcma_i4_gemm_nt       any number of rows M: up to a few hundred the weights' bytes decide, for long prompts lcma_gemm_nt with 16-bit weights is faster
+ *   lcma_i4_gemm_experts  rows offsets[e] .. offsets[e + 1] - 1 of X times the weights of expert e, as lcma_i8_gemm_experts; rows of C from offsets[experts] on are set to zero
+ */
+int64_t lcma_i4_prepared_bytes(int64_t N, int64_t K, int group);
+lcma_status lcma_i4_quantize(int experts, int64_t N, int64_t K, int group, const void *W, int64_t ldw, lcma_dtype dtype, void *Wp, void *stream);
+lcma_status lcma_i4_prepare(int experts, int64_t N, int64_t K, int group, const int8_t *codes, const float *scales, void *Wp, void *stream);
+lcma_status lcma_i4_gemm_nt(int64_t M, int64_t N, int64_t K, int group, const void *X, int64_t ldx, const void *Wp, const float *bias, void *C, int64_t ldc,
+                            lcma_dtype dtype, void *stream);
+lcma_status lcma_i4_gemm_experts(int64_t rows, int64_t N, int64_t K, int group, int experts, const int32_t *offsets, const void *X, int64_t ldx, const void *Wp,
+                                 const float *bias, void *C, int64_t ldc, lcma_dtype dtype, void *stream);
+
 /* ------------------------------------------------------------------ tile scheduling (Sec. 3.2, Split-Group Parallelism)
  * Wave counts for `groups` groups of R tile-products on `units` compute units:
  * tile-level scheduling needs ceil(groups*R/units) waves, group-level ceil(groups/units)*R.

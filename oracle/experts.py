@@ -80,3 +80,40 @@ def tokens_combine_grad(dx, y, position, weights):
             dy[row] = float(weights[t, j]) * dx[t]
             dw[t, j] = dx[t] @ y[row]
     return dy, dw
+
+
+def gemm_experts(a, offsets, w, b_nk=True):
+    """Rows of a, in groups by offsets, times w[e]^T (experts x N x K), or w[e] (experts x K x N)."""
+    c = np.zeros((a.shape[0], w.shape[1 if b_nk else 2]))
+    for e in range(w.shape[0]):
+        c[offsets[e]:offsets[e + 1]] = a[offsets[e]:offsets[e + 1]] @ (w[e].T if b_nk else w[e])
+    return c
+
+
+def gemm_experts_grad(dc, a, offsets):
+    return np.stack([dc[b:e].T @ a[b:e] for b, e in zip(offsets, offsets[1:])])
+
+
+def silu_gate_grad(dy, x):
+    g, u = np.split(x.astype(np.float64), 2, axis=1)
+    s = 1 / (1 + np.exp(-g))
+    return np.concatenate([dy * u * s * (1 + g * (1 - s)), dy * g * s], axis=1)
+
+
+def i4_quantize(w: np.ndarray, group: int):
+    """Codes (int8, -7 .. 7) and scales (float32) of the rows of w (N x K): the arithmetic is defined in fp32."""
+    w = w.astype(np.float32)
+    N, K = w.shape
+    q, s = np.zeros((N, K), np.int8), np.zeros((N, -(-K // group)), np.float32)
+    for g in range(s.shape[1]):
+        part = w[:, g * group:(g + 1) * group]
+        amax = np.where(np.isnan(part).any(axis=1), np.float32(np.nan), np.abs(part).max(axis=1, initial=0))
+        s[:, g] = amax / np.float32(7)
+        with np.errstate(all="ignore"):
+            codes = np.clip(np.rint(part / s[:, g:g + 1]), -7, 7)
+        q[:, g * group:(g + 1) * group] = np.where((s[:, g:g + 1] > 0) & np.isfinite(s[:, g:g + 1]), codes, 0)
+    return q, s
+
+
+def i4_dequantize(q, s, group: int):
+    return q.astype(np.float64) * np.repeat(s.astype(np.float64), group, axis=-1)[..., : q.shape[-1]]

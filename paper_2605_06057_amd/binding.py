@@ -1,4 +1,4 @@
-"""Thin binding of liblcma.so: argument marshalling only (ctypes; the 8-bit-integer calls and the tokens' through _calls.so), same names as include/lcma.h.
+"""Thin binding of liblcma.so: argument marshalling only (ctypes; the calls in 8 and 4 bits, the experts' and the tokens' through _calls.so), same names as include/lcma.h.
 
 Every step of the GEMM runs in the library's HIP kernels.  There is no CPU or PyTorch
 fallback: if the shared library is missing, loading raises.
@@ -36,6 +36,8 @@ EXPORTS = [
     "lcma_fp8_prepare_w", "lcma_fp8_workspace_bytes", "lcma_fp8_gemm_lcma",
     "lcma_i8_code_pitch", "lcma_i8_quantize", "lcma_i8_quantize_dispatch", "lcma_i8_gemm_nt", "lcma_i8_gemm_experts",
     "lcma_tokens_sort_workspace_bytes", "lcma_tokens_sort", "lcma_tokens_dispatch", "lcma_tokens_combine", "lcma_tokens_combine_grad",
+    "lcma_gemm_experts", "lcma_gemm_experts_grad", "lcma_gated_silu", "lcma_gated_silu_grad",
+    "lcma_i4_prepared_bytes", "lcma_i4_quantize", "lcma_i4_prepare", "lcma_i4_gemm_nt", "lcma_i4_gemm_experts",
 ]
 
 
@@ -148,6 +150,16 @@ def lib() -> ctypes.CDLL:
         L.lcma_tokens_dispatch.argtypes = [i64, i32, i64, vp, i64, i32, vp, vp, i64, vp]
         L.lcma_tokens_combine.argtypes = [i64, i32, i64, vp, i64, i32, vp, vp, vp, i64, vp]
         L.lcma_tokens_combine_grad.argtypes = [i64, i32, i64, vp, i64, vp, i64, i32, vp, vp, vp, i64, vp, vp]
+        L.lcma_gemm_experts.argtypes = [i32, i64, i64, i64, i32, vp, vp, i64, vp, vp, i64, i32, vp]
+        L.lcma_gemm_experts_grad.argtypes = [i64, i64, i64, i32, vp, vp, i64, vp, i64, vp, i32, vp]
+        L.lcma_gated_silu.argtypes = [i64, i64, vp, i64, vp, i64, i32, vp]
+        L.lcma_gated_silu_grad.argtypes = [i64, i64, vp, i64, vp, i64, vp, i64, i32, vp]
+        L.lcma_i4_prepared_bytes.argtypes = [i64, i64, i32]
+        L.lcma_i4_prepared_bytes.restype = i64
+        L.lcma_i4_quantize.argtypes = [i32, i64, i64, i32, vp, i64, i32, vp, vp]
+        L.lcma_i4_prepare.argtypes = [i32, i64, i64, i32, vp, vp, vp, vp]
+        L.lcma_i4_gemm_nt.argtypes = [i64, i64, i64, i32, vp, i64, vp, vp, vp, i64, i32, vp]
+        L.lcma_i4_gemm_experts.argtypes = [i64, i64, i64, i32, i32, vp, vp, i64, vp, vp, vp, i64, i32, vp]
         _lib = L
         # schemes that kernels were generated for beyond the paper's three
         for sid in range(4, int(L.lcma_scheme_id_max()) + 1):
@@ -638,6 +650,82 @@ def lcma_tokens_combine_grad(dX, Y, position, weights, dY=None, dweights=None):
     if status := (_calls or _native()).tokens_combine_grad(dX, Y, position, weights, dY, dweights):
         _check(status)
     return dY, dweights
+
+
+# ---------------------------------------------------------------- products of experts in their own type, their gate, and the gradients of both
+def lcma_gemm_experts(A, offsets, W, C=None, b_nk: bool = True):
+    """C (rows x N): rows offsets[e] .. offsets[e + 1] - 1 of A (rows x K) times the weights W[e]^T (W: experts x N x K), or, without b_nk, times W[e] (experts x K x N:
+    the gradient of A from that of C, with the weights of the other layout); rows of C behind the last expert's are set to zero."""
+    if C is None:
+        C = _empty(A, A.shape[0], W.shape[1 if b_nk else 2])
+    if status := (_calls or _native()).gemm_experts(A, offsets, W, C, b_nk):
+        _check(status)
+    return C
+
+
+def lcma_gemm_experts_grad(dC, A, offsets, dW=None):
+    """Gradient of the weights of lcma_gemm_experts: dW[e] (N x K) = dC^T A over the rows of expert e (dC: rows x N, A: rows x K), zeros for an expert without rows."""
+    if dW is None:
+        dW = _empty(A, offsets.shape[0] - 1, dC.shape[1], A.shape[1])
+    if status := (_calls or _native()).gemm_experts_grad(dC, A, offsets, dW):
+        _check(status)
+    return dW
+
+
+def lcma_gated_silu(X, Y=None):
+    """Y (rows x F) = silu(first half) * second half of the rows of X (rows x 2 F)."""
+    if Y is None:
+        Y = _empty(X, X.shape[0], X.shape[1] // 2)
+    if status := (_calls or _native()).gated_silu(X, Y):
+        _check(status)
+    return Y
+
+
+def lcma_gated_silu_grad(dY, X, dX=None):
+    """Gradient of lcma_gated_silu: dX (rows x 2 F) from dY (rows x F) and X."""
+    if dX is None:
+        dX = _empty(X, *X.shape)
+    if status := (_calls or _native()).gated_silu_grad(dY, X, dX):
+        _check(status)
+    return dX
+
+
+# ---------------------------------------------------------------- weights of 4 bits (a scale for each group of columns)
+def lcma_i4_prepared_bytes(N: int, K: int, group: int = 128) -> int:
+    return int(lib().lcma_i4_prepared_bytes(N, K, group))
+
+
+def lcma_i4_quantize(W, group: int = 128, Wp=None):
+    """The weights W (N x K, or experts x N x K) quantised to 4 bits with a scale for each group of columns and laid out for the products (uint8, one row for each expert)."""
+    if Wp is None:
+        Wp = _empty(W, *W.shape[:-2], max(lcma_i4_prepared_bytes(*W.shape[-2:], group), 0), dtype="uint8")
+    if status := (_calls or _native()).i4_quantize(W, group, Wp):
+        _check(status)
+    return Wp
+
+
+def lcma_i4_prepare(codes, scales, group: int = 128, Wp=None):
+    """Weights given as codes (int8 of -8 .. 7, N x K or experts x N x K) and scales (fp32, a group's in the place of its columns) laid out for the products."""
+    if Wp is None:
+        Wp = _empty(codes, *codes.shape[:-2], max(lcma_i4_prepared_bytes(*codes.shape[-2:], group), 0), dtype="uint8")
+    if status := (_calls or _native()).i4_prepare(codes, scales, group, Wp):
+        _check(status)
+    return Wp
+
+
+def lcma_i4_gemm_nt(X, Wp, C, group: int = 128, bias=None):
+    """C (M x N) = X (M x K) times the prepared 4-bit weights Wp (N x K), plus bias (fp32)."""
+    if status := (_calls or _native()).i4_gemm_nt(X, Wp, C, group, bias):
+        _check(status)
+    return C
+
+
+def lcma_i4_gemm_experts(X, offsets, Wp, C, group: int = 128, bias=None):
+    """lcma_i4_gemm_nt over experts: rows offsets[e] .. offsets[e + 1] - 1 of X times the weights Wp[e], bias experts x N; rows of C behind the last expert's are
+    set to zero."""
+    if status := (_calls or _native()).i4_gemm_experts(X, offsets, Wp, C, group, bias):
+        _check(status)
+    return C
 
 
 def lcma_set_tuning(key: str, value: str = ""):

@@ -73,7 +73,7 @@ def _build_calls(force: bool) -> str:
     if os.path.exists(CALLS):
         os.remove(CALLS)
     if missing := _calls_missing():
-        return f"not built  calls.cc: {missing} not found; the 8-bit-integer calls and the tokens' are left out of the Python binding"
+        return f"not built  calls.cc: {missing} not found; the calls in 8 and 4 bits, the experts' and the tokens' are left out of the Python binding"
     import sysconfig
 
     import torch
@@ -98,11 +98,11 @@ def build(force: bool = False, jobs: int | None = None, verbose: bool = True) ->
     from .gen.generate import generate
 
     hips = generate(GEN)
-    headers = [os.path.join(CSRC, h) for h in ("lcma_device.hpp", "lcma_prepare_b.hpp", "lcma_combine_h.hpp", "lcma_params.h", "host_common.h", "lcma_fp8.hpp", "lcma_plane_gemm.hpp", "lcma_pingpong.hpp", "lcma_kpair.hpp", "lcma_pingpong_narrow.hpp", "lcma_few_rows.hpp", "lcma_direct.hpp", "lcma_direct16.hpp", "lcma_i8.hpp", "lcma_i8_pingpong.hpp", "lcma_i8_narrow.hpp", "lcma_i8_few_rows.hpp", "lcma_lanes.hpp", "lcma_experts_params.h", "experts_host.h")]
+    headers = [os.path.join(CSRC, h) for h in ("lcma_device.hpp", "lcma_prepare_b.hpp", "lcma_combine_h.hpp", "lcma_params.h", "host_common.h", "lcma_fp8.hpp", "lcma_plane_gemm.hpp", "lcma_pingpong.hpp", "lcma_kpair.hpp", "lcma_pingpong_narrow.hpp", "lcma_few_rows.hpp", "lcma_direct.hpp", "lcma_direct16.hpp", "lcma_i8.hpp", "lcma_i8_pingpong.hpp", "lcma_i8_narrow.hpp", "lcma_i8_few_rows.hpp", "lcma_lanes.hpp", "lcma_experts.hpp", "lcma_gated.hpp", "lcma_i4.hpp", "lcma_experts_params.h", "experts_host.h")]
     headers.append(os.path.join(PKG, "..", "include", "lcma.h"))
     headers.append(os.path.join(GEN, "builtin_schemes.inc"))
     units = [(h, h[:-4] + ".o") for h in hips]
-    for name in ("api.cc", "scheme.cc", "model.cc", "unfused.cc", "lcma_aux.hip", "lcma_static.hip", "lcma_fp8.hip", "fp8_api.cc", "lcma_plane_gemm.hip", "plane_gemm.cc", "lcma_few_rows.hip", "lcma_small_plain.hip", "lcma_i8.hip", "i8_api.cc", "lcma_tokens.hip", "tokens_api.cc"):
+    for name in ("api.cc", "scheme.cc", "model.cc", "unfused.cc", "lcma_aux.hip", "lcma_static.hip", "lcma_fp8.hip", "fp8_api.cc", "lcma_plane_gemm.hip", "plane_gemm.cc", "lcma_few_rows.hip", "lcma_small_plain.hip", "lcma_i8.hip", "i8_api.cc", "lcma_tokens.hip", "tokens_api.cc", "lcma_experts.hip", "lcma_gated.hip", "experts_api.cc", "lcma_i4.hip", "i4_api.cc"):
         units.append((os.path.join(CSRC, name), os.path.join(GEN, os.path.splitext(name)[0] + ".o")))
     units.append((os.path.join(GEN, "registry.cc"), os.path.join(GEN, "registry.o")))
     jobs = jobs or min(8, os.cpu_count() or 1)

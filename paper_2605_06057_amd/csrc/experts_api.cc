@@ -1,0 +1,164 @@
+// Host side of the experts' products in their own type and of their gate: argument checks, launches.
+#include "experts_host.h"
+
+#include <cstring>
+
+extern "C" int lcma_launch_experts_gemm(const lcma::ExpertsGemmParams *p, int form, int kernel, int dtype, int grid, void *stream);
+extern "C" int lcma_launch_gated(const lcma::GatedParams *p, int dtype, int back, int gx, int gy, void *stream);
+
+using namespace lcma;
+
+namespace {
+
+const int kTile[kExpKernels][2] = {{64, 64}, {128, 128}}; // rows and columns of the kernels' tiles
+
+int64_t span(int64_t rows, int64_t ld, int64_t cols, int es) { return rows > 0 && cols > 0 ? ((rows - 1) * ld + cols) * es : 0; }
+int64_t tiles(int64_t n, int64_t of) { return (n + of - 1) / of; }
+
+// Tiles, at most: every group of rows may end in one of its own that is not full.
+int64_t product_tiles(int kernel, int64_t rows, int64_t N, int experts) {
+    return (rows / kTile[kernel][0] + (rows < experts ? rows : experts)) * tiles(N, kTile[kernel][1]);
+}
+int64_t gradient_tiles(int kernel, int64_t M, int64_t N, int experts) { return experts * tiles(M, kTile[kernel][0]) * tiles(N, kTile[kernel][1]); }
+bool launches(int64_t jobs) { return (jobs + 8) * 512 < kGridLimit / 2; } // (numbers of tiles are 32-bit on the device)
+
+lcma_status check_sizes(const char *who, int64_t rows, int64_t N, int64_t K, int experts, int dtype) {
+    if (!dtype_size(dtype)) return fail(LCMA_ERR_DTYPE, "%s: unknown dtype %d", who, dtype);
+    if (rows < 0 || N < 0 || K < 0) return fail(LCMA_ERR_ARG, "%s: negative size", who);
+    if (experts < 1) return fail(LCMA_ERR_ARG, "%s: experts = %d must be at least 1", who, experts);
+    if (experts > kMaxExperts) return fail(LCMA_ERR_SHAPE, "%s: experts = %d is more than %d", who, experts, kMaxExperts);
+    if (rows >= kRowLimit) return fail(LCMA_ERR_SHAPE, "%s: 2^31 rows or more", who);
+    if (N >= kPitchLimit || K >= kPitchLimit || N * K > kMatrixLimit) return fail(LCMA_ERR_SHAPE, "%s: 2^29 columns or more, or a matrix of more than 2^44 elements", who);
+    return LCMA_OK;
+}
+lcma_status check_pitch(const char *who, int64_t ld, int64_t row) {
+    if (ld < row) return fail(LCMA_ERR_ARG, "%s: leading dimension smaller than the row", who);
+    if (ld >= kPitchLimit) return fail(LCMA_ERR_SHAPE, "%s: leading dimension of 2^29 or more", who);
+    return LCMA_OK;
+}
+
+} // namespace
+
+extern "C" lcma_status lcma_gemm_experts(int b_layout, int64_t rows, int64_t N, int64_t K, int experts, const int32_t *offsets, const void *A, int64_t lda, const void *B,
+                                         void *C, int64_t ldc, lcma_dtype dtype, void *stream) {
+    const char *who = "lcma_gemm_experts";
+    if (b_layout != 0 && b_layout != 2) return fail(LCMA_ERR_ARG, "%s: b_layout = %d must be 0 (K x N) or 2 (N x K)", who, b_layout);
+    if (const lcma_status st = check_sizes(who, rows, N, K, experts, dtype)) return st;
+    if (rows == 0 || N == 0) return LCMA_OK;
+    if (!offsets || !C || (K && (!A || !B))) return fail(LCMA_ERR_ARG, "%s: null pointer", who);
+    if (const lcma_status st = check_pitch(who, lda, K)) return st;
+    if (const lcma_status st = check_pitch(who, ldc, N)) return st;
+    const int es = dtype_size(dtype);
+    if (((uintptr_t)A | (uintptr_t)B | (uintptr_t)C) % es || ((uintptr_t)offsets & 3))
+        return fail(LCMA_ERR_ARG, "%s: matrices must have the alignment of their elements, offsets 4-byte alignment", who);
+    const int64_t c_bytes = span(rows, ldc, N, es);
+    if (touch(C, c_bytes, A, span(rows, lda, K, es)) || touch(C, c_bytes, B, experts * N * K * es) || touch(C, c_bytes, offsets, ((int64_t)experts + 1) * 4))
+        return fail(LCMA_ERR_ARG, "%s: C overlaps an operand", who);
+    ExpertsGemmParams p;
+    std::memset(&p, 0, sizeof p);
+    p.A = (const char *)A;
+    p.B = (const char *)B;
+    p.C = (char *)C;
+    p.offsets = offsets;
+    p.lda_b = lda * es;
+    p.ldb_b = (b_layout ? K : N) * es;
+    p.ldc_b = ldc * es;
+    p.expert_b = N * K * es;
+    p.rows = (int32_t)rows;
+    p.N = (int32_t)N;
+    p.K = (int32_t)K;
+    p.experts = experts;
+    p.panel = 8;
+    int kernel = rows < 64 * (int64_t)experts ? kExpStaged64 : kExpStaged128;
+    if (!launches(product_tiles(kernel, rows, N, experts))) kernel = kExpStaged128;
+    const int64_t jobs = product_tiles(kernel, rows, N, experts);
+    if (!launches(jobs)) return fail(LCMA_ERR_SHAPE, "%s: too many tiles for a launch", who);
+    p.nz = (int32_t)tiles(N, kTile[kernel][1]);
+    if (const int err = lcma_launch_experts_gemm(&p, b_layout ? 0 : 1, kernel, dtype, (int)((jobs + 7) / 8 * 8), stream))
+        return fail(LCMA_ERR_HIP, "%s: launch failed with HIP error %d", who, err);
+    return LCMA_OK;
+}
+
+extern "C" lcma_status lcma_gemm_experts_grad(int64_t rows, int64_t N, int64_t K, int experts, const int32_t *offsets, const void *dC, int64_t lddc, const void *A, int64_t lda,
+                                              void *dW, lcma_dtype dtype, void *stream) {
+    const char *who = "lcma_gemm_experts_grad";
+    if (const lcma_status st = check_sizes(who, rows, N, K, experts, dtype)) return st;
+    if (N == 0 || K == 0) return LCMA_OK;
+    if (!offsets || !dW || (rows && (!dC || !A))) return fail(LCMA_ERR_ARG, "%s: null pointer", who);
+    if (const lcma_status st = check_pitch(who, lddc, N)) return st;
+    if (const lcma_status st = check_pitch(who, lda, K)) return st;
+    const int es = dtype_size(dtype);
+    if (((uintptr_t)A | (uintptr_t)dC | (uintptr_t)dW) % es || ((uintptr_t)offsets & 3))
+        return fail(LCMA_ERR_ARG, "%s: matrices must have the alignment of their elements, offsets 4-byte alignment", who);
+    const int64_t w_bytes = experts * N * K * es;
+    if (touch(dW, w_bytes, dC, span(rows, lddc, N, es)) || touch(dW, w_bytes, A, span(rows, lda, K, es)) || touch(dW, w_bytes, offsets, ((int64_t)experts + 1) * 4))
+        return fail(LCMA_ERR_ARG, "%s: dW overlaps an operand", who);
+    ExpertsGemmParams p;
+    std::memset(&p, 0, sizeof p);
+    p.A = (const char *)dC;
+    p.B = (const char *)A;
+    p.C = (char *)dW;
+    p.offsets = offsets;
+    p.lda_b = lddc * es;
+    p.ldb_b = lda * es;
+    p.ldc_b = K * es;
+    p.expert_b = N * K * es;
+    p.rows = (int32_t)rows;
+    p.M = (int32_t)N;
+    p.N = (int32_t)K;
+    p.experts = experts;
+    int kernel = gradient_tiles(kExpStaged128, N, K, experts) < 512 ? kExpStaged64 : kExpStaged128;
+    const int64_t jobs = gradient_tiles(kernel, N, K, experts);
+    if (!launches(jobs)) return fail(LCMA_ERR_SHAPE, "%s: too many tiles for a launch", who);
+    p.nx = (int32_t)tiles(N, kTile[kernel][0]);
+    p.nz = (int32_t)tiles(K, kTile[kernel][1]);
+    if (const int err = lcma_launch_experts_gemm(&p, 2, kernel, dtype, (int)((jobs + 7) / 8 * 8), stream))
+        return fail(LCMA_ERR_HIP, "%s: launch failed with HIP error %d", who, err);
+    return LCMA_OK;
+}
+
+namespace {
+
+// dY null: forward, Y from X; else Y is dX.
+lcma_status gated(const char *who, int64_t rows, int64_t F, const void *dY, int64_t lddy, const void *X, int64_t ldx, void *Y, int64_t ldy, int dtype, bool back, void *stream) {
+    const int es = dtype_size(dtype);
+    if (!es) return fail(LCMA_ERR_DTYPE, "%s: unknown dtype %d", who, dtype);
+    if (rows < 0 || F < 0) return fail(LCMA_ERR_ARG, "%s: negative size", who);
+    if (rows >= kRowLimit) return fail(LCMA_ERR_SHAPE, "%s: 2^31 rows or more", who);
+    if (F >= kPitchLimit / 8) return fail(LCMA_ERR_SHAPE, "%s: a row is too long", who);
+    if (rows == 0 || F == 0) return LCMA_OK;
+    if (!X || !Y || (back && !dY)) return fail(LCMA_ERR_ARG, "%s: null pointer", who);
+    const int64_t width = back ? 2 * F : F;
+    if (ldx < 2 * F || ldy < width || (back && lddy < F)) return fail(LCMA_ERR_ARG, "%s: leading dimension smaller than the row", who);
+    if (ldx >= kPitchLimit || ldy >= kPitchLimit || (back && lddy >= kPitchLimit)) return fail(LCMA_ERR_SHAPE, "%s: leading dimension of 2^29 or more", who);
+    if (((uintptr_t)X | (uintptr_t)Y | (uintptr_t)dY) % es) return fail(LCMA_ERR_ARG, "%s: rows must have the alignment of their elements", who);
+    const int64_t y_bytes = span(rows, ldy, width, es);
+    if (touch(Y, y_bytes, X, span(rows, ldx, 2 * F, es)) || (back && touch(Y, y_bytes, dY, span(rows, lddy, F, es)))) return fail(LCMA_ERR_ARG, "%s: the result overlaps an input", who);
+    GatedParams p;
+    std::memset(&p, 0, sizeof p);
+    p.X = (const char *)X;
+    p.dY = (const char *)dY;
+    p.Y = (char *)Y;
+    p.ldx_b = ldx * es;
+    p.lddy_b = lddy * es;
+    p.ldy_b = ldy * es;
+    p.rows = (int32_t)rows;
+    p.F = (int32_t)F;
+    const int64_t vectors = (F + 7) / 8;
+    while (p.lane_shift < 8 && ((int64_t)1 << p.lane_shift) < vectors) ++p.lane_shift;
+    const int64_t per = 256 >> p.lane_shift, gx = (rows + per - 1) / per, gy = tiles(vectors, (int64_t)1 << p.lane_shift);
+    const int64_t most = 1 << 20; // (work-groups along x; each then takes several groups of rows)
+    if (const int err = lcma_launch_gated(&p, dtype, back, (int)(gx < most ? gx : most), (int)gy, stream)) return fail(LCMA_ERR_HIP, "%s: launch failed with HIP error %d", who, err);
+    return LCMA_OK;
+}
+
+} // namespace
+
+extern "C" lcma_status lcma_gated_silu(int64_t rows, int64_t F, const void *X, int64_t ldx, void *Y, int64_t ldy, lcma_dtype dtype, void *stream) {
+    return gated("lcma_gated_silu", rows, F, nullptr, 0, X, ldx, Y, ldy, dtype, false, stream);
+}
+
+extern "C" lcma_status lcma_gated_silu_grad(int64_t rows, int64_t F, const void *dY, int64_t lddy, const void *X, int64_t ldx, void *dX, int64_t lddx, lcma_dtype dtype,
+                                            void *stream) {
+    return gated("lcma_gated_silu_grad", rows, F, dY, lddy, X, ldx, dX, lddx, dtype, true, stream);
+}

@@ -8,6 +8,8 @@ namespace lcma {
 constexpr int64_t kRowLimit = (int64_t)1 << 31;   // rows, columns and slots are counted in 32 bits on the device
 constexpr int64_t kPitchLimit = (int64_t)1 << 29; // leading dimensions: 2^31 rows of 2^29 elements of 4 bytes are 2^62 bytes
 
+constexpr int64_t kMatrixLimit = (int64_t)1 << 44; // elements of an expert's matrix: 1024 of them are 2^56 bytes at most
+
 constexpr int64_t kGridLimit = (int64_t)1 << 32;  // threads of a launch along a dimension
 
 // the kernels of the product by number (lcma_experts_params.h), named by the rows and columns of their tiles

@@ -1,5 +1,5 @@
-// Argument blocks of the 8-bit-integer product and of the tokens' way to their experts and back, shared by the host launchers and
-// the kernels.
+// Argument blocks of the 8-bit-integer product, of the tokens' way to their experts and back, of the experts' products in their own type and of their gate,
+// shared by the host launchers and the kernels.
 #pragma once
 #include <stdint.h>
 
@@ -61,6 +61,55 @@ struct I8GemmParams {
     int32_t rows, N, pitch; // pitch: bytes of a row of A and W, a multiple of 128
     int32_t experts, steps; // steps of 128 bytes of K
     int32_t nz, panel;      // tiles along N, and the width of a column panel of the tile order
+};
+
+// Kernels of the experts' products (csrc/lcma_experts.hpp).
+enum { kExpStaged64 = 0, kExpStaged128, kExpKernels };
+
+// lcma_gemm_experts: rows of A (k-contiguous) in groups, group e times the matrix of expert e (N x K, or K x N).
+// lcma_gemm_experts_grad: for every expert the product of its rows of A, transposed, and its rows of B: M x N, summed over the rows.
+struct ExpertsGemmParams {
+    const char *A, *B;
+    char *C;
+    const int32_t *offsets;         // experts + 1
+    int64_t lda_b, ldb_b, ldc_b;    // bytes from a row of the stored matrices to the next
+    int64_t expert_b;               // bytes from an expert's matrix to the next: of B (product), of C (gradient)
+    int32_t rows, M, N, K, experts; // M: rows of an expert's C (gradient); K: what a product sums over
+    int32_t nx, nz, panel;          // tiles along M (gradient) and N; width of a column panel of the tile order (product)
+};
+
+// lcma_gated_silu, lcma_gated_silu_grad: row pitches in bytes.
+struct GatedParams {
+    const char *X, *dY;
+    char *Y; // or dX
+    int64_t ldx_b, lddy_b, ldy_b;
+    int32_t rows, F;
+    int32_t lane_shift; // 2^lane_shift neighbouring threads along a row
+};
+
+// 4-bit weights (csrc/lcma_i4.hpp): blocks of 16 rows x 128 columns, a row of blocks behind the other; a block is its codes (1024 bytes) and, for every group of
+// columns, 16 scales (fp32).
+inline int64_t i4_block_bytes(int group) { return 1024 + 128 / group * 64; }
+// lcma_i4_quantize, lcma_i4_prepare: rows x K values, or codes and scales, laid out as blocks.
+struct I4PrepareParams {
+    const void *W;       // values in a storage type, or codes (int8)
+    const float *S;      // scales (rows x groups), or null: quantise
+    char *Q;
+    int64_t ldw_b, expert_b, expert_q; // bytes from row to row, from expert to expert
+    int32_t N, K, group, experts;
+};
+// Kernels of the product with them: tiles of 16 and of 64 rows.
+enum { kI4Rows16 = 0, kI4Rows64, kI4Kernels };
+// lcma_i4_gemm_nt, lcma_i4_gemm_experts.
+struct I4GemmParams {
+    const char *X, *Q;
+    const float *bias;      // N, or experts x N; may be null
+    char *C;
+    const int32_t *offsets; // experts + 1; null: one group of all rows
+    int64_t ldx_b, ldc, expert_q; // ldc: elements
+    int32_t rows, N, K, experts;
+    int32_t blocks;         // of 128 columns
+    int32_t nz, panel;      // tiles along N
 };
 
 } // namespace lcma

@@ -1,0 +1,61 @@
+// The gate of an experts' layer and its gradient: rows X = (g, u) of 2 F values, Y = silu(g) u; dX = dY (silu'(g) u, silu(g)).
+// Bound by the bytes it moves: three rows of F values forward, five back.  All arithmetic is in fp32, one rounding; the exponential is the accurate form for
+// every type (about 20 operations forward and 30 back for a value, where the memory leaves room for 43 and 71).
+#include "lcma_gated.hpp"
+#include "lcma_i8.hpp"
+
+using namespace lcma;
+
+namespace {
+
+template <class T> LCMA_DEV void put_eight(char *at, const float (&v)[8], int n) { // n values, up to 8, from v on
+    if constexpr (T::ES == 4) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) i8_store16<T>(at + h * 16, __builtin_bit_cast(u32x4, f32x4{v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]}), n - 4 * h);
+    } else {
+        u32x4 raw;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) raw[i] = Round<T>::run(v[2 * i]) | (Round<T>::run(v[2 * i + 1]) << 16);
+        i8_store16<T>(at, raw, n);
+    }
+}
+
+// A thread: eight values of every gridDim.x-th group of rows.
+template <class T, bool BACK> __global__ __launch_bounds__(256) void gated(const GatedParams p) {
+    const int lanes = 1 << p.lane_shift, rows_of = 256 >> p.lane_shift, k = ((int)blockIdx.y * lanes + (int)(threadIdx.x & (lanes - 1))) * 8;
+    if (k >= p.F) return;
+    const int64_t up = (int64_t)p.F * T::ES, at = (int64_t)k * T::ES;
+    for (int64_t r = (int64_t)blockIdx.x * rows_of + (threadIdx.x >> p.lane_shift); r < p.rows; r += (int64_t)gridDim.x * rows_of) {
+        float g[8], u[8], y[8];
+        const char *x = p.X + r * p.ldx_b;
+        eight<T>(x, k, p.F, g);
+        eight<T>(x + up, k, p.F, u);
+        if constexpr (BACK) {
+            float dg[8], du[8];
+            eight<T>(p.dY + r * p.lddy_b, k, p.F, y);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) gated_back(g[i], u[i], y[i], dg[i], du[i]);
+            char *to = p.Y + r * p.ldy_b + at;
+            put_eight<T>(to, dg, p.F - k);
+            put_eight<T>(to + up, du, p.F - k);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[i] = gated_far(g[i], u[i]);
+            put_eight<T>(p.Y + r * p.ldy_b + at, y, p.F - k);
+        }
+    }
+}
+
+} // namespace
+
+extern "C" int lcma_launch_gated(const lcma::GatedParams *p, int dtype, int back, int gx, int gy, void *stream) {
+    const hipStream_t s = (hipStream_t)stream;
+#define LCMA_GATED(T)                                                                  \
+    if (back) gated<T, true><<<dim3(gx, gy), dim3(256), 0, s>>>(*p);                   \
+    else gated<T, false><<<dim3(gx, gy), dim3(256), 0, s>>>(*p);
+    if (dtype == 0) { LCMA_GATED(F32) }
+    else if (dtype == 1) { LCMA_GATED(BF16) }
+    else { LCMA_GATED(F16) }
+#undef LCMA_GATED
+    return (int)hipGetLastError();
+}

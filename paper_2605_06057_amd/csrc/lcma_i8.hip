@@ -1,7 +1,7 @@
 // Rows quantised to 8-bit integers, and the instances of the 8-bit-integer product (csrc/lcma_i8.hpp).
+#include "lcma_gated.hpp"
 #include "lcma_i8_few_rows.hpp"
 #include "lcma_i8_narrow.hpp"
-#include "lcma_prepare_b.hpp"
 
 using namespace lcma;
 
@@ -15,44 +15,6 @@ namespace {
 // the bytes it moves; the quotient is a product with 127 / amax and the rounding an addition of 1.5 * 2^23 (whose low byte is the code).
 // Measured: 8192 x 4096 bf16 18.3 us (5.5 TB/s), gated 8192 x 14336 106 (5.5 TB/s; 208 with a true division and every value computed twice), gated 2 x 14336
 // 4.5 (15 with a quarter of the threads), where the shortest launches take 2.8: a row is one work-group's, loads of all of it, a meeting of its 16 waves and its stores one after the other.
-template <class T> LCMA_DEV void eight(const char *at, int k, int K, float (&v)[8]) { // values k .. k + 7 of a row, zeros from K on
-    if (k + 8 <= K) {
-        if constexpr (T::ES == 4) {
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                f32x4 raw;
-                __builtin_memcpy(&raw, at + (int64_t)(k + 4 * h) * 4, 16);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) v[4 * h + i] = raw[i];
-            }
-        } else {
-            u32x4 raw;
-            __builtin_memcpy(&raw, at + (int64_t)k * 2, 16);
-            Widen<T>::run(raw, v);
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            v[i] = 0.f;
-            if (k + i < K) {
-                if constexpr (T::ES == 4) v[i] = ((const float *)at)[k + i];
-                else if constexpr (std::is_same_v<T, F16>) v[i] = (float)((const _Float16 *)at)[k + i];
-                else v[i] = __builtin_bit_cast(float, (uint32_t)((const uint16_t *)at)[k + i] << 16);
-            }
-        }
-    }
-}
-// silu(g) u = g / (1 + exp(-g)) u for gates far below zero.  exp(-g) leaves fp32 at g = -88.7, where silu is 2^-121 and u may be anything: so the exponential h is
-// taken of -|g| / 2 and used twice, g h / (1 + h^2) u h, which holds down to g = -174.  Its argument, to base 2, is in two parts, the second one a linear term: rounded to
-// one, it would cost 2^-24 |g| of the result.  |g| is held at 400, where h is zero, for the infinities.
-LCMA_DEV float gated_far(float g, float u) {
-#pragma clang fp contract(off)
-    const float HALF_LOG2E = -0x1.715476p-1f, REST_LN2 = -0x1.4ae0cp-27f * 0x1.62e43p-1f; // -log2(e) / 2 in fp32, and what is left of it times ln(2)
-    const float a = __builtin_fminf(__builtin_fabsf(g), 400.f), t = a * HALF_LOG2E;
-    const float rest = __builtin_fmaf(a, REST_LN2, __builtin_fmaf(a, HALF_LOG2E, -t) * 0x1.62e43p-1f);
-    const float e = __builtin_amdgcn_exp2f(t), h = __builtin_fmaf(e, rest, e), s = g < 0.f ? h : 1.f;
-    return g * s * __builtin_amdgcn_rcpf(__builtin_fmaf(h, h, 1.f)) * u * s;
-}
 template <class T, bool GATED> LCMA_DEV void values(const char *row, int k, int K, float (&v)[8]) {
     eight<T>(row, k, K, v);
     if constexpr (GATED) {

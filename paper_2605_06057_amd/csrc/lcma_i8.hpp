@@ -26,7 +26,7 @@ struct I8Place {
 };
 
 // First row of group e (experts: of the rows behind the groups), inside A whatever the offsets say; tiles of TM rows that a group takes.
-LCMA_DEV int i8_row(const I8GemmParams &p, int e) {
+template <class P> LCMA_DEV int i8_row(const P &p, int e) {
     const int row = p.offsets[e];
     return row < 0 ? 0 : row > p.rows ? p.rows : row;
 }
@@ -34,11 +34,12 @@ template <int TM> LCMA_DEV int i8_tiles(int begin, int end) { return end > begin
 
 // The tiles of TM rows of all groups, in expert order, every group in tiles of its own: how many there are, and the rows of tile x.  Every wave
 // by itself, a lane per expert; the first 64 experts are kept, which are mostly all.
-template <int TM> struct I8Rows {
+// P: an argument block with rows, offsets and experts.
+template <int TM, class P = I8GemmParams> struct I8Rows {
     int begin, end, upto; // rows of this lane's expert, tiles up to and with it
     int tiles, behind;    // all tiles, and the first row behind the groups
 
-    LCMA_DEV void experts_from(const I8GemmParams &p, int e0, int before) {
+    LCMA_DEV void experts_from(const P &p, int e0, int before) {
         const int e = e0 + (int)(threadIdx.x & 63);
         begin = end = 0;
         if (e < p.experts) {
@@ -47,7 +48,7 @@ template <int TM> struct I8Rows {
         }
         upto = before + lanes_upto(i8_tiles<TM>(begin, end));
     }
-    LCMA_DEV I8Rows(const I8GemmParams &p) {
+    LCMA_DEV I8Rows(const P &p) {
         if (!p.offsets) {
             tiles = i8_tiles<TM>(0, p.rows);
             behind = p.rows;
@@ -63,7 +64,7 @@ template <int TM> struct I8Rows {
             behind = __builtin_amdgcn_readlane(more.end, (p.experts - 1) & 63);
         }
     }
-    LCMA_DEV I8Place place(const I8GemmParams &p, int x) const {
+    LCMA_DEV I8Place place(const P &p, int x) const {
         if (!p.offsets) return {x * TM, p.rows - x * TM < TM ? p.rows - x * TM : TM, 0, 0};
         I8Rows at = *this;
         int e0 = 0;
@@ -111,7 +112,7 @@ template <class OUT> LCMA_DEV void i8_store16(char *at, u32x4 v, int cols) {
 }
 
 // Rows of C behind the groups are zero: the work-groups of the launch share them.
-template <class OUT> LCMA_DEV void i8_zero_behind(const I8GemmParams &p, int behind, int groups, int threads) {
+template <class OUT, class P> LCMA_DEV void i8_zero_behind(const P &p, int behind, int groups, int threads) {
     constexpr int V = 16 / OUT::ES;
     for (uint32_t row = behind + blockIdx.x; row < (uint32_t)p.rows; row += groups) // (past 2^31 before it ends)
         for (int n = threadIdx.x * V; n < p.N; n += threads * V) i8_store16<OUT>((char *)p.C + ((int64_t)row * p.ldc + n) * OUT::ES, u32x4{0, 0, 0, 0}, p.N - n);
