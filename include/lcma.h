@@ -404,6 +404,10 @@ double lcma_predict_seconds(int scheme_id, int64_t M, int64_t N, int64_t K, lcma
  *                                                   32x32, 64x64, 64x128, 128x128, 128x256 or 256x256 (another value, or more tiles than its
  *                                                   launch holds: default).  Their
  *                                                   sums are exact, so this changes no result.
+ *   "experts_kernel"   LCMA_EXPERTS_KERNEL=<name>   lcma_gemm_experts and lcma_gemm_experts_grad run the kernel with that name: any64x64 and any128x128 (any sizes and
+ *                                                   alignments) or 256x256 (16 bit, whole 16 bytes); where it does not fit, and for another value: default.  It groups
+ *                                                   fp32 sums differently.
+ *   "i4_kernel"        LCMA_I4_KERNEL=16|64         lcma_i4_gemm_nt and lcma_i4_gemm_experts run the kernel with tiles of so many rows.  It groups fp32 sums differently.
  */
 lcma_status lcma_set_tuning(const char *key, const char *value);
 

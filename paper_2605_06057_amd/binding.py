@@ -729,7 +729,7 @@ def lcma_i4_gemm_experts(X, offsets, Wp, C, group: int = 128, bias=None):
 
 
 def lcma_set_tuning(key: str, value: str = ""):
-    """Measurement aid: "variant", "unfused_variant", "panel", "batch_order", "schedule", "unfused_stages" or "i8_kernel"; an empty value restores the default."""
+    """Measurement aid: "variant", "unfused_variant", "panel", "batch_order", "schedule", "unfused_stages", "i8_kernel", "experts_kernel" or "i4_kernel"; an empty value restores the default."""
     _check(lib().lcma_set_tuning(key.encode(), value.encode()))
 
 

@@ -125,7 +125,7 @@ static const Variant *find_variant(const char *name) {
 // Measurement aids (see lcma_set_tuning): process-wide, initialised once from the environment, never read from it again.
 namespace {
 std::atomic<const Variant *> g_forced{nullptr}, g_forced_unfused{nullptr};
-std::atomic<int> g_panel{8}, g_batch_order{0}, g_schedule{0}, g_stages{15}, g_i8_kernel{-1};
+std::atomic<int> g_panel{8}, g_batch_order{0}, g_schedule{0}, g_stages{15}, g_i8_kernel{-1}, g_experts_kernel{-1}, g_i4_kernel{-1};
 std::once_flag g_tuning_once;
 bool set_tuning(const char *key, const char *value) {
     const char *v = value ? value : "";
@@ -139,6 +139,14 @@ bool set_tuning(const char *key, const char *value) {
         g_i8_kernel = -1;
         for (int k = 0; k < kI8Kernels; ++k)
             if (!std::strcmp(v, kI8KernelNames[k])) g_i8_kernel = k;
+    } else if (!std::strcmp(key, "experts_kernel")) {
+        g_experts_kernel = -1;
+        for (int k = 0; k < kExpKernels; ++k)
+            if (!std::strcmp(v, kExpKernelNames[k])) g_experts_kernel = k;
+    } else if (!std::strcmp(key, "i4_kernel")) {
+        g_i4_kernel = -1;
+        for (int k = 0; k < kI4Kernels; ++k)
+            if (!std::strcmp(v, kI4KernelNames[k])) g_i4_kernel = k;
     } else return false;
     return true;
 }
@@ -151,6 +159,8 @@ void init_tuning() {
         if (const char *e = std::getenv("LCMA_SCHEDULE")) set_tuning("schedule", e);
         if (const char *e = std::getenv("LCMA_UNFUSED_STAGES")) set_tuning("unfused_stages", e);
         if (const char *e = std::getenv("LCMA_I8_KERNEL")) set_tuning("i8_kernel", e);
+        if (const char *e = std::getenv("LCMA_EXPERTS_KERNEL")) set_tuning("experts_kernel", e);
+        if (const char *e = std::getenv("LCMA_I4_KERNEL")) set_tuning("i4_kernel", e);
     });
 }
 } // namespace
@@ -161,6 +171,8 @@ int tuning_batch_order() { init_tuning(); return g_batch_order.load(); }
 int tuning_schedule() { init_tuning(); return g_schedule.load(); }
 int tuning_unfused_stages() { init_tuning(); return g_stages.load(); }
 int tuning_i8_kernel() { init_tuning(); return g_i8_kernel.load(); }
+int tuning_experts_kernel() { init_tuning(); return g_experts_kernel.load(); }
+int tuning_i4_kernel() { init_tuning(); return g_i4_kernel.load(); }
 
 // [p, p + bytes) and [q, q + qbytes) share a byte
 static bool overlap(const void *p, int64_t bytes, const void *q, int64_t qbytes) {

@@ -10,7 +10,7 @@ using namespace lcma;
 
 namespace {
 
-const int kTile[kExpKernels][2] = {{64, 64}, {128, 128}}; // rows and columns of the kernels' tiles
+const int kTile[kExpKernels][2] = {{64, 64}, {128, 128}, {256, 256}}; // rows and columns of the kernels' tiles
 
 int64_t span(int64_t rows, int64_t ld, int64_t cols, int es) { return rows > 0 && cols > 0 ? ((rows - 1) * ld + cols) * es : 0; }
 int64_t tiles(int64_t n, int64_t of) { return (n + of - 1) / of; }
@@ -20,7 +20,15 @@ int64_t product_tiles(int kernel, int64_t rows, int64_t N, int experts) {
     return (rows / kTile[kernel][0] + (rows < experts ? rows : experts)) * tiles(N, kTile[kernel][1]);
 }
 int64_t gradient_tiles(int kernel, int64_t M, int64_t N, int experts) { return experts * tiles(M, kTile[kernel][0]) * tiles(N, kTile[kernel][1]); }
-bool launches(int64_t jobs) { return (jobs + 8) * 512 < kGridLimit / 2; } // (numbers of tiles are 32-bit on the device)
+bool needs_vectors(int kernel) { return kernel >= kExpPingPong; }
+bool walks(int kernel) { return kernel == kExpPingPong; } // 256 work-groups walk through tiles; the other kernels have one for every tile
+bool launches(int kernel, int64_t jobs) { return walks(kernel) ? jobs < kRowLimit - 1024 : (jobs + 8) * 512 < kGridLimit / 2; } // (numbers of tiles are 32-bit on the device)
+int grid_of(int kernel, int64_t jobs) { return walks(kernel) ? 256 : (int)((jobs + 7) / 8 * 8); }
+// What the kernels that load straight into LDS need: 16-bit types, operands in whole 16 bytes (of a k-contiguous one K too, of the other form the rows), and offsets inside
+// a tile (256 rows of a k-contiguous operand, 128 rows along k of the other) below 2^30 bytes.
+bool whole_vectors(int es, const void *A, int64_t lda_b, const void *B, int64_t ldb_b, int64_t k_b) {
+    return es == 2 && !(((uintptr_t)A | (uintptr_t)B | (uint64_t)lda_b | (uint64_t)ldb_b | (uint64_t)k_b) & 15) && lda_b <= 1 << 22 && ldb_b <= 1 << 22;
+}
 
 lcma_status check_sizes(const char *who, int64_t rows, int64_t N, int64_t K, int experts, int dtype) {
     if (!dtype_size(dtype)) return fail(LCMA_ERR_DTYPE, "%s: unknown dtype %d", who, dtype);
@@ -69,12 +77,15 @@ extern "C" lcma_status lcma_gemm_experts(int b_layout, int64_t rows, int64_t N, 
     p.K = (int32_t)K;
     p.experts = experts;
     p.panel = 8;
-    int kernel = rows < 64 * (int64_t)experts ? kExpStaged64 : kExpStaged128;
-    if (!launches(product_tiles(kernel, rows, N, experts))) kernel = kExpStaged128;
-    const int64_t jobs = product_tiles(kernel, rows, N, experts);
-    if (!launches(jobs)) return fail(LCMA_ERR_SHAPE, "%s: too many tiles for a launch", who);
+    const bool vectors = K > 0 && whole_vectors(es, A, p.lda_b, B, p.ldb_b, K * es);
+    auto tiles_of = [&](int k) { return product_tiles(k, rows, N, experts); };
+    auto fits = [&](int k) { return (vectors || !needs_vectors(k)) && launches(k, tiles_of(k)); };
+    int kernel = tuning_experts_kernel();
+    if (kernel < 0 || !fits(kernel)) kernel = fits(kExpPingPong) && rows >= 128 * (int64_t)experts ? kExpPingPong : rows < 64 * (int64_t)experts ? kExpStaged64 : kExpStaged128;
+    if (!fits(kernel)) kernel = fits(kExpStaged128) ? kExpStaged128 : kExpPingPong;
+    if (!fits(kernel)) return fail(LCMA_ERR_SHAPE, "%s: too many tiles for a launch", who);
     p.nz = (int32_t)tiles(N, kTile[kernel][1]);
-    if (const int err = lcma_launch_experts_gemm(&p, b_layout ? 0 : 1, kernel, dtype, (int)((jobs + 7) / 8 * 8), stream))
+    if (const int err = lcma_launch_experts_gemm(&p, b_layout ? 0 : 1, kernel, dtype, grid_of(kernel, tiles_of(kernel)), stream))
         return fail(LCMA_ERR_HIP, "%s: launch failed with HIP error %d", who, err);
     return LCMA_OK;
 }
@@ -107,12 +118,17 @@ extern "C" lcma_status lcma_gemm_experts_grad(int64_t rows, int64_t N, int64_t K
     p.M = (int32_t)N;
     p.N = (int32_t)K;
     p.experts = experts;
-    int kernel = gradient_tiles(kExpStaged128, N, K, experts) < 512 ? kExpStaged64 : kExpStaged128;
-    const int64_t jobs = gradient_tiles(kernel, N, K, experts);
-    if (!launches(jobs)) return fail(LCMA_ERR_SHAPE, "%s: too many tiles for a launch", who);
+    p.panel = 8;
+    const bool vectors = whole_vectors(es, dC, p.lda_b, A, p.ldb_b, 0);
+    auto tiles_of = [&](int k) { return gradient_tiles(k, N, K, experts); };
+    auto fits = [&](int k) { return (vectors || !needs_vectors(k)) && launches(k, tiles_of(k)); };
+    int kernel = tuning_experts_kernel();
+    if (kernel < 0 || !fits(kernel)) kernel = fits(kExpPingPong) && tiles_of(kExpPingPong) >= 128 ? kExpPingPong : tiles_of(kExpStaged128) < 512 ? kExpStaged64 : kExpStaged128;
+    if (!fits(kernel)) kernel = fits(kExpStaged128) ? kExpStaged128 : kExpPingPong;
+    if (!fits(kernel)) return fail(LCMA_ERR_SHAPE, "%s: too many tiles for a launch", who);
     p.nx = (int32_t)tiles(N, kTile[kernel][0]);
     p.nz = (int32_t)tiles(K, kTile[kernel][1]);
-    if (const int err = lcma_launch_experts_gemm(&p, 2, kernel, dtype, (int)((jobs + 7) / 8 * 8), stream))
+    if (const int err = lcma_launch_experts_gemm(&p, 2, kernel, dtype, grid_of(kernel, tiles_of(kernel)), stream))
         return fail(LCMA_ERR_HIP, "%s: launch failed with HIP error %d", who, err);
     return LCMA_OK;
 }

@@ -1,4 +1,4 @@
-// Checks that the 8-bit-integer product and the tokens' way to their experts share (host side).
+// Checks that the calls in 8 and 4 bits, the experts' products and the tokens' way to their experts share (host side).
 #pragma once
 #include "host_common.h"
 #include "lcma_experts_params.h"
@@ -15,6 +15,11 @@ constexpr int64_t kGridLimit = (int64_t)1 << 32;  // threads of a launch along a
 // the kernels of the product by number (lcma_experts_params.h), named by the rows and columns of their tiles
 constexpr const char *kI8KernelNames[kI8Kernels] = {"16x16", "32x32", "64x64", "64x128", "128x128", "128x256", "256x256"};
 int tuning_i8_kernel(); // csrc/api.cc; -1: choose
+// of the experts' products: those that take any sizes and alignments, and those for whole 16 bytes; of the product with 4-bit weights
+constexpr const char *kExpKernelNames[kExpKernels] = {"any64x64", "any128x128", "256x256"};
+int tuning_experts_kernel();
+constexpr const char *kI4KernelNames[kI4Kernels] = {"16", "64"};
+int tuning_i4_kernel();
 
 // whether two ranges of bytes have one in common
 inline bool touch(const void *a, int64_t a_bytes, const void *b, int64_t b_bytes) {

@@ -92,7 +92,8 @@ lcma_status gemm(const char *who, int64_t rows, int64_t N, int64_t K, int group,
     p.experts = experts;
     p.blocks = (int32_t)column_blocks(K);
     p.panel = 1;
-    int kernel = rows <= 16 * (int64_t)experts ? kI4Rows16 : kI4Rows64;
+    int kernel = tuning_i4_kernel();
+    if (kernel < 0) kernel = rows <= 16 * (int64_t)experts ? kI4Rows16 : kI4Rows64;
     if (!launches(tiles_of(kernel, rows, N, experts, offsets != nullptr))) kernel = kI4Rows64;
     const int64_t jobs = tiles_of(kernel, rows, N, experts, offsets != nullptr);
     if (!launches(jobs)) return fail(LCMA_ERR_SHAPE, "%s: too many tiles for a launch", who);

@@ -1,5 +1,5 @@
 // Instances of the experts' products (csrc/lcma_experts.hpp).
-#include "lcma_experts.hpp"
+#include "lcma_experts_pingpong.hpp"
 
 using namespace lcma;
 
@@ -9,6 +9,12 @@ template <class T, bool ACOL, bool BCOL, bool GRAD, int TM, int TN, int WGM, int
     using G = ExpStaged<T, ACOL, BCOL, GRAD, TM, TN, WGM, WGN>;
     __shared__ __attribute__((aligned(16))) char smem[G::LDS_BYTES];
     G::run(p, (LCMA_LDS char *)smem);
+}
+
+template <class T, bool ACOL, bool BCOL, bool GRAD> __global__ __launch_bounds__(512, 2) void exp_256(const ExpertsGemmParams) {
+    using G = ExpPingPong<T, ACOL, BCOL, GRAD>;
+    __shared__ __attribute__((aligned(16))) char smem[G::LDS_BYTES];
+    G::run((LCMA_LDS char *)smem);
 }
 
 } // namespace
@@ -27,7 +33,15 @@ extern "C" int lcma_launch_experts_gemm(const lcma::ExpertsGemmParams *p, int fo
     break;
     switch (kernel) {
     case kExpStaged64: LCMA_EXP(exp_staged, 256, 64, 64, 2, 2)
-    default: LCMA_EXP(exp_staged, 256, 128, 128, 2, 2)
+    case kExpStaged128: LCMA_EXP(exp_staged, 256, 128, 128, 2, 2)
+    default:
+#define LCMA_EXP_256(T)                                                                               \
+    if (form == 0) exp_256<T, false, false, false><<<dim3(grid), dim3(512), 0, s>>>(*p);              \
+    else if (form == 1) exp_256<T, false, true, false><<<dim3(grid), dim3(512), 0, s>>>(*p);          \
+    else exp_256<T, true, true, true><<<dim3(grid), dim3(512), 0, s>>>(*p);
+        if (dtype == 1) { LCMA_EXP_256(BF16) }
+        else { LCMA_EXP_256(F16) }
+#undef LCMA_EXP_256
     }
 #undef LCMA_EXP
 #undef LCMA_EXP_T

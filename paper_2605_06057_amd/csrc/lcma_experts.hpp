@@ -32,7 +32,9 @@ template <class T, bool BCOL, int TM, int TN> LCMA_DEV ExpJob product_job(const 
 }
 // Tile `job` of the gradient: expert by expert.
 template <class T, int TM, int TN> LCMA_DEV ExpJob gradient_job(const ExpertsGemmParams &p, int job) {
-    const int of = p.nx * p.nz, e = job / of, x = (job - e * of) / p.nz, z = (job - e * of) % p.nz;
+    const int of = p.nx * p.nz, e = job / of;
+    int x, z;
+    i8_tile_of_job(p.nx, p.nz, p.panel, job - e * of, x, z);
     const int begin = i8_row(p, e), end = i8_row(p, e + 1);
     ExpJob j;
     j.a = p.A + (int64_t)begin * p.lda_b + (int64_t)x * TM * T::ES;
@@ -92,20 +94,24 @@ template <class T, bool COL, int R> LCMA_DEV void exp_fragments(const LCMA_LDS c
     }
 }
 
-// A wave's part of a tile of C (NMI x NNI blocks of 32 x 32; rows and columns of it that are inside C: rows, cols) rounded and stored: through 4 KB of LDS that are
-// the wave's own, so that it leaves as whole lines, 16 bytes a lane.  The right operand is the left one of the matrix instruction: a lane holds four neighbouring columns.
-// down: bytes from block mi of rows to the next, col_blocks: from block ni of columns (bytes) to the next.
-template <class T, int NMI, int NNI> LCMA_DEV void exp_store(LCMA_LDS char *strip, char *c, int64_t ldc_b, int rows, int cols, const f32x16 (&acc)[NMI][NNI]) {
+// A wave's part of a tile of C (NMI x NNI blocks of 32 x 32; rows, cols: of C from its first element on) rounded and stored: through 4 KB of LDS that are the wave's own,
+// so that it leaves as whole lines, 16 bytes a lane.  The right operand is the left one of the matrix instruction: a lane holds four neighbouring columns.
+// Blocks of rows follow each other, or, TWO, the second pair of them is 128 rows on; the blocks of columns are GAP columns apart.
+// FULL: all of it lies inside C.
+template <class T, int NMI, int NNI, bool TWO, int GAP, bool FULL>
+LCMA_DEV void exp_store_rows(LCMA_LDS char *strip, char *c, int64_t ldc_b, int rows, int cols, const f32x16 (&acc)[NMI][NNI]) {
     constexpr int ES = T::ES, BLOCKS = ES == 4 ? 1 : NNI == 1 ? 1 : 2, L = BLOCKS * 32 * ES / 16, RPS = 64 / L; // 32-column blocks of a pass; lanes of a row, rows of a store
     static_assert(NNI % BLOCKS == 0, "whole passes");
     // (the lane number anew, hidden: what derives from it would otherwise be kept in registers through the steps)
     int lane = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));
     asm volatile("" : "+v"(lane));
     const int l32 = lane & 31, lh = lane >> 5, row_of = lane / L, ch = lane % L;
-    if (rows <= 0 || cols <= 0) return;
+    if (!FULL && (rows <= 0 || cols <= 0)) return;
+    char *const at = c + (int64_t)row_of * ldc_b;
 #pragma unroll
     for (int mi = 0; mi < NMI; ++mi) {
-        if (mi * 32 >= rows) return;
+        const int row0 = TWO ? mi / 2 * 128 + mi % 2 * 32 : mi * 32;
+        if (!FULL && row0 >= rows) return;
 #pragma unroll
         for (int n0 = 0; n0 < NNI; n0 += BLOCKS) {
 #pragma unroll
@@ -125,13 +131,26 @@ template <class T, int NMI, int NNI> LCMA_DEV void exp_store(LCMA_LDS char *stri
             lanes_meet();
 #pragma unroll
             for (int it = 0; it < 32 / RPS; ++it) {
-                const int row = it * RPS + row_of, col = n0 * 32 + ch * (16 / ES);
+                const int row = it * RPS + row_of, of = ch * (16 / ES), col = (n0 + of / 32) * GAP + of % 32;
                 const u32x4 v = *(const LCMA_LDS u32x4 *)(strip + row * (L * 16) + (ch ^ (row & (L - 1))) * 16);
-                if (mi * 32 + row < rows && col < cols) i8_store16<T>(c + (int64_t)(mi * 32 + row) * ldc_b + (int64_t)col * ES, v, cols - col);
+                char *to = at + (int64_t)(row0 + it * RPS) * ldc_b + col * ES;
+                if constexpr (FULL) __builtin_memcpy(to, &v, 16);
+                else if (row0 + row < rows && col < cols) i8_store16<T>(to, v, cols - col);
             }
             lanes_meet();
         }
     }
+}
+template <class T, int NMI, int NNI, bool TWO = false, int GAP = 32>
+LCMA_DEV void exp_store(LCMA_LDS char *strip, char *c, int64_t ldc_b, int rows, int cols, const f32x16 (&acc)[NMI][NNI]) {
+    if (rows >= (TWO ? (NMI - 1) / 2 * 128 + (NMI - 1) % 2 * 32 : (NMI - 1) * 32) + 32 && cols >= (NNI - 1) * GAP + 32) exp_store_rows<T, NMI, NNI, TWO, GAP, true>(strip, c, ldc_b, rows, cols, acc);
+    else exp_store_rows<T, NMI, NNI, TWO, GAP, false>(strip, c, ldc_b, rows, cols, acc);
+}
+
+// Rows of C behind the last expert's are zero: the work-groups of the launch share them.
+template <class T, int NT> LCMA_DEV void exp_zero_behind(const ExpertsGemmParams &p, int behind) {
+    for (uint32_t row = behind + blockIdx.x; row < (uint32_t)p.rows; row += gridDim.x) // (past 2^31 before it ends)
+        for (int n = threadIdx.x * T::CH; n < p.N; n += NT * T::CH) i8_store16<T>(p.C + (int64_t)row * p.ldc_b + (int64_t)n * T::ES, u32x4{0, 0, 0, 0}, p.N - n);
 }
 
 // `n` (up to 16 / ES, none: not read) elements from `at`, which has the alignment of an element, zeros behind.
@@ -188,7 +207,7 @@ template <class T, bool ACOL, bool BCOL, bool GRAD, int TM, int TN, int WGM, int
             j = gradient_job<T, TM, TN>(p, job);
         } else {
             const I8Rows<TM, ExpertsGemmParams> groups(p);
-            zero_behind(p, groups.behind);
+            exp_zero_behind<T, NT>(p, groups.behind);
             const int nx = groups.tiles, jobs = nx * p.nz, per = (jobs + 7) / 8, job = (int)(blockIdx.x & 7) * per + (int)(blockIdx.x >> 3);
             if ((int)(blockIdx.x >> 3) >= per || job >= jobs) return;
             int x, z;
@@ -231,10 +250,6 @@ template <class T, bool ACOL, bool BCOL, bool GRAD, int TM, int TN, int WGM, int
         __syncthreads(); // the strips take the place of the stages
         const int row = wm * NMI * 32, col = wn * NNI * 32;
         exp_store<T, NMI, NNI>(lds + w * 4096, j.c + (int64_t)row * p.ldc_b + (int64_t)col * T::ES, p.ldc_b, j.am - row, j.bn - col, acc);
-    }
-    static LCMA_DEV void zero_behind(const ExpertsGemmParams &p, int behind) { // the work-groups of the launch share these rows
-        for (uint32_t row = behind + blockIdx.x; row < (uint32_t)p.rows; row += gridDim.x)
-            for (int n = threadIdx.x * T::CH; n < p.N; n += NT * T::CH) i8_store16<T>(p.C + (int64_t)row * p.ldc_b + (int64_t)n * T::ES, u32x4{0, 0, 0, 0}, p.N - n);
     }
 };
 

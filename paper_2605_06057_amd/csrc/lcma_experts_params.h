@@ -63,8 +63,8 @@ struct I8GemmParams {
     int32_t nz, panel;      // tiles along N, and the width of a column panel of the tile order
 };
 
-// Kernels of the experts' products (csrc/lcma_experts.hpp).
-enum { kExpStaged64 = 0, kExpStaged128, kExpKernels };
+// Kernels of the experts' products: any sizes (csrc/lcma_experts.hpp); whole 16 bytes in 16 bit (csrc/lcma_experts_pingpong.hpp).
+enum { kExpStaged64 = 0, kExpStaged128, kExpPingPong, kExpKernels };
 
 // lcma_gemm_experts: rows of A (k-contiguous) in groups, group e times the matrix of expert e (N x K, or K x N).
 // lcma_gemm_experts_grad: for every expert the product of its rows of A, transposed, and its rows of B: M x N, summed over the rows.

@@ -23,6 +23,14 @@ def _lib():
     return binding
 
 
+@pytest.fixture(params=["", "any64x64", "any128x128", "256x256"], scope="module")
+def kernel(request):
+    """The kernel of the rule, and every kernel by name where it takes the sizes."""
+    _lib().lcma_set_tuning("experts_kernel", request.param)
+    yield request.param
+    _lib().lcma_set_tuning("experts_kernel", "")
+
+
 def _offsets(counts):
     torch, _ = _torch()
     return torch.tensor(np.cumsum([0] + list(counts)), dtype=torch.int32, device="cuda")
@@ -65,7 +73,7 @@ COUNTS = [
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("counts", COUNTS, ids=lambda c: f"{sum(c)}of{len(c)}")
 @pytest.mark.parametrize("N,K,pad,behind", [(64, 64, 0, 0), (1, 1, 0, 2), (8, 200, 8, 1), (130, 72, 0, 5), (200, 136, 16, 0), (33, 77, 3, 40)])
-def test_product_of_whole_numbers(counts, N, K, pad, behind, dtype, b_nk):
+def test_product_of_whole_numbers(kernel, counts, N, K, pad, behind, dtype, b_nk):
     torch, types = _torch()
     gen = torch.Generator(device="cuda").manual_seed(sum(counts) + N)
     E, rows = len(counts), sum(counts) + behind
@@ -85,7 +93,7 @@ def test_product_of_whole_numbers(counts, N, K, pad, behind, dtype, b_nk):
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("counts", COUNTS, ids=lambda c: f"{sum(c)}of{len(c)}")
 @pytest.mark.parametrize("N,K,pad,behind", [(64, 64, 0, 0), (1, 1, 0, 2), (8, 200, 8, 1), (130, 72, 0, 5), (200, 136, 16, 0), (33, 77, 3, 40)])
-def test_gradient_of_whole_numbers(counts, N, K, pad, behind, dtype):
+def test_gradient_of_whole_numbers(kernel, counts, N, K, pad, behind, dtype):
     torch, types = _torch()
     gen = torch.Generator(device="cuda").manual_seed(sum(counts) + N)
     E, rows = len(counts), sum(counts) + behind
@@ -118,7 +126,7 @@ REAL = [([1, 0, 1, 0], 520, 1032), ([3, 2, 0, 5, 1, 4], 264, 2056), ([100, 90, 1
 
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("counts,N,K", REAL, ids=str)
-def test_real_numbers_and_both_gradients(counts, N, K, dtype):
+def test_real_numbers_and_both_gradients(kernel, counts, N, K, dtype):
     torch, types = _torch()
     gen = torch.Generator(device="cuda").manual_seed(N + K)
     E, rows = len(counts), sum(counts)
@@ -157,7 +165,7 @@ def test_gradients_against_differences(dtype):
 
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("rows,N,K,pad", [(40, 64, 64, 0), (300, 264, 136, 8), (70, 33, 77, 3)])
-def test_infinities_and_nan_stay_where_they_are(rows, N, K, pad, dtype):
+def test_infinities_and_nan_stay_where_they_are(kernel, rows, N, K, pad, dtype):
     """Padding of the rows, rows of other experts, rows of none: what is not part of an element's sum does not reach it."""
     torch, types = _torch()
     gen = torch.Generator(device="cuda").manual_seed(rows)
@@ -210,7 +218,7 @@ def test_empty_calls():
 
 
 @pytest.mark.parametrize("counts,N,K", [([1, 0, 1], 264, 520), ([200, 0, 311], 264, 328), ([40, 70], 77, 33)])
-def test_captured_and_replayed(counts, N, K):
+def test_captured_and_replayed(kernel, counts, N, K):
     """New rows, weights and offsets in the same places: every replay gives the eager calls' bits."""
     torch, types = _torch()
     gen = torch.Generator(device="cuda").manual_seed(9)
