@@ -10,7 +10,7 @@ using namespace lcma;
 
 namespace {
 
-const int kTile[kI4Kernels][2] = {{16, 16}, {64, 128}}; // rows and columns of the kernels' tiles
+const int kTile[kI4Kernels][2] = {{16, 16}, {16, 32}, {16, 64}, {32, 32}, {64, 64}}; // rows and columns of the kernels' tiles
 
 bool group_fits(int group) { return group == 32 || group == 64 || group == 128; }
 int64_t row_blocks(int64_t N) { return (N + 15) / 16; }
@@ -59,6 +59,11 @@ int64_t tiles_of(int kernel, int64_t rows, int64_t N, int experts, bool grouped)
 }
 bool launches(int64_t jobs) { return (jobs + 8) * 512 < kGridLimit / 2; } // (numbers of tiles are 32-bit on the device)
 
+int pick(int64_t rows, int64_t N, int64_t K, int experts) {
+    const int64_t hit = rows < experts ? rows : experts, strips = ((rows + 15) / 16 > hit ? (rows + 15) / 16 : hit) * row_blocks(N); // (blocks of rows that are read)
+    return strips >= 4096 ? kI4Rows16 : strips >= 512 ? kI4Rows16K4 : kI4Rows16K8;
+}
+
 lcma_status gemm(const char *who, int64_t rows, int64_t N, int64_t K, int group, int experts, const int32_t *offsets, const void *X, int64_t ldx, const void *Wp, const float *bias,
                  void *C, int64_t ldc, int dtype, void *stream) {
     const int es = dtype_size(dtype);
@@ -92,11 +97,12 @@ lcma_status gemm(const char *who, int64_t rows, int64_t N, int64_t K, int group,
     p.experts = experts;
     p.blocks = (int32_t)column_blocks(K);
     p.panel = 1;
+    auto fits = [&](int k) { return (es == 2 || k != kI4Rows64) && launches(tiles_of(k, rows, N, experts, offsets != nullptr)); };
     int kernel = tuning_i4_kernel();
-    if (kernel < 0) kernel = rows <= 16 * (int64_t)experts ? kI4Rows16 : kI4Rows64;
-    if (!launches(tiles_of(kernel, rows, N, experts, offsets != nullptr))) kernel = kI4Rows64;
+    if (kernel < 0 || !fits(kernel)) kernel = pick(rows, N, K, experts);
+    if (!fits(kernel)) kernel = kI4Rows32;
+    if (!fits(kernel)) return fail(LCMA_ERR_SHAPE, "%s: too many tiles for a launch", who);
     const int64_t jobs = tiles_of(kernel, rows, N, experts, offsets != nullptr);
-    if (!launches(jobs)) return fail(LCMA_ERR_SHAPE, "%s: too many tiles for a launch", who);
     p.nz = (int32_t)((N + kTile[kernel][1] - 1) / kTile[kernel][1]);
     if (const int err = lcma_launch_i4_gemm(&p, kernel, group, dtype, (int)((jobs + 7) / 8 * 8), stream)) return fail(LCMA_ERR_HIP, "%s: launch failed with HIP error %d", who, err);
     return LCMA_OK;

@@ -11,6 +11,16 @@ template <class T, bool ACOL, bool BCOL, bool GRAD, int TM, int TN, int WGM, int
     G::run(p, (LCMA_LDS char *)smem);
 }
 
+template <class T, bool ACOL, bool BCOL, bool GRAD, int TM, int TN, int WGM, int WGN, int S> __global__ __launch_bounds__(64 * WGM * WGN, 2) void exp_ring(const ExpertsGemmParams p) {
+    using G = ExpRing<T, ACOL, BCOL, GRAD, TM, TN, WGM, WGN, S>;
+    __shared__ __attribute__((aligned(16))) char smem[G::LDS_BYTES];
+    G::run(p, (LCMA_LDS char *)smem);
+}
+template <class T, bool BCOL, int R, int WK, int S> __global__ __launch_bounds__(64 * WK) void exp_few(const ExpertsGemmParams p) {
+    using G = ExpFewRows<T, BCOL, R, WK, S>;
+    __shared__ __attribute__((aligned(16))) char smem[G::LDS_BYTES];
+    G::run(p, (LCMA_LDS char *)smem);
+}
 template <class T, bool ACOL, bool BCOL, bool GRAD> __global__ __launch_bounds__(512, 2) void exp_256(const ExpertsGemmParams) {
     using G = ExpPingPong<T, ACOL, BCOL, GRAD>;
     __shared__ __attribute__((aligned(16))) char smem[G::LDS_BYTES];
@@ -22,28 +32,42 @@ template <class T, bool ACOL, bool BCOL, bool GRAD> __global__ __launch_bounds__
 // form: 0 the right operand N x K, 1 K x N, 2 the gradient
 extern "C" int lcma_launch_experts_gemm(const lcma::ExpertsGemmParams *p, int form, int kernel, int dtype, int grid, void *stream) {
     const hipStream_t s = (hipStream_t)stream;
-#define LCMA_EXP_T(NAME, THREADS, ...)                                                                   \
-    if (dtype == 0) NAME<F32, __VA_ARGS__><<<dim3(grid), dim3(THREADS), 0, s>>>(*p);                     \
-    else if (dtype == 1) NAME<BF16, __VA_ARGS__><<<dim3(grid), dim3(THREADS), 0, s>>>(*p);               \
-    else NAME<F16, __VA_ARGS__><<<dim3(grid), dim3(THREADS), 0, s>>>(*p);
-#define LCMA_EXP(NAME, THREADS, ...)                                          \
-    if (form == 0) { LCMA_EXP_T(NAME, THREADS, false, false, false, __VA_ARGS__) } \
-    else if (form == 1) { LCMA_EXP_T(NAME, THREADS, false, true, false, __VA_ARGS__) } \
-    else { LCMA_EXP_T(NAME, THREADS, true, true, true, __VA_ARGS__) }         \
+#define LCMA_EXP_LAUNCH(THREADS, ...) __VA_ARGS__<<<dim3(grid), dim3(THREADS), 0, s>>>(*p)
+#define LCMA_EXP_FORM(NAME, THREADS, T, ...)                                                          \
+    if (form == 0) LCMA_EXP_LAUNCH(THREADS, NAME<T, false, false, false __VA_ARGS__>);                \
+    else if (form == 1) LCMA_EXP_LAUNCH(THREADS, NAME<T, false, true, false __VA_ARGS__>);            \
+    else LCMA_EXP_LAUNCH(THREADS, NAME<T, true, true, true __VA_ARGS__>);
+#define LCMA_EXP(NAME, THREADS, ...)                                           \
+    if (dtype == 1) { LCMA_EXP_FORM(NAME, THREADS, BF16, __VA_ARGS__) }        \
+    else { LCMA_EXP_FORM(NAME, THREADS, F16, __VA_ARGS__) }                    \
     break;
+#define LCMA_EXP_ANY(NAME, THREADS, ...)                                       \
+    if (dtype == 0) { LCMA_EXP_FORM(NAME, THREADS, F32, __VA_ARGS__) }         \
+    else LCMA_EXP(NAME, THREADS, __VA_ARGS__)                                  \
+    break;
+#define LCMA_COMMA ,
     switch (kernel) {
-    case kExpStaged64: LCMA_EXP(exp_staged, 256, 64, 64, 2, 2)
-    case kExpStaged128: LCMA_EXP(exp_staged, 256, 128, 128, 2, 2)
-    default:
-#define LCMA_EXP_256(T)                                                                               \
-    if (form == 0) exp_256<T, false, false, false><<<dim3(grid), dim3(512), 0, s>>>(*p);              \
-    else if (form == 1) exp_256<T, false, true, false><<<dim3(grid), dim3(512), 0, s>>>(*p);          \
-    else exp_256<T, true, true, true><<<dim3(grid), dim3(512), 0, s>>>(*p);
-        if (dtype == 1) { LCMA_EXP_256(BF16) }
-        else { LCMA_EXP_256(F16) }
-#undef LCMA_EXP_256
+    case kExpStaged64: LCMA_EXP_ANY(exp_staged, 256, LCMA_COMMA 64, 64, 2, 2)
+    case kExpStaged128: LCMA_EXP_ANY(exp_staged, 256, LCMA_COMMA 128, 128, 2, 2)
+    case kExpFew16:
+        if (dtype == 1) LCMA_EXP_LAUNCH(256, exp_few<BF16, false, 16, 4, 2>);
+        else LCMA_EXP_LAUNCH(256, exp_few<F16, false, 16, 4, 2>);
+        break;
+    case kExpFew32:
+        if (dtype == 1 && form == 0) LCMA_EXP_LAUNCH(256, exp_few<BF16, false, 32, 4, 2>);
+        else if (dtype == 1) LCMA_EXP_LAUNCH(256, exp_few<BF16, true, 32, 4, 2>);
+        else if (form == 0) LCMA_EXP_LAUNCH(256, exp_few<F16, false, 32, 4, 2>);
+        else LCMA_EXP_LAUNCH(256, exp_few<F16, true, 32, 4, 2>);
+        break;
+    case kExpRing64: LCMA_EXP(exp_ring, 256, LCMA_COMMA 64, 64, 2, 2, 4)
+    case kExpRing64x128: LCMA_EXP(exp_ring, 256, LCMA_COMMA 64, 128, 2, 2, 3)
+    case kExpRing128: LCMA_EXP(exp_ring, 512, LCMA_COMMA 128, 128, 4, 2, 4)
+    default: LCMA_EXP(exp_256, 512, )
     }
+#undef LCMA_EXP_LAUNCH
+#undef LCMA_EXP_FORM
 #undef LCMA_EXP
-#undef LCMA_EXP_T
+#undef LCMA_EXP_ANY
+#undef LCMA_COMMA
     return (int)hipGetLastError();
 }

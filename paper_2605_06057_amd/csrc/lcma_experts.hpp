@@ -47,11 +47,11 @@ template <class T, int TM, int TN> LCMA_DEV ExpJob gradient_job(const ExpertsGem
 }
 
 // Where 16-byte chunk c of a row lies in LDS.  k-contiguous rows of 128 bytes: 16 rows at one chunk column meet all banks once.  Rows of columns, 16 bit: the four
-// rows (k) of a transposing read, 64 bytes of each, meet different banks (rows of 128 or 256 bytes; fp32 needs nothing).
+// rows (k) of a transposing read, 64 bytes of each, meet different banks (rows of 64 bytes do so by themselves; fp32 needs nothing).
 LCMA_DEV constexpr int exp_row_chunk(int row, int c) { return c ^ ((row >> 1) & 7); }
 template <class T, int R> LCMA_DEV constexpr int exp_col_chunk(int k, int c) {
-    static_assert(T::ES == 4 || R == 64 || R == 128, "rows of 128 or 256 bytes");
-    return T::ES == 4 ? c : R == 64 ? c ^ ((k >> 1 & 1) << 2) : c ^ ((k & 3) << 2);
+    static_assert(T::ES == 4 || R <= 32 || R == 64 || R == 128, "rows of 64, 128 or 256 bytes");
+    return T::ES == 4 || R <= 32 ? c : R == 64 ? c ^ ((k >> 1 & 1) << 2) : c ^ ((k & 3) << 2);
 }
 
 // Fragments of 32 columns, 32 block and on, of R columns in LDS for the four instructions of a step (16 bit): eight k of a column are two transposing reads of four.

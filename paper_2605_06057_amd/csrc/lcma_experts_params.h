@@ -63,8 +63,9 @@ struct I8GemmParams {
     int32_t nz, panel;      // tiles along N, and the width of a column panel of the tile order
 };
 
-// Kernels of the experts' products: any sizes (csrc/lcma_experts.hpp); whole 16 bytes in 16 bit (csrc/lcma_experts_pingpong.hpp).
-enum { kExpStaged64 = 0, kExpStaged128, kExpPingPong, kExpKernels };
+// Kernels of the experts' products: any sizes (csrc/lcma_experts.hpp); whole 16 bytes in 16 bit (csrc/lcma_experts_ring.hpp, lcma_experts_pingpong.hpp).  Tiles of 16 x 16:
+// weights N x K alone; of 16 and 32: no gradient of weights.
+enum { kExpStaged64 = 0, kExpStaged128, kExpFew16, kExpFew32, kExpRing64, kExpRing64x128, kExpRing128, kExpPingPong, kExpKernels };
 
 // lcma_gemm_experts: rows of A (k-contiguous) in groups, group e times the matrix of expert e (N x K, or K x N).
 // lcma_gemm_experts_grad: for every expert the product of its rows of A, transposed, and its rows of B: M x N, summed over the rows.
@@ -87,8 +88,8 @@ struct GatedParams {
     int32_t lane_shift; // 2^lane_shift neighbouring threads along a row
 };
 
-// 4-bit weights (csrc/lcma_i4.hpp): blocks of 16 rows x 128 columns, a row of blocks behind the other; a block is its codes (1024 bytes) and, for every group of
-// columns, 16 scales (fp32).
+// 4-bit weights (csrc/lcma_i4.hpp): blocks of 16 rows x 128 columns, a row of blocks behind the other; a block is its codes (1024 bytes) and the scales
+// (fp32) of its 16 rows' groups.
 inline int64_t i4_block_bytes(int group) { return 1024 + 128 / group * 64; }
 // lcma_i4_quantize, lcma_i4_prepare: rows x K values, or codes and scales, laid out as blocks.
 struct I4PrepareParams {
@@ -98,8 +99,8 @@ struct I4PrepareParams {
     int64_t ldw_b, expert_b, expert_q; // bytes from row to row, from expert to expert
     int32_t N, K, group, experts;
 };
-// Kernels of the product with them: tiles of 16 and of 64 rows.
-enum { kI4Rows16 = 0, kI4Rows64, kI4Kernels };
+// Kernels of the product with them: rows of a tile; blocks of rows of the weights in it; waves along K.
+enum { kI4Rows16K8 = 0, kI4Rows16K4, kI4Rows16, kI4Rows32, kI4Rows64, kI4Kernels };
 // lcma_i4_gemm_nt, lcma_i4_gemm_experts.
 struct I4GemmParams {
     const char *X, *Q;

@@ -6,7 +6,7 @@
 // reaches elements of C alone that are not there.  What lies past the last k reads as zero, on both sides: k-contiguous, 16 bytes at a time from past the extent; else by the extent.
 // Every work-group walks through tiles of its own, in turn; the loads run two steps ahead, into the next tile too.
 #pragma once
-#include "lcma_experts.hpp"
+#include "lcma_experts_ring.hpp"
 
 namespace lcma {
 
@@ -82,15 +82,8 @@ template <class T, bool ACOL, bool BCOL, bool GRAD> struct ExpPingPong {
     }
     // The operand from step y on, for two steps: k-contiguous rows with their steps as offsets, or the rows of the stored matrix from k = 64 y on.
     template <bool COL> static LCMA_DEV __amdgpu_buffer_rsrc_t operand(const char *at, int wide, int k, uint32_t ld_b, int y) {
-        int bytes;
-        if constexpr (COL) {
-            const int left = k - y * KS, n = left < 2 * KS ? left : 2 * KS;
-            at += (int64_t)y * KS * ld_b;
-            bytes = n > 0 ? (n - 1) * (int)ld_b + wide * T::ES : 0;
-        } else {
-            bytes = k > 0 ? (wide - 1) * (int)ld_b + k * T::ES : 0;
-        }
-        return __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(at), 0, bytes, 0x00020000);
+        if constexpr (COL) return exp_columns_from<T>(at, wide, k, ld_b, y, 2);
+        else return exp_rows_of<T>(at, wide, k, ld_b);
     }
 
     static LCMA_DEV void run(LCMA_LDS char *lds) { // (the argument block has to be the kernel's first argument)

@@ -1,0 +1,247 @@
+// The experts' products in 16 bit on tiles below 256 x 256, operands in whole 16 bytes straight into LDS (either form of both, csrc/lcma_experts.hpp).
+#pragma once
+#include "lcma_experts.hpp"
+
+namespace lcma {
+
+// The rows of the stored matrix from k = 64 y on, `steps` steps of them; none past the last k.
+template <class T> LCMA_DEV __amdgpu_buffer_rsrc_t exp_columns_from(const char *at, int wide, int k, uint32_t ld_b, int y, int steps) {
+    const int left = k - y * 64, n = left < steps * 64 ? left : steps * 64;
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(at) + (int64_t)y * 64 * ld_b, 0, n > 0 ? (n - 1) * (int)ld_b + wide * T::ES : 0, 0x00020000);
+}
+template <class T> LCMA_DEV __amdgpu_buffer_rsrc_t exp_rows_of(const char *at, int wide, int k, uint32_t ld_b) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(at), 0, k > 0 ? (wide - 1) * (int)ld_b + k * T::ES : 0, 0x00020000);
+}
+
+// One tile of TM x TN per work-group of WGM x WGN waves.  A step is 64 k; S stages of LDS hold the steps in flight, the loads run S - 1 steps ahead and are waited for by
+// count, and one barrier a step says that all waves' parts of it have landed and that all have read the stage that is loaded anew (csrc/lcma_i8.hpp has the
+// same with its measurements).
+template <class T, bool ACOL, bool BCOL, bool GRAD, int TM, int TN, int WGM, int WGN, int S> struct ExpRing {
+    static constexpr int NT = 64 * WGM * WGN, NMI = TM / WGM / 32, NNI = TN / WGN / 32, KS = 64;
+    static constexpr int A_STAGE = TM * 128, STAGE = (TM + TN) * 128, LDS_BYTES = S * STAGE, QA = TM * 8 / NT, QB = TN * 8 / NT;
+    static_assert(T::ES == 2 && NT / 64 * 4096 <= LDS_BYTES && TM * 8 % NT == 0 && TN * 8 % NT == 0 && LDS_BYTES <= 160 * 1024 && (S == 3 || S == 4) && (S - 1) * (QA + QB) <= 63, "tile and wave grid");
+    using Frag = typename Mma<T>::frag;
+    static constexpr uint32_t NONE = 1u << 30; // an offset past any extent
+
+    static LCMA_DEV void run(const ExpertsGemmParams &p, LCMA_LDS char *lds) {
+        ExpJob j;
+        if constexpr (GRAD) {
+            const int jobs = p.experts * p.nx * p.nz, per = (jobs + 7) / 8, job = (int)(blockIdx.x & 7) * per + (int)(blockIdx.x >> 3); // an eighth of the tiles to every XCD
+            if ((int)(blockIdx.x >> 3) >= per || job >= jobs) return;
+            j = gradient_job<T, TM, TN>(p, job);
+        } else {
+            const I8Rows<TM, ExpertsGemmParams> groups(p);
+            exp_zero_behind<T, NT>(p, groups.behind);
+            const int nx = groups.tiles, jobs = nx * p.nz, per = (jobs + 7) / 8, job = (int)(blockIdx.x & 7) * per + (int)(blockIdx.x >> 3);
+            if ((int)(blockIdx.x >> 3) >= per || job >= jobs) return;
+            int x, z;
+            i8_tile_of_job(nx, p.nz, p.panel, job, x, z);
+            j = product_job<T, BCOL, TM, TN>(p, groups.place(p, x), z * TN);
+        }
+        const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = w / WGN, wn = w % WGN;
+        f32x16 acc[NMI][NNI];
+#pragma unroll
+        for (int i = 0; i < NMI; ++i)
+#pragma unroll
+            for (int n = 0; n < NNI; ++n) zero(acc[i][n]);
+        multiply(p, j, w, wm, wn, acc, lds, lds + STAGE, lds + 2 * STAGE, lds + (S == 4 ? 3 * STAGE : 0));
+        __syncthreads(); // no load is in flight and every wave has read its last step: the strips take the place of the stages
+        const int row = wm * NMI * 32, col = wn * NNI * 32;
+        exp_store<T, NMI, NNI>(lds + w * 4096, j.c + (int64_t)row * p.ldc_b + (int64_t)col * T::ES, p.ldc_b, j.am - row, j.bn - col, acc);
+    }
+    // restrict: the loads in flight towards one stage do not touch what is read from another (the compiler would otherwise wait for all of them in
+    // front of every read)
+    static LCMA_DEV void multiply(const ExpertsGemmParams &p, const ExpJob &j, int w, int wm, int wn, f32x16 (&acc)[NMI][NNI], LCMA_LDS char *__restrict__ s0,
+                                  LCMA_LDS char *__restrict__ s1, LCMA_LDS char *__restrict__ s2, LCMA_LDS char *__restrict__ s3) {
+        constexpr int CA = TM * 2 / 16, CB = TN * 2 / 16; // 16-byte chunks of a row of the other form
+        const int tid = threadIdx.x, steps = (int)(((uint32_t)j.k + (KS - 1)) / KS), chunk = exp_row_chunk(tid >> 3, tid & 7) * 16;
+        const uint32_t lda = (uint32_t)p.lda_b, ldb = (uint32_t)p.ldb_b;
+        const auto rows_a = exp_rows_of<T>(j.a, j.am, j.k, lda), rows_b = exp_rows_of<T>(j.b, j.bn, j.k, ldb);
+        const uint32_t a_voff = ACOL ? tid / CA * lda + exp_col_chunk<T, TM>(tid / CA, tid % CA) * 16 : (uint32_t)(tid >> 3) * lda + chunk;
+        const uint32_t b_voff = BCOL ? tid / CB * ldb + exp_col_chunk<T, TN>(tid / CB, tid % CB) * 16 : (uint32_t)(tid >> 3) * ldb + chunk;
+        const bool past = chunk >= ((j.k - 1) % KS + 1) * 2; // (of the last step, k-contiguous)
+        const uint32_t a_last = !ACOL && past ? NONE : a_voff, b_last = !BCOL && past ? NONE : b_voff;
+        const uint32_t a_down = NT / (ACOL ? CA : 8) * lda, b_down = NT / (BCOL ? CB : 8) * ldb;
+        auto load = [&](LCMA_LDS char *st, int y) { // a step past the end: zeros, from past the extents
+            const uint32_t off = y < steps ? (uint32_t)y * 128 : NONE, av = y == steps - 1 ? a_last : a_voff, bv = y == steps - 1 ? b_last : b_voff;
+            const auto ra = ACOL ? exp_columns_from<T>(j.a, j.am, j.k, lda, y, 1) : rows_a, rb = BCOL ? exp_columns_from<T>(j.b, j.bn, j.k, ldb, y, 1) : rows_b;
+#pragma unroll
+            for (int q = 0; q < QB; ++q)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (LCMA_LDS void *)(st + A_STAGE + (q * NT + w * 64) * 16), 16, (int)bv, (int)((BCOL ? 0 : off) + q * b_down), 0, 0);
+#pragma unroll
+            for (int q = 0; q < QA; ++q)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (LCMA_LDS void *)(st + (q * NT + w * 64) * 16), 16, (int)av, (int)((ACOL ? 0 : off) + q * a_down), 0, 0);
+        };
+        auto step = [&](LCMA_LDS char *st, LCMA_LDS char *before, int y) {
+            wait_loads<(S - 2) * (QA + QB)>();
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_sched_barrier(0);
+            load(before, y + S - 1);
+            u32x4 a[NMI][4], b[NNI][4];
+#pragma unroll
+            for (int n = 0; n < NNI; ++n) exp_fragments<T, BCOL, TN>(st + A_STAGE, wn * NNI + n, b[n]);
+#pragma unroll
+            for (int i = 0; i < NMI; ++i) exp_fragments<T, ACOL, TM>(st, wm * NMI + i, a[i]);
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+                for (int i = 0; i < NMI; ++i)
+#pragma unroll
+                    for (int n = 0; n < NNI; ++n) Mma<T>::run(__builtin_bit_cast(Frag, b[n][k]), __builtin_bit_cast(Frag, a[i][k]), acc[i][n]);
+            __builtin_amdgcn_sched_barrier(0); // (the multiplications stay in front of the next wait; what they read has left LDS)
+        };
+        load(s0, 0);
+        load(s1, 1);
+        if constexpr (S == 4) load(s2, 2);
+        for (int y = 0; y < steps;) {
+            step(s0, S == 4 ? s3 : s2, y);
+            if (++y >= steps) break;
+            step(s1, s0, y);
+            if (++y >= steps) break;
+            step(s2, s1, y);
+            ++y;
+            if constexpr (S == 4) {
+                if (y >= steps) break;
+                step(s3, s2, y);
+                ++y;
+            }
+        }
+        wait_loads<0>(); // the loads past the end land before the LDS is another work-group's
+    }
+};
+
+// Few rows: a work-group owns a tile of R x R of C and its waves split K between them, a step (64 k, 128 bytes of every row) to a wave in turn; nothing is shared between
+// waves, so there is no barrier in the loop, and the waves' sums are added at the end, in fp32 and in ascending order (csrc/lcma_few_rows.hpp has the same for one product,
+// with the reasons and measurements).  S steps of a wave in flight.
+template <class T, bool BCOL, int R, int WK, int S> struct ExpFewRows {
+    static constexpr int F = R == 16 ? 16 : 32, NF = R / F, KF = 64 / (512 / F); // 16x16x32 or 32x32x16 instructions; fragments of a step along K
+    static constexpr int LOADS = R / 8, HALF = R * 128, STAGE = 2 * HALF, PITCH = R + 4, SUMS = WK * R * PITCH * 4, STAGES = WK * S * STAGE, LDS_BYTES = SUMS > STAGES ? SUMS : STAGES;
+    static_assert(T::ES == 2 && (R >= 32 || !BCOL) && LDS_BYTES <= 160 * 1024 && (S == 2 || S == 4) && 2 * LOADS * S <= 63, "LDS budget of one CU; counter of loads");
+    using Frag = typename Mma<T>::frag;
+    using Acc = std::conditional_t<F == 16, f32x4, f32x16>;
+    static constexpr uint32_t NONE = 1u << 30;
+
+    static LCMA_DEV void run(const ExpertsGemmParams &p, LCMA_LDS char *lds) {
+        const int lane = threadIdx.x & 63, fr = lane & (F - 1), fk = lane / F, wk = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const I8Rows<R, ExpertsGemmParams> groups(p);
+        exp_zero_behind<T, 64 * WK>(p, groups.behind);
+        const int nx = groups.tiles, jobs = nx * p.nz, per = (jobs + 7) / 8;
+        const int job = (blockIdx.x & 7) * per + (blockIdx.x >> 3); // an eighth of the tiles to every XCD, row tiles that share weights next to each other
+        if ((int)(blockIdx.x >> 3) >= per || job >= jobs) return;
+        int x, z;
+        i8_tile_of_job(nx, p.nz, p.panel, job, x, z);
+        const ExpJob j = product_job<T, BCOL, R, R>(p, groups.place(p, x), z * R);
+        Acc acc[NF][NF];
+#pragma unroll
+        for (int i = 0; i < NF; ++i)
+#pragma unroll
+            for (int n = 0; n < NF; ++n)
+#pragma unroll
+                for (int v = 0; v < F * F / 64; ++v) acc[i][n][v] = 0.f;
+        LCMA_LDS char *st = lds + wk * (S * STAGE);
+        steps_of_wave(p, j, wk, acc, st, st + STAGE, st + (S == 4 ? 2 * STAGE : 0), st + (S == 4 ? 3 * STAGE : 0));
+        __syncthreads(); // no load is in flight and every wave has read its last step: the sums take the place of the stages
+        LCMA_LDS float *mine = (LCMA_LDS float *)lds + wk * (R * PITCH);
+#pragma unroll
+        for (int i = 0; i < NF; ++i)
+#pragma unroll
+            for (int n = 0; n < NF; ++n)
+#pragma unroll
+                for (int g = 0; g < F * F / 256; ++g) // four neighbouring columns of row fr
+                    *(LCMA_LDS f32x4 *)(mine + (i * F + fr) * PITCH + n * F + g * 8 + fk * 4) = f32x4{acc[i][n][g * 4], acc[i][n][g * 4 + 1], acc[i][n][g * 4 + 2], acc[i][n][g * 4 + 3]};
+        __syncthreads();
+        for (int t = threadIdx.x; t < R * R / 4; t += 64 * WK) {
+            const int row = t / (R / 4), n = t % (R / 4) * 4;
+            if (row >= j.am || n >= j.bn) continue;
+            const LCMA_LDS float *of = (const LCMA_LDS float *)lds + row * PITCH + n;
+            f32x4 sum = *(const LCMA_LDS f32x4 *)of;
+#pragma unroll
+            for (int k = 1; k < WK; ++k) sum += *(const LCMA_LDS f32x4 *)(of + k * R * PITCH);
+            i8_store4<T>(j.c + (int64_t)row * p.ldc_b + n * T::ES, sum, j.bn - n);
+        }
+    }
+    // Steps `y`, y + WK, ...
+    static LCMA_DEV void steps_of_wave(const ExpertsGemmParams &p, const ExpJob &j, int y, Acc (&acc)[NF][NF], LCMA_LDS char *__restrict__ s0, LCMA_LDS char *__restrict__ s1,
+                                       LCMA_LDS char *__restrict__ s2, LCMA_LDS char *__restrict__ s3) {
+        constexpr int CPR = R * 2 / 16, RPL = 64 / CPR; // the other form: 16-byte chunks of a row, rows of a load
+        const int lane = threadIdx.x & 63, fr = lane & (F - 1), fk = lane / F, steps = (int)(((uint32_t)j.k + 63) / 64);
+        const uint32_t lda = (uint32_t)p.lda_b, ldb = (uint32_t)p.ldb_b;
+        const auto ra = exp_rows_of<T>(j.a, j.am, j.k, lda), rows_b = exp_rows_of<T>(j.b, j.bn, j.k, ldb);
+        // a load brings 8 rows of 128 bytes, lanes 8 i to 8 i + 7 one row; `last`: what is past K from past the extents
+        uint32_t av[2], bv[2], al[2], bl[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const uint32_t c = ((lane & 7) ^ (lane >> 4) ^ (4 * i)) * 16;
+            const bool past = c >= (uint32_t)((j.k - 1) % 64 + 1) * 2;
+            av[i] = (uint32_t)(lane >> 3) * lda + c;
+            al[i] = past ? NONE : av[i];
+            bv[i] = BCOL ? (uint32_t)(lane / CPR) * ldb + exp_col_chunk<T, R>(lane / CPR, lane % CPR) * 16 : (uint32_t)(lane >> 3) * ldb + c;
+            bl[i] = !BCOL && past ? NONE : bv[i];
+        }
+        auto load = [&](LCMA_LDS char *st, int y) { // a step past the end: zeros, from past the extents
+            const uint32_t off = y < steps ? (uint32_t)y * 128 : NONE;
+            const bool last = y == steps - 1;
+            const auto rb = BCOL ? exp_columns_from<T>(j.b, j.bn, j.k, ldb, y, 1) : rows_b;
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (LCMA_LDS void *)(st + HALF + i * 1024), 16, (int)(last ? bl[i & 1] : bv[i & 1]), (int)(BCOL ? i * RPL * ldb : off + i * 8 * ldb), 0, 0);
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (LCMA_LDS void *)(st + i * 1024), 16, (int)(last ? al[i & 1] : av[i & 1]), (int)(off + i * 8 * lda), 0, 0);
+        };
+        uint32_t frag[KF]; // of this lane's 16 bytes in k-contiguous rows
+#pragma unroll
+        for (int k = 0; k < KF; ++k) frag[k] = fr * 128 + ((k * (64 / F) + fk) ^ (fr >> 1 & 7)) * 16;
+        auto step = [&](LCMA_LDS char *st, int y) {
+            u32x4 a[NF][KF], b[NF][KF];
+            wait_loads<2 * LOADS *(S - 1)>();
+#pragma unroll
+            for (int i = 0; i < NF; ++i) {
+                if constexpr (BCOL) exp_columns<T, R>(st + HALF, i, b[i]);
+#pragma unroll
+                for (int k = 0; k < KF; ++k) {
+                    a[i][k] = *(const LCMA_LDS u32x4 *)(st + frag[k] + i * F * 128);
+                    if constexpr (!BCOL) b[i][k] = *(const LCMA_LDS u32x4 *)(st + HALF + frag[k] + i * F * 128);
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_s_waitcnt(0xC07F); // lgkmcnt(0): what was read has left LDS, so its place may be loaded anew
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_sched_barrier(0);
+            load(st, y + S * WK);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int k = 0; k < KF; ++k)
+#pragma unroll
+                for (int i = 0; i < NF; ++i)
+#pragma unroll
+                    for (int n = 0; n < NF; ++n) {
+                        const Frag fa = __builtin_bit_cast(Frag, a[i][k]), fb = __builtin_bit_cast(Frag, b[n][k]);
+                        if constexpr (F == 16) acc[i][n] = Mma16<T>::run(fb, fa, acc[i][n]);
+                        else Mma<T>::run(fb, fa, acc[i][n]);
+                    }
+        };
+        load(s0, y);
+        load(s1, y + WK);
+        if constexpr (S == 4) {
+            load(s2, y + 2 * WK);
+            load(s3, y + 3 * WK);
+        }
+        while (y < steps) {
+            step(s0, y);
+            if ((y += WK) >= steps) break;
+            step(s1, y);
+            if constexpr (S == 4) {
+                if ((y += WK) >= steps) break;
+                step(s2, y);
+                if ((y += WK) >= steps) break;
+                step(s3, y);
+            }
+            y += WK;
+        }
+        wait_loads<0>();
+    }
+};
+
+} // namespace lcma

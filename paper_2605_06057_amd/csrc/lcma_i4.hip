@@ -69,7 +69,7 @@ template <class T, bool CODES> __global__ __launch_bounds__(256) void i4_prepare
             }
             char *to = q + (int64_t)y * block_bytes;
             *(u32x4 *)(to + lane * 16) = out;
-            const int g = lane >> 4; // (a group's 16 scales: one row of lanes)
+            const int g = lane >> 4; // (a group's scales: 16 lanes)
             if (g < groups) {
                 float s;
                 if constexpr (CODES) {
@@ -79,14 +79,14 @@ template <class T, bool CODES> __global__ __launch_bounds__(256) void i4_prepare
                     const int j = g * (4 / groups);
                     s = j == 0 ? scale[0] : j == 1 ? scale[1] : j == 2 ? scale[2] : scale[3];
                 }
-                *(float *)(to + 1024 + g * 64 + (lane & 15) * 4) = s * 16.f; // (the product's sums are of q / 16)
+                *(float *)(to + 1024 + ((lane & 15) * groups + g) * 4) = s * 16.f; // (the product's sums are of q / 16)
             }
         }
     }
 }
 
-template <class T, int G, int MT, int NB, int WN, int WK, int KC> __global__ __launch_bounds__(64 * WN * WK) void i4_gemm(const I4GemmParams p) {
-    using K = I4Gemm<T, G, MT, NB, WN, WK, KC>;
+template <class T, int G, int MT, int NB, int WN, int WK, int D, int XB> __global__ __launch_bounds__(64 * WN * WK) void i4_gemm(const I4GemmParams p) {
+    using K = I4Gemm<T, G, MT, NB, WN, WK, D, XB>;
     __shared__ __attribute__((aligned(16))) char smem[K::LDS_BYTES];
     K::run(p, (LCMA_LDS char *)smem);
 }
@@ -109,14 +109,20 @@ extern "C" int lcma_launch_i4_gemm(const lcma::I4GemmParams *p, int kernel, int 
     if (group == 32) i4_gemm<T, 32, __VA_ARGS__><<<dim3(grid), dim3(THREADS), 0, s>>>(*p);          \
     else if (group == 64) i4_gemm<T, 64, __VA_ARGS__><<<dim3(grid), dim3(THREADS), 0, s>>>(*p);     \
     else i4_gemm<T, 128, __VA_ARGS__><<<dim3(grid), dim3(THREADS), 0, s>>>(*p);
-#define LCMA_I4(THREADS, MT, NB, WN, WK, KC, KC32)                          \
-    if (dtype == 0) { LCMA_I4_G(F32, THREADS, MT, NB, WN, WK, KC32) }       \
-    else if (dtype == 1) { LCMA_I4_G(BF16, THREADS, MT, NB, WN, WK, KC) }   \
-    else { LCMA_I4_G(F16, THREADS, MT, NB, WN, WK, KC) }                    \
+// (fp32: three parts of X in LDS)
+#define LCMA_I4(MT, NB, WN, WK, D, XB, D32, XB32)                                      \
+    if (dtype == 0) { LCMA_I4_G(F32, 64 * WN * WK, MT, NB, WN, WK, D32, XB32) }        \
+    else if (dtype == 1) { LCMA_I4_G(BF16, 64 * WN * WK, MT, NB, WN, WK, D, XB) }      \
+    else { LCMA_I4_G(F16, 64 * WN * WK, MT, NB, WN, WK, D, XB) }                       \
     break;
     switch (kernel) {
-    case kI4Rows16: LCMA_I4(256, 1, 1, 1, 4, 16, 4)
-    default: LCMA_I4(256, 4, 2, 4, 1, 4, 1)
+    case kI4Rows16K8: LCMA_I4(1, 1, 1, 8, 2, 66048, 1, 99072)
+    case kI4Rows16K4: LCMA_I4(1, 1, 2, 4, 4, 66048, 1, 50048)
+    case kI4Rows16: LCMA_I4(1, 1, 4, 1, 4, 33024, 2, 50048)
+    case kI4Rows32: LCMA_I4(2, 1, 2, 4, 2, 66048, 1, 99840)
+    default: // (16 bit: three parts of 64 rows do not stay in registers)
+        if (dtype == 1) { LCMA_I4_G(BF16, 512, 4, 1, 4, 2, 2, 66560) }
+        else { LCMA_I4_G(F16, 512, 4, 1, 4, 2, 2, 66560) }
     }
 #undef LCMA_I4
 #undef LCMA_I4_G

@@ -3,7 +3,7 @@
 //
 // Weights are laid out once, in the order in which a wave takes them: blocks of 16 rows x 128 columns, those of 16 rows one behind the other, so that a wave reads
 // memory from front to back.  A block is 1024 bytes of codes, 16 for every lane (row lane % 16; four dwords, dword j the columns 32 j + 8 (lane / 16) .. + 7, which are what
-// the lane holds of a 16x16x32 instruction), and then the scales of its groups, 16 rows each.  Column i of the eight is nibble i / 2 + 4 (i % 2): shifted to place,
+// the lane holds of a 16x16x32 instruction), and then the scales of every row's groups.  Column i of the eight is nibble i / 2 + 4 (i % 2): shifted to place,
 // the nibbles p and p + 4 are the two halves of a register.
 //
 // A code becomes a 16-bit float by its bits alone: u under the exponent of one is 1 + u / 16 = (24 + q) / 16 with q = u - 8, exactly, in bf16 and fp16: a shift and an
@@ -11,7 +11,7 @@
 // sum is then 1/16 of sum q x in fp32 and is added to the row's times 16 S.  (What that costs: the terms are up to 1.94 x where q x / 16 is up to 0.5 x, so roundings
 // of the fp32 sums count about eight times: 2^-21 of sum |x|, where C's own rounding is 2^-9 or 2^-12.)  fp32 activations are three bf16 numbers, whose sum is the value.
 #pragma once
-#include "lcma_i8.hpp"
+#include "lcma_experts.hpp"
 
 namespace lcma {
 
@@ -35,37 +35,36 @@ template <class T> LCMA_DEV u32x4 i4_widened(uint32_t v) {
     return r;
 }
 
-// WN x WK waves: the first along N, NB blocks of rows each, the others along K, a block of columns to a wave in turn.  MT x 16 rows of X, chunks of KC blocks of columns of
-// them in LDS.  Rows past the tile's are whatever is in LDS: their sums are dropped.
-template <class T, int G, int MT, int NB, int WN, int WK, int KC> struct I4Gemm {
+// WN x WK waves: the first along N, NB blocks of rows (of the weights) each, the others along K, a block of columns to a wave in turn; the weights of D of a wave's blocks are in
+// flight.  MT x 16 rows of X; as many blocks of columns of them are in LDS at a time as XB bytes hold.
+// What bounds it is the latency of the weights' way from memory, not the arithmetic: a block takes a wave about 60 vector instructions, 240 of the 420 clocks in which a CU's fourth of the
+// memory's rate brings it.
+template <class T, int G, int MT, int NB, int WN, int WK, int D, int XB> struct I4Gemm {
     using I = I4Type<T>;
     using Mul = typename I::Mul;
     using Frag = typename Mma16<Mul>::frag;
-    static constexpr int NT = 64 * WN * WK, TM = 16 * MT, TN = 16 * NB * WN, GROUPS = 128 / G, BLOCK = 1024 + GROUPS * 64;
-    static constexpr int PITCH = KC * 256 + 16, PART = TM * PITCH; // (16: 16 rows at one column meet different banks)
-    static constexpr int SUMS = (WK - 1) * WN * NB * MT * 1024, X_BYTES = I::PARTS * PART, LDS_BYTES = SUMS > X_BYTES ? SUMS : X_BYTES;
-    static_assert(LDS_BYTES <= 160 * 1024, "LDS budget of one CU");
+    static constexpr int NT = 64 * WN * WK, TM = 16 * MT, TN = 16 * NB * WN, GROUPS = 128 / G, BLOCK = 1024 + GROUPS * 64, PER = 4 / GROUPS; // PER: instructions of a group
+    static constexpr int PITCH = TN + 4, SUMS = WK * TM * PITCH * 4, LDS_BYTES = SUMS > XB ? SUMS : XB;
+    static_assert(LDS_BYTES <= 160 * 1024 && I::PARTS * TM * (WK * D * 256 + 16) <= XB, "LDS budget of one CU; a turn of all waves");
 
-    // Columns k .. k + 7 of a row of X as the parts that are multiplied; zeros from K on.
-    static LCMA_DEV void stage(const char *row, int k, int K, LCMA_LDS char *to) {
-        constexpr int ES = T::ES;
-        if constexpr (ES == 2) {
-            u32x4 v = {0, 0, 0, 0};
-            if (k + 8 <= K) __builtin_memcpy(&v, row + (int64_t)k * 2, 16);
-            else
+    // Columns k .. k + 7 of a row of X, zeros from K on; put into LDS as the parts that are multiplied.
+    struct Eight {
+        u32x4 v[T::ES / 2];
+    };
+    static LCMA_DEV Eight take(const char *row, int k, int K) {
+        Eight e;
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (k + i < K) v[i / 2] |= (uint32_t)((const uint16_t *)row)[k + i] << (i & 1) * 16;
-            *(LCMA_LDS u32x4 *)to = v;
+        for (int h = 0; h < T::ES / 2; ++h) e.v[h] = exp_chunk<T>(row + (int64_t)(k + h * T::CH) * T::ES, K - (k + h * T::CH));
+        return e;
+    }
+    static LCMA_DEV void put(const Eight &e, LCMA_LDS char *to, int part_bytes) {
+        if constexpr (T::ES == 2) {
+            *(LCMA_LDS u32x4 *)to = e.v[0];
         } else {
+            const f32x4 half[2] = {__builtin_bit_cast(f32x4, e.v[0]), __builtin_bit_cast(f32x4, e.v[T::ES / 2 - 1])};
             float v[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = 0.f;
-            if (k + 8 <= K) __builtin_memcpy(v, row + (int64_t)k * 4, 32);
-            else
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (k + i < K) v[i] = ((const float *)row)[k + i];
+            for (int i = 0; i < 8; ++i) v[i] = half[i / 4][i % 4];
 #pragma unroll
             for (int part = 0; part < 3; ++part) { // the upper 8 bits of what is left, twice, and the rest: each exact
                 u32x4 w;
@@ -76,20 +75,80 @@ template <class T, int G, int MT, int NB, int WN, int WK, int KC> struct I4Gemm 
                     else w[i / 2] = top >> 16;
                     v[i] -= __builtin_bit_cast(float, top);
                 }
-                *(LCMA_LDS u32x4 *)(to + part * PART) = w;
+                *(LCMA_LDS u32x4 *)(to + part * part_bytes) = w;
             }
+        }
+    }
+    // Blocks c0 .. end - 1 of the tile's rows of X, by all threads, four loads of each in flight.
+    static LCMA_DEV void stage(const I4GemmParams &p, const I8Place &at, int c0, int end, int pitch, int part_bytes, LCMA_LDS char *lds) {
+        constexpr int U = 4;
+        const int vectors = (end - c0) * 16, n = at.rows * vectors;
+        const char *x = p.X + (int64_t)at.row0 * p.ldx_b;
+        for (int i0 = threadIdx.x; i0 < n; i0 += U * NT) {
+            Eight e[U];
+            int to[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int i = i0 + u * NT, row = (int)((uint32_t)i / (uint32_t)vectors), v = i - row * vectors;
+                to[u] = i < n ? row * pitch + v * 16 : -1;
+                if (i < n) e[u] = take(x + (int64_t)row * p.ldx_b, c0 * 128 + v * 8, p.K);
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (to[u] >= 0) put(e[u], lds + to[u], part_bytes);
         }
     }
 
     struct Block {
         u32x4 codes;
-        f32x4 scales[GROUPS];
+        float scales[GROUPS]; // of row lane % 16
     };
     static LCMA_DEV void fetch(const char *at, Block &b) { // at: of the block
         const int lane = threadIdx.x & 63;
         b.codes = *(const u32x4 *)(at + lane * 16);
+        __builtin_memcpy(b.scales, __builtin_assume_aligned(at + 1024 + (lane & 15) * (GROUPS * 4), GROUPS * 4), GROUPS * 4);
+    }
+
+    // A block of columns: x, this lane's row of X in LDS (`row` of every 16), at the block's columns.
+    static LCMA_DEV void multiply(const LCMA_LDS char *(&x)[MT], int at, int part_bytes, const Block (&blk)[NB], f32x4 (&acc)[NB][MT]) {
+        const Frag minus = __builtin_bit_cast(Frag, u32x4{I::MINUS, I::MINUS, I::MINUS, I::MINUS});
 #pragma unroll
-        for (int g = 0; g < GROUPS; ++g) b.scales[g] = *(const f32x4 *)(at + 1024 + g * 64 + (lane >> 4) * 16);
+        for (int g = 0; g < GROUPS; ++g) {
+            Frag xf[PER][MT][I::PARTS];
+            f32x4 off[MT];
+#pragma unroll
+            for (int j = 0; j < PER; ++j)
+#pragma unroll
+                for (int i = 0; i < MT; ++i)
+#pragma unroll
+                    for (int part = 0; part < I::PARTS; ++part) xf[j][i][part] = __builtin_bit_cast(Frag, *(const LCMA_LDS u32x4 *)(x[i] + at + part * part_bytes + (g * PER + j) * 64));
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+                off[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int j = 0; j < PER; ++j)
+#pragma unroll
+                    for (int part = 0; part < I::PARTS; ++part) off[i] = Mma16<Mul>::run(xf[j][i][part], minus, off[i]);
+            }
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+                f32x4 sum[MT];
+#pragma unroll
+                for (int i = 0; i < MT; ++i) sum[i] = off[i];
+#pragma unroll
+                for (int j = 0; j < PER; ++j) {
+                    const Frag wf = __builtin_bit_cast(Frag, i4_widened<T>(blk[b].codes[g * PER + j]));
+#pragma unroll
+                    for (int i = 0; i < MT; ++i)
+#pragma unroll
+                        for (int part = 0; part < I::PARTS; ++part) sum[i] = Mma16<Mul>::run(xf[j][i][part], wf, sum[i]);
+                }
+#pragma unroll
+                for (int i = 0; i < MT; ++i)
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) acc[b][i][v] = __builtin_fmaf(sum[i][v], blk[b].scales[g], acc[b][i][v]);
+            }
+        }
     }
 
     static LCMA_DEV void run(const I4GemmParams &p, LCMA_LDS char *lds) {
@@ -98,100 +157,76 @@ template <class T, int G, int MT, int NB, int WN, int WK, int KC> struct I4Gemm 
         const int nx = groups.tiles, jobs = nx * p.nz, per = (jobs + 7) / 8;
         const int job = (blockIdx.x & 7) * per + (blockIdx.x >> 3); // an eighth of the tiles to every XCD, row tiles that share weights next to each other
         if ((int)(blockIdx.x >> 3) >= per || job >= jobs) return;
-        int x, z;
-        i8_tile_of_job(nx, p.nz, p.panel, job, x, z);
-        const I8Place at = groups.place(p, x);
-        const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wk = w / WN, wn = w % WN, m = lane & 15, kb = lane >> 4;
-        const int first = (z * WN + wn) * NB, all = (p.N + 15) / 16; // blocks of rows
+        int tile, z;
+        i8_tile_of_job(nx, p.nz, p.panel, job, tile, z);
+        const I8Place at = groups.place(p, tile);
+        const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wk = w / WN, wn = w % WN;
+        const int first = (z * WN + wn) * NB, all = (p.N + 15) / 16, blocks = p.blocks; // blocks of rows; of columns
         const char *q[NB];
 #pragma unroll
-        for (int b = 0; b < NB; ++b) q[b] = p.Q + at.expert * p.expert_q + (int64_t)(first + b < all ? first + b : all - 1) * p.blocks * BLOCK; // (past the last: the last again, dropped)
+        for (int b = 0; b < NB; ++b) q[b] = p.Q + at.expert * p.expert_q + (int64_t)(first + b < all ? first + b : all - 1) * blocks * BLOCK; // (past the last: the last again, dropped)
+        auto fetch_from = [&](int y, Block (&blk)[NB]) { // (past the last: the last again, not used)
+            const int64_t off = (int64_t)(y < blocks ? y : blocks - 1) * BLOCK;
+#pragma unroll
+            for (int b = 0; b < NB; ++b) fetch(q[b] + off, blk[b]);
+        };
         f32x4 acc[NB][MT];
 #pragma unroll
         for (int b = 0; b < NB; ++b)
 #pragma unroll
             for (int i = 0; i < MT; ++i) acc[b][i] = f32x4{0.f, 0.f, 0.f, 0.f};
-        const Frag minus = __builtin_bit_cast(Frag, u32x4{I::MINUS, I::MINUS, I::MINUS, I::MINUS});
-        for (int c0 = 0; c0 < p.blocks; c0 += KC) {
-            const int chunk = p.blocks - c0 < KC ? p.blocks - c0 : KC;
-            if (c0) __syncthreads(); // all have read the chunk before
-            for (int i = threadIdx.x; i < at.rows * chunk * 16; i += NT) {
-                const int row = i / (chunk * 16), v = i % (chunk * 16);
-                stage(p.X + (int64_t)(at.row0 + row) * p.ldx_b, c0 * 128 + v * 8, p.K, lds + row * PITCH + v * 16);
+        if (blocks) {
+            Block now[D][NB], next[D][NB];
+            int y = wk;
+#pragma unroll
+            for (int d = 0; d < D; ++d) fetch_from(y + d * WK, next[d]);
+            // whole turns of all waves in LDS at a time, D blocks each, as often as the rows there are leave room for
+            const int room = (XB / (I::PARTS * at.rows) - 16) / (WK * D * 256) * (WK * D), chunk = room < blocks ? room : blocks, pitch = chunk * 256 + 16; // (16: 16 rows at one column meet different banks)
+            const int part_bytes = at.rows * pitch;
+            const LCMA_LDS char *x[MT];
+#pragma unroll
+            for (int i = 0; i < MT; ++i) { // (rows past the tile's: the last one again, dropped)
+                const int row = i * 16 + (lane & 15);
+                x[i] = lds + (row < at.rows ? row : at.rows - 1) * pitch + (lane >> 4) * 16;
             }
-            __syncthreads();
-            for (int y = wk; y < chunk; y += WK) {
-                Block blk[NB];
+            for (int c0 = 0; c0 < blocks; c0 += chunk) {
+                const int end = c0 + chunk < blocks ? c0 + chunk : blocks;
+                if (c0) __syncthreads(); // all have read the blocks before
+                stage(p, at, c0, end, pitch, part_bytes, lds);
+                __syncthreads();
+                for (; y < end; y += WK * D) {
 #pragma unroll
-                for (int b = 0; b < NB; ++b) fetch(q[b] + (int64_t)(c0 + y) * BLOCK, blk[b]);
+                    for (int d = 0; d < D; ++d)
 #pragma unroll
-                for (int g = 0; g < GROUPS; ++g) {
-                    Frag xf[4 / GROUPS][MT][I::PARTS];
-                    f32x4 off[MT], sum[NB][MT];
+                        for (int b = 0; b < NB; ++b) now[d][b] = next[d][b];
+                    if (y + WK * D < blocks)
 #pragma unroll
-                    for (int j = 0; j < 4 / GROUPS; ++j)
+                        for (int d = 0; d < D; ++d) fetch_from(y + (D + d) * WK, next[d]);
 #pragma unroll
-                        for (int i = 0; i < MT; ++i)
-#pragma unroll
-                            for (int part = 0; part < I::PARTS; ++part)
-                                xf[j][i][part] = __builtin_bit_cast(
-                                    Frag, *(const LCMA_LDS u32x4 *)(lds + part * PART + (i * 16 + m) * PITCH + y * 256 + (g * (4 / GROUPS) + j) * 64 + kb * 16));
-#pragma unroll
-                    for (int i = 0; i < MT; ++i) {
-                        off[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                        for (int j = 0; j < 4 / GROUPS; ++j)
-#pragma unroll
-                            for (int part = 0; part < I::PARTS; ++part) off[i] = Mma16<Mul>::run(minus, xf[j][i][part], off[i]);
-                    }
-#pragma unroll
-                    for (int b = 0; b < NB; ++b) {
-#pragma unroll
-                        for (int i = 0; i < MT; ++i) sum[b][i] = off[i];
-#pragma unroll
-                        for (int j = 0; j < 4 / GROUPS; ++j) {
-                            const Frag wf = __builtin_bit_cast(Frag, i4_widened<T>(blk[b].codes[g * (4 / GROUPS) + j]));
-#pragma unroll
-                            for (int i = 0; i < MT; ++i)
-#pragma unroll
-                                for (int part = 0; part < I::PARTS; ++part) sum[b][i] = Mma16<Mul>::run(wf, xf[j][i][part], sum[b][i]);
-                        }
-#pragma unroll
-                        for (int i = 0; i < MT; ++i)
-#pragma unroll
-                            for (int v = 0; v < 4; ++v) acc[b][i][v] = __builtin_fmaf(sum[b][i][v], blk[b].scales[g][v], acc[b][i][v]);
-                    }
+                    for (int d = 0; d < D; ++d)
+                        if (y + d * WK < end) multiply(x, (y + d * WK - c0) * 256, part_bytes, now[d], acc);
                 }
             }
+            __syncthreads(); // the sums take the place of X
         }
-        if constexpr (WK > 1) { // the sums of the waves along K, in ascending order
-            __syncthreads();
-            LCMA_LDS f32x4 *sums = (LCMA_LDS f32x4 *)lds;
-            if (wk)
+        // lane: column lane % 16 of rows 4 (lane / 16) .. + 3
+        LCMA_LDS float *mine = (LCMA_LDS float *)lds + wk * (TM * PITCH) + (lane >> 4) * 4 * PITCH + wn * NB * 16 + (lane & 15);
 #pragma unroll
-                for (int b = 0; b < NB; ++b)
+        for (int b = 0; b < NB; ++b)
 #pragma unroll
-                    for (int i = 0; i < MT; ++i) sums[((((wk - 1) * WN + wn) * NB + b) * MT + i) * 64 + lane] = acc[b][i];
-            __syncthreads();
-            if (wk) return;
+            for (int i = 0; i < MT; ++i)
 #pragma unroll
-            for (int k = 1; k < WK; ++k)
+                for (int v = 0; v < 4; ++v) mine[(i * 16 + v) * PITCH + b * 16] = acc[b][i][v];
+        __syncthreads();
+        for (int t = threadIdx.x; t < TM * TN / 4; t += NT) { // four neighbouring columns of a row; the waves along K in ascending order
+            const int row = t / (TN / 4), n = t % (TN / 4) * 4, col = z * TN + n;
+            if (row >= at.rows || col >= p.N) continue;
+            const LCMA_LDS float *of = (const LCMA_LDS float *)lds + row * PITCH + n;
+            f32x4 sum = *(const LCMA_LDS f32x4 *)of;
 #pragma unroll
-                for (int b = 0; b < NB; ++b)
-#pragma unroll
-                    for (int i = 0; i < MT; ++i) acc[b][i] += sums[((((k - 1) * WN + wn) * NB + b) * MT + i) * 64 + lane];
-        }
-#pragma unroll
-        for (int b = 0; b < NB; ++b) {
-            const int col = (first + b) * 16 + kb * 4;
-            if (col >= p.N) continue;
-            f32x4 bias = {0.f, 0.f, 0.f, 0.f};
-            if (p.bias) bias = i8_four(p.bias + (int64_t)at.expert * p.N, col, p.N);
-#pragma unroll
-            for (int i = 0; i < MT; ++i) {
-                const int row = i * 16 + m;
-                if (row < at.rows) i8_store4<T>(p.C + ((int64_t)(at.row0 + row) * p.ldc + col) * T::ES, acc[b][i] + bias, p.N - col);
-            }
+            for (int k = 1; k < WK; ++k) sum += *(const LCMA_LDS f32x4 *)(of + k * TM * PITCH);
+            if (p.bias) sum += i8_four(p.bias + (int64_t)at.expert * p.N, col, p.N);
+            i8_store4<T>(p.C + ((int64_t)(at.row0 + row) * p.ldc + col) * T::ES, sum, p.N - col);
         }
     }
 };

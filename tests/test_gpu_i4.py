@@ -22,6 +22,14 @@ def _lib():
     return binding
 
 
+@pytest.fixture(params=["", "16x16", "16x32", "16x64", "32x32", "64x64"], scope="module")
+def kernel(request):
+    """The kernel of the rule, and every kernel by name."""
+    _lib().lcma_set_tuning("i4_kernel", request.param)
+    yield request.param
+    _lib().lcma_set_tuning("i4_kernel", "")
+
+
 def _np(t):
     return t.double().cpu().numpy()
 
@@ -50,7 +58,7 @@ def _close(got, x, q, s, group, bias, dtype):
 @pytest.mark.parametrize("group", [32, 64, 128])
 @pytest.mark.parametrize("M,N,K,pad,bias", [(1, 1, 1, 0, False), (1, 64, 128, 0, True), (1, 272, 4096, 0, False), (3, 33, 77, 3, True), (16, 48, 2200, 8, False), (17, 200, 520, 0, True),
                                             (45, 101, 1545, 24, True), (64, 128, 256, 0, False), (100, 130, 300, 5, False), (257, 144, 1100, 0, True)])
-def test_linear(M, N, K, pad, bias, group, dtype):
+def test_linear(kernel, M, N, K, pad, bias, group, dtype):
     torch, types = _torch()
     gen = torch.Generator(device="cuda").manual_seed(M + N + K)
     codes, scales = _weights(gen, (), N, K, group)
@@ -70,7 +78,7 @@ def test_linear(M, N, K, pad, bias, group, dtype):
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("counts,behind,N,K,group,bias", [([1, 0, 1], 0, 264, 520, 128, False), ([0, 5, 2, 0, 16], 3, 77, 300, 32, True), ([17, 40, 0, 3], 0, 130, 1100, 64, False),
                                                           ([1] * 70, 5, 40, 136, 128, True), ([100, 33], 1, 200, 260, 64, True), ([0, 0], 4, 24, 64, 32, True)], ids=str)
-def test_experts(counts, behind, N, K, group, bias, dtype):
+def test_experts(kernel, counts, behind, N, K, group, bias, dtype):
     torch, types = _torch()
     gen = torch.Generator(device="cuda").manual_seed(N + K)
     E, n = len(counts), sum(counts)
@@ -90,7 +98,7 @@ def test_experts(counts, behind, N, K, group, bias, dtype):
 
 
 @pytest.mark.parametrize("group", [32, 64, 128])
-def test_every_code_in_every_place(group):
+def test_every_code_in_every_place(kernel, group):
     """One row of X with a single one at a time: C is the column of weights, exactly (16 S q / 16 in fp32, scales are powers of two)."""
     torch, types = _torch()
     gen = torch.Generator(device="cuda").manual_seed(group)
@@ -168,7 +176,7 @@ def test_empty_calls():
 
 
 @pytest.mark.parametrize("M", [1, 30])
-def test_captured_and_replayed(M):
+def test_captured_and_replayed(kernel, M):
     torch, types = _torch()
     gen = torch.Generator(device="cuda").manual_seed(2)
     L = _lib()
