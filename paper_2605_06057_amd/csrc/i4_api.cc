@@ -1,6 +1,7 @@
 // Host side of the linear layer with 4-bit weights, alone and over experts: argument checks, launches.
 #include "experts_host.h"
 
+#include <cmath>
 #include <cstring>
 
 extern "C" int lcma_launch_i4_prepare(const lcma::I4PrepareParams *p, int dtype, int grid, void *stream);
@@ -10,7 +11,7 @@ using namespace lcma;
 
 namespace {
 
-const int kTile[kI4Kernels][2] = {{16, 16}, {16, 32}, {16, 64}, {32, 32}, {64, 64}}; // rows and columns of the kernels' tiles
+const int kTile[kI4Kernels][2] = {{16, 16}, {16, 32}, {16, 64}, {64, 64}}; // rows and columns of the kernels' tiles
 
 bool group_fits(int group) { return group == 32 || group == 64 || group == 128; }
 int64_t row_blocks(int64_t N) { return (N + 15) / 16; }
@@ -59,9 +60,24 @@ int64_t tiles_of(int kernel, int64_t rows, int64_t N, int experts, bool grouped)
 }
 bool launches(int64_t jobs) { return (jobs + 8) * 512 < kGridLimit / 2; } // (numbers of tiles are 32-bit on the device)
 
-int pick(int64_t rows, int64_t N, int64_t K, int experts) {
-    const int64_t hit = rows < experts ? rows : experts, strips = ((rows + 15) / 16 > hit ? (rows + 15) / 16 : hit) * row_blocks(N); // (blocks of rows that are read)
-    return strips >= 4096 ? kI4Rows16 : strips >= 512 ? kI4Rows16K4 : kI4Rows16K8;
+// What a kernel takes, in us: `start`; a tile: `end`, `step` for every turn of its waves along K (fp32: 2.2 of them, three parts of X), `stage` for every byte of a column
+// of the rows of X that go through LDS, 256 * `slots` tiles at a time; and no less than the bytes at `rate` GB/us take.  Fitted to 268 products, alone and over experts, of 1 to 1024 rows, timed on every
+// kernel: a single time is predicted within 14 % (root mean square), the kernel with the smallest prediction is 1.3 % slower than the fastest one on average, 38 % at worst.
+const struct Cost {
+    int along_k; // waves
+    double start, end, step, stage, rate, slots;
+} kCost[kI4Kernels] = {{8, 2.69, 0.768, 0.318, 0.00298, 16.4, 0.903}, {4, 2.49, 0.998, 0.279, 0.00407, 5.32, 1.08}, {1, 2.56, 0.819, 0.215, 0.00677, 4.86, 1.67}, {2, 2.73, 0.738, 0.67, 0.00475, 4.63, 0.831}};
+double predicted_us(int kernel, int64_t rows, int64_t N, int64_t K, int group, int experts, bool grouped, int es) {
+    const Cost &c = kCost[kernel];
+    const double tm = kTile[kernel][0], hit = rows < experts ? (double)rows : experts, blocks = (double)column_blocks(K);
+    // (the rows of each expert are known on the device alone: half a tile left over for each that can have any)
+    double nx = std::ceil(rows / tm);
+    if (grouped) nx = rows / tm + 0.5 * hit > hit ? rows / tm + 0.5 * hit : hit;
+    const double nz = std::ceil((double)N / kTile[kernel][1]), per = rows / hit < tm ? rows / hit : tm, n = nx * nz / 256 / c.slots;
+    const double tile = c.end + std::ceil(blocks / c.along_k) * c.step * (es == 4 ? 2.2 : 1) + blocks * per * c.stage * es;
+    const double bytes = hit * N * (0.5 * K + 4.0 * K / group) + 2.0 * rows * (N + K);
+    const double t = c.start + tile * (n > 1 ? n : 1), memory = c.start + bytes / (c.rate * 1e6);
+    return std::sqrt(std::sqrt(t * t * t * t + memory * memory * memory * memory));
 }
 
 lcma_status gemm(const char *who, int64_t rows, int64_t N, int64_t K, int group, int experts, const int32_t *offsets, const void *X, int64_t ldx, const void *Wp, const float *bias,
@@ -99,9 +115,16 @@ lcma_status gemm(const char *who, int64_t rows, int64_t N, int64_t K, int group,
     p.panel = 1;
     auto fits = [&](int k) { return (es == 2 || k != kI4Rows64) && launches(tiles_of(k, rows, N, experts, offsets != nullptr)); };
     int kernel = tuning_i4_kernel();
-    if (kernel < 0 || !fits(kernel)) kernel = pick(rows, N, K, experts);
-    if (!fits(kernel)) kernel = kI4Rows32;
-    if (!fits(kernel)) return fail(LCMA_ERR_SHAPE, "%s: too many tiles for a launch", who);
+    if (kernel < 0 || !fits(kernel)) {
+        kernel = -1;
+        double least = 0;
+        for (int k = 0; k < kI4Kernels; ++k)
+            if (const double t = predicted_us(k, rows, N, K, group, experts, offsets != nullptr, es); fits(k) && (kernel < 0 || t < least)) {
+                least = t;
+                kernel = k;
+            }
+    }
+    if (kernel < 0) return fail(LCMA_ERR_SHAPE, "%s: too many tiles for a launch", who);
     const int64_t jobs = tiles_of(kernel, rows, N, experts, offsets != nullptr);
     p.nz = (int32_t)((N + kTile[kernel][1] - 1) / kTile[kernel][1]);
     if (const int err = lcma_launch_i4_gemm(&p, kernel, group, dtype, (int)((jobs + 7) / 8 * 8), stream)) return fail(LCMA_ERR_HIP, "%s: launch failed with HIP error %d", who, err);

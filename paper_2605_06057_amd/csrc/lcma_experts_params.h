@@ -100,7 +100,7 @@ struct I4PrepareParams {
     int32_t N, K, group, experts;
 };
 // Kernels of the product with them: rows of a tile; blocks of rows of the weights in it; waves along K.
-enum { kI4Rows16K8 = 0, kI4Rows16K4, kI4Rows16, kI4Rows32, kI4Rows64, kI4Kernels };
+enum { kI4Rows16K8 = 0, kI4Rows16K4, kI4Rows16, kI4Rows64, kI4Kernels };
 // lcma_i4_gemm_nt, lcma_i4_gemm_experts.
 struct I4GemmParams {
     const char *X, *Q;

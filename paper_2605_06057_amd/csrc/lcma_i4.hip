@@ -119,7 +119,6 @@ extern "C" int lcma_launch_i4_gemm(const lcma::I4GemmParams *p, int kernel, int 
     case kI4Rows16K8: LCMA_I4(1, 1, 1, 8, 2, 66048, 1, 99072)
     case kI4Rows16K4: LCMA_I4(1, 1, 2, 4, 4, 66048, 1, 50048)
     case kI4Rows16: LCMA_I4(1, 1, 4, 1, 4, 33024, 2, 50048)
-    case kI4Rows32: LCMA_I4(2, 1, 2, 4, 2, 66048, 1, 99840)
     default: // (16 bit: three parts of 64 rows do not stay in registers)
         if (dtype == 1) { LCMA_I4_G(BF16, 512, 4, 1, 4, 2, 2, 66560) }
         else { LCMA_I4_G(F16, 512, 4, 1, 4, 2, 2, 66560) }

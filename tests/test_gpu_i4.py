@@ -22,7 +22,7 @@ def _lib():
     return binding
 
 
-@pytest.fixture(params=["", "16x16", "16x32", "16x64", "32x32", "64x64"], scope="module")
+@pytest.fixture(params=["", "16x16", "16x32", "16x64", "64x64"], scope="module")
 def kernel(request):
     """The kernel of the rule, and every kernel by name."""
     _lib().lcma_set_tuning("i4_kernel", request.param)
