@@ -24,10 +24,10 @@ bool needs_vectors(int kernel) { return kernel >= kExpFew16; }
 bool walks(int kernel) { return kernel == kExpPingPong; } // 256 work-groups walk through tiles; the other kernels have one for every tile
 bool launches(int kernel, int64_t jobs) { return walks(kernel) ? jobs < kRowLimit - 1024 : (jobs + 8) * 512 < kGridLimit / 2; } // (numbers of tiles are 32-bit on the device)
 int grid_of(int kernel, int64_t jobs) { return walks(kernel) ? 256 : (int)((jobs + 7) / 8 * 8); }
-// What the kernels that load straight into LDS need: 16-bit types, operands in whole 16 bytes (of a k-contiguous one K too, of the other form the rows), and offsets inside
-// a tile (256 rows of a k-contiguous operand, 128 rows along k of the other) below 2^30 bytes.
+// What the kernels that load straight into LDS need: offsets inside a tile (256 rows of a k-contiguous operand, 128 rows along k of the other) below 2^30 bytes, and, 16-bit types,
+// operands in whole 16 bytes (of a k-contiguous one K too, of the other form the rows).
 bool whole_vectors(int es, const void *A, int64_t lda_b, const void *B, int64_t ldb_b, int64_t k_b) {
-    return es == 2 && !(((uintptr_t)A | (uintptr_t)B | (uint64_t)lda_b | (uint64_t)ldb_b | (uint64_t)k_b) & 15) && lda_b <= 1 << 22 && ldb_b <= 1 << 22;
+    return lda_b <= 1 << 22 && ldb_b <= 1 << 22 && (es == 4 || !(((uintptr_t)A | (uintptr_t)B | (uint64_t)lda_b | (uint64_t)ldb_b | (uint64_t)k_b) & 15));
 }
 
 lcma_status check_sizes(const char *who, int64_t rows, int64_t N, int64_t K, int experts, int dtype) {
@@ -79,7 +79,7 @@ extern "C" lcma_status lcma_gemm_experts(int b_layout, int64_t rows, int64_t N, 
     p.panel = 8;
     const bool vectors = K > 0 && whole_vectors(es, A, p.lda_b, B, p.ldb_b, K * es);
     auto tiles_of = [&](int k) { return product_tiles(k, rows, N, experts); };
-    auto fits = [&](int k) { return (vectors || !needs_vectors(k)) && (b_layout || k != kExpFew16) && launches(k, tiles_of(k)); };
+    auto fits = [&](int k) { return (vectors || !needs_vectors(k)) && (k != kExpFew16 || (b_layout && es == 2)) && (k != kExpPingPong || es == 2) && launches(k, tiles_of(k)); };
     int kernel = tuning_experts_kernel();
     if (kernel < 0 || !fits(kernel)) kernel = fits(kExpPingPong) && rows >= 128 * (int64_t)experts ? kExpPingPong : rows < 64 * (int64_t)experts ? kExpStaged64 : kExpStaged128;
     if (!fits(kernel)) kernel = fits(kExpStaged128) ? kExpStaged128 : kExpPingPong;
@@ -121,7 +121,7 @@ extern "C" lcma_status lcma_gemm_experts_grad(int64_t rows, int64_t N, int64_t K
     p.panel = 8;
     const bool vectors = whole_vectors(es, dC, p.lda_b, A, p.ldb_b, 0);
     auto tiles_of = [&](int k) { return gradient_tiles(k, N, K, experts); };
-    auto fits = [&](int k) { return (vectors || !needs_vectors(k)) && k != kExpFew16 && k != kExpFew32 && launches(k, tiles_of(k)); };
+    auto fits = [&](int k) { return (vectors || !needs_vectors(k)) && k != kExpFew16 && k != kExpFew32 && (k != kExpPingPong || es == 2) && launches(k, tiles_of(k)); };
     int kernel = tuning_experts_kernel();
     if (kernel < 0 || !fits(kernel)) kernel = fits(kExpPingPong) && tiles_of(kExpPingPong) >= 128 ? kExpPingPong : tiles_of(kExpStaged128) < 512 ? kExpStaged64 : kExpStaged128;
     if (!fits(kernel)) kernel = fits(kExpStaged128) ? kExpStaged128 : kExpPingPong;

@@ -54,14 +54,16 @@ extern "C" int lcma_launch_experts_gemm(const lcma::ExpertsGemmParams *p, int fo
         else LCMA_EXP_LAUNCH(256, exp_few<F16, false, 16, 4, 2>);
         break;
     case kExpFew32:
-        if (dtype == 1 && form == 0) LCMA_EXP_LAUNCH(256, exp_few<BF16, false, 32, 4, 2>);
+        if (dtype == 0 && form == 0) LCMA_EXP_LAUNCH(256, exp_few<F32, false, 32, 4, 2>);
+        else if (dtype == 0) LCMA_EXP_LAUNCH(256, exp_few<F32, true, 32, 4, 2>);
+        else if (dtype == 1 && form == 0) LCMA_EXP_LAUNCH(256, exp_few<BF16, false, 32, 4, 2>);
         else if (dtype == 1) LCMA_EXP_LAUNCH(256, exp_few<BF16, true, 32, 4, 2>);
         else if (form == 0) LCMA_EXP_LAUNCH(256, exp_few<F16, false, 32, 4, 2>);
         else LCMA_EXP_LAUNCH(256, exp_few<F16, true, 32, 4, 2>);
         break;
-    case kExpRing64: LCMA_EXP(exp_ring, 256, LCMA_COMMA 64, 64, 2, 2, 4)
-    case kExpRing64x128: LCMA_EXP(exp_ring, 256, LCMA_COMMA 64, 128, 2, 2, 3)
-    case kExpRing128: LCMA_EXP(exp_ring, 512, LCMA_COMMA 128, 128, 4, 2, 4)
+    case kExpRing64: LCMA_EXP_ANY(exp_ring, 256, LCMA_COMMA 64, 64, 2, 2, 4)
+    case kExpRing64x128: LCMA_EXP_ANY(exp_ring, 256, LCMA_COMMA 64, 128, 2, 2, 3)
+    case kExpRing128: LCMA_EXP_ANY(exp_ring, 512, LCMA_COMMA 128, 128, 4, 2, 4)
     default: LCMA_EXP(exp_256, 512, )
     }
 #undef LCMA_EXP_LAUNCH

@@ -63,8 +63,8 @@ struct I8GemmParams {
     int32_t nz, panel;      // tiles along N, and the width of a column panel of the tile order
 };
 
-// Kernels of the experts' products: any sizes (csrc/lcma_experts.hpp); whole 16 bytes in 16 bit (csrc/lcma_experts_ring.hpp, lcma_experts_pingpong.hpp).  Tiles of 16 x 16:
-// weights N x K alone; of 16 and 32: no gradient of weights.
+// Kernels of the experts' products: any sizes and alignments (csrc/lcma_experts.hpp); 16 bit in whole 16 bytes and fp32 (csrc/lcma_experts_ring.hpp); 16 bit in whole 16 bytes
+// (csrc/lcma_experts_pingpong.hpp).  Tiles of 16 x 16: 16 bit, weights N x K alone; of 16 and 32: no gradient of weights.
 enum { kExpStaged64 = 0, kExpStaged128, kExpFew16, kExpFew32, kExpRing64, kExpRing64x128, kExpRing128, kExpPingPong, kExpKernels };
 
 // lcma_gemm_experts: rows of A (k-contiguous) in groups, group e times the matrix of expert e (N x K, or K x N).

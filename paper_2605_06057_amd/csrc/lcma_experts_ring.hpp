@@ -1,25 +1,39 @@
-// The experts' products in 16 bit on tiles below 256 x 256, operands in whole 16 bytes straight into LDS (either form of both, csrc/lcma_experts.hpp).
+// The experts' products on tiles below 256 x 256, operands straight into LDS (either form of both, csrc/lcma_experts.hpp): 16-bit types in whole 16 bytes, fp32 at any
+// sizes (a load needs the alignment of four bytes).  What lies past a tile's rows or columns may be anything: it reaches elements of C alone that are not there.  What lies past the
+// last k is zero on both sides: by the extent where k goes from row to row; in k-contiguous rows 16 bytes at a time from past the extent (16 bit), or in
+// the fragments of the last step (fp32).
 #pragma once
 #include "lcma_experts.hpp"
 
 namespace lcma {
 
-// The rows of the stored matrix from k = 64 y on, `steps` steps of them; none past the last k.
+// The rows of the stored matrix from step y on, `steps` steps of them; none past the last k.
 template <class T> LCMA_DEV __amdgpu_buffer_rsrc_t exp_columns_from(const char *at, int wide, int k, uint32_t ld_b, int y, int steps) {
-    const int left = k - y * 64, n = left < steps * 64 ? left : steps * 64;
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(at) + (int64_t)y * 64 * ld_b, 0, n > 0 ? (n - 1) * (int)ld_b + wide * T::ES : 0, 0x00020000);
+    constexpr int KS = 128 / T::ES;
+    const int left = k - y * KS, n = left < steps * KS ? left : steps * KS;
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(at) + (int64_t)y * KS * ld_b, 0, n > 0 ? (n - 1) * (int)ld_b + wide * T::ES : 0, 0x00020000);
 }
 template <class T> LCMA_DEV __amdgpu_buffer_rsrc_t exp_rows_of(const char *at, int wide, int k, uint32_t ld_b) {
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(at), 0, k > 0 ? (wide - 1) * (int)ld_b + k * T::ES : 0, 0x00020000);
 }
+// fp32: zeros in the place of what is past the `left` k of the last step.
+template <int N> LCMA_DEV void exp_end_of_k(u32x4 (&f)[N][4], int left) {
+    const int lh = (threadIdx.x >> 5) & 1;
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+            for (int t = 0; t < 4; ++t) f[n][k][t] = k * 8 + lh * 4 + t < left ? f[n][k][t] : 0;
+}
 
-// One tile of TM x TN per work-group of WGM x WGN waves.  A step is 64 k; S stages of LDS hold the steps in flight, the loads run S - 1 steps ahead and are waited for by
+// One tile of TM x TN per work-group of WGM x WGN waves.  A step is 64 k (fp32: 32); S stages of LDS hold the steps in flight, the loads run S - 1 steps ahead and are waited for by
 // count, and one barrier a step says that all waves' parts of it have landed and that all have read the stage that is loaded anew (csrc/lcma_i8.hpp has the
 // same with its measurements).
 template <class T, bool ACOL, bool BCOL, bool GRAD, int TM, int TN, int WGM, int WGN, int S> struct ExpRing {
-    static constexpr int NT = 64 * WGM * WGN, NMI = TM / WGM / 32, NNI = TN / WGN / 32, KS = 64;
+    static constexpr int NT = 64 * WGM * WGN, NMI = TM / WGM / 32, NNI = TN / WGN / 32, KS = 128 / T::ES;
     static constexpr int A_STAGE = TM * 128, STAGE = (TM + TN) * 128, LDS_BYTES = S * STAGE, QA = TM * 8 / NT, QB = TN * 8 / NT;
-    static_assert(T::ES == 2 && NT / 64 * 4096 <= LDS_BYTES && TM * 8 % NT == 0 && TN * 8 % NT == 0 && LDS_BYTES <= 160 * 1024 && (S == 3 || S == 4) && (S - 1) * (QA + QB) <= 63, "tile and wave grid");
+    static_assert(NT / 64 * 4096 <= LDS_BYTES && TM * 8 % NT == 0 && TN * 8 % NT == 0 && LDS_BYTES <= 160 * 1024 && (S == 3 || S == 4) && (S - 1) * (QA + QB) <= 63, "tile and wave grid");
     using Frag = typename Mma<T>::frag;
     static constexpr uint32_t NONE = 1u << 30; // an offset past any extent
 
@@ -53,13 +67,14 @@ template <class T, bool ACOL, bool BCOL, bool GRAD, int TM, int TN, int WGM, int
     // front of every read)
     static LCMA_DEV void multiply(const ExpertsGemmParams &p, const ExpJob &j, int w, int wm, int wn, f32x16 (&acc)[NMI][NNI], LCMA_LDS char *__restrict__ s0,
                                   LCMA_LDS char *__restrict__ s1, LCMA_LDS char *__restrict__ s2, LCMA_LDS char *__restrict__ s3) {
-        constexpr int CA = TM * 2 / 16, CB = TN * 2 / 16; // 16-byte chunks of a row of the other form
+        constexpr int CA = TM * T::ES / 16, CB = TN * T::ES / 16; // 16-byte chunks of a row of the other form
         const int tid = threadIdx.x, steps = (int)(((uint32_t)j.k + (KS - 1)) / KS), chunk = exp_row_chunk(tid >> 3, tid & 7) * 16;
         const uint32_t lda = (uint32_t)p.lda_b, ldb = (uint32_t)p.ldb_b;
         const auto rows_a = exp_rows_of<T>(j.a, j.am, j.k, lda), rows_b = exp_rows_of<T>(j.b, j.bn, j.k, ldb);
         const uint32_t a_voff = ACOL ? tid / CA * lda + exp_col_chunk<T, TM>(tid / CA, tid % CA) * 16 : (uint32_t)(tid >> 3) * lda + chunk;
         const uint32_t b_voff = BCOL ? tid / CB * ldb + exp_col_chunk<T, TN>(tid / CB, tid % CB) * 16 : (uint32_t)(tid >> 3) * ldb + chunk;
-        const bool past = chunk >= ((j.k - 1) % KS + 1) * 2; // (of the last step, k-contiguous)
+        const int in_last = (j.k - 1) % KS + 1;
+        const bool past = T::ES == 2 && chunk >= in_last * 2; // (of the last step, k-contiguous)
         const uint32_t a_last = !ACOL && past ? NONE : a_voff, b_last = !BCOL && past ? NONE : b_voff;
         const uint32_t a_down = NT / (ACOL ? CA : 8) * lda, b_down = NT / (BCOL ? CB : 8) * ldb;
         auto load = [&](LCMA_LDS char *st, int y) { // a step past the end: zeros, from past the extents
@@ -83,6 +98,10 @@ template <class T, bool ACOL, bool BCOL, bool GRAD, int TM, int TN, int WGM, int
             for (int n = 0; n < NNI; ++n) exp_fragments<T, BCOL, TN>(st + A_STAGE, wn * NNI + n, b[n]);
 #pragma unroll
             for (int i = 0; i < NMI; ++i) exp_fragments<T, ACOL, TM>(st, wm * NMI + i, a[i]);
+            if (T::ES == 4 && y == steps - 1) {
+                if constexpr (!ACOL) exp_end_of_k(a, in_last);
+                if constexpr (!BCOL) exp_end_of_k(b, in_last);
+            }
 #pragma unroll
             for (int k = 0; k < 4; ++k)
 #pragma unroll
@@ -111,13 +130,13 @@ template <class T, bool ACOL, bool BCOL, bool GRAD, int TM, int TN, int WGM, int
     }
 };
 
-// Few rows: a work-group owns a tile of R x R of C and its waves split K between them, a step (64 k, 128 bytes of every row) to a wave in turn; nothing is shared between
+// Few rows: a work-group owns a tile of R x R of C and its waves split K between them, a step (64 k, fp32: 32, 128 bytes of every row) to a wave in turn; nothing is shared between
 // waves, so there is no barrier in the loop, and the waves' sums are added at the end, in fp32 and in ascending order (csrc/lcma_few_rows.hpp has the same for one product,
 // with the reasons and measurements).  S steps of a wave in flight.
 template <class T, bool BCOL, int R, int WK, int S> struct ExpFewRows {
-    static constexpr int F = R == 16 ? 16 : 32, NF = R / F, KF = 64 / (512 / F); // 16x16x32 or 32x32x16 instructions; fragments of a step along K
+    static constexpr int F = R == 16 ? 16 : 32, NF = R / F, KF = 64 / (512 / F), KS = 128 / T::ES; // 16x16x32 or 32x32x16 instructions; fragments of a step along K
     static constexpr int LOADS = R / 8, HALF = R * 128, STAGE = 2 * HALF, PITCH = R + 4, SUMS = WK * R * PITCH * 4, STAGES = WK * S * STAGE, LDS_BYTES = SUMS > STAGES ? SUMS : STAGES;
-    static_assert(T::ES == 2 && (R >= 32 || !BCOL) && LDS_BYTES <= 160 * 1024 && (S == 2 || S == 4) && 2 * LOADS * S <= 63, "LDS budget of one CU; counter of loads");
+    static_assert((R >= 32 || (!BCOL && T::ES == 2)) && LDS_BYTES <= 160 * 1024 && (S == 2 || S == 4) && 2 * LOADS * S <= 63, "LDS budget of one CU; counter of loads");
     using Frag = typename Mma<T>::frag;
     using Acc = std::conditional_t<F == 16, f32x4, f32x16>;
     static constexpr uint32_t NONE = 1u << 30;
@@ -164,8 +183,8 @@ template <class T, bool BCOL, int R, int WK, int S> struct ExpFewRows {
     // Steps `y`, y + WK, ...
     static LCMA_DEV void steps_of_wave(const ExpertsGemmParams &p, const ExpJob &j, int y, Acc (&acc)[NF][NF], LCMA_LDS char *__restrict__ s0, LCMA_LDS char *__restrict__ s1,
                                        LCMA_LDS char *__restrict__ s2, LCMA_LDS char *__restrict__ s3) {
-        constexpr int CPR = R * 2 / 16, RPL = 64 / CPR; // the other form: 16-byte chunks of a row, rows of a load
-        const int lane = threadIdx.x & 63, fr = lane & (F - 1), fk = lane / F, steps = (int)(((uint32_t)j.k + 63) / 64);
+        constexpr int CPR = R * T::ES / 16, RPL = 64 / CPR; // the other form: 16-byte chunks of a row, rows of a load
+        const int lane = threadIdx.x & 63, fr = lane & (F - 1), fk = lane / F, steps = (int)(((uint32_t)j.k + (KS - 1)) / KS), in_last = (j.k - 1) % KS + 1;
         const uint32_t lda = (uint32_t)p.lda_b, ldb = (uint32_t)p.ldb_b;
         const auto ra = exp_rows_of<T>(j.a, j.am, j.k, lda), rows_b = exp_rows_of<T>(j.b, j.bn, j.k, ldb);
         // a load brings 8 rows of 128 bytes, lanes 8 i to 8 i + 7 one row; `last`: what is past K from past the extents
@@ -173,7 +192,7 @@ template <class T, bool BCOL, int R, int WK, int S> struct ExpFewRows {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const uint32_t c = ((lane & 7) ^ (lane >> 4) ^ (4 * i)) * 16;
-            const bool past = c >= (uint32_t)((j.k - 1) % 64 + 1) * 2;
+            const bool past = T::ES == 2 && c >= (uint32_t)in_last * 2;
             av[i] = (uint32_t)(lane >> 3) * lda + c;
             al[i] = past ? NONE : av[i];
             bv[i] = BCOL ? (uint32_t)(lane / CPR) * ldb + exp_col_chunk<T, R>(lane / CPR, lane % CPR) * 16 : (uint32_t)(lane >> 3) * ldb + c;
@@ -198,7 +217,7 @@ template <class T, bool BCOL, int R, int WK, int S> struct ExpFewRows {
             wait_loads<2 * LOADS *(S - 1)>();
 #pragma unroll
             for (int i = 0; i < NF; ++i) {
-                if constexpr (BCOL) exp_columns<T, R>(st + HALF, i, b[i]);
+                if constexpr (BCOL) exp_fragments<T, true, R>(st + HALF, i, b[i]);
 #pragma unroll
                 for (int k = 0; k < KF; ++k) {
                     a[i][k] = *(const LCMA_LDS u32x4 *)(st + frag[k] + i * F * 128);
@@ -211,6 +230,11 @@ template <class T, bool BCOL, int R, int WK, int S> struct ExpFewRows {
             __builtin_amdgcn_sched_barrier(0);
             load(st, y + S * WK);
             __builtin_amdgcn_sched_barrier(0);
+            if constexpr (T::ES == 4)
+                if (y == steps - 1) {
+                    exp_end_of_k(a, in_last);
+                    if constexpr (!BCOL) exp_end_of_k(b, in_last);
+                }
 #pragma unroll
             for (int k = 0; k < KF; ++k)
 #pragma unroll
