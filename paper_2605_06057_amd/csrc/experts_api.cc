@@ -10,7 +10,7 @@ using namespace lcma;
 
 namespace {
 
-const int kTile[kExpKernels][2] = {{64, 64}, {128, 128}, {16, 16}, {32, 32}, {64, 64}, {64, 128}, {128, 128}, {256, 256}}; // rows and columns of the kernels' tiles
+const int kTile[kExpKernels][2] = {{64, 64}, {128, 128}, {16, 16}, {32, 32}, {64, 64}, {64, 128}, {128, 128}, {128, 256}, {256, 256}}; // rows and columns of the kernels' tiles
 
 int64_t span(int64_t rows, int64_t ld, int64_t cols, int es) { return rows > 0 && cols > 0 ? ((rows - 1) * ld + cols) * es : 0; }
 int64_t tiles(int64_t n, int64_t of) { return (n + of - 1) / of; }
@@ -21,7 +21,7 @@ int64_t product_tiles(int kernel, int64_t rows, int64_t N, int experts) {
 }
 int64_t gradient_tiles(int kernel, int64_t M, int64_t N, int experts) { return experts * tiles(M, kTile[kernel][0]) * tiles(N, kTile[kernel][1]); }
 bool needs_vectors(int kernel) { return kernel >= kExpFew16; }
-bool walks(int kernel) { return kernel == kExpPingPong; } // 256 work-groups walk through tiles; the other kernels have one for every tile
+bool walks(int kernel) { return kernel >= kExpNarrow; } // 256 work-groups walk through tiles; the other kernels have one for every tile
 bool launches(int kernel, int64_t jobs) { return walks(kernel) ? jobs < kRowLimit - 1024 : (jobs + 8) * 512 < kGridLimit / 2; } // (numbers of tiles are 32-bit on the device)
 int grid_of(int kernel, int64_t jobs) { return walks(kernel) ? 256 : (int)((jobs + 7) / 8 * 8); }
 // What the kernels that load straight into LDS need: offsets inside a tile (256 rows of a k-contiguous operand, 128 rows along k of the other) below 2^30 bytes, and, 16-bit types,
@@ -79,7 +79,7 @@ extern "C" lcma_status lcma_gemm_experts(int b_layout, int64_t rows, int64_t N, 
     p.panel = 8;
     const bool vectors = K > 0 && whole_vectors(es, A, p.lda_b, B, p.ldb_b, K * es);
     auto tiles_of = [&](int k) { return product_tiles(k, rows, N, experts); };
-    auto fits = [&](int k) { return (vectors || !needs_vectors(k)) && (k != kExpFew16 || (b_layout && es == 2)) && (k != kExpPingPong || es == 2) && launches(k, tiles_of(k)); };
+    auto fits = [&](int k) { return (vectors || !needs_vectors(k)) && (k != kExpFew16 || (b_layout && es == 2)) && (k < kExpNarrow || es == 2) && launches(k, tiles_of(k)); };
     int kernel = tuning_experts_kernel();
     if (kernel < 0 || !fits(kernel)) kernel = fits(kExpPingPong) && rows >= 128 * (int64_t)experts ? kExpPingPong : rows < 64 * (int64_t)experts ? kExpStaged64 : kExpStaged128;
     if (!fits(kernel)) kernel = fits(kExpStaged128) ? kExpStaged128 : kExpPingPong;
@@ -121,7 +121,7 @@ extern "C" lcma_status lcma_gemm_experts_grad(int64_t rows, int64_t N, int64_t K
     p.panel = 8;
     const bool vectors = whole_vectors(es, dC, p.lda_b, A, p.ldb_b, 0);
     auto tiles_of = [&](int k) { return gradient_tiles(k, N, K, experts); };
-    auto fits = [&](int k) { return (vectors || !needs_vectors(k)) && k != kExpFew16 && k != kExpFew32 && (k != kExpPingPong || es == 2) && launches(k, tiles_of(k)); };
+    auto fits = [&](int k) { return (vectors || !needs_vectors(k)) && k != kExpFew16 && k != kExpFew32 && (k < kExpNarrow || es == 2) && launches(k, tiles_of(k)); };
     int kernel = tuning_experts_kernel();
     if (kernel < 0 || !fits(kernel)) kernel = fits(kExpPingPong) && tiles_of(kExpPingPong) >= 128 ? kExpPingPong : tiles_of(kExpStaged128) < 512 ? kExpStaged64 : kExpStaged128;
     if (!fits(kernel)) kernel = fits(kExpStaged128) ? kExpStaged128 : kExpPingPong;

@@ -94,14 +94,14 @@ template <class T, bool COL, int R> LCMA_DEV void exp_fragments(const LCMA_LDS c
     }
 }
 
-// A wave's part of a tile of C (NMI x NNI blocks of 32 x 32; rows, cols: of C from its first element on) rounded and stored: through 4 KB of LDS that are the wave's own,
-// so that it leaves as whole lines, 16 bytes a lane.  The right operand is the left one of the matrix instruction: a lane holds four neighbouring columns.
+// A wave's part of a tile of C (NMI x NNI blocks of 32 x 32; rows, cols: of C from its first element on) rounded and stored: through SR rows of 128 bytes of LDS that are the
+// wave's own, so that it leaves as whole lines, 16 bytes a lane.  The right operand is the left one of the matrix instruction: a lane holds four neighbouring columns.
 // Blocks of rows follow each other, or, TWO, the second pair of them is 128 rows on; the blocks of columns are GAP columns apart.
 // FULL: all of it lies inside C.
-template <class T, int NMI, int NNI, bool TWO, int GAP, bool FULL>
+template <class T, int NMI, int NNI, bool TWO, int GAP, int SR, bool FULL>
 LCMA_DEV void exp_store_rows(LCMA_LDS char *strip, char *c, int64_t ldc_b, int rows, int cols, const f32x16 (&acc)[NMI][NNI]) {
     constexpr int ES = T::ES, BLOCKS = ES == 4 ? 1 : NNI == 1 ? 1 : 2, L = BLOCKS * 32 * ES / 16, RPS = 64 / L; // 32-column blocks of a pass; lanes of a row, rows of a store
-    static_assert(NNI % BLOCKS == 0, "whole passes");
+    static_assert(NNI % BLOCKS == 0 && SR % RPS == 0, "whole passes");
     // (the lane number anew, hidden: what derives from it would otherwise be kept in registers through the steps)
     int lane = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));
     asm volatile("" : "+v"(lane));
@@ -115,36 +115,41 @@ LCMA_DEV void exp_store_rows(LCMA_LDS char *strip, char *c, int64_t ldc_b, int r
 #pragma unroll
         for (int n0 = 0; n0 < NNI; n0 += BLOCKS) {
 #pragma unroll
-            for (int b = 0; b < BLOCKS; ++b)
+            for (int h = 0; h < 32 / SR; ++h) {
+                if (SR == 32 || l32 / SR == h) {
 #pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    const f32x16 &v = acc[mi][n0 + b];
-                    const int byte = (b * 32 + g * 8 + lh * 4) * ES;
-                    LCMA_LDS char *to = strip + l32 * (L * 16) + ((byte >> 4) ^ (l32 & (L - 1))) * 16 + (byte & 15);
-                    if constexpr (ES == 2) {
-                        const uint32_t lo = Round<T>::run(v[g * 4]) | (Round<T>::run(v[g * 4 + 1]) << 16), hi = Round<T>::run(v[g * 4 + 2]) | (Round<T>::run(v[g * 4 + 3]) << 16);
-                        *(LCMA_LDS uint64_t *)to = (uint64_t)hi << 32 | lo;
-                    } else {
-                        *(LCMA_LDS f32x4 *)to = f32x4{v[g * 4], v[g * 4 + 1], v[g * 4 + 2], v[g * 4 + 3]};
-                    }
+                    for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+                        for (int g = 0; g < 4; ++g) {
+                            const f32x16 &v = acc[mi][n0 + b];
+                            const int byte = (b * 32 + g * 8 + lh * 4) * ES;
+                            LCMA_LDS char *to = strip + l32 % SR * (L * 16) + ((byte >> 4) ^ (l32 & (L - 1))) * 16 + (byte & 15);
+                            if constexpr (ES == 2) {
+                                const uint32_t lo = Round<T>::run(v[g * 4]) | (Round<T>::run(v[g * 4 + 1]) << 16), hi = Round<T>::run(v[g * 4 + 2]) | (Round<T>::run(v[g * 4 + 3]) << 16);
+                                *(LCMA_LDS uint64_t *)to = (uint64_t)hi << 32 | lo;
+                            } else {
+                                *(LCMA_LDS f32x4 *)to = f32x4{v[g * 4], v[g * 4 + 1], v[g * 4 + 2], v[g * 4 + 3]};
+                            }
+                        }
                 }
-            lanes_meet();
+                lanes_meet();
 #pragma unroll
-            for (int it = 0; it < 32 / RPS; ++it) {
-                const int row = it * RPS + row_of, of = ch * (16 / ES), col = (n0 + of / 32) * GAP + of % 32;
-                const u32x4 v = *(const LCMA_LDS u32x4 *)(strip + row * (L * 16) + (ch ^ (row & (L - 1))) * 16);
-                char *to = at + (int64_t)(row0 + it * RPS) * ldc_b + col * ES;
-                if constexpr (FULL) __builtin_memcpy(to, &v, 16);
-                else if (row0 + row < rows && col < cols) i8_store16<T>(to, v, cols - col);
+                for (int it = 0; it < SR / RPS; ++it) {
+                    const int in = it * RPS + row_of, row = h * SR + in, of = ch * (16 / ES), col = (n0 + of / 32) * GAP + of % 32;
+                    const u32x4 v = *(const LCMA_LDS u32x4 *)(strip + in * (L * 16) + (ch ^ (row & (L - 1))) * 16);
+                    char *to = at + (int64_t)(row0 + h * SR + it * RPS) * ldc_b + col * ES;
+                    if constexpr (FULL) __builtin_memcpy(to, &v, 16);
+                    else if (row0 + row < rows && col < cols) i8_store16<T>(to, v, cols - col);
+                }
+                lanes_meet();
             }
-            lanes_meet();
         }
     }
 }
-template <class T, int NMI, int NNI, bool TWO = false, int GAP = 32>
+template <class T, int NMI, int NNI, bool TWO = false, int GAP = 32, int SR = 32>
 LCMA_DEV void exp_store(LCMA_LDS char *strip, char *c, int64_t ldc_b, int rows, int cols, const f32x16 (&acc)[NMI][NNI]) {
-    if (rows >= (TWO ? (NMI - 1) / 2 * 128 + (NMI - 1) % 2 * 32 : (NMI - 1) * 32) + 32 && cols >= (NNI - 1) * GAP + 32) exp_store_rows<T, NMI, NNI, TWO, GAP, true>(strip, c, ldc_b, rows, cols, acc);
-    else exp_store_rows<T, NMI, NNI, TWO, GAP, false>(strip, c, ldc_b, rows, cols, acc);
+    if (rows >= (TWO ? (NMI - 1) / 2 * 128 + (NMI - 1) % 2 * 32 : (NMI - 1) * 32) + 32 && cols >= (NNI - 1) * GAP + 32) exp_store_rows<T, NMI, NNI, TWO, GAP, SR, true>(strip, c, ldc_b, rows, cols, acc);
+    else exp_store_rows<T, NMI, NNI, TWO, GAP, SR, false>(strip, c, ldc_b, rows, cols, acc);
 }
 
 // Rows of C behind the last expert's are zero: the work-groups of the launch share them.

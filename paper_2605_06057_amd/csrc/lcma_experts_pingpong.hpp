@@ -61,11 +61,7 @@ template <class T, bool ACOL, bool BCOL, bool GRAD> struct ExpPingPong {
         char *c;
         int am, bn, k;
     };
-    template <class P> static LCMA_DEV P *uniform(P *at) {
-        const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)at), hi = __builtin_amdgcn_readfirstlane((uint32_t)((uintptr_t)at >> 32));
-        return (P *)((uint64_t)hi << 32 | lo);
-    }
-    static LCMA_DEV Source source(Args args, int nx, int jobs, int job) {
+    template <int TM, int TN> static LCMA_DEV Source source(Args args, int nx, int jobs, int job) {
         ExpJob j = {nullptr, nullptr, nullptr, 0, 0, 0};
         if (job < jobs) {
             const ExpertsGemmParams p = arguments(args);
@@ -78,7 +74,7 @@ template <class T, bool ACOL, bool BCOL, bool GRAD> struct ExpPingPong {
             }
         }
         // (uniform anyway; said here so that the descriptors stay in scalar registers)
-        return {uniform(j.a), uniform(j.b), uniform(j.c), __builtin_amdgcn_readfirstlane(j.am), __builtin_amdgcn_readfirstlane(j.bn), __builtin_amdgcn_readfirstlane(j.k)};
+        return {exp_uniform(j.a), exp_uniform(j.b), exp_uniform(j.c), __builtin_amdgcn_readfirstlane(j.am), __builtin_amdgcn_readfirstlane(j.bn), __builtin_amdgcn_readfirstlane(j.k)};
     }
     // The operand from step y on, for two steps: k-contiguous rows with their steps as offsets, or the rows of the stored matrix from k = 64 y on.
     template <bool COL> static LCMA_DEV __amdgpu_buffer_rsrc_t operand(const char *at, int wide, int k, uint32_t ld_b, int y) {
@@ -124,7 +120,7 @@ template <class T, bool ACOL, bool BCOL, bool GRAD> struct ExpPingPong {
         const uint32_t a_step = ACOL ? KS * lda : ROW, b_step = BCOL ? KS * ldb : ROW;
         // k-contiguous: the 16 bytes past the last k in the last step, read from past the extent
         auto last_voff = [&](bool col, uint32_t voff, int k) { return !col && (uint32_t)pos * 8 >= (uint32_t)((k - 1) % KS + 1) ? NONE : voff; };
-        Source cur = source(args, nx, jobs, job), nxt;
+        Source cur = source<TM, TN>(args, nx, jobs, job), nxt;
         u32x4 fa0[2][NK], fa1[2][NK], fb0[NK], fb1[NK];
         f32x16 acc[NMI][NNI];
         auto read_a = [&](const LCMA_LDS char *half, u32x4 (&f)[2][NK]) {
@@ -154,7 +150,7 @@ template <class T, bool ACOL, bool BCOL, bool GRAD> struct ExpPingPong {
         while (true) {
             int next = job + units;
             if (next >= whole && job < whole && whole < jobs) next = whole + (int)blockIdx.x;
-            nxt = source(args, nx, jobs, next);
+            nxt = source<TM, TN>(args, nx, jobs, next);
             const int ny = steps_of(cur.k), n2 = (ny + 1) & ~1, ny_next = steps_of(nxt.k);
 #pragma unroll
             for (int mi = 0; mi < NMI; ++mi)

@@ -7,6 +7,12 @@
 
 namespace lcma {
 
+// A pointer that is the same in all lanes, in scalar registers.  (Global memory, said so: the compiler takes a pointer made of two numbers for one into any memory, and stores through it
+// count as LDS accesses too.)
+template <class P> LCMA_DEV P *exp_uniform(P *at) {
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)at), hi = __builtin_amdgcn_readfirstlane((uint32_t)((uintptr_t)at >> 32));
+    return (P *)(__attribute__((address_space(1))) P *)((uint64_t)hi << 32 | lo);
+}
 // The rows of the stored matrix from step y on, `steps` steps of them; none past the last k.
 template <class T> LCMA_DEV __amdgpu_buffer_rsrc_t exp_columns_from(const char *at, int wide, int k, uint32_t ld_b, int y, int steps) {
     constexpr int KS = 128 / T::ES;
