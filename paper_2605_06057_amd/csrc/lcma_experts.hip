@@ -22,8 +22,8 @@ template <class T, bool BCOL, int R, int WK, int S> __global__ __launch_bounds__
     __shared__ __attribute__((aligned(16))) char smem[G::LDS_BYTES];
     G::run(p, (LCMA_LDS char *)smem);
 }
-template <class T, bool ACOL, bool BCOL, bool GRAD> __global__ __launch_bounds__(512, 2) void exp_narrow(const ExpertsGemmParams) {
-    using G = ExpNarrow<T, ACOL, BCOL, GRAD>;
+template <class T, bool BCOL> __global__ __launch_bounds__(512, 2) void exp_narrow(const ExpertsGemmParams) {
+    using G = ExpNarrow<T, BCOL>;
     __shared__ __attribute__((aligned(16))) char smem[G::LDS_BYTES];
     G::run((LCMA_LDS char *)smem);
 }
@@ -68,9 +68,13 @@ extern "C" int lcma_launch_experts_gemm(const lcma::ExpertsGemmParams *p, int fo
         else LCMA_EXP_LAUNCH(256, exp_few<F16, true, 32, 4, 2>);
         break;
     case kExpRing64: LCMA_EXP_ANY(exp_ring, 256, LCMA_COMMA 64, 64, 2, 2, 3)
-    case kExpRing64x128: LCMA_EXP_ANY(exp_ring, 256, LCMA_COMMA 64, 128, 2, 2, 3)
-    case kExpRing128: LCMA_EXP_ANY(exp_ring, 512, LCMA_COMMA 128, 128, 4, 2, 4)
-    case kExpNarrow: LCMA_EXP(exp_narrow, 512, )
+    case kExpRing64x128: LCMA_EXP(exp_ring, 256, LCMA_COMMA 64, 128, 2, 2, 3)
+    case kExpNarrow:
+        if (dtype == 1 && form == 0) LCMA_EXP_LAUNCH(512, exp_narrow<BF16, false>);
+        else if (dtype == 1) LCMA_EXP_LAUNCH(512, exp_narrow<BF16, true>);
+        else if (form == 0) LCMA_EXP_LAUNCH(512, exp_narrow<F16, false>);
+        else LCMA_EXP_LAUNCH(512, exp_narrow<F16, true>);
+        break;
     default: LCMA_EXP(exp_256, 512, )
     }
 #undef LCMA_EXP_LAUNCH

@@ -2,14 +2,14 @@
 // 256 x 256 tile has, and where there are too few of those to fill the chip or to end its last round.  Wave tiles of 64 x 64, the two groups below each other; a step of 64 k is two
 // phases (the upper and the lower 32 rows of the wave tile) of eight matrix instructions.  Loads go two whole steps ahead into one of three stages (144 KB), and the wait
 // for them is the count of one step's.  Work-groups walk through tiles and the loads run on into the next one; so that every tile starts in the first stage its steps are rounded up to
-// threes by steps that load zeros and multiply nothing.  Operands whose columns are contiguous lie in LDS in halves of 128 columns.
+// threes by steps that load zeros and multiply nothing.  K x N weights lie in LDS in halves of 128 columns.
 #pragma once
 #include "lcma_experts_pingpong.hpp"
 
 namespace lcma {
 
-template <class T, bool ACOL, bool BCOL, bool GRAD> struct ExpNarrow {
-    using Turns = ExpPingPong<T, ACOL, BCOL, GRAD>;
+template <class T, bool BCOL> struct ExpNarrow {
+    using Turns = ExpPingPong<T, false, BCOL, false>;
     using Args = typename Turns::Args;
     using Frag = typename Mma<T>::frag;
     static constexpr int NT = 512, TM = 128, TN = 256, NK = 4, KS = 64, HALF = 128 * 128, STAGE = 3 * HALF, STRIP = 16 * 128, LDS_BYTES = 3 * STAGE + 8 * STRIP;
@@ -37,15 +37,10 @@ template <class T, bool ACOL, bool BCOL, bool GRAD> struct ExpNarrow {
         int nx, jobs;
         {
             const ExpertsGemmParams p = Turns::arguments(args);
-            if constexpr (GRAD) {
-                nx = p.nx;
-                jobs = p.experts * p.nx * p.nz;
-            } else {
-                const I8Rows<TM, ExpertsGemmParams> groups(p);
-                exp_zero_behind<T, NT>(p, groups.behind);
-                nx = groups.tiles;
-                jobs = nx * p.nz;
-            }
+            const I8Rows<TM, ExpertsGemmParams> groups(p);
+            exp_zero_behind<T, NT>(p, groups.behind);
+            nx = groups.tiles;
+            jobs = nx * p.nz;
         }
         const int units = gridDim.x, per = units >> 3; // rounds of one tile per work-group, as in ExpPingPong
         const int unit = (int)blockIdx.x < (per << 3) ? (int)(blockIdx.x & 7) * per + (int)(blockIdx.x >> 3) : (int)blockIdx.x;
@@ -53,9 +48,9 @@ template <class T, bool ACOL, bool BCOL, bool GRAD> struct ExpNarrow {
         int job = unit < whole ? unit : (int)blockIdx.x;
         if (job >= jobs) return;
         const uint32_t lda = (uint32_t)args->lda_b, ldb = (uint32_t)args->ldb_b;
-        // load q of a thread fills row q * 64 + tid / 8 of an operand, position tid % 8; of the other form row (k) q % 2 * 32 + tid / 16 of half q / 2, position tid % 16
+        // load q of a thread fills row q * 64 + tid / 8 of an operand, position tid % 8; where B's columns are contiguous row (k) q % 2 * 32 + tid / 16 of half q / 2, position tid % 16
         const int row = tid >> 3, pos = exp_row_chunk(row, tid & 7), k16 = tid >> 4, pos16 = exp_col_chunk<T, 128>(k16, tid & 15);
-        const uint32_t a_voff = ACOL ? k16 * lda + pos16 * 16 : row * lda + pos * 16, b_voff = BCOL ? k16 * ldb + pos16 * 16 : row * ldb + pos * 16;
+        const uint32_t a_voff = row * lda + pos * 16, b_voff = BCOL ? k16 * ldb + pos16 * 16 : row * ldb + pos * 16;
         using Source = typename Turns::Source;
         auto source = [&](int job) { return Turns::template source<TM, TN>(args, nx, jobs, job); };
         Source cur = source(job), nxt;
@@ -65,13 +60,13 @@ template <class T, bool ACOL, bool BCOL, bool GRAD> struct ExpNarrow {
             const int ny = steps_of(s.k);
             const uint32_t off = y < ny ? (uint32_t)y * 128 : NONE;
             const bool past = y == ny - 1 && (uint32_t)pos * 8 >= (uint32_t)((s.k - 1) % KS + 1); // 16 bytes past the last k
-            const uint32_t av = !ACOL && past ? NONE : a_voff, bv = !BCOL && past ? NONE : b_voff;
-            const auto ra = ACOL ? exp_columns_from<T>(s.a, s.am, s.k, lda, y, 1) : exp_rows_of<T>(s.a, s.am, s.k, lda);
+            const uint32_t av = past ? NONE : a_voff, bv = !BCOL && past ? NONE : b_voff;
+            const auto ra = exp_rows_of<T>(s.a, s.am, s.k, lda);
             const auto rb = BCOL ? exp_columns_from<T>(s.b, s.bn, s.k, ldb, y, 1) : exp_rows_of<T>(s.b, s.bn, s.k, ldb);
 #pragma unroll
             for (int q = from; q < to; ++q) {
                 const int i = q - 2; // of B
-                if (q < 2) __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (LCMA_LDS void *)(st + (q * NT + w * 64) * 16), 16, (int)av, (int)(ACOL ? q * 32 * lda : off + q * 64 * lda), 0, 0);
+                if (q < 2) __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (LCMA_LDS void *)(st + (q * NT + w * 64) * 16), 16, (int)av, (int)(off + q * 64 * lda), 0, 0);
                 else __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (LCMA_LDS void *)(st + (q * NT + w * 64) * 16), 16, (int)bv, (int)(BCOL ? i % 2 * 32 * ldb + i / 2 * 256 : off + i * 64 * ldb), 0, 0);
             }
         };
@@ -86,7 +81,7 @@ template <class T, bool ACOL, bool BCOL, bool GRAD> struct ExpNarrow {
         if (wm) Turns::slot_end(); // the second group runs one slot behind the first
         f32x16 acc[2][2];
         u32x4 a[NK], b[2][NK];
-        auto read_a = [&](const LCMA_LDS char *st, int i) { exp_fragments<T, ACOL, 128>(st, wm * 2 + i, a); };
+        auto read_a = [&](const LCMA_LDS char *st, int i) { exp_fragments<T, false, 128>(st, wm * 2 + i, a); };
         auto read_b = [&](const LCMA_LDS char *st, int i) { // (columns: two waves to a half)
             if constexpr (BCOL) exp_fragments<T, true, 128>(st + HALF + (wn >> 1) * HALF, (wn & 1) * 2 + i, b[i]);
             else exp_fragments<T, false, 256>(st + HALF, wn * 2 + i, b[i]);
@@ -94,30 +89,25 @@ template <class T, bool ACOL, bool BCOL, bool GRAD> struct ExpNarrow {
         // one step out of stage st; `of`, y2: the step two on, which goes into the stage that the step before has read.  (Reads that wait for their results: behind the loads.)
         auto step = [&](bool real, LCMA_LDS char *st, LCMA_LDS char *into, const Source &of, int y2) {
             if (real) {
-                if constexpr (!ACOL) read_a(st, 0);
+                read_a(st, 0);
                 if constexpr (!BCOL) {
                     read_b(st, 0);
                     read_b(st, 1);
                 }
             }
             load(c0, c3, of, into, y2);
-            if (real) {
-                if constexpr (ACOL) read_a(st, 0);
-                if constexpr (BCOL) {
+            if constexpr (BCOL)
+                if (real) {
                     read_b(st, 0);
                     read_b(st, 1);
                 }
-            }
             __builtin_amdgcn_sched_barrier(0);
             __builtin_amdgcn_s_waitcnt(0xC07F); // lgkmcnt(0)
             Turns::slot_end();
             if (real) multiply(a, b, acc[0]);
             Turns::slot_end();
-            if constexpr (!ACOL)
-                if (real) read_a(st, 1);
+            if (real) read_a(st, 1);
             load(c3, c6, of, into, y2);
-            if constexpr (ACOL)
-                if (real) read_a(st, 1);
             __builtin_amdgcn_sched_barrier(0);
             __builtin_amdgcn_s_waitcnt(0x0076); // vmcnt(6) lgkmcnt(0): the next step has landed
             Turns::slot_end();
