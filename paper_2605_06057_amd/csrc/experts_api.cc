@@ -209,6 +209,7 @@ lcma_status gated(const char *who, int64_t rows, int64_t F, const void *dY, int6
     p.ldy_b = ldy * es;
     p.rows = (int32_t)rows;
     p.F = (int32_t)F;
+    p.stream = rows * width * es >= (int64_t)64 << 20; // (a quarter of the Infinity Cache written)
     const int64_t vectors = (F + 7) / 8;
     while (p.lane_shift < 8 && ((int64_t)1 << p.lane_shift) < vectors) ++p.lane_shift;
     const int64_t per = 256 >> p.lane_shift, gx = (rows + per - 1) / per, gy = tiles(vectors, (int64_t)1 << p.lane_shift);

@@ -87,6 +87,7 @@ struct GatedParams {
     int64_t ldx_b, lddy_b, ldy_b;
     int32_t rows, F;
     int32_t lane_shift; // 2^lane_shift neighbouring threads along a row
+    int32_t stream;     // the rows pass the caches by
 };
 
 // 4-bit weights (csrc/lcma_i4.hpp): blocks of 16 rows x 128 columns, a row of blocks behind the other; a block is its codes (1024 bytes) and the scales
