@@ -404,8 +404,8 @@ double lcma_predict_seconds(int scheme_id, int64_t M, int64_t N, int64_t K, lcma
  *                                                   32x32, 64x64, 64x128, 128x128, 128x256 or 256x256 (another value, or more tiles than its
  *                                                   launch holds: default).  Their
  *                                                   sums are exact, so this changes no result.
- *   "experts_kernel"   LCMA_EXPERTS_KERNEL=<name>   lcma_gemm_experts and lcma_gemm_experts_grad run the kernel with that name: any64x64 and any128x128 (any sizes and
- *                                                   alignments), 32x32 and 64x64 (16 bit in whole 16 bytes, fp32), 16x16, 64x128, 128x256 and 256x256 (16 bit in whole
+ *   "experts_kernel"   LCMA_EXPERTS_KERNEL=<name>   lcma_gemm_experts and lcma_gemm_experts_grad run the kernel with that name: any64x64, any128x128 and (16 bit, not
+ *                                                   for the gradient) any32x32 (any sizes and alignments), 32x32 and 64x64 (16 bit in whole 16 bytes, fp32), 16x16, 64x128, 128x256 and 256x256 (16 bit in whole
  *                                                   16 bytes); where it does not fit, and for another value: default.  It groups fp32 sums differently.
  *   "i4_kernel"        LCMA_I4_KERNEL=<rows>x<cols> lcma_i4_gemm_nt and lcma_i4_gemm_experts run the kernel with tiles of that size: 16x16, 16x32, 16x64 or (16 bit) 64x64.  It
  *                                                   groups fp32 sums differently.

@@ -11,7 +11,7 @@ using namespace lcma;
 
 namespace {
 
-const int kTile[kExpKernels][2] = {{64, 64}, {128, 128}, {16, 16}, {32, 32}, {64, 64}, {64, 128}, {128, 256}, {256, 256}}; // rows and columns of the kernels' tiles
+const int kTile[kExpKernels][2] = {{64, 64}, {128, 128}, {32, 32}, {16, 16}, {32, 32}, {64, 64}, {64, 128}, {128, 256}, {256, 256}}; // rows and columns of the kernels' tiles
 
 int64_t span(int64_t rows, int64_t ld, int64_t cols, int es) { return rows > 0 && cols > 0 ? ((rows - 1) * ld + cols) * es : 0; }
 int64_t tiles(int64_t n, int64_t of) { return (n + of - 1) / of; }
@@ -27,36 +27,43 @@ bool launches(int kernel, int64_t jobs) { return walks(kernel) ? jobs < kRowLimi
 int grid_of(int kernel, int64_t jobs) { return walks(kernel) ? 256 : (int)((jobs + 7) / 8 * 8); }
 // What the kernels that load straight into LDS need: offsets inside a tile (256 rows of a k-contiguous operand, 128 rows along k of the other) below 2^30 bytes, and, 16-bit types,
 // operands in whole 16 bytes (of a k-contiguous one K too, of the other form the rows).
+const int64_t kShortRow = 1 << 22;
 bool whole_vectors(int es, const void *A, int64_t lda_b, const void *B, int64_t ldb_b, int64_t k_b) {
-    return lda_b <= 1 << 22 && ldb_b <= 1 << 22 && (es == 4 || !(((uintptr_t)A | (uintptr_t)B | (uint64_t)lda_b | (uint64_t)ldb_b | (uint64_t)k_b) & 15));
+    return es == 4 || !(((uintptr_t)A | (uintptr_t)B | (uint64_t)lda_b | (uint64_t)ldb_b | (uint64_t)k_b) & 15);
 }
 
 // What a kernel takes, in us: `start`; a tile: `end`, and `step` for every 128 bytes of K, 256 * `slots` tiles at a time; and no less than the bytes at `rate` GB/us take.  With rows that
-// are no whole lines of 128 bytes a step takes `off` of its time more and the bytes half of that.  start 0: not taken.  Fitted to 164 layers in 16 bit, 94 in fp32 and 90 of sizes
-// that are no whole 16 bytes, of 1 to 8192 tokens and 8 to 128 experts, timed on every kernel: a single time is predicted within 10 to 25 % (root mean square); the kernel with the smallest
-// prediction is 1.3 to 2.4 % slower than the fastest one on average in whole 16 bytes (37 % at worst), 0.2 to 1.4 % in fp32 (32 %), 0.7 to 2.8 % in other sizes (68 %).
+// are no whole lines of 128 bytes a step takes `off` of its time more and the bytes half of that.  start 0: not taken.  Fitted to 164 layers in 16 bit, 94 in fp32 and 130 of sizes
+// that are no whole 16 bytes, of 1 to 8192 tokens and 8 to 128 experts, timed on every kernel: a single time is predicted within 10 to 31 % (root mean square); the kernel with the smallest
+// prediction is 1.3 to 2.4 % slower than the fastest one on average in whole 16 bytes (37 % at worst), 0.2 to 1.4 % in fp32 (32 %), 1.4 to 3.5 % in other sizes (73 %).
 struct Cost {
     double start, end, step, rate, slots, off;
 };
 enum { kNt, kNn, kGrad, kForms };
 const Cost kVectors[kForms][kExpKernels] = {
-    {{}, {}, {2.18, 0.29, 0.0312, 7.08, 0.655, 0.17}, {2.02, 0.655, 0.063, 6.15, 0.62, 0.118}, {2.06, 0.384, 0.209, 6.01, 0.812, 0.122}, {2.24, 0.706, 0.315, 5.88, 0.752, 0.133},
+    {{}, {}, {}, {2.18, 0.29, 0.0312, 7.08, 0.655, 0.17}, {2.02, 0.655, 0.063, 6.15, 0.62, 0.118}, {2.06, 0.384, 0.209, 6.01, 0.812, 0.122}, {2.24, 0.706, 0.315, 5.88, 0.752, 0.133},
      {3.57, 1.83, 0.71, 5.44, 0.591, 0.0682}, {4.63, 0.567, 0.977, 4.55, 0.584, 0.0691}},
-    {{}, {}, {}, {1.97, 0.596, 0.0866, 5.53, 0.604, 0.0683}, {2.15, 0.344, 0.256, 6.65, 0.821, 0.0253}, {2.25, 0.764, 0.373, 6.08, 0.788, 0}, {3.23, 2.24, 0.768, 5.83, 0.633, 0},
+    {{}, {}, {}, {}, {1.97, 0.596, 0.0866, 5.53, 0.604, 0.0683}, {2.15, 0.344, 0.256, 6.65, 0.821, 0.0253}, {2.25, 0.764, 0.373, 6.08, 0.788, 0}, {3.23, 2.24, 0.768, 5.83, 0.633, 0},
      {4.99, 0.065, 1.01, 4.75, 0.615, 0}},
-    {{}, {}, {}, {}, {2.19, 0.0769, 0.0613, 3.11, 0.177, 0.0761}, {2.53, 0.695, 0.43, 3.93, 0.781, 0.0505}, {}, {5.6, 2.17, 1.14, 4.96, 0.565, 0.227}}};
-const Cost kF32[kForms][kExpKernels] = {{{}, {}, {}, {2.59, 0.891, 0.152, 5.93, 0.928, 0.0706}, {2.86, 0.396, 0.563, 6.81, 1.03, 0}},
-                                        {{}, {}, {}, {2.24, 1.22, 0.16, 7.18, 0.961, 0.0109}, {2.3, 0.878, 0.599, 5.28, 1.11, 0.0132}},
-                                        {{2.93, 0.007, 1.62, 11.7, 1.5, 0.0153}, {}, {}, {}, {2.6, 0.0063, 0.0374, 3.73, 0.0456, 0.0594}}};
-const Cost kAny[kForms][kExpKernels] = {{{2.17, 1.35, 0.816, 5.14, 2.2, 0.158}, {1.64, 3.46, 1.31, 4.41, 1.57, 0.271}},
-                                        {{1.54, 0, 1.77, 3.49, 3.17, 0.27}, {0.925, 0, 3.46, 2.02, 3.08, 0.27}},
-                                        {{3.17, 0, 4.16, 3.42, 7.28, 0.319}, {4.92, 0, 6.07, 4.4, 3.26, 0.326}}};
+    {{}, {}, {}, {}, {}, {2.19, 0.0769, 0.0613, 3.11, 0.177, 0.0761}, {2.53, 0.695, 0.43, 3.93, 0.781, 0.0505}, {}, {5.6, 2.17, 1.14, 4.96, 0.565, 0.227}}};
+const Cost kF32[kForms][kExpKernels] = {{{}, {}, {}, {}, {2.59, 0.891, 0.152, 5.93, 0.928, 0.0706}, {2.86, 0.396, 0.563, 6.81, 1.03, 0}},
+                                        {{}, {}, {}, {}, {2.24, 1.22, 0.16, 7.18, 0.961, 0.0109}, {2.3, 0.878, 0.599, 5.28, 1.11, 0.0132}},
+                                        {{2.93, 0.007, 1.62, 11.7, 1.5, 0.0153}, {}, {}, {}, {}, {2.6, 0.0063, 0.0374, 3.73, 0.0456, 0.0594}}};
+const Cost kAny[kForms][kExpKernels] = {{{1.98, 1.45, 0.774, 5.02, 2.17, 0.208}, {2.21, 3.11, 1.37, 4.11, 1.51, 0.191}, {1.74, 3.17, 0.401, 3.66, 1.98, 0.05}},
+                                        {{1.25, 0, 1.82, 3.62, 3.35, 0.25}, {0.395, 0, 3.4, 2, 3.17, 0.269}, {1.53, 1.51, 0.833, 2.71, 2.97, 0.193}},
+                                        {{2.38, 0, 3.69, 3.08, 6.56, 0.297}, {3.76, 0, 5.01, 3.67, 2.82, 0.33}}};
 double predicted_us(const Cost &c, double tiles, double steps, bool off, double bytes) {
     const double o = off ? c.off : 0, n = tiles / 256 / c.slots, t = c.start + (c.end + steps * c.step * (1 + o)) * (n > 1 ? n : 1), memory = c.start + bytes / (c.rate * 1e6) * (1 + 0.5 * o);
     return std::sqrt(std::sqrt(t * t * t * t + memory * memory * memory * memory));
 }
+// Whether a kernel takes the call at all: by name, one that the rule leaves out may be asked for.  short_rows: offsets inside a tile are below 2^30 bytes.
+bool takes(int kernel, int form, bool vectors, bool short_rows, int es) {
+    if (kernel < 0 || kernel >= kExpKernels) return false;
+    if (kernel == kExpAnyFew32) return es == 2 && short_rows && form != kGrad;
+    return !needs_vectors(kernel) || (vectors && (es == 2 ? kVectors : kF32)[form][kernel].start > 0);
+}
 // form, and the sizes of the call; -1: no launch holds the tiles
-int pick(int form, bool vectors, int es, int64_t rows, int64_t N, int64_t K, int experts) {
+int pick(int form, bool vectors, bool short_rows, int es, int64_t rows, int64_t N, int64_t K, int experts) {
     const Cost(&costs)[kExpKernels] = (!vectors ? kAny : es == 2 ? kVectors : kF32)[form];
     auto tiles_of = [&](int k) { return form == kGrad ? gradient_tiles(k, N, K, experts) : product_tiles(k, rows, N, experts); };
     // (the rows of each expert are known on the device alone: half a tile left over for each that can have any)
@@ -70,20 +77,13 @@ int pick(int form, bool vectors, int es, int64_t rows, int64_t N, int64_t K, int
     int best = -1;
     double least = 0;
     for (int k = 0; k < kExpKernels; ++k)
-        if (costs[k].start > 0 && launches(k, tiles_of(k)))
+        if (takes(k, form, vectors, short_rows, es) && costs[k].start > 0 && launches(k, tiles_of(k)))
             if (const double t = seconds(k); best < 0 || t < least) {
                 least = t;
                 best = k;
             }
     return best;
 }
-// Whether a kernel takes the call at all: by name, one that the rule leaves out may be asked for.
-bool takes(int kernel, int form, bool vectors, int es) {
-    if (kernel < 0 || kernel >= kExpKernels) return false;
-    if (!needs_vectors(kernel)) return true;
-    return vectors && (es == 2 ? kVectors : kF32)[form][kernel].start > 0;
-}
-
 lcma_status check_sizes(const char *who, int64_t rows, int64_t N, int64_t K, int experts, int dtype) {
     if (!dtype_size(dtype)) return fail(LCMA_ERR_DTYPE, "%s: unknown dtype %d", who, dtype);
     if (rows < 0 || N < 0 || K < 0) return fail(LCMA_ERR_ARG, "%s: negative size", who);
@@ -131,10 +131,10 @@ extern "C" lcma_status lcma_gemm_experts(int b_layout, int64_t rows, int64_t N, 
     p.K = (int32_t)K;
     p.experts = experts;
     p.panel = 8;
-    const bool vectors = K > 0 && whole_vectors(es, A, p.lda_b, B, p.ldb_b, K * es);
+    const bool short_rows = K > 0 && p.lda_b <= kShortRow && p.ldb_b <= kShortRow, vectors = short_rows && whole_vectors(es, A, p.lda_b, B, p.ldb_b, K * es);
     const int form = b_layout ? kNt : kNn;
     int kernel = tuning_experts_kernel();
-    if (!takes(kernel, form, vectors, es) || !launches(kernel, product_tiles(kernel, rows, N, experts))) kernel = pick(form, vectors, es, rows, N, K, experts);
+    if (!takes(kernel, form, vectors, short_rows, es) || !launches(kernel, product_tiles(kernel, rows, N, experts))) kernel = pick(form, vectors, short_rows, es, rows, N, K, experts);
     if (kernel < 0) return fail(LCMA_ERR_SHAPE, "%s: too many tiles for a launch", who);
     p.nz = (int32_t)tiles(N, kTile[kernel][1]);
     if (const int err = lcma_launch_experts_gemm(&p, form, kernel, dtype, grid_of(kernel, product_tiles(kernel, rows, N, experts)), stream))
@@ -171,9 +171,9 @@ extern "C" lcma_status lcma_gemm_experts_grad(int64_t rows, int64_t N, int64_t K
     p.N = (int32_t)K;
     p.experts = experts;
     p.panel = 8;
-    const bool vectors = whole_vectors(es, dC, p.lda_b, A, p.ldb_b, 0);
+    const bool short_rows = p.lda_b <= kShortRow && p.ldb_b <= kShortRow, vectors = short_rows && whole_vectors(es, dC, p.lda_b, A, p.ldb_b, 0);
     int kernel = tuning_experts_kernel();
-    if (!takes(kernel, kGrad, vectors, es) || !launches(kernel, gradient_tiles(kernel, N, K, experts))) kernel = pick(kGrad, vectors, es, rows, N, K, experts);
+    if (!takes(kernel, kGrad, vectors, short_rows, es) || !launches(kernel, gradient_tiles(kernel, N, K, experts))) kernel = pick(kGrad, vectors, short_rows, es, rows, N, K, experts);
     if (kernel < 0) return fail(LCMA_ERR_SHAPE, "%s: too many tiles for a launch", who);
     p.nx = (int32_t)tiles(N, kTile[kernel][0]);
     p.nz = (int32_t)tiles(K, kTile[kernel][1]);

@@ -16,7 +16,7 @@ constexpr int64_t kGridLimit = (int64_t)1 << 32;  // threads of a launch along a
 constexpr const char *kI8KernelNames[kI8Kernels] = {"16x16", "32x32", "64x64", "64x128", "128x128", "128x256", "256x256"};
 int tuning_i8_kernel(); // csrc/api.cc; -1: choose
 // of the experts' products: those that take any sizes and alignments, and those for whole 16 bytes; of the product with 4-bit weights
-constexpr const char *kExpKernelNames[kExpKernels] = {"any64x64", "any128x128", "16x16", "32x32", "64x64", "64x128", "128x256", "256x256"};
+constexpr const char *kExpKernelNames[kExpKernels] = {"any64x64", "any128x128", "any32x32", "16x16", "32x32", "64x64", "64x128", "128x256", "256x256"};
 int tuning_experts_kernel();
 constexpr const char *kI4KernelNames[kI4Kernels] = {"16x16", "16x32", "16x64", "64x64"};
 int tuning_i4_kernel();

@@ -1,5 +1,6 @@
 // Instances of the experts' products (csrc/lcma_experts.hpp).
 #include "lcma_experts_pingpong.hpp"
+#include "lcma_experts_any.hpp"
 #include "lcma_experts_narrow.hpp"
 
 using namespace lcma;
@@ -19,6 +20,11 @@ template <class T, bool ACOL, bool BCOL, bool GRAD, int TM, int TN, int WGM, int
 }
 template <class T, bool BCOL, int R, int WK, int S> __global__ __launch_bounds__(64 * WK) void exp_few(const ExpertsGemmParams p) {
     using G = ExpFewRows<T, BCOL, R, WK, S>;
+    __shared__ __attribute__((aligned(16))) char smem[G::LDS_BYTES];
+    G::run(p, (LCMA_LDS char *)smem);
+}
+template <class T, bool BCOL, int WK> __global__ __launch_bounds__(64 * WK) void exp_any_few(const ExpertsGemmParams p) {
+    using G = ExpAnyFewRows<T, BCOL, WK>;
     __shared__ __attribute__((aligned(16))) char smem[G::LDS_BYTES];
     G::run(p, (LCMA_LDS char *)smem);
 }
@@ -55,6 +61,12 @@ extern "C" int lcma_launch_experts_gemm(const lcma::ExpertsGemmParams *p, int fo
     switch (kernel) {
     case kExpStaged64: LCMA_EXP_ANY(exp_staged, 256, LCMA_COMMA 64, 64, 2, 2)
     case kExpStaged128: LCMA_EXP_ANY(exp_staged, 256, LCMA_COMMA 128, 128, 2, 2)
+    case kExpAnyFew32:
+        if (dtype == 1 && form == 0) LCMA_EXP_LAUNCH(256, exp_any_few<BF16, false, 4>);
+        else if (dtype == 1) LCMA_EXP_LAUNCH(256, exp_any_few<BF16, true, 4>);
+        else if (form == 0) LCMA_EXP_LAUNCH(256, exp_any_few<F16, false, 4>);
+        else LCMA_EXP_LAUNCH(256, exp_any_few<F16, true, 4>);
+        break;
     case kExpFew16:
         if (dtype == 1) LCMA_EXP_LAUNCH(256, exp_few<BF16, false, 16, 4, 2>);
         else LCMA_EXP_LAUNCH(256, exp_few<F16, false, 16, 4, 2>);

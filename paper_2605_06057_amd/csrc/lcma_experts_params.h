@@ -63,10 +63,11 @@ struct I8GemmParams {
     int32_t nz, panel;      // tiles along N, and the width of a column panel of the tile order
 };
 
-// Kernels of the experts' products: any sizes and alignments (csrc/lcma_experts.hpp); 16 bit in whole 16 bytes and fp32 (csrc/lcma_experts_ring.hpp); 16 bit in whole 16 bytes
+// Kernels of the experts' products: any sizes and alignments (csrc/lcma_experts.hpp, and in 16 bit
+// lcma_experts_any.hpp); 16 bit in whole 16 bytes and fp32 (csrc/lcma_experts_ring.hpp); 16 bit in whole 16 bytes
 // (csrc/lcma_experts_narrow.hpp, lcma_experts_pingpong.hpp).  Tiles of 16 x 16: 16 bit, weights N x K alone; of 64 x 128: 16 bit; of 16,
 // 32 and 128 rows: no gradient of weights.
-enum { kExpStaged64 = 0, kExpStaged128, kExpFew16, kExpFew32, kExpRing64, kExpRing64x128, kExpNarrow, kExpPingPong, kExpKernels };
+enum { kExpStaged64 = 0, kExpStaged128, kExpAnyFew32, kExpFew16, kExpFew32, kExpRing64, kExpRing64x128, kExpNarrow, kExpPingPong, kExpKernels };
 
 // lcma_gemm_experts: rows of A (k-contiguous) in groups, group e times the matrix of expert e (N x K, or K x N).
 // lcma_gemm_experts_grad: for every expert the product of its rows of A, transposed, and its rows of B: M x N, summed over the rows.

@@ -23,7 +23,7 @@ def _lib():
     return binding
 
 
-@pytest.fixture(params=["", "any64x64", "any128x128", "16x16", "32x32", "64x64", "64x128", "128x256", "256x256"], scope="module")
+@pytest.fixture(params=["", "any64x64", "any128x128", "any32x32", "16x16", "32x32", "64x64", "64x128", "128x256", "256x256"], scope="module")
 def kernel(request):
     """The kernel of the rule, and every kernel by name where it takes the sizes."""
     _lib().lcma_set_tuning("experts_kernel", request.param)
