@@ -1,4 +1,4 @@
-"""A mixture-of-experts feed-forward layer: served in 8-bit integers, and trained in bf16.
+"""A mixture-of-experts feed-forward layer: served in 8-bit integers or with 4-bit weights, and trained in bf16.
 
   python examples/experts_layer.py [--tokens 4096] [--experts 8] [--top 2] [--hidden 2048] [--ffn 4096]
 
@@ -6,7 +6,9 @@ Serving: the tokens are sorted by expert, quantised on their way into the expert
 gated and quantised again, multiplied with the down weights, and summed back into tokens with the router's weights.  Nothing leaves the GPU and
 the host never learns how many rows an expert has.
 
-Training: the movement and its gradients are the library's calls as well; the products of each expert are its 16-bit ones.
+For single tokens the weights may have 4 bits, with a scale for each group of columns; the activations stay in 16.
+
+Training: the movement, the products over all experts, the gate between them and the gradients of all these are the library's calls as well.
 """
 import argparse
 import os
@@ -47,15 +49,19 @@ class ServedExperts:
         return lcma.lcma_tokens_combine(y, position, weights)
 
 
-def _product(a, b, b_nk):
-    """a b (a b^T) by the library's plain product, whose sizes along both axes of b are multiples of 8."""
-    c = a.new_empty((a.shape[0], b.shape[0] if b_nk else b.shape[1]))
-    return lcma.lcma_gemm_nt(a, b, c) if b_nk else lcma.lcma_gemm(a, b, c)
+class ServedExperts4:
+    """Experts whose weights have 4 bits and a scale for each `group` of columns, laid out as ServedExperts': for the few rows of single tokens, which stay in 16 bits."""
 
+    def __init__(self, w_in, w_out, group=128):
+        self.experts, self.ffn, self.hidden, self.group = w_in.shape[0], w_in.shape[1] // 2, w_in.shape[2], group
+        self.q_in, self.q_out = lcma.lcma_i4_quantize(w_in, group), lcma.lcma_i4_quantize(w_out, group)
 
-def _padded(t):
-    """t with zero rows behind, to a multiple of 8."""
-    return torch.nn.functional.pad(t, (0, 0, 0, -t.shape[0] % 8))
+    def __call__(self, x, ids, weights):
+        rows = ids.numel()
+        _, position, offsets = lcma.lcma_tokens_sort(ids, self.experts)
+        h = lcma.lcma_i4_gemm_experts(lcma.lcma_tokens_dispatch(x, position), offsets, self.q_in, x.new_empty((rows, 2 * self.ffn)), self.group)
+        y = lcma.lcma_i4_gemm_experts(lcma.lcma_gated_silu(h), offsets, self.q_out, x.new_empty((rows, self.hidden)), self.group)
+        return lcma.lcma_tokens_combine(y, position, weights)
 
 
 class TrainedLinearExperts(torch.autograd.Function):
@@ -65,25 +71,39 @@ class TrainedLinearExperts(torch.autograd.Function):
     def forward(ctx, x, w, ids, weights):
         _, position, offsets = lcma.lcma_tokens_sort(ids, w.shape[0])
         rows = lcma.lcma_tokens_dispatch(x, position)
-        ends = offsets.tolist()  # (the products of the experts are calls of their own: the host needs their sizes)
-        y = torch.zeros((rows.shape[0], w.shape[1]), dtype=x.dtype, device=x.device)
-        for e, (a, b) in enumerate(zip(ends, ends[1:])):
-            if b > a:
-                y[a:b] = _product(rows[a:b], w[e], True)
-        ctx.save_for_backward(rows, w, position, weights, y)
-        ctx.ends = ends
+        y = lcma.lcma_gemm_experts(rows, offsets, w)
+        ctx.save_for_backward(rows, w, position, offsets, weights, y)
         return lcma.lcma_tokens_combine(y, position, weights)
 
     @staticmethod
     def backward(ctx, grad):
-        rows, w, position, weights, y = ctx.saved_tensors
+        rows, w, position, offsets, weights, y = ctx.saved_tensors
         dy, dweights = lcma.lcma_tokens_combine_grad(grad.contiguous(), y, position, weights)
-        drows, dw = torch.zeros_like(rows), torch.zeros_like(w)
-        for e, (a, b) in enumerate(zip(ctx.ends, ctx.ends[1:])):
-            if b > a:
-                drows[a:b] = _product(dy[a:b], w[e], False)
-                dw[e] = _product(_padded(dy[a:b]).t().contiguous(), _padded(rows[a:b]), False)
-        return lcma.lcma_tokens_combine(drows, position), dw, None, dweights
+        dx = lcma.lcma_tokens_combine(lcma.lcma_gemm_experts(dy, offsets, w, b_nk=False), position)
+        return dx, lcma.lcma_gemm_experts_grad(dy, rows, offsets), None, dweights
+
+
+class TrainedExperts(torch.autograd.Function):
+    """The whole layer: y[t] = sum over j of weights[t, j] * w_out[e] (silu(g) * u), (g, u) = w_in[e] x[t], e = ids[t, j], with the gradients of x, of both of the experts' matrices
+    (w_in: experts x 2 ffn x hidden, gate rows first; w_out: experts x hidden x ffn) and of weights.  What the gate gives is computed anew for the gradients instead of kept."""
+
+    @staticmethod
+    def forward(ctx, x, w_in, w_out, ids, weights):
+        _, position, offsets = lcma.lcma_tokens_sort(ids, w_in.shape[0])
+        rows = lcma.lcma_tokens_dispatch(x, position)
+        h = lcma.lcma_gemm_experts(rows, offsets, w_in)
+        y = lcma.lcma_gemm_experts(lcma.lcma_gated_silu(h), offsets, w_out)
+        ctx.save_for_backward(rows, h, y, w_in, w_out, position, offsets, weights)
+        return lcma.lcma_tokens_combine(y, position, weights)
+
+    @staticmethod
+    def backward(ctx, grad):
+        rows, h, y, w_in, w_out, position, offsets, weights = ctx.saved_tensors
+        dy, dweights = lcma.lcma_tokens_combine_grad(grad.contiguous(), y, position, weights)
+        dw_out = lcma.lcma_gemm_experts_grad(dy, lcma.lcma_gated_silu(h), offsets)
+        dh = lcma.lcma_gated_silu_grad(lcma.lcma_gemm_experts(dy, offsets, w_out, b_nk=False), h)
+        dx = lcma.lcma_tokens_combine(lcma.lcma_gemm_experts(dh, offsets, w_in, b_nk=False), position)
+        return dx, lcma.lcma_gemm_experts_grad(dh, rows, offsets), dw_out, None, dweights
 
 
 def train(x, target, w, router, top, steps):
@@ -122,17 +142,28 @@ def main():
         g, u = (x[t].float() @ w_in[e].float().t()).chunk(2, dim=1)
         want.index_add_(0, t, weights[t, j, None] * ((torch.nn.functional.silu(g) * u) @ w_out[e].float().t()))
     print(f"served in 8 bit: relative error against the unquantised layer {((got - want).norm() / want.norm()).item():.4f}")
-    begin, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
-    for _ in range(3):
-        layer(x, ids, weights)
-    begin.record()
-    for _ in range(20):
-        layer(x, ids, weights)
-    end.record()
-    torch.cuda.synchronize()
-    ms = begin.elapsed_time(end) / 20
+    four = ServedExperts4(w_in, w_out)
+    print(f"served in 4 bit: {((four(x, ids, weights).float() - want).norm() / want.norm()).item():.4f}")
+
+    def timed(f):
+        begin, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        for _ in range(3):
+            f()
+        begin.record()
+        for _ in range(20):
+            f()
+        end.record()
+        torch.cuda.synchronize()
+        return begin.elapsed_time(end) / 20
+
+    ms = timed(lambda: layer(x, ids, weights))
     ops = 2.0 * ids.numel() * 3 * a.ffn * a.hidden
     print(f"{a.tokens} tokens, {a.top} of {a.experts} experts, {a.hidden} x {a.ffn}: {ms * 1e3:.0f} us, {ops / ms / 1e9:.0f} TOP/s")
+    one = [t[:1].contiguous() for t in (x, ids, weights)]
+    print(f"one token: 8 bit {timed(lambda: layer(*one)) * 1e3:.0f} us, 4 bit {timed(lambda: four(*one)) * 1e3:.0f} us")
+    leaves = [t.clone().requires_grad_() for t in (x, w_in, w_out, weights)]
+    ms = timed(lambda: TrainedExperts.apply(*leaves[:3], ids, leaves[3]).backward(x))
+    print(f"a training step of the layer, forward and back: {ms * 1e3:.0f} us, {3 * ops / ms / 1e9:.0f} TFLOP/s")
 
     w = normal(a.experts, 512, a.hidden, spread=a.hidden ** -0.5)
     losses = train(x, normal(a.tokens, 512, spread=0.1), w, router, a.top, 8)
