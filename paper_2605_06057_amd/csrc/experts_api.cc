@@ -82,6 +82,7 @@ int pick(int form, bool vectors, bool short_rows, int es, int64_t rows, int64_t 
                 least = t;
                 best = k;
             }
+    if (best < 0 && launches(kExpStaged128, tiles_of(kExpStaged128))) best = kExpStaged128; // (the fewest tiles of those that have a work-group each)
     return best;
 }
 lcma_status check_sizes(const char *who, int64_t rows, int64_t N, int64_t K, int experts, int dtype) {

@@ -182,15 +182,17 @@ template <class T, bool ACOL, bool BCOL, bool GRAD, int TM, int TN, int WGM, int
 
     template <bool COL, int R, int Q> static LCMA_DEV void load(const char *at, int64_t ld_b, int wide, int k, int y, u32x4 (&v)[Q]) {
         constexpr int CPR = R * T::ES / 16;
+        const int left = k - y * KS; // (k may be up to 2^31 - 1: the numbers past it do not fit)
+        at += (int64_t)y * KS * (COL ? ld_b : T::ES);
 #pragma unroll
         for (int q = 0; q < Q; ++q) {
             const int i = q * NT + (int)threadIdx.x;
             if constexpr (!COL) {
-                const int row = i >> 3, k0 = y * KS + (i & 7) * T::CH;
-                v[q] = exp_chunk<T>(at + (int64_t)row * ld_b + (int64_t)k0 * T::ES, row < wide ? k - k0 : 0);
+                const int row = i >> 3, k0 = (i & 7) * T::CH;
+                v[q] = exp_chunk<T>(at + (int64_t)row * ld_b + k0 * T::ES, row < wide ? left - k0 : 0);
             } else {
-                const int k0 = y * KS + i / CPR, col = i % CPR * T::CH;
-                v[q] = exp_chunk<T>(at + (int64_t)k0 * ld_b + (int64_t)col * T::ES, k0 < k ? wide - col : 0);
+                const int k0 = i / CPR, col = i % CPR * T::CH;
+                v[q] = exp_chunk<T>(at + (int64_t)k0 * ld_b + col * T::ES, k0 < left ? wide - col : 0);
             }
         }
     }

@@ -16,7 +16,7 @@ template <class P> LCMA_DEV P *exp_uniform(P *at) {
 // The rows of the stored matrix from step y on, `steps` steps of them; none past the last k.
 template <class T> LCMA_DEV __amdgpu_buffer_rsrc_t exp_columns_from(const char *at, int wide, int k, uint32_t ld_b, int y, int steps) {
     constexpr int KS = 128 / T::ES;
-    const int left = k - y * KS, n = left < steps * KS ? left : steps * KS;
+    const int left = (int)((uint32_t)k - (uint32_t)y * KS), n = left < steps * KS ? left : steps * KS; // (unsigned: y * KS may lie past 2^31, behind k)
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(at) + (int64_t)y * KS * ld_b, 0, n > 0 ? (n - 1) * (int)ld_b + wide * T::ES : 0, 0x00020000);
 }
 template <class T> LCMA_DEV __amdgpu_buffer_rsrc_t exp_rows_of(const char *at, int wide, int k, uint32_t ld_b) {
