@@ -25,6 +25,10 @@ bool needs_vectors(int kernel) { return kernel >= kExpFew16; }
 bool walks(int kernel) { return kernel >= kExpNarrow; } // 256 work-groups walk through tiles; the other kernels have one for every tile
 bool launches(int kernel, int64_t jobs) { return walks(kernel) ? jobs < kRowLimit - 1024 : (jobs + 8) * 512 < kGridLimit / 2; } // (numbers of tiles are 32-bit on the device)
 int grid_of(int kernel, int64_t jobs) { return walks(kernel) ? 256 : (int)((jobs + 7) / 8 * 8); }
+int gradient_grid(int kernel, int64_t jobs, int64_t of) { // of: tiles of an expert; the kernels deal out eighths of them (exp_gradient_tile)
+    const int64_t whole = (of + 7) / 8 * 8;
+    return walks(kernel) ? 256 : (int)((jobs + whole - 1) / whole * whole);
+}
 // What the kernels that load straight into LDS need: offsets inside a tile (256 rows of a k-contiguous operand, 128 rows along k of the other) below 2^30 bytes, and, 16-bit types,
 // operands in whole 16 bytes (of a k-contiguous one K too, of the other form the rows).
 const int64_t kShortRow = 1 << 22;
@@ -178,7 +182,7 @@ extern "C" lcma_status lcma_gemm_experts_grad(int64_t rows, int64_t N, int64_t K
     if (kernel < 0) return fail(LCMA_ERR_SHAPE, "%s: too many tiles for a launch", who);
     p.nx = (int32_t)tiles(N, kTile[kernel][0]);
     p.nz = (int32_t)tiles(K, kTile[kernel][1]);
-    if (const int err = lcma_launch_experts_gemm(&p, kGrad, kernel, dtype, grid_of(kernel, gradient_tiles(kernel, N, K, experts)), stream))
+    if (const int err = lcma_launch_experts_gemm(&p, kGrad, kernel, dtype, gradient_grid(kernel, gradient_tiles(kernel, N, K, experts), (int64_t)p.nx * p.nz), stream))
         return fail(LCMA_ERR_HIP, "%s: launch failed with HIP error %d", who, err);
     return LCMA_OK;
 }

@@ -46,6 +46,14 @@ template <class T, int TM, int TN> LCMA_DEV ExpJob gradient_job(const ExpertsGem
     return j;
 }
 
+// Tiles of the gradient to work-groups, one each: eighths of an expert's tiles to the XCDs in turn (work-groups go to the eight in turn), so that each of them has a share of every
+// expert: an expert's tiles take as long as it has rows, and an XCD that had whole experts would be done long before another (fp32, 2331 rows spread
+// unequally over 12 experts, 1001 x 515: 41 us so, now 37).  -1: none.  The launch holds whole eights of such eighths.
+LCMA_DEV int exp_gradient_tile(const ExpertsGemmParams &p) {
+    const int of = p.nx * p.nz, q = (of + 7) >> 3, i = (int)(blockIdx.x >> 3), job = (i / q * 8 + (int)(blockIdx.x & 7)) * q + i % q;
+    return job < p.experts * of ? job : -1;
+}
+
 // Where 16-byte chunk c of a row lies in LDS.  k-contiguous rows of 128 bytes: 16 rows at one chunk column meet all banks once.  Rows of columns, 16 bit: the four
 // rows (k) of a transposing read, 64 bytes of each, meet different banks (rows of 64 bytes do so by themselves; fp32 needs nothing).
 LCMA_DEV constexpr int exp_row_chunk(int row, int c) { return c ^ ((row >> 1) & 7); }
@@ -209,8 +217,8 @@ template <class T, bool ACOL, bool BCOL, bool GRAD, int TM, int TN, int WGM, int
     static LCMA_DEV void run(const ExpertsGemmParams &p, LCMA_LDS char *lds) {
         ExpJob j;
         if constexpr (GRAD) {
-            const int jobs = p.experts * p.nx * p.nz, per = (jobs + 7) / 8, job = (int)(blockIdx.x & 7) * per + (int)(blockIdx.x >> 3);
-            if ((int)(blockIdx.x >> 3) >= per || job >= jobs) return;
+            const int job = exp_gradient_tile(p);
+            if (job < 0) return;
             j = gradient_job<T, TM, TN>(p, job);
         } else {
             const I8Rows<TM, ExpertsGemmParams> groups(p);

@@ -46,8 +46,8 @@ template <class T, bool ACOL, bool BCOL, bool GRAD, int TM, int TN, int WGM, int
     static LCMA_DEV void run(const ExpertsGemmParams &p, LCMA_LDS char *lds) {
         ExpJob j;
         if constexpr (GRAD) {
-            const int jobs = p.experts * p.nx * p.nz, per = (jobs + 7) / 8, job = (int)(blockIdx.x & 7) * per + (int)(blockIdx.x >> 3); // an eighth of the tiles to every XCD
-            if ((int)(blockIdx.x >> 3) >= per || job >= jobs) return;
+            const int job = exp_gradient_tile(p);
+            if (job < 0) return;
             j = gradient_job<T, TM, TN>(p, job);
         } else {
             const I8Rows<TM, ExpertsGemmParams> groups(p);

@@ -87,8 +87,9 @@ def most_tiles(name, rows, N, E):
     return (rows // tm + min(rows, E)) * -(-N // tn)
 
 
-def fits(name, grid, tiles, walking=("128x256", "256x256")):
-    return grid == 256 if name in walking else tiles <= grid < tiles + 8 and grid % 8 == 0 and grid * 512 < 1 << 31
+def fits(name, grid, tiles, walking=("128x256", "256x256"), dealt=8):
+    """dealt: the tiles that the work-groups are dealt in one go."""
+    return grid == 256 if name in walking else tiles <= grid < tiles + dealt and grid % 8 == 0 and grid * 512 < 1 << 32
 
 
 ROWS = (1, 2, 4, 8, 16, 32, 64, 100, 128, 250, 512, 1000, 2048, 4096, 16384)
@@ -127,7 +128,8 @@ def test_launches_cover_every_tile(lib, ask):
                 assert lib.seen(2) == -(-N // int(name.split("x")[1]))
             name, grid = gradient(lib, rows, N, K, E, dtype)
             tm, tn = map(int, name.removeprefix("any").split("x"))
-            assert fits(name, grid, E * -(-N // tm) * -(-K // tn)) and lib.seen(4) == GRAD
+            of = -(-N // tm) * -(-K // tn)
+            assert fits(name, grid, E * of, dealt=-(-of // 8) * 8) and lib.seen(4) == GRAD
             assert lib.seen(3) == -(-N // tm) and lib.seen(2) == -(-K // tn)
 
 
