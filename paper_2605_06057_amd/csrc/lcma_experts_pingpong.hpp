@@ -5,6 +5,8 @@
 // 128 h .. + 127, so a wave has rows 64 wm .. + 63 of both halves (right operand: columns 32 wn .. + 31).  What lies past a tile's rows or columns may be anything: it
 // reaches elements of C alone that are not there.  What lies past the last k reads as zero, on both sides: k-contiguous, 16 bytes at a time from past the extent; else by the extent.
 // Every work-group walks through tiles of its own, in turn; the loads run two steps ahead, into the next tile too.
+// Bound by power, as one large product: bf16, 8192 x 2 of 8, 4096 x 14336: 1620 us, 1.19 PFLOP/s (128 x 256 takes 1960, 64 x 128 2790), gradients 1550 and 1600; the matrix pipe is at work in 83, 83 and
+// 71 % of the clocks, of which there are 1.5 to 1.8 in a nanosecond.
 #pragma once
 #include "lcma_experts_ring.hpp"
 

@@ -35,7 +35,9 @@ template <int N> LCMA_DEV void exp_end_of_k(u32x4 (&f)[N][4], int left) {
 
 // One tile of TM x TN per work-group of WGM x WGN waves.  A step is 64 k (fp32: 32); S stages of LDS hold the steps in flight, the loads run S - 1 steps ahead and are waited for by
 // count, and one barrier a step says that all waves' parts of it have landed and that all have read the stage that is loaded anew (csrc/lcma_i8.hpp has the
-// same with its measurements).
+// same with its measurements).  Bound by memory at hundreds of rows, by the loads' way through LDS above: bf16, rows of 128 x 2 of 8, 2048 x 1024: 8.3 us on 64 x 64 (weights at 4.0 TB/s; 32 x 32 takes
+// 11.1), 9.0 on 64 x 128; fp16 1021 x 6 of 64, 2816 x 2056: 287 and 255 against 213 on 128 x 256.  fp32 (64 x 64 alone, by the matrix pipe, 68 % of which is at work): 777 x 3 of 12, 1001 x 515: 33 us,
+// gradients 38 and 37; 4096 x 2 of 8, 2048 x 2048: 538 (128 TFLOP/s).
 template <class T, bool ACOL, bool BCOL, bool GRAD, int TM, int TN, int WGM, int WGN, int S> struct ExpRing {
     static constexpr int NT = 64 * WGM * WGN, NMI = TM / WGM / 32, NNI = TN / WGN / 32, KS = 128 / T::ES;
     static constexpr int A_STAGE = TM * 128, STAGE = (TM + TN) * 128, LDS_BYTES = S * STAGE, QA = TM * 8 / NT, QB = TN * 8 / NT;
@@ -138,7 +140,8 @@ template <class T, bool ACOL, bool BCOL, bool GRAD, int TM, int TN, int WGM, int
 
 // Few rows: a work-group owns a tile of R x R of C and its waves split K between them, a step (64 k, fp32: 32, 128 bytes of every row) to a wave in turn; nothing is shared between
 // waves, so there is no barrier in the loop, and the waves' sums are added at the end, in fp32 and in ascending order (csrc/lcma_few_rows.hpp has the same for one product,
-// with the reasons and measurements).  S steps of a wave in flight.
+// with the reasons and measurements).  S steps of a wave in flight.  Bound by memory: bf16, 2 rows of 8 experts, 28672 x 4096: 77 us, 6.1 TB/s, which is what a large read reaches; weights K x N
+// 113 (32 columns are half a line; 64 x 64 takes 164).
 template <class T, bool BCOL, int R, int WK, int S> struct ExpFewRows {
     static constexpr int F = R == 16 ? 16 : 32, NF = R / F, KF = 64 / (512 / F), KS = 128 / T::ES; // 16x16x32 or 32x32x16 instructions; fragments of a step along K
     static constexpr int LOADS = R / 8, HALF = R * 128, STAGE = 2 * HALF, PITCH = R + 4, SUMS = WK * R * PITCH * 4, STAGES = WK * S * STAGE, LDS_BYTES = SUMS > STAGES ? SUMS : STAGES;

@@ -1,6 +1,7 @@
 // The gate of an experts' layer and its gradient: rows X = (g, u) of 2 F values, Y = silu(g) u; dX = dY (silu'(g) u, silu(g)).
 // Bound by the bytes it moves: three rows of F values forward, five back.  All arithmetic is in fp32, one rounding; the exponential is the accurate form for
-// every type (about 20 operations forward and 30 back for a value, where the memory leaves room for 43 and 71).
+// every type (about 20 operations forward and 30 back for a value, where the memory leaves room for 43 and 71).  bf16, 16384 x 14336: 244 us forward and 428 back, 5.8
+// and 5.5 TB/s; passing the caches by made both together 727 -> 675 us (from 64 MiB written on: what follows finds less than that in them anyway); 2 rows: 3 us each, a launch.
 #include "lcma_gated.hpp"
 #include "lcma_i8.hpp"
 

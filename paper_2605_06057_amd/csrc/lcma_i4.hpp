@@ -37,6 +37,8 @@ template <class T> LCMA_DEV u32x4 i4_widened(uint32_t v) {
 
 // WN x WK waves: the first along N, NB blocks of rows (of the weights) each, the others along K, a block of columns to a wave in turn; the weights of D of a wave's blocks are in
 // flight.  MT x 16 rows of X; as many blocks of columns of them are in LDS at a time as XB bytes hold.
+// bf16, groups of 128: a row, 14336 x 4096: 9.1 us (31 MB at 3.4 TB/s, 6.6 without the 2.5 of an empty launch: 448 tiles of 16 x 32, all at once, no second round to hide a start behind);
+// 16 rows over 8 experts, 28672 x 4096: 80 us, 5.6 TB/s; fp16, groups of 64, 366 rows over 64 experts, 2816 x 2048: 48 us, 4.3 TB/s.
 // What bounds it is the latency of the weights' way from memory, not the arithmetic: a block takes a wave about 60 vector instructions, 240 of the 420 clocks in which a CU's fourth of the
 // memory's rate brings it.
 template <class T, int G, int MT, int NB, int WN, int WK, int D, int XB> struct I4Gemm {
