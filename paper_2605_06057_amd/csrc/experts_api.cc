@@ -176,6 +176,8 @@ extern "C" lcma_status lcma_gemm_experts_grad(int64_t rows, int64_t N, int64_t K
     p.N = (int32_t)K;
     p.experts = experts;
     p.panel = 8;
+    p.stream = !(((uintptr_t)dW | (uint64_t)p.ldc_b) & 127); // (rows of whole lines: every store writes some; parts of them to memory cost up to twice the time instead)
+    p.lines = rows <= (int64_t)512 * experts; // (512 rows an expert: 88 -> 82 us at 2048 x 4096, 1024: 141 -> 145)
     const bool short_rows = p.lda_b <= kShortRow && p.ldb_b <= kShortRow, vectors = short_rows && whole_vectors(es, dC, p.lda_b, A, p.ldb_b, 0);
     int kernel = tuning_experts_kernel();
     if (!takes(kernel, kGrad, vectors, short_rows, es) || !launches(kernel, gradient_tiles(kernel, N, K, experts))) kernel = pick(kGrad, vectors, short_rows, es, rows, N, K, experts);

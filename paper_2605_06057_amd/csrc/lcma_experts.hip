@@ -33,8 +33,8 @@ template <class T, bool BCOL> __global__ __launch_bounds__(512, 2) void exp_narr
     __shared__ __attribute__((aligned(16))) char smem[G::LDS_BYTES];
     G::run((LCMA_LDS char *)smem);
 }
-template <class T, bool ACOL, bool BCOL, bool GRAD> __global__ __launch_bounds__(512, 2) void exp_256(const ExpertsGemmParams) {
-    using G = ExpPingPong<T, ACOL, BCOL, GRAD>;
+template <class T, bool ACOL, bool BCOL, bool GRAD, bool LINES = false> __global__ __launch_bounds__(512, 2) void exp_256(const ExpertsGemmParams) {
+    using G = ExpPingPong<T, ACOL, BCOL, GRAD, LINES>;
     __shared__ __attribute__((aligned(16))) char smem[G::LDS_BYTES];
     G::run((LCMA_LDS char *)smem);
 }
@@ -87,7 +87,13 @@ extern "C" int lcma_launch_experts_gemm(const lcma::ExpertsGemmParams *p, int fo
         else if (form == 0) LCMA_EXP_LAUNCH(512, exp_narrow<F16, false>);
         else LCMA_EXP_LAUNCH(512, exp_narrow<F16, true>);
         break;
-    default: LCMA_EXP(exp_256, 512, )
+    default:
+        if (form == 2 && p->lines) {
+            if (dtype == 1) LCMA_EXP_LAUNCH(512, exp_256<BF16, true, true, true, true>);
+            else LCMA_EXP_LAUNCH(512, exp_256<F16, true, true, true, true>);
+            break;
+        }
+        LCMA_EXP(exp_256, 512, )
     }
 #undef LCMA_EXP_LAUNCH
 #undef LCMA_EXP_FORM

@@ -105,8 +105,8 @@ template <class T, bool COL, int R> LCMA_DEV void exp_fragments(const LCMA_LDS c
 // A wave's part of a tile of C (NMI x NNI blocks of 32 x 32; rows, cols: of C from its first element on) rounded and stored: through SR rows of 128 bytes of LDS that are the
 // wave's own, so that it leaves as whole lines, 16 bytes a lane.  The right operand is the left one of the matrix instruction: a lane holds four neighbouring columns.
 // Blocks of rows follow each other, or, TWO, the second pair of them is 128 rows on; the blocks of columns are GAP columns apart.
-// FULL: all of it lies inside C.
-template <class T, int NMI, int NNI, bool TWO, int GAP, int SR, bool FULL>
+// FULL: all of it lies inside C.  STREAM: and passes the caches by, in whole 16 bytes.
+template <class T, int NMI, int NNI, bool TWO, int GAP, int SR, bool FULL, bool STREAM>
 LCMA_DEV void exp_store_rows(LCMA_LDS char *strip, char *c, int64_t ldc_b, int rows, int cols, const f32x16 (&acc)[NMI][NNI]) {
     constexpr int ES = T::ES, BLOCKS = ES == 4 ? 1 : NNI == 1 ? 1 : 2, L = BLOCKS * 32 * ES / 16, RPS = 64 / L; // 32-column blocks of a pass; lanes of a row, rows of a store
     static_assert(NNI % BLOCKS == 0 && SR % RPS == 0, "whole passes");
@@ -146,7 +146,8 @@ LCMA_DEV void exp_store_rows(LCMA_LDS char *strip, char *c, int64_t ldc_b, int r
                     const int in = it * RPS + row_of, row = h * SR + in, of = ch * (16 / ES), col = (n0 + of / 32) * GAP + of % 32;
                     const u32x4 v = *(const LCMA_LDS u32x4 *)(strip + in * (L * 16) + (ch ^ (row & (L - 1))) * 16);
                     char *to = at + (int64_t)(row0 + h * SR + it * RPS) * ldc_b + col * ES;
-                    if constexpr (FULL) __builtin_memcpy(to, &v, 16);
+                    if constexpr (STREAM) __builtin_nontemporal_store(v, (u32x4 *)to);
+                    else if constexpr (FULL) __builtin_memcpy(to, &v, 16);
                     else if (row0 + row < rows && col < cols) i8_store16<T>(to, v, cols - col);
                 }
                 lanes_meet();
@@ -154,10 +155,12 @@ LCMA_DEV void exp_store_rows(LCMA_LDS char *strip, char *c, int64_t ldc_b, int r
         }
     }
 }
-template <class T, int NMI, int NNI, bool TWO = false, int GAP = 32, int SR = 32>
-LCMA_DEV void exp_store(LCMA_LDS char *strip, char *c, int64_t ldc_b, int rows, int cols, const f32x16 (&acc)[NMI][NNI]) {
-    if (rows >= (TWO ? (NMI - 1) / 2 * 128 + (NMI - 1) % 2 * 32 : (NMI - 1) * 32) + 32 && cols >= (NNI - 1) * GAP + 32) exp_store_rows<T, NMI, NNI, TWO, GAP, SR, true>(strip, c, ldc_b, rows, cols, acc);
-    else exp_store_rows<T, NMI, NNI, TWO, GAP, SR, false>(strip, c, ldc_b, rows, cols, acc);
+template <class T, int NMI, int NNI, bool TWO = false, int GAP = 32, int SR = 32, bool GRAD = false>
+LCMA_DEV void exp_store(LCMA_LDS char *strip, char *c, int64_t ldc_b, int rows, int cols, const f32x16 (&acc)[NMI][NNI], bool stream = false) {
+    const bool full = rows >= (TWO ? (NMI - 1) / 2 * 128 + (NMI - 1) % 2 * 32 : (NMI - 1) * 32) + 32 && cols >= (NNI - 1) * GAP + 32;
+    if (GRAD && full && stream) exp_store_rows<T, NMI, NNI, TWO, GAP, SR, true, GRAD>(strip, c, ldc_b, rows, cols, acc);
+    else if (full) exp_store_rows<T, NMI, NNI, TWO, GAP, SR, true, false>(strip, c, ldc_b, rows, cols, acc);
+    else exp_store_rows<T, NMI, NNI, TWO, GAP, SR, false, false>(strip, c, ldc_b, rows, cols, acc);
 }
 
 // Rows of C behind the last expert's are zero: the work-groups of the launch share them.
@@ -267,7 +270,7 @@ template <class T, bool ACOL, bool BCOL, bool GRAD, int TM, int TN, int WGM, int
         }
         __syncthreads(); // the strips take the place of the stages
         const int row = wm * NMI * 32, col = wn * NNI * 32;
-        exp_store<T, NMI, NNI>(lds + w * 4096, j.c + (int64_t)row * p.ldc_b + (int64_t)col * T::ES, p.ldc_b, j.am - row, j.bn - col, acc);
+        exp_store<T, NMI, NNI, false, 32, 32, GRAD>(lds + w * 4096, j.c + (int64_t)row * p.ldc_b + (int64_t)col * T::ES, p.ldc_b, j.am - row, j.bn - col, acc, p.stream);
     }
 };
 

@@ -79,6 +79,7 @@ struct ExpertsGemmParams {
     int64_t expert_b;               // bytes from an expert's matrix to the next: of B (product), of C (gradient)
     int32_t rows, M, N, K, experts; // M: rows of an expert's C (gradient); K: what a product sums over
     int32_t nx, nz, panel;          // tiles along M (gradient) and N; width of a column panel of the tile order (product)
+    int32_t stream, lines;          // the gradient passes the caches by; the 256 x 256 tiles' waves write whole lines of it
 };
 
 // lcma_gated_silu, lcma_gated_silu_grad: row pitches in bytes.

@@ -2,7 +2,10 @@
 // placing of the operand halves are described there), for rows in groups, either form of both operands (csrc/lcma_experts.hpp), 64-bit bases, and as many steps as the rows of
 // an expert take (the gradient).
 // Half h of a k-contiguous operand holds the tile's rows 128 wm + 64 h .. + 63 of both wm (right operand: 64 wn + 32 h .. + 31 of all wn); of the other form it holds the columns
-// 128 h .. + 127, so a wave has rows 64 wm .. + 63 of both halves (right operand: columns 32 wn .. + 31).  What lies past a tile's rows or columns may be anything: it
+// 128 h .. + 127, so a wave has rows 64 wm .. + 63 of both halves (right operand: columns 32 wn .. + 31).  LINES (gradients of few rows, which their stores bound): the right operand
+// is cut as a k-contiguous one all the same, so that a wave's 64 columns of C lie together and leave as whole lines, past the caches where they are such in memory; what it costs is loads of half lines
+// (1021 x 6 of 64, 2816 x 2048: 226 -> 179 us, 2816 x 2056, off lines: 272 -> 260; 1024 x 2 of 8, 4096 x 14336: 402 -> 324, but with 8192 tokens 1529 -> 1596; weights K x N, which come from
+// memory: 3 to 14 % slower).  What lies past a tile's rows or columns may be anything: it
 // reaches elements of C alone that are not there.  What lies past the last k reads as zero, on both sides: k-contiguous, 16 bytes at a time from past the extent; else by the extent.
 // Every work-group walks through tiles of its own, in turn; the loads run two steps ahead, into the next tile too.
 // Bound by power, as one large product: bf16, 8192 x 2 of 8, 4096 x 14336: 1620 us, 1.19 PFLOP/s (128 x 256 takes 1960, 64 x 128 2790), gradients 1550 and 1600; the matrix pipe is at work in 83, 83 and
@@ -12,10 +15,11 @@
 
 namespace lcma {
 
-template <class T, bool ACOL, bool BCOL, bool GRAD> struct ExpPingPong {
+template <class T, bool ACOL, bool BCOL, bool GRAD, bool LINES = false> struct ExpPingPong {
     static constexpr int NT = 512, ROW = 128, NK = 4, TM = 256, TN = 256, NMI = 4, NNI = 2, KS = 64;
     static constexpr int HALF = 128 * ROW, LDS_BYTES = 8 * HALF + 8 * 4096;
-    static_assert(LDS_BYTES <= 160 * 1024 && T::ES == 2, "LDS budget of one CU");
+    static constexpr int B_GAP = BCOL && !LINES ? 128 : 32; // columns of C from a wave's first 32 to its others
+    static_assert(LDS_BYTES <= 160 * 1024 && T::ES == 2 && (GRAD || !LINES), "LDS budget of one CU");
     static constexpr uint32_t NONE = 1u << 30; // an offset past any extent
     using Frag = typename Mma<T>::frag;
     typedef const __attribute__((address_space(4))) ExpertsGemmParams *Args;
@@ -23,7 +27,7 @@ template <class T, bool ACOL, bool BCOL, bool GRAD> struct ExpPingPong {
     // (the argument block is read where it is needed: its fields, kept through the steps, would push the offsets of the loads out of the scalar registers)
     static LCMA_DEV ExpertsGemmParams arguments(Args at) {
         asm volatile("" : "+s"(at));
-        return ExpertsGemmParams{at->A, at->B, at->C, at->offsets, at->lda_b, at->ldb_b, at->ldc_b, at->expert_b, at->rows, at->M, at->N, at->K, at->experts, at->nx, at->nz, at->panel};
+        return ExpertsGemmParams{at->A, at->B, at->C, at->offsets, at->lda_b, at->ldb_b, at->ldc_b, at->expert_b, at->rows, at->M, at->N, at->K, at->experts, at->nx, at->nz, at->panel, at->stream};
     }
     static LCMA_DEV void slot_end() {
         __builtin_amdgcn_sched_barrier(0);
@@ -115,10 +119,11 @@ template <class T, bool ACOL, bool BCOL, bool GRAD> struct ExpPingPong {
         int job = unit < whole ? unit : (int)blockIdx.x;
         if (job >= jobs) return;
         const uint32_t lda = (uint32_t)args->lda_b, ldb = (uint32_t)args->ldb_b;
-        // load q of a thread fills row q * 64 + tid / 8 of a half, position tid % 8; of the other form row (k) q * 32 + tid / 16, position tid % 16
+        // load q of a thread fills row q * 64 + tid / 8 of a half, position tid % 8; of the other form row (k) q * 32 + tid / 16, position tid % 16 (LINES, right
+        // operand: four chunks of every 64 columns)
         const int row = tid >> 3, pos = exp_row_chunk(row, tid & 7), k16 = tid >> 4, pos16 = exp_col_chunk<T, 128>(k16, tid & 15);
-        const uint32_t a_voff = ACOL ? k16 * lda + pos16 * 16 : row * lda + pos * 16, b_voff = BCOL ? k16 * ldb + pos16 * 16 : (uint32_t)((row >> 5) * 64 + (row & 31)) * ldb + pos * 16;
-        const uint32_t a_rows = (ACOL ? 32 : 128) * lda, b_rows = (BCOL ? 32 : 128) * ldb, a_half = ACOL ? 256 : 64 * lda, b_half = BCOL ? 256 : 32 * ldb;
+        const uint32_t a_voff = ACOL ? k16 * lda + pos16 * 16 : row * lda + pos * 16, b_voff = BCOL ? k16 * ldb + (LINES ? (pos16 >> 2) * 128 + (pos16 & 3) * 16 : pos16 * 16) : (uint32_t)((row >> 5) * 64 + (row & 31)) * ldb + pos * 16;
+        const uint32_t a_rows = (ACOL ? 32 : 128) * lda, b_rows = (BCOL ? 32 : 128) * ldb, a_half = ACOL ? 256 : 64 * lda, b_half = LINES ? 64 : BCOL ? 256 : 32 * ldb;
         const uint32_t a_step = ACOL ? KS * lda : ROW, b_step = BCOL ? KS * ldb : ROW;
         // k-contiguous: the 16 bytes past the last k in the last step, read from past the extent
         auto last_voff = [&](bool col, uint32_t voff, int k) { return !col && (uint32_t)pos * 8 >= (uint32_t)((k - 1) % KS + 1) ? NONE : voff; };
@@ -201,9 +206,10 @@ template <class T, bool ACOL, bool BCOL, bool GRAD> struct ExpPingPong {
             if (!wm) slot_end(); // both groups write their halves of the tile in one slot
             if (next >= jobs) __builtin_amdgcn_s_waitcnt(0x0070); // loads past the end land before the LDS is another work-group's
             {
-                const int64_t ldc_b = arguments(args).ldc_b;
-                const int r0 = wm * (ACOL ? 64 : 128), c0 = wn * (BCOL ? 32 : 64);
-                exp_store<T, NMI, NNI, ACOL, BCOL ? 128 : 32>(strips + w * 4096, cur.c + r0 * ldc_b + c0 * T::ES, ldc_b, cur.am - r0, cur.bn - c0, acc);
+                const ExpertsGemmParams p = arguments(args);
+                const int64_t ldc_b = p.ldc_b;
+                const int r0 = wm * (ACOL ? 64 : 128), c0 = wn * (B_GAP == 128 ? 32 : 64);
+                exp_store<T, NMI, NNI, ACOL, B_GAP, 32, LINES>(strips + w * 4096, cur.c + r0 * ldc_b + c0 * T::ES, ldc_b, cur.am - r0, cur.bn - c0, acc, p.stream);
             }
             if (wm) slot_end();
             if (next >= jobs) break;

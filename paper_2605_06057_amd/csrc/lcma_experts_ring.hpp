@@ -69,7 +69,7 @@ template <class T, bool ACOL, bool BCOL, bool GRAD, int TM, int TN, int WGM, int
         multiply(p, j, w, wm, wn, acc, lds, lds + STAGE, lds + 2 * STAGE, lds + (S == 4 ? 3 * STAGE : 0));
         __syncthreads(); // no load is in flight and every wave has read its last step: the strips take the place of the stages
         const int row = wm * NMI * 32, col = wn * NNI * 32;
-        exp_store<T, NMI, NNI>(lds + w * 4096, j.c + (int64_t)row * p.ldc_b + (int64_t)col * T::ES, p.ldc_b, j.am - row, j.bn - col, acc);
+        exp_store<T, NMI, NNI, false, 32, 32, GRAD>(lds + w * 4096, j.c + (int64_t)row * p.ldc_b + (int64_t)col * T::ES, p.ldc_b, j.am - row, j.bn - col, acc, p.stream);
     }
     // restrict: the loads in flight towards one stage do not touch what is read from another (the compiler would otherwise wait for all of them in
     // front of every read)

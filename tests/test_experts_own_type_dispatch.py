@@ -20,7 +20,7 @@ static int g_ask = -1;
 extern "C" long seen(int i) { return g_seen[i]; }
 extern "C" void ask(int kernel) { g_ask = kernel; }
 extern "C" int lcma_launch_experts_gemm(const lcma::ExpertsGemmParams *p, int form, int kernel, int dtype, int grid, void *) {
-    g_seen[0] = kernel; g_seen[1] = grid; g_seen[2] = p->nz; g_seen[3] = p->nx; g_seen[4] = form; g_seen[5] = dtype; return 0; }
+    g_seen[0] = kernel; g_seen[1] = grid; g_seen[2] = p->nz; g_seen[3] = p->nx; g_seen[4] = form; g_seen[5] = dtype; g_seen[6] = p->stream; g_seen[7] = p->lines; return 0; }
 extern "C" int lcma_launch_i4_gemm(const lcma::I4GemmParams *p, int kernel, int group, int dtype, int grid, void *) {
     g_seen[0] = kernel; g_seen[1] = grid; g_seen[2] = p->nz; g_seen[3] = group; g_seen[4] = p->blocks; g_seen[5] = dtype; return 0; }
 extern "C" int lcma_launch_i4_prepare(const lcma::I4PrepareParams *, int dtype, int grid, void *) { g_seen[0] = dtype; g_seen[1] = grid; return 0; }
@@ -160,6 +160,16 @@ def test_operands_off_whole_16_bytes_go_to_kernels_that_take_any(lib, ask):
         assert not product(lib, rows, 512, 512, 8, ldc=513)[0].startswith("any") or ask in (0, 1, 2)
         # fp32 has kernels for any sizes alone
         assert product(lib, rows, 511, 333, 8, dtype=F32, lda=335, a=4, w=4)[0] == product(lib, rows, 511, 333, 8, dtype=F32)[0]
+
+
+def test_gradients_that_pass_the_caches_by(lib):
+    """In rows of whole 128-byte lines from such a line on; the largest tiles' waves write lines where an expert has up to 512 rows on average."""
+    def of(rows, K, E, at=0, dtype=BF16):
+        assert lib.lcma_gemm_experts_grad(rows, 512, K, E, AT[4], AT[0], 512, AT[1], K, AT[2] + at, dtype, None) == 0
+        return bool(lib.seen(6)), bool(lib.seen(7))
+
+    assert of(4096, 512, 8) == (True, True) and of(4097, 512, 8) == (True, False)
+    assert of(100, 32, 8)[0] is False and of(100, 32, 8, dtype=F32)[0] is True and of(100, 520, 8)[0] is False and of(100, 512, 8, at=16)[0] is False
 
 
 @pytest.mark.parametrize("ask", range(-1, len(NAMES)))

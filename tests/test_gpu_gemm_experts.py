@@ -111,6 +111,24 @@ def test_gradient_of_whole_numbers(kernel, counts, N, K, pad, behind, dtype):
     assert (dw[0] == 99.0).all() and (dw[-1] == 99.0).all()
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("off", [0, 8, 32])
+@pytest.mark.parametrize("counts", [[1], [0, 40, 300], [1500, 100]], ids=lambda c: f"{sum(c)}of{len(c)}")
+@pytest.mark.parametrize("N,K", [(300, 320), (512, 576), (256, 256), (257, 1024), (70, 64)])
+def test_gradient_in_rows_of_whole_lines(kernel, N, K, counts, off, dtype):
+    """Rows of 128, 512, ... bytes from a multiple of 128 on or not: what is written past the caches and what is not, with many rows an expert and with few."""
+    torch, types = _torch()
+    gen = torch.Generator(device="cuda").manual_seed(N + K + off)
+    E, rows = len(counts), sum(counts)
+    dc, a = _whole(gen, rows, N).to(types[dtype]), _whole(gen, rows, K).to(types[dtype])
+    room = torch.full((E * N * K + off + 64,), 99.0, device="cuda").to(types[dtype])
+    dw = room[off:off + E * N * K].view(E, N, K)
+    offsets = _offsets(counts)
+    _lib().lcma_gemm_experts_grad(dc, a, offsets, dw)
+    assert np.array_equal(_np(dw), _rounded(X.gemm_experts_grad(_np(dc), _np(a), offsets.cpu().numpy()), dtype))
+    assert (room[:off] == 99.0).all() and (room[off + E * N * K:] == 99.0).all()
+
+
 def _close(got, want, magnitude, k, dtype):
     torch, types = _torch()
     f = torch.finfo(types[dtype])
