@@ -48,7 +48,7 @@ template <class T, int TM, int TN> LCMA_DEV ExpJob gradient_job(const ExpertsGem
 
 // Tiles of the gradient to work-groups, one each: eighths of an expert's tiles to the XCDs in turn (work-groups go to the eight in turn), so that each of them has a share of every
 // expert: an expert's tiles take as long as it has rows, and an XCD that had whole experts would be done long before another (fp32, 2331 rows spread
-// unequally over 12 experts, 1001 x 515: 41 us so, now 37).  -1: none.  The launch holds whole eights of such eighths.
+// unequally over 12 experts, 1001 x 515: 41 us so, 37 now).  -1: none.  The launch holds whole eights of such eighths.
 LCMA_DEV int exp_gradient_tile(const ExpertsGemmParams &p) {
     const int of = p.nx * p.nz, q = (of + 7) >> 3, i = (int)(blockIdx.x >> 3), job = (i / q * 8 + (int)(blockIdx.x & 7)) * q + i % q;
     return job < p.experts * of ? job : -1;
@@ -85,6 +85,39 @@ template <class T, int R> LCMA_DEV void exp_columns(const LCMA_LDS char *tile, i
 #pragma unroll
     for (int j = 0; j < 4; ++j) f[j] = u32x4{r[j][0][0], r[j][0][1], r[j][1][0], r[j][1][1]};
 }
+// Two blocks of 32 columns, `block` even: one wait for both (gradient of 8192 x 2 of 8, 4096 x 14336: 1594 -> 1565 us).
+template <class T, int R> LCMA_DEV void exp_columns_pair(const LCMA_LDS char *tile, int block, u32x4 (&f0)[4], u32x4 (&f1)[4]) {
+    constexpr int P = R * 2;
+    const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4, k = i >> 2, c = block * 4 + (g & 1) * 2 + ((i & 3) >> 1);
+    const uint32_t row = (uint32_t)(uintptr_t)tile + ((g >> 1) * 8 + k) * P + (i & 1) * 8, a0 = row + exp_col_chunk<T, R>(k, c) * 16, a1 = row + exp_col_chunk<T, R>(k, c + 4) * 16;
+    u32x2 r[4][2], s[4][2];
+    asm volatile("ds_read_b64_tr_b16 %0, %16\n"
+                 "ds_read_b64_tr_b16 %1, %16 offset:%18\n"
+                 "ds_read_b64_tr_b16 %8, %17\n"
+                 "ds_read_b64_tr_b16 %9, %17 offset:%18\n"
+                 "ds_read_b64_tr_b16 %2, %16 offset:%19\n"
+                 "ds_read_b64_tr_b16 %3, %16 offset:%20\n"
+                 "ds_read_b64_tr_b16 %10, %17 offset:%19\n"
+                 "ds_read_b64_tr_b16 %11, %17 offset:%20\n"
+                 "ds_read_b64_tr_b16 %4, %16 offset:%21\n"
+                 "ds_read_b64_tr_b16 %5, %16 offset:%22\n"
+                 "ds_read_b64_tr_b16 %12, %17 offset:%21\n"
+                 "ds_read_b64_tr_b16 %13, %17 offset:%22\n"
+                 "ds_read_b64_tr_b16 %6, %16 offset:%23\n"
+                 "ds_read_b64_tr_b16 %7, %16 offset:%24\n"
+                 "ds_read_b64_tr_b16 %14, %17 offset:%23\n"
+                 "ds_read_b64_tr_b16 %15, %17 offset:%24\n"
+                 "s_waitcnt lgkmcnt(0)"
+                 : "=&v"(r[0][0]), "=&v"(r[0][1]), "=&v"(r[1][0]), "=&v"(r[1][1]), "=&v"(r[2][0]), "=&v"(r[2][1]), "=&v"(r[3][0]), "=&v"(r[3][1]), "=&v"(s[0][0]),
+                   "=&v"(s[0][1]), "=&v"(s[1][0]), "=&v"(s[1][1]), "=&v"(s[2][0]), "=&v"(s[2][1]), "=&v"(s[3][0]), "=&v"(s[3][1])
+                 : "v"(a0), "v"(a1), "n"(4 * P), "n"(16 * P), "n"(20 * P), "n"(32 * P), "n"(36 * P), "n"(48 * P), "n"(52 * P)
+                 : "memory");
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        f0[j] = u32x4{r[j][0][0], r[j][0][1], r[j][1][0], r[j][1][1]};
+        f1[j] = u32x4{s[j][0][0], s[j][0][1], s[j][1][0], s[j][1][1]};
+    }
+}
 // The four fragments of 32 rows (columns) from 32 block on of an operand with R of them.
 template <class T, bool COL, int R> LCMA_DEV void exp_fragments(const LCMA_LDS char *tile, int block, u32x4 (&f)[4]) {
     const int lane = threadIdx.x & 63, l32 = lane & 31, lh = lane >> 5;
@@ -105,7 +138,8 @@ template <class T, bool COL, int R> LCMA_DEV void exp_fragments(const LCMA_LDS c
 // A wave's part of a tile of C (NMI x NNI blocks of 32 x 32; rows, cols: of C from its first element on) rounded and stored: through SR rows of 128 bytes of LDS that are the
 // wave's own, so that it leaves as whole lines, 16 bytes a lane.  The right operand is the left one of the matrix instruction: a lane holds four neighbouring columns.
 // Blocks of rows follow each other, or, TWO, the second pair of them is 128 rows on; the blocks of columns are GAP columns apart.
-// FULL: all of it lies inside C.  STREAM: and passes the caches by, in whole 16 bytes.
+// FULL: all of it lies inside C.  STREAM: and passes the caches by, in whole lines (64 x 128 tiles, gradient of 1021 x 6 of 64, 2816 x 2048: 355 -> 292 us;
+// half lines a store were 340 -> 540 at 2 rows of 8 experts, 28672 x 4096).
 template <class T, int NMI, int NNI, bool TWO, int GAP, int SR, bool FULL, bool STREAM>
 LCMA_DEV void exp_store_rows(LCMA_LDS char *strip, char *c, int64_t ldc_b, int rows, int cols, const f32x16 (&acc)[NMI][NNI]) {
     constexpr int ES = T::ES, BLOCKS = ES == 4 ? 1 : NNI == 1 ? 1 : 2, L = BLOCKS * 32 * ES / 16, RPS = 64 / L; // 32-column blocks of a pass; lanes of a row, rows of a store

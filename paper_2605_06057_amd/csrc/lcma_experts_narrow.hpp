@@ -85,25 +85,23 @@ template <class T, bool BCOL> struct ExpNarrow {
         f32x16 acc[2][2];
         u32x4 a[NK], b[2][NK];
         auto read_a = [&](const LCMA_LDS char *st, int i) { exp_fragments<T, false, 128>(st, wm * 2 + i, a); };
-        auto read_b = [&](const LCMA_LDS char *st, int i) { // (columns: two waves to a half)
-            if constexpr (BCOL) exp_fragments<T, true, 128>(st + HALF + (wn >> 1) * HALF, (wn & 1) * 2 + i, b[i]);
-            else exp_fragments<T, false, 256>(st + HALF, wn * 2 + i, b[i]);
+        auto read_b = [&](const LCMA_LDS char *st) { // (columns: two waves to a half)
+            if constexpr (BCOL) {
+                exp_columns_pair<T, 128>(st + HALF + (wn >> 1) * HALF, (wn & 1) * 2, b[0], b[1]);
+            } else {
+                exp_fragments<T, false, 256>(st + HALF, wn * 2, b[0]);
+                exp_fragments<T, false, 256>(st + HALF, wn * 2 + 1, b[1]);
+            }
         };
         // one step out of stage st; `of`, y2: the step two on, which goes into the stage that the step before has read.  (Reads that wait for their results: behind the loads.)
         auto step = [&](bool real, LCMA_LDS char *st, LCMA_LDS char *into, const Source &of, int y2) {
             if (real) {
                 read_a(st, 0);
-                if constexpr (!BCOL) {
-                    read_b(st, 0);
-                    read_b(st, 1);
-                }
+                if constexpr (!BCOL) read_b(st);
             }
             load(c0, c3, of, into, y2);
             if constexpr (BCOL)
-                if (real) {
-                    read_b(st, 0);
-                    read_b(st, 1);
-                }
+                if (real) read_b(st);
             __builtin_amdgcn_sched_barrier(0);
             __builtin_amdgcn_s_waitcnt(0xC07F); // lgkmcnt(0)
             Turns::slot_end();

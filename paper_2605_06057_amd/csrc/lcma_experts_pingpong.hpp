@@ -8,7 +8,7 @@
 // memory: 3 to 14 % slower).  What lies past a tile's rows or columns may be anything: it
 // reaches elements of C alone that are not there.  What lies past the last k reads as zero, on both sides: k-contiguous, 16 bytes at a time from past the extent; else by the extent.
 // Every work-group walks through tiles of its own, in turn; the loads run two steps ahead, into the next tile too.
-// Bound by power, as one large product: bf16, 8192 x 2 of 8, 4096 x 14336: 1620 us, 1.19 PFLOP/s (128 x 256 takes 1960, 64 x 128 2790), gradients 1550 and 1600; the matrix pipe is at work in 83, 83 and
+// Bound by power, as one large product: bf16, 8192 x 2 of 8, 4096 x 14336: 1620 us, 1.19 PFLOP/s (128 x 256 takes 1960, 64 x 128 2790), gradients 1550 and 1570; the matrix pipe is at work in 83, 83 and
 // 71 % of the clocks, of which there are 1.5 to 1.8 in a nanosecond.
 #pragma once
 #include "lcma_experts_ring.hpp"
@@ -131,8 +131,12 @@ template <class T, bool ACOL, bool BCOL, bool GRAD, bool LINES = false> struct E
         u32x4 fa0[2][NK], fa1[2][NK], fb0[NK], fb1[NK];
         f32x16 acc[NMI][NNI];
         auto read_a = [&](const LCMA_LDS char *half, u32x4 (&f)[2][NK]) {
-            read<ACOL>(half, wm * 2, f[0]);
-            read<ACOL>(half, wm * 2 + 1, f[1]);
+            if constexpr (ACOL) {
+                exp_columns_pair<T, 128>(half, wm * 2, f[0], f[1]);
+            } else {
+                read<false>(half, wm * 2, f[0]);
+                read<false>(half, wm * 2 + 1, f[1]);
+            }
         };
         auto read_b = [&](const LCMA_LDS char *half, u32x4 (&f)[NK]) { read<BCOL>(half, wn, f); };
         auto steps_of = [&](int k) { return k > KS ? (int)(((uint32_t)k + (KS - 1)) / KS) : 1; };

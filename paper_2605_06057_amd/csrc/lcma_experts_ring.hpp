@@ -37,7 +37,7 @@ template <int N> LCMA_DEV void exp_end_of_k(u32x4 (&f)[N][4], int left) {
 // count, and one barrier a step says that all waves' parts of it have landed and that all have read the stage that is loaded anew (csrc/lcma_i8.hpp has the
 // same with its measurements).  Bound by memory at hundreds of rows, by the loads' way through LDS above: bf16, rows of 128 x 2 of 8, 2048 x 1024: 8.3 us on 64 x 64 (weights at 4.0 TB/s; 32 x 32 takes
 // 11.1), 9.0 on 64 x 128; fp16 1021 x 6 of 64, 2816 x 2056: 287 and 255 against 213 on 128 x 256.  fp32 (64 x 64 alone, by the matrix pipe, 68 % of which is at work): 777 x 3 of 12, 1001 x 515: 33 us,
-// gradients 38 and 37; 4096 x 2 of 8, 2048 x 2048: 538 (128 TFLOP/s).
+// gradients 39 and 35; 4096 x 2 of 8, 2048 x 2048: 538 (128 TFLOP/s).
 template <class T, bool ACOL, bool BCOL, bool GRAD, int TM, int TN, int WGM, int WGN, int S> struct ExpRing {
     static constexpr int NT = 64 * WGM * WGN, NMI = TM / WGM / 32, NNI = TN / WGN / 32, KS = 128 / T::ES;
     static constexpr int A_STAGE = TM * 128, STAGE = (TM + TN) * 128, LDS_BYTES = S * STAGE, QA = TM * 8 / NT, QB = TN * 8 / NT;
