@@ -657,7 +657,7 @@ def lcma_gemm_experts(A, offsets, W, C=None, b_nk: bool = True):
     """C (rows x N): rows offsets[e] .. offsets[e + 1] - 1 of A (rows x K) times the weights W[e]^T (W: experts x N x K), or, without b_nk, times W[e] (experts x K x N:
     the gradient of A from that of C, with the weights of the other layout); rows of C behind the last expert's are set to zero."""
     if C is None:
-        C = _empty(A, A.shape[0], W.shape[1 if b_nk else 2])
+        C = _empty(A, A.shape[0], W.shape[-2 if b_nk else -1])
     if status := (_calls or _native()).gemm_experts(A, offsets, W, C, b_nk):
         _check(status)
     return C
