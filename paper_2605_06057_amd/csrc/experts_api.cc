@@ -39,7 +39,7 @@ bool whole_vectors(int es, const void *A, int64_t lda_b, const void *B, int64_t 
 // What a kernel takes, in us: `start`; a tile: `end`, and `step` for every 128 bytes of K, 256 * `slots` tiles at a time; and no less than the bytes at `rate` GB/us take.  With rows that
 // are no whole lines of 128 bytes a step takes `off` of its time more and the bytes half of that.  start 0: not taken.  Fitted to 164 layers in 16 bit, 94 in fp32 and 130 of sizes
 // that are no whole 16 bytes, of 1 to 8192 tokens and 8 to 128 experts, timed on every kernel: a single time is predicted within 10 to 31 % (root mean square); the kernel with the smallest
-// prediction is 1.3 to 2.4 % slower than the fastest one on average in whole 16 bytes (37 % at worst), 0.2 to 1.4 % in fp32 (32 %), 1.4 to 3.5 % in other sizes (73 %).
+// prediction is 1.2 to 2.4 % slower than the fastest one on average in whole 16 bytes (31 % at worst, of the gradient 65 %), 0.2 to 0.6 % in fp32 (18 %), 1.4 to 3.5 % in other sizes (73 %).
 struct Cost {
     double start, end, step, rate, slots, off;
 };
@@ -49,10 +49,10 @@ const Cost kVectors[kForms][kExpKernels] = {
      {3.57, 1.83, 0.71, 5.44, 0.591, 0.0682}, {4.63, 0.567, 0.977, 4.55, 0.584, 0.0691}},
     {{}, {}, {}, {}, {1.97, 0.596, 0.0866, 5.53, 0.604, 0.0683}, {2.15, 0.344, 0.256, 6.65, 0.821, 0.0253}, {2.25, 0.764, 0.373, 6.08, 0.788, 0}, {3.23, 2.24, 0.768, 5.83, 0.633, 0},
      {4.99, 0.065, 1.01, 4.75, 0.615, 0}},
-    {{}, {}, {}, {}, {}, {2.19, 0.0769, 0.0613, 3.11, 0.177, 0.0761}, {2.53, 0.695, 0.43, 3.93, 0.781, 0.0505}, {}, {5.6, 2.17, 1.14, 4.96, 0.565, 0.227}}};
+    {{}, {}, {}, {}, {}, {2.41, 1.19, 0.459, 3.86, 2.25, 0.284}, {2.77, 1.17, 0.448, 4.53, 1.31, 0.273}, {}, {5.47, 1.85, 0.977, 5.66, 0.552, 0.386}}};
 const Cost kF32[kForms][kExpKernels] = {{{}, {}, {}, {}, {2.59, 0.891, 0.152, 5.93, 0.928, 0.0706}, {2.86, 0.396, 0.563, 6.81, 1.03, 0}},
                                         {{}, {}, {}, {}, {2.24, 1.22, 0.16, 7.18, 0.961, 0.0109}, {2.3, 0.878, 0.599, 5.28, 1.11, 0.0132}},
-                                        {{2.93, 0.007, 1.62, 11.7, 1.5, 0.0153}, {}, {}, {}, {}, {2.6, 0.0063, 0.0374, 3.73, 0.0456, 0.0594}}};
+                                        {{3.11, 0.013, 1.09, 5.6, 1.5, 0.12}, {}, {}, {}, {}, {2.89, 0.000258, 0.000758, 4.66, 0.00135, 0.203}}};
 const Cost kAny[kForms][kExpKernels] = {{{1.98, 1.45, 0.774, 5.02, 2.17, 0.208}, {2.21, 3.11, 1.37, 4.11, 1.51, 0.191}, {1.74, 3.17, 0.401, 3.66, 1.98, 0.05}},
                                         {{1.25, 0, 1.82, 3.62, 3.35, 0.25}, {0.395, 0, 3.4, 2, 3.17, 0.269}, {1.53, 1.51, 0.833, 2.71, 2.97, 0.193}},
                                         {{2.38, 0, 3.69, 3.08, 6.56, 0.297}, {3.76, 0, 5.01, 3.67, 2.82, 0.33}}};
