@@ -263,7 +263,7 @@ template <class T, bool ACOL, bool BCOL, bool GRAD, int TM, int TN, int WGM, int
         } else {
             const I8Rows<TM, ExpertsGemmParams> groups(p);
             exp_zero_behind<T, NT>(p, groups.behind);
-            const int nx = groups.tiles, jobs = nx * p.nz, per = (jobs + 7) / 8, job = (int)(blockIdx.x & 7) * per + (int)(blockIdx.x >> 3);
+            const int nx = groups.within(p), jobs = nx * p.nz, per = (jobs + 7) / 8, job = (int)(blockIdx.x & 7) * per + (int)(blockIdx.x >> 3);
             if ((int)(blockIdx.x >> 3) >= per || job >= jobs) return;
             int x, z;
             i8_tile_of_job(nx, p.nz, p.panel, job, x, z);

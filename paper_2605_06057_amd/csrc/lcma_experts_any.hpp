@@ -33,7 +33,7 @@ template <class T, bool BCOL, int WK> struct ExpAnyFewRows {
         const int lane = threadIdx.x & 63, l32 = lane & 31, lh = lane >> 5, wk = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         const I8Rows<R, ExpertsGemmParams> groups(p);
         exp_zero_behind<T, 64 * WK>(p, groups.behind);
-        const int nx = groups.tiles, jobs = nx * p.nz, per = (jobs + 7) / 8;
+        const int nx = groups.within(p), jobs = nx * p.nz, per = (jobs + 7) / 8;
         const int job = (blockIdx.x & 7) * per + (blockIdx.x >> 3); // an eighth of the tiles to every XCD, row tiles that share weights next to each other
         if ((int)(blockIdx.x >> 3) >= per || job >= jobs) return;
         int x, z;

@@ -42,7 +42,7 @@ template <class T, bool BCOL> struct ExpNarrow {
             const ExpertsGemmParams p = Turns::arguments(args);
             const I8Rows<TM, ExpertsGemmParams> groups(p);
             exp_zero_behind<T, NT>(p, groups.behind);
-            nx = groups.tiles;
+            nx = groups.within(p);
             jobs = nx * p.nz;
         }
         const int units = gridDim.x, per = units >> 3; // rounds of one tile per work-group, as in ExpPingPong

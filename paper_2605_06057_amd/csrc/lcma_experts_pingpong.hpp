@@ -107,7 +107,7 @@ template <class T, bool ACOL, bool BCOL, bool GRAD, bool LINES = false> struct E
             } else {
                 const I8Rows<TM, ExpertsGemmParams> groups(p);
                 exp_zero_behind<T, NT>(p, groups.behind);
-                nx = groups.tiles;
+                nx = groups.within(p);
                 jobs = nx * p.nz;
             }
         }

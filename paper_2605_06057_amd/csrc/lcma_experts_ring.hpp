@@ -54,7 +54,7 @@ template <class T, bool ACOL, bool BCOL, bool GRAD, int TM, int TN, int WGM, int
         } else {
             const I8Rows<TM, ExpertsGemmParams> groups(p);
             exp_zero_behind<T, NT>(p, groups.behind);
-            const int nx = groups.tiles, jobs = nx * p.nz, per = (jobs + 7) / 8, job = (int)(blockIdx.x & 7) * per + (int)(blockIdx.x >> 3);
+            const int nx = groups.within(p), jobs = nx * p.nz, per = (jobs + 7) / 8, job = (int)(blockIdx.x & 7) * per + (int)(blockIdx.x >> 3);
             if ((int)(blockIdx.x >> 3) >= per || job >= jobs) return;
             int x, z;
             i8_tile_of_job(nx, p.nz, p.panel, job, x, z);
@@ -154,7 +154,7 @@ template <class T, bool BCOL, int R, int WK, int S> struct ExpFewRows {
         const int lane = threadIdx.x & 63, fr = lane & (F - 1), fk = lane / F, wk = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         const I8Rows<R, ExpertsGemmParams> groups(p);
         exp_zero_behind<T, 64 * WK>(p, groups.behind);
-        const int nx = groups.tiles, jobs = nx * p.nz, per = (jobs + 7) / 8;
+        const int nx = groups.within(p), jobs = nx * p.nz, per = (jobs + 7) / 8;
         const int job = (blockIdx.x & 7) * per + (blockIdx.x >> 3); // an eighth of the tiles to every XCD, row tiles that share weights next to each other
         if ((int)(blockIdx.x >> 3) >= per || job >= jobs) return;
         int x, z;

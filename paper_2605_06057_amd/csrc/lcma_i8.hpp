@@ -64,6 +64,11 @@ template <int TM, class P = I8GemmParams> struct I8Rows {
             behind = __builtin_amdgcn_readlane(more.end, (p.experts - 1) & 63);
         }
     }
+    // All tiles, and no more than ascending offsets can make: the launch's count, which fits 32 bits with the tiles along the columns.
+    LCMA_DEV int within(const P &p) const {
+        const int most = p.rows / TM + (p.rows < p.experts ? p.rows : p.experts);
+        return tiles < most ? tiles : most;
+    }
     LCMA_DEV I8Place place(const P &p, int x) const {
         if (!p.offsets) return {x * TM, p.rows - x * TM < TM ? p.rows - x * TM : TM, 0, 0};
         I8Rows at = *this;

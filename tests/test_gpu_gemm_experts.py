@@ -224,6 +224,24 @@ def test_offsets_outside_the_rows_reach_nothing():
                                        X.gemm_experts_grad(_np(a), _np(a), [0, 3, 5])[1], "bf16"))
 
 
+def test_offsets_that_do_not_ascend_write_nothing_else(kernel):
+    """What the rows hold then is not specified; what lies around them stays, and other calls are right."""
+    torch, types = _torch()
+    L, gen = _lib(), torch.Generator(device="cuda").manual_seed(5)
+    rows, N, K, E = 300, 136, 72, 64
+    a, w = _whole(gen, rows, K).bfloat16(), _whole(gen, E, N, K).bfloat16()
+    room = torch.full((rows + 20, N), 7.0, device="cuda").bfloat16()
+    weights = torch.full((E + 2, N, K), 7.0, device="cuda").bfloat16()
+    for values in ([0, rows] * 32 + [0], [rows, 0] * 32 + [rows], [0, 2 ** 31 - 1] * 32 + [5], [-2 ** 31, 2 ** 31 - 1] * 32 + [7]):
+        offsets = torch.tensor(values, dtype=torch.int32, device="cuda")
+        L.lcma_gemm_experts(a, offsets, w, room[10:-10])
+        L.lcma_gemm_experts_grad(room[10:-10].nan_to_num(0.0), a, offsets, weights[1:-1])
+        torch.cuda.synchronize()
+        assert all((t == 7.0).all() for t in (room[:10], room[-10:], weights[0], weights[-1]))
+    right = L.lcma_gemm_experts(a, torch.tensor([0] * 64 + [rows], dtype=torch.int32, device="cuda"), w)
+    assert torch.equal(right, (a.float() @ w[-1].float().t()).bfloat16())
+
+
 def test_empty_calls():
     torch, types = _torch()
     L, new = _lib(), lambda *s: torch.full(s, 5.0, device="cuda").bfloat16()
