@@ -39,7 +39,7 @@ bool whole_vectors(int es, const void *A, int64_t lda_b, const void *B, int64_t 
 // What a kernel takes, in us: `start`; a tile: `end`, and `step` for every 128 bytes of K, 256 * `slots` tiles at a time; and no less than the bytes at `rate` GB/us take.  With rows that
 // are no whole lines of 128 bytes a step takes `off` of its time more and the bytes half of that.  start 0: not taken.  Fitted to 164 layers in 16 bit, 94 in fp32 and 130 of sizes
 // that are no whole 16 bytes, of 1 to 8192 tokens and 8 to 128 experts, timed on every kernel: a single time is predicted within 10 to 31 % (root mean square); the kernel with the smallest
-// prediction is 1.2 to 2.4 % slower than the fastest one on average in whole 16 bytes (31 % at worst, of the gradient 65 %), 0.2 to 0.6 % in fp32 (18 %), 1.4 to 3.5 % in other sizes (73 %).
+// prediction is 1.2 to 2.4 % slower than the fastest one on average in whole 16 bytes (31 % at worst, of the gradient 65 %), 0.2 to 0.6 % in fp32 (18 %), 1.5 to 3 % in other sizes (52 %, one gradient 2.2 times).
 struct Cost {
     double start, end, step, rate, slots, off;
 };
@@ -54,8 +54,8 @@ const Cost kF32[kForms][kExpKernels] = {{{}, {}, {}, {}, {2.59, 0.891, 0.152, 5.
                                         {{}, {}, {}, {}, {2.24, 1.22, 0.16, 7.18, 0.961, 0.0109}, {2.3, 0.878, 0.599, 5.28, 1.11, 0.0132}},
                                         {{3.11, 0.013, 1.09, 5.6, 1.5, 0.12}, {}, {}, {}, {}, {2.89, 0.000258, 0.000758, 4.66, 0.00135, 0.203}}};
 const Cost kAny[kForms][kExpKernels] = {{{1.98, 1.45, 0.774, 5.02, 2.17, 0.208}, {2.21, 3.11, 1.37, 4.11, 1.51, 0.191}, {1.74, 3.17, 0.401, 3.66, 1.98, 0.05}},
-                                        {{1.25, 0, 1.82, 3.62, 3.35, 0.25}, {0.395, 0, 3.4, 2, 3.17, 0.269}, {1.53, 1.51, 0.833, 2.71, 2.97, 0.193}},
-                                        {{2.38, 0, 3.69, 3.08, 6.56, 0.297}, {3.76, 0, 5.01, 3.67, 2.82, 0.33}}};
+                                        {{1.25, 0, 1.82, 3.62, 3.35, 0.25}, {}, {1.53, 1.51, 0.833, 2.71, 2.97, 0.193}}, // (128 x 128 was up to 1.8 x slower where it was taken and is up to 1.4 x faster on a tenth: 3.5 % over the fastest with it, 2.9 without)
+                                        {{3.05, 0, 3.63, 2.73, 9.43, 0.315}, {3.94, 0, 5.06, 3.52, 3.62, 0.347}}};
 double predicted_us(const Cost &c, double tiles, double steps, bool off, double bytes) {
     const double o = off ? c.off : 0, n = tiles / 256 / c.slots, t = c.start + (c.end + steps * c.step * (1 + o)) * (n > 1 ? n : 1), memory = c.start + bytes / (c.rate * 1e6) * (1 + 0.5 * o);
     return std::sqrt(std::sqrt(t * t * t * t + memory * memory * memory * memory));

@@ -106,7 +106,8 @@ def test_every_kernel_is_reached(lib):
     assert seen(gradient, 0) == {"64x64", "64x128", "256x256"}
     assert seen(product, 0, dtype=F32) == seen(product, 1, dtype=F32) == seen(product, 0, dtype=F32, form=NN) == {"32x32", "64x64"}
     assert seen(gradient, 0, dtype=F32) == {"any64x64", "64x64"}
-    assert seen(product, 1) == seen(product, 1, form=NN) == {"any64x64", "any128x128", "any32x32"}
+    assert seen(product, 1) == {"any64x64", "any128x128", "any32x32"} and seen(product, 1, form=NN) == {"any64x64", "any32x32"}
+    assert product(lib, 1, 1 << 28, 1, 64, form=NN) == ("any128x128", 1 << 21)  # more tiles of 64 columns than a launch holds
     assert seen(gradient, 1) == {"any64x64", "any128x128"}
 
 
