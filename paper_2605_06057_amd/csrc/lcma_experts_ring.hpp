@@ -13,11 +13,12 @@ template <class P> LCMA_DEV P *exp_uniform(P *at) {
     const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)at), hi = __builtin_amdgcn_readfirstlane((uint32_t)((uintptr_t)at >> 32));
     return (P *)(__attribute__((address_space(1))) P *)((uint64_t)hi << 32 | lo);
 }
-// The rows of the stored matrix from step y on, `steps` steps of them; none past the last k.
+// The rows of the stored matrix from step y on, `steps` steps of them; none past the last k.  The extent ends behind the dword of the last column: the range is checked by whole dwords, and a 16-bit
+// gradient's columns may be odd in rows of whole 16 bytes (what the dword holds besides belongs to a column that is not there).
 template <class T> LCMA_DEV __amdgpu_buffer_rsrc_t exp_columns_from(const char *at, int wide, int k, uint32_t ld_b, int y, int steps) {
     constexpr int KS = 128 / T::ES;
     const int left = (int)((uint32_t)k - (uint32_t)y * KS), n = left < steps * KS ? left : steps * KS; // (unsigned: y * KS may lie past 2^31, behind k)
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(at) + (int64_t)y * KS * ld_b, 0, n > 0 ? (n - 1) * (int)ld_b + wide * T::ES : 0, 0x00020000);
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(at) + (int64_t)y * KS * ld_b, 0, n > 0 ? (n - 1) * (int)ld_b + ((wide * T::ES + 3) & ~3) : 0, 0x00020000);
 }
 template <class T> LCMA_DEV __amdgpu_buffer_rsrc_t exp_rows_of(const char *at, int wide, int k, uint32_t ld_b) {
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(at), 0, k > 0 ? (wide - 1) * (int)ld_b + k * T::ES : 0, 0x00020000);
