@@ -64,6 +64,12 @@ class ServedExperts4:
         return lcma.lcma_tokens_combine(y, position, weights)
 
 
+def first_derivative_only(ctx):
+    """The library's calls have no derivatives of their own: with create_graph, where gradients are computed to be differentiated, they would count as constants."""
+    if torch.is_grad_enabled() and any(getattr(ctx, "needs_input_grad", ())):
+        raise RuntimeError("the experts' layer has no second derivative: create_graph is not supported")
+
+
 class TrainedLinearExperts(torch.autograd.Function):
     """y[t] = sum over j of weights[t, j] * W[ids[t, j]] x[t], with the gradients of x, of the experts' matrices W (experts x out x in) and of weights."""
 
@@ -77,6 +83,7 @@ class TrainedLinearExperts(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, grad):
+        first_derivative_only(ctx)
         rows, w, position, offsets, weights, y = ctx.saved_tensors
         dy, dweights = lcma.lcma_tokens_combine_grad(grad.contiguous(), y, position, weights)
         dx = lcma.lcma_tokens_combine(lcma.lcma_gemm_experts(dy, offsets, w, b_nk=False), position)
@@ -98,6 +105,7 @@ class TrainedExperts(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, grad):
+        first_derivative_only(ctx)
         rows, h, y, w_in, w_out, position, offsets, weights = ctx.saved_tensors
         dy, dweights = lcma.lcma_tokens_combine_grad(grad.contiguous(), y, position, weights)
         dw_out = lcma.lcma_gemm_experts_grad(dy, lcma.lcma_gated_silu(h), offsets)
