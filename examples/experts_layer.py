@@ -64,10 +64,13 @@ class ServedExperts4:
         return lcma.lcma_tokens_combine(y, position, weights)
 
 
-def first_derivative_only(ctx):
-    """The library's calls have no derivatives of their own: with create_graph, where gradients are computed to be differentiated, they would count as constants."""
-    if torch.is_grad_enabled() and any(getattr(ctx, "needs_input_grad", ())):
+def asked_for(ctx, n):
+    """Which of the n inputs' gradients a backward pass has to give: those that autograd names, all where it is called by itself.
+    The library's calls have no derivatives of their own: with create_graph, where gradients are computed to be differentiated, they would count as constants."""
+    needs = getattr(ctx, "needs_input_grad", None)
+    if needs is not None and torch.is_grad_enabled():
         raise RuntimeError("the experts' layer has no second derivative: create_graph is not supported")
+    return needs or (True,) * n
 
 
 class TrainedLinearExperts(torch.autograd.Function):
@@ -83,11 +86,11 @@ class TrainedLinearExperts(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, grad):
-        first_derivative_only(ctx)
+        need_x, need_w, _, need_weights = asked_for(ctx, 4)
         rows, w, position, offsets, weights, y = ctx.saved_tensors
         dy, dweights = lcma.lcma_tokens_combine_grad(grad.contiguous(), y, position, weights)
-        dx = lcma.lcma_tokens_combine(lcma.lcma_gemm_experts(dy, offsets, w, b_nk=False), position)
-        return dx, lcma.lcma_gemm_experts_grad(dy, rows, offsets), None, dweights
+        dx = lcma.lcma_tokens_combine(lcma.lcma_gemm_experts(dy, offsets, w, b_nk=False), position) if need_x else None
+        return dx, lcma.lcma_gemm_experts_grad(dy, rows, offsets) if need_w else None, None, dweights if need_weights else None
 
 
 class TrainedExperts(torch.autograd.Function):
@@ -105,13 +108,17 @@ class TrainedExperts(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, grad):
-        first_derivative_only(ctx)
+        need_x, need_in, need_out, _, need_weights = asked_for(ctx, 5)
         rows, h, y, w_in, w_out, position, offsets, weights = ctx.saved_tensors
         dy, dweights = lcma.lcma_tokens_combine_grad(grad.contiguous(), y, position, weights)
-        dw_out = lcma.lcma_gemm_experts_grad(dy, lcma.lcma_gated_silu(h), offsets)
-        dh = lcma.lcma_gated_silu_grad(lcma.lcma_gemm_experts(dy, offsets, w_out, b_nk=False), h)
-        dx = lcma.lcma_tokens_combine(lcma.lcma_gemm_experts(dh, offsets, w_in, b_nk=False), position)
-        return dx, lcma.lcma_gemm_experts_grad(dh, rows, offsets), dw_out, None, dweights
+        dx = dw_in = dw_out = None
+        if need_out:
+            dw_out = lcma.lcma_gemm_experts_grad(dy, lcma.lcma_gated_silu(h), offsets)
+        if need_x or need_in:
+            dh = lcma.lcma_gated_silu_grad(lcma.lcma_gemm_experts(dy, offsets, w_out, b_nk=False), h)
+            dx = lcma.lcma_tokens_combine(lcma.lcma_gemm_experts(dh, offsets, w_in, b_nk=False), position) if need_x else None
+            dw_in = lcma.lcma_gemm_experts_grad(dh, rows, offsets) if need_in else None
+        return dx, dw_in, dw_out, None, dweights if need_weights else None
 
 
 def train(x, target, w, router, top, steps):

@@ -1,4 +1,4 @@
-"""What autograd may ask of the experts' layers of examples/experts_layer.py beside the gradients themselves: second derivatives, which there are none of."""
+"""What autograd may ask of the experts' layers of examples/experts_layer.py beside the gradients themselves: some of them alone, and second derivatives, which there are none of."""
 import importlib.util
 import os
 
@@ -27,6 +27,24 @@ def _call(layer, name, needs):
     for t, n in zip(leaves, needs):
         t.requires_grad_(n)
     return getattr(layer, name).apply(*leaves[:-1], ids, leaves[-1]), leaves
+
+
+CASES = [("TrainedLinearExperts", n) for n in ((1, 1, 1), (1, 0, 0), (0, 1, 0), (0, 0, 1), (1, 0, 1))] + [
+    ("TrainedExperts", n) for n in ((1, 1, 1, 1), (1, 0, 0, 0), (0, 1, 0, 0), (0, 0, 1, 0), (0, 0, 0, 1), (1, 0, 0, 1))]
+
+
+@pytest.mark.parametrize("name,needs", CASES, ids=str)
+def test_gradients_that_are_not_asked_for_are_not_computed(layer, name, needs, monkeypatch):
+    import torch
+    everything, all_leaves = _call(layer, name, [True] * len(needs))
+    torch.autograd.backward(everything, torch.ones_like(everything))
+    grads, real = [], layer.lcma.lcma_gemm_experts_grad
+    monkeypatch.setattr(layer.lcma, "lcma_gemm_experts_grad", lambda *a: grads.append(1) or real(*a))
+    out, leaves = _call(layer, name, [bool(n) for n in needs])
+    torch.autograd.backward(out, torch.ones_like(out))
+    for t, full, n in zip(leaves, all_leaves, needs):
+        assert torch.equal(t.grad, full.grad) if n else t.grad is None
+    assert len(grads) == sum(needs[1:-1])
 
 
 @pytest.mark.parametrize("name", ["TrainedLinearExperts", "TrainedExperts"])
