@@ -276,7 +276,7 @@ PyObject *i4_quantize(PyObject *, PyObject *const *a, Py_ssize_t n) { // W, grou
         const int group = group_of(a[1]), gpu = gpu_of(w, "W");
         const On on((c10::DeviceIndex)gpu);
         if (K > 1 && w.stride(d - 1) != 1) refuse("W", "neighbouring elements in a row");
-        if (d == 3 && E > 1 && w.stride(0) != N * ld) refuse("W", "experts one behind the other");
+        if (d == 3 && E > 1 && N > 0 && w.stride(0) != N * ld) refuse("W", "experts one behind the other");
         void *q = prepared(a[2], d == 3 ? E : -1, lcma_i4_prepared_bytes(N, K, group), gpu);
         if (E == 0) return LCMA_OK;
         return lcma_i4_quantize(as_int(E), N, K, group, w.data_ptr(), ld, storage(w, "W"), q, stream_of(gpu));
