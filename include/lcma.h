@@ -508,8 +508,9 @@ lcma_status lcma_gated_silu_grad(int64_t rows, int64_t F, const void *dY, int64_
 /* ------------------------------------------------------------------ weights of 4 bits: a scale for each group of columns
  * The linear layer with weights of 4-bit integers and activations as they are (F32, BF16 or F16), for the few rows of single tokens, where reading the weights is all:
  *   C[m][n] = sum_k X[m][k] * q[n][k] * S[n][k / group]  (+ bias[n]),   q = -8 .. 7
- * group: 32, 64 or 128; the last group of a row may be short.  Every activation is multiplied exactly, sums run in fp32 (the terms of a group first, which are then
- * multiplied with its scale; their roundings count up to 2^-20 of sum |X| 8 S), one rounding.  An infinity or a NaN in a row of X, or a bf16 or fp32 value above 2^125, may give NaN in all of that
+ * group: 32, 64 or 128; the last group of a row may be short.  Every activation is multiplied exactly (of F32 the bits from 2^-126 up), sums run in fp32 (the terms of a group first, which are then
+ * multiplied with its scale: additions of up to 2 sum |X| of the group, times 16 S, so at the very worst, every one off the same way, by group * 2^-20 of sum |X| 8 S, F32 three times that; measured up
+ * to 2^-19.5, a plain fp32 sum over K up to 2^-19.4), one rounding.  An infinity or a NaN in a row of X, or a bf16 or fp32 value above 2^125, may give NaN in all of that
  * row of C; scales have to be below 2^123.
  * Weights are laid out once, into Wp (device memory, 16-byte aligned, lcma_i4_prepared_bytes() bytes for each expert; -1: bad sizes):
  *   lcma_i4_quantize   from values W (experts x N x K, rows ldw elements apart, experts N * ldw; experts = 1: one matrix): S = max |w| / 7 over a group, q = rint(w / S) with ties to
