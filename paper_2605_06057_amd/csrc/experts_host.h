@@ -12,6 +12,11 @@ constexpr int64_t kMatrixLimit = (int64_t)1 << 44; // elements of an expert's ma
 
 constexpr int64_t kGridLimit = (int64_t)1 << 32;  // threads of a launch along a dimension
 
+// Kernels with a work-group of up to 512 threads for each tile: whether one launch holds them all, whether several do (the device counts tiles in 32 bits), and what fills one: tiles of an eighth of them.
+inline bool one_launch(int64_t tiles) { return (tiles + 8) * 512 < kGridLimit / 2; }
+inline bool several_launches(int64_t tiles) { return tiles < kRowLimit - 1024; }
+constexpr int64_t kLaunchEighth = kGridLimit / 2 / 512 / 8 - 2;
+
 // the kernels of the product by number (lcma_experts_params.h), named by the rows and columns of their tiles
 constexpr const char *kI8KernelNames[kI8Kernels] = {"16x16", "32x32", "64x64", "64x128", "128x128", "128x256", "256x256"};
 int tuning_i8_kernel(); // csrc/api.cc; -1: choose

@@ -58,7 +58,6 @@ int64_t tiles_of(int kernel, int64_t rows, int64_t N, int experts, bool grouped)
     const int64_t tm = kTile[kernel][0], tn = kTile[kernel][1];
     return (grouped ? rows / tm + (rows < experts ? rows : experts) : (rows + tm - 1) / tm) * ((N + tn - 1) / tn);
 }
-bool launches(int64_t jobs) { return (jobs + 8) * 512 < kGridLimit / 2; } // (numbers of tiles are 32-bit on the device)
 
 // What a kernel takes, in us: `start`; a tile: `end`, `step` for every turn of its waves along K (fp32: 2.2 of them, three parts of X), `stage` for every byte of a column
 // of the rows of X that go through LDS, 256 * `slots` tiles at a time; and no less than the bytes at `rate` GB/us take.  Fitted to 268 products, alone and over experts, of 1 to 1024 rows, timed on every
@@ -113,21 +112,29 @@ lcma_status gemm(const char *who, int64_t rows, int64_t N, int64_t K, int group,
     p.experts = experts;
     p.blocks = (int32_t)column_blocks(K);
     p.panel = 1;
-    auto fits = [&](int k) { return (es == 2 || k != kI4Rows64) && launches(tiles_of(k, rows, N, experts, offsets != nullptr)); };
+    auto fits = [&](int k, bool once) {
+        const int64_t jobs = tiles_of(k, rows, N, experts, offsets != nullptr);
+        return (es == 2 || k != kI4Rows64) && (once ? one_launch(jobs) : several_launches(jobs));
+    };
     int kernel = tuning_i4_kernel();
-    if (kernel < 0 || !fits(kernel)) {
-        kernel = -1;
+    if (kernel < 0 || !fits(kernel, true)) kernel = -1;
+    for (bool once : {true, false}) {
+        if (kernel >= 0) break;
         double least = 0;
         for (int k = 0; k < kI4Kernels; ++k)
-            if (const double t = predicted_us(k, rows, N, K, group, experts, offsets != nullptr, es); fits(k) && (kernel < 0 || t < least)) {
+            if (const double t = predicted_us(k, rows, N, K, group, experts, offsets != nullptr, es); fits(k, once) && (kernel < 0 || t < least)) {
                 least = t;
                 kernel = k;
             }
     }
-    if (kernel < 0) return fail(LCMA_ERR_SHAPE, "%s: too many tiles for a launch", who);
-    const int64_t jobs = tiles_of(kernel, rows, N, experts, offsets != nullptr);
+    if (kernel < 0) return fail(LCMA_ERR_SHAPE, "%s: 2^31 tiles or more", who);
+    const int64_t jobs = tiles_of(kernel, rows, N, experts, offsets != nullptr), eighth = (jobs + 7) / 8, most = one_launch(jobs) ? eighth : kLaunchEighth;
     p.nz = (int32_t)((N + kTile[kernel][1] - 1) / kTile[kernel][1]);
-    if (const int err = lcma_launch_i4_gemm(&p, kernel, group, dtype, (int)((jobs + 7) / 8 * 8), stream)) return fail(LCMA_ERR_HIP, "%s: launch failed with HIP error %d", who, err);
+    for (int64_t from = 0; from < eighth; from += most) {
+        p.from = (int32_t)from;
+        if (const int err = lcma_launch_i4_gemm(&p, kernel, group, dtype, (int)((eighth - from < most ? eighth - from : most) * 8), stream))
+            return fail(LCMA_ERR_HIP, "%s: launch failed with HIP error %d", who, err);
+    }
     return LCMA_OK;
 }
 

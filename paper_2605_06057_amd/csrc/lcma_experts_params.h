@@ -115,6 +115,7 @@ struct I4GemmParams {
     int32_t rows, N, K, experts;
     int32_t blocks;         // of 128 columns
     int32_t nz, panel;      // tiles along N
+    int32_t from;           // the launch's first tile of each eighth of them
 };
 
 } // namespace lcma

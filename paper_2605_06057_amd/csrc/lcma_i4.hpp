@@ -157,10 +157,10 @@ template <class T, int G, int MT, int NB, int WN, int WK, int D, int XB> struct 
 
     static LCMA_DEV void run(const I4GemmParams &p, LCMA_LDS char *lds) {
         const I8Rows<TM, I4GemmParams> groups(p);
-        i8_zero_behind<T>(p, groups.behind, gridDim.x, NT);
-        const int nx = groups.within(p), jobs = nx * p.nz, per = (jobs + 7) / 8;
-        const int job = (blockIdx.x & 7) * per + (blockIdx.x >> 3); // an eighth of the tiles to every XCD, row tiles that share weights next to each other
-        if ((int)(blockIdx.x >> 3) >= per || job >= jobs) return;
+        if (!p.from) i8_zero_behind<T>(p, groups.behind, gridDim.x, NT);
+        const int nx = groups.within(p), jobs = nx * p.nz, per = (jobs + 7) / 8, i = p.from + (int)(blockIdx.x >> 3);
+        const int job = (int)(blockIdx.x & 7) * per + i; // an eighth of the tiles to every XCD, row tiles that share weights next to each other
+        if (i >= per || job >= jobs) return;
         int tile, z;
         i8_tile_of_job(nx, p.nz, p.panel, job, tile, z);
         const I8Place at = groups.place(p, tile);
