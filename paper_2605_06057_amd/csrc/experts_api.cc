@@ -23,11 +23,16 @@ int64_t product_tiles(int kernel, int64_t rows, int64_t N, int experts) {
 int64_t gradient_tiles(int kernel, int64_t M, int64_t N, int experts) { return experts * tiles(M, kTile[kernel][0]) * tiles(N, kTile[kernel][1]); }
 bool needs_vectors(int kernel) { return kernel >= kExpFew16; }
 bool walks(int kernel) { return kernel >= kExpNarrow; } // 256 work-groups walk through tiles; the other kernels have one for every tile
-bool launches(int kernel, int64_t jobs) { return walks(kernel) ? jobs < kRowLimit - 1024 : (jobs + 8) * 512 < kGridLimit / 2; } // (numbers of tiles are 32-bit on the device)
-int grid_of(int kernel, int64_t jobs) { return walks(kernel) ? 256 : (int)((jobs + 7) / 8 * 8); }
-int gradient_grid(int kernel, int64_t jobs, int64_t of) { // of: tiles of an expert; the kernels deal out eighths of them (exp_gradient_tile)
-    const int64_t whole = (of + 7) / 8 * 8;
-    return walks(kernel) ? 256 : (int)((jobs + whole - 1) / whole * whole);
+bool launches(int kernel, int64_t jobs) { return walks(kernel) ? several_launches(jobs) : one_launch(jobs); }
+// Work-groups for `jobs` tiles, dealt out `whole` at a time (a multiple of eight); several launches where one does not hold them.
+int launch(ExpertsGemmParams &p, int form, int kernel, int dtype, int64_t jobs, int64_t whole, void *stream) {
+    if (walks(kernel)) return lcma_launch_experts_gemm(&p, form, kernel, dtype, 256, stream);
+    const int64_t eighth = (jobs + whole - 1) / whole * whole / 8, most = one_launch(jobs) ? eighth : kLaunchEighth;
+    for (int64_t from = 0; from < eighth; from += most) {
+        p.from = (int32_t)from;
+        if (const int err = lcma_launch_experts_gemm(&p, form, kernel, dtype, (int)((eighth - from < most ? eighth - from : most) * 8), stream)) return err;
+    }
+    return 0;
 }
 // What the kernels that load straight into LDS need: offsets inside a tile (256 rows of a k-contiguous operand, 128 rows along k of the other) below 2^30 bytes, and, 16-bit types,
 // operands in whole 16 bytes (of a k-contiguous one K too, of the other form the rows).
@@ -66,7 +71,7 @@ bool takes(int kernel, int form, bool vectors, bool short_rows, int es) {
     if (kernel == kExpAnyFew32) return es == 2 && short_rows && form != kGrad;
     return !needs_vectors(kernel) || (vectors && (es == 2 ? kVectors : kF32)[form][kernel].start > 0);
 }
-// form, and the sizes of the call; -1: no launch holds the tiles
+// form, and the sizes of the call; -1: 2^31 tiles or more
 int pick(int form, bool vectors, bool short_rows, int es, int64_t rows, int64_t N, int64_t K, int experts) {
     const Cost(&costs)[kExpKernels] = (!vectors ? kAny : es == 2 ? kVectors : kF32)[form];
     auto tiles_of = [&](int k) { return form == kGrad ? gradient_tiles(k, N, K, experts) : product_tiles(k, rows, N, experts); };
@@ -86,7 +91,8 @@ int pick(int form, bool vectors, bool short_rows, int es, int64_t rows, int64_t 
                 least = t;
                 best = k;
             }
-    if (best < 0 && launches(kExpStaged128, tiles_of(kExpStaged128))) best = kExpStaged128; // (the fewest tiles of those that have a work-group each)
+    // (the fewest tiles of those that have a work-group each, in several launches; of the gradient, eight times the eighth of each expert's)
+    if (best < 0 && several_launches(tiles_of(kExpStaged128) + (form == kGrad ? 7 * experts : 0))) best = kExpStaged128;
     return best;
 }
 lcma_status check_sizes(const char *who, int64_t rows, int64_t N, int64_t K, int experts, int dtype) {
@@ -140,9 +146,9 @@ extern "C" lcma_status lcma_gemm_experts(int b_layout, int64_t rows, int64_t N, 
     const int form = b_layout ? kNt : kNn;
     int kernel = tuning_experts_kernel();
     if (!takes(kernel, form, vectors, short_rows, es) || !launches(kernel, product_tiles(kernel, rows, N, experts))) kernel = pick(form, vectors, short_rows, es, rows, N, K, experts);
-    if (kernel < 0) return fail(LCMA_ERR_SHAPE, "%s: too many tiles for a launch", who);
+    if (kernel < 0) return fail(LCMA_ERR_SHAPE, "%s: 2^31 tiles or more", who);
     p.nz = (int32_t)tiles(N, kTile[kernel][1]);
-    if (const int err = lcma_launch_experts_gemm(&p, form, kernel, dtype, grid_of(kernel, product_tiles(kernel, rows, N, experts)), stream))
+    if (const int err = launch(p, form, kernel, dtype, product_tiles(kernel, rows, N, experts), 8, stream))
         return fail(LCMA_ERR_HIP, "%s: launch failed with HIP error %d", who, err);
     return LCMA_OK;
 }
@@ -181,10 +187,11 @@ extern "C" lcma_status lcma_gemm_experts_grad(int64_t rows, int64_t N, int64_t K
     const bool short_rows = p.lda_b <= kShortRow && p.ldb_b <= kShortRow, vectors = short_rows && whole_vectors(es, dC, p.lda_b, A, p.ldb_b, 0);
     int kernel = tuning_experts_kernel();
     if (!takes(kernel, kGrad, vectors, short_rows, es) || !launches(kernel, gradient_tiles(kernel, N, K, experts))) kernel = pick(kGrad, vectors, short_rows, es, rows, N, K, experts);
-    if (kernel < 0) return fail(LCMA_ERR_SHAPE, "%s: too many tiles for a launch", who);
+    if (kernel < 0) return fail(LCMA_ERR_SHAPE, "%s: 2^31 tiles or more", who);
     p.nx = (int32_t)tiles(N, kTile[kernel][0]);
     p.nz = (int32_t)tiles(K, kTile[kernel][1]);
-    if (const int err = lcma_launch_experts_gemm(&p, kGrad, kernel, dtype, gradient_grid(kernel, gradient_tiles(kernel, N, K, experts), (int64_t)p.nx * p.nz), stream))
+    // (the kernels deal out eighths of an expert's tiles, exp_gradient_tile)
+    if (const int err = launch(p, kGrad, kernel, dtype, gradient_tiles(kernel, N, K, experts), ((int64_t)p.nx * p.nz + 7) / 8 * 8, stream))
         return fail(LCMA_ERR_HIP, "%s: launch failed with HIP error %d", who, err);
     return LCMA_OK;
 }

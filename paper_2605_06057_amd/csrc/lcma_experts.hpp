@@ -50,7 +50,7 @@ template <class T, int TM, int TN> LCMA_DEV ExpJob gradient_job(const ExpertsGem
 // expert: an expert's tiles take as long as it has rows, and an XCD that had whole experts would be done long before another (fp32, 2331 rows spread
 // unequally over 12 experts, 1001 x 515: 41 us so, 37 now).  -1: none.  The launch holds whole eights of such eighths.
 LCMA_DEV int exp_gradient_tile(const ExpertsGemmParams &p) {
-    const int of = p.nx * p.nz, q = (of + 7) >> 3, i = (int)(blockIdx.x >> 3), job = (i / q * 8 + (int)(blockIdx.x & 7)) * q + i % q;
+    const int of = p.nx * p.nz, q = (of + 7) >> 3, i = p.from + (int)(blockIdx.x >> 3), job = (i / q * 8 + (int)(blockIdx.x & 7)) * q + i % q;
     return job < p.experts * of ? job : -1;
 }
 
@@ -262,9 +262,9 @@ template <class T, bool ACOL, bool BCOL, bool GRAD, int TM, int TN, int WGM, int
             j = gradient_job<T, TM, TN>(p, job);
         } else {
             const I8Rows<TM, ExpertsGemmParams> groups(p);
-            exp_zero_behind<T, NT>(p, groups.behind);
-            const int nx = groups.within(p), jobs = nx * p.nz, per = (jobs + 7) / 8, job = (int)(blockIdx.x & 7) * per + (int)(blockIdx.x >> 3);
-            if ((int)(blockIdx.x >> 3) >= per || job >= jobs) return;
+            if (!p.from) exp_zero_behind<T, NT>(p, groups.behind);
+            const int nx = groups.within(p), jobs = nx * p.nz, per = (jobs + 7) / 8, i = p.from + (int)(blockIdx.x >> 3), job = (int)(blockIdx.x & 7) * per + i;
+            if (i >= per || job >= jobs) return;
             int x, z;
             i8_tile_of_job(nx, p.nz, p.panel, job, x, z);
             j = product_job<T, BCOL, TM, TN>(p, groups.place(p, x), z * TN);
