@@ -13,13 +13,13 @@ template <class T, bool ACOL, bool BCOL, bool GRAD, int TM, int TN, int WGM, int
     G::run(p, (LCMA_LDS char *)smem);
 }
 
-template <class T, bool ACOL, bool BCOL, bool GRAD, int TM, int TN, int WGM, int WGN, int S> __global__ __launch_bounds__(64 * WGM * WGN, 2) void exp_ring(const ExpertsGemmParams p) {
-    using G = ExpRing<T, ACOL, BCOL, GRAD, TM, TN, WGM, WGN, S>;
+template <class T, bool ACOL, bool BCOL, bool GRAD, int TM, int TN, int WGM, int WGN> __global__ __launch_bounds__(64 * WGM * WGN, 2) void exp_ring(const ExpertsGemmParams p) {
+    using G = ExpRing<T, ACOL, BCOL, GRAD, TM, TN, WGM, WGN>;
     __shared__ __attribute__((aligned(16))) char smem[G::LDS_BYTES];
     G::run(p, (LCMA_LDS char *)smem);
 }
-template <class T, bool BCOL, int R, int WK, int S> __global__ __launch_bounds__(64 * WK) void exp_few(const ExpertsGemmParams p) {
-    using G = ExpFewRows<T, BCOL, R, WK, S>;
+template <class T, bool BCOL, int R, int WK> __global__ __launch_bounds__(64 * WK) void exp_few(const ExpertsGemmParams p) {
+    using G = ExpFewRows<T, BCOL, R, WK>;
     __shared__ __attribute__((aligned(16))) char smem[G::LDS_BYTES];
     G::run(p, (LCMA_LDS char *)smem);
 }
@@ -68,19 +68,19 @@ extern "C" int lcma_launch_experts_gemm(const lcma::ExpertsGemmParams *p, int fo
         else LCMA_EXP_LAUNCH(256, exp_any_few<F16, true, 4>);
         break;
     case kExpFew16:
-        if (dtype == 1) LCMA_EXP_LAUNCH(256, exp_few<BF16, false, 16, 4, 2>);
-        else LCMA_EXP_LAUNCH(256, exp_few<F16, false, 16, 4, 2>);
+        if (dtype == 1) LCMA_EXP_LAUNCH(256, exp_few<BF16, false, 16, 4>);
+        else LCMA_EXP_LAUNCH(256, exp_few<F16, false, 16, 4>);
         break;
     case kExpFew32:
-        if (dtype == 0 && form == 0) LCMA_EXP_LAUNCH(256, exp_few<F32, false, 32, 4, 2>);
-        else if (dtype == 0) LCMA_EXP_LAUNCH(256, exp_few<F32, true, 32, 4, 2>);
-        else if (dtype == 1 && form == 0) LCMA_EXP_LAUNCH(256, exp_few<BF16, false, 32, 4, 2>);
-        else if (dtype == 1) LCMA_EXP_LAUNCH(256, exp_few<BF16, true, 32, 4, 2>);
-        else if (form == 0) LCMA_EXP_LAUNCH(256, exp_few<F16, false, 32, 4, 2>);
-        else LCMA_EXP_LAUNCH(256, exp_few<F16, true, 32, 4, 2>);
+        if (dtype == 0 && form == 0) LCMA_EXP_LAUNCH(256, exp_few<F32, false, 32, 4>);
+        else if (dtype == 0) LCMA_EXP_LAUNCH(256, exp_few<F32, true, 32, 4>);
+        else if (dtype == 1 && form == 0) LCMA_EXP_LAUNCH(256, exp_few<BF16, false, 32, 4>);
+        else if (dtype == 1) LCMA_EXP_LAUNCH(256, exp_few<BF16, true, 32, 4>);
+        else if (form == 0) LCMA_EXP_LAUNCH(256, exp_few<F16, false, 32, 4>);
+        else LCMA_EXP_LAUNCH(256, exp_few<F16, true, 32, 4>);
         break;
-    case kExpRing64: LCMA_EXP_ANY(exp_ring, 256, LCMA_COMMA 64, 64, 2, 2, 3)
-    case kExpRing64x128: LCMA_EXP(exp_ring, 256, LCMA_COMMA 64, 128, 2, 2, 3)
+    case kExpRing64: LCMA_EXP_ANY(exp_ring, 256, LCMA_COMMA 64, 64, 2, 2)
+    case kExpRing64x128: LCMA_EXP(exp_ring, 256, LCMA_COMMA 64, 128, 2, 2)
     case kExpNarrow:
         if (dtype == 1 && form == 0) LCMA_EXP_LAUNCH(512, exp_narrow<BF16, false>);
         else if (dtype == 1) LCMA_EXP_LAUNCH(512, exp_narrow<BF16, true>);

@@ -34,15 +34,15 @@ template <int N> LCMA_DEV void exp_end_of_k(u32x4 (&f)[N][4], int left) {
             for (int t = 0; t < 4; ++t) f[n][k][t] = k * 8 + lh * 4 + t < left ? f[n][k][t] : 0;
 }
 
-// One tile of TM x TN per work-group of WGM x WGN waves.  A step is 64 k (fp32: 32); S stages of LDS hold the steps in flight, the loads run S - 1 steps ahead and are waited for by
+// One tile of TM x TN per work-group of WGM x WGN waves.  A step is 64 k (fp32: 32); three stages of LDS hold the steps in flight, the loads run two steps ahead and are waited for by
 // count, and one barrier a step says that all waves' parts of it have landed and that all have read the stage that is loaded anew (csrc/lcma_i8.hpp has the
 // same with its measurements).  Bound by memory at hundreds of rows, by the loads' way through LDS above: bf16, rows of 128 x 2 of 8, 2048 x 1024: 8.3 us on 64 x 64 (weights at 4.0 TB/s; 32 x 32 takes
 // 11.1), 9.0 on 64 x 128; fp16 1021 x 6 of 64, 2816 x 2056: 287 and 255 against 213 on 128 x 256.  fp32 (64 x 64 alone, by the matrix pipe, 68 % of which is at work): 777 x 3 of 12, 1001 x 515: 33 us,
 // gradients 39 and 35; 4096 x 2 of 8, 2048 x 2048: 538 (128 TFLOP/s).
-template <class T, bool ACOL, bool BCOL, bool GRAD, int TM, int TN, int WGM, int WGN, int S> struct ExpRing {
+template <class T, bool ACOL, bool BCOL, bool GRAD, int TM, int TN, int WGM, int WGN> struct ExpRing {
     static constexpr int NT = 64 * WGM * WGN, NMI = TM / WGM / 32, NNI = TN / WGN / 32, KS = 128 / T::ES;
-    static constexpr int A_STAGE = TM * 128, STAGE = (TM + TN) * 128, LDS_BYTES = S * STAGE, QA = TM * 8 / NT, QB = TN * 8 / NT;
-    static_assert(NT / 64 * 4096 <= LDS_BYTES && TM * 8 % NT == 0 && TN * 8 % NT == 0 && LDS_BYTES <= 160 * 1024 && (S == 3 || S == 4) && (S - 1) * (QA + QB) <= 63, "tile and wave grid");
+    static constexpr int A_STAGE = TM * 128, STAGE = (TM + TN) * 128, LDS_BYTES = 3 * STAGE, QA = TM * 8 / NT, QB = TN * 8 / NT;
+    static_assert(NT / 64 * 4096 <= LDS_BYTES && TM * 8 % NT == 0 && TN * 8 % NT == 0 && LDS_BYTES <= 160 * 1024 && 2 * (QA + QB) <= 63, "tile and wave grid");
     using Frag = typename Mma<T>::frag;
     static constexpr uint32_t NONE = 1u << 30; // an offset past any extent
 
@@ -67,7 +67,7 @@ template <class T, bool ACOL, bool BCOL, bool GRAD, int TM, int TN, int WGM, int
         for (int i = 0; i < NMI; ++i)
 #pragma unroll
             for (int n = 0; n < NNI; ++n) zero(acc[i][n]);
-        multiply(p, j, w, wm, wn, acc, lds, lds + STAGE, lds + 2 * STAGE, lds + (S == 4 ? 3 * STAGE : 0));
+        multiply(p, j, w, wm, wn, acc, lds, lds + STAGE, lds + 2 * STAGE);
         __syncthreads(); // no load is in flight and every wave has read its last step: the strips take the place of the stages
         const int row = wm * NMI * 32, col = wn * NNI * 32;
         exp_store<T, NMI, NNI, false, 32, 32, GRAD>(lds + w * 4096, j.c + (int64_t)row * p.ldc_b + (int64_t)col * T::ES, p.ldc_b, j.am - row, j.bn - col, acc, p.stream);
@@ -75,7 +75,7 @@ template <class T, bool ACOL, bool BCOL, bool GRAD, int TM, int TN, int WGM, int
     // restrict: the loads in flight towards one stage do not touch what is read from another (the compiler would otherwise wait for all of them in
     // front of every read)
     static LCMA_DEV void multiply(const ExpertsGemmParams &p, const ExpJob &j, int w, int wm, int wn, f32x16 (&acc)[NMI][NNI], LCMA_LDS char *__restrict__ s0,
-                                  LCMA_LDS char *__restrict__ s1, LCMA_LDS char *__restrict__ s2, LCMA_LDS char *__restrict__ s3) {
+                                  LCMA_LDS char *__restrict__ s1, LCMA_LDS char *__restrict__ s2) {
         constexpr int CA = TM * T::ES / 16, CB = TN * T::ES / 16; // 16-byte chunks of a row of the other form
         const int tid = threadIdx.x, steps = (int)(((uint32_t)j.k + (KS - 1)) / KS), chunk = exp_row_chunk(tid >> 3, tid & 7) * 16;
         const uint32_t lda = (uint32_t)p.lda_b, ldb = (uint32_t)p.ldb_b;
@@ -97,11 +97,11 @@ template <class T, bool ACOL, bool BCOL, bool GRAD, int TM, int TN, int WGM, int
                 __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (LCMA_LDS void *)(st + (q * NT + w * 64) * 16), 16, (int)av, (int)((ACOL ? 0 : off) + q * a_down), 0, 0);
         };
         auto step = [&](LCMA_LDS char *st, LCMA_LDS char *before, int y) {
-            wait_loads<(S - 2) * (QA + QB)>();
+            wait_loads<QA + QB>();
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
             __builtin_amdgcn_sched_barrier(0);
-            load(before, y + S - 1);
+            load(before, y + 2);
             u32x4 a[NMI][4], b[NNI][4];
 #pragma unroll
             for (int n = 0; n < NNI; ++n) exp_fragments<T, BCOL, TN>(st + A_STAGE, wn * NNI + n, b[n]);
@@ -121,19 +121,12 @@ template <class T, bool ACOL, bool BCOL, bool GRAD, int TM, int TN, int WGM, int
         };
         load(s0, 0);
         load(s1, 1);
-        if constexpr (S == 4) load(s2, 2);
-        for (int y = 0; y < steps;) {
-            step(s0, S == 4 ? s3 : s2, y);
+        for (int y = 0; y < steps; ++y) {
+            step(s0, s2, y);
             if (++y >= steps) break;
             step(s1, s0, y);
             if (++y >= steps) break;
             step(s2, s1, y);
-            ++y;
-            if constexpr (S == 4) {
-                if (y >= steps) break;
-                step(s3, s2, y);
-                ++y;
-            }
         }
         wait_loads<0>(); // the loads past the end land before the LDS is another work-group's
     }
@@ -141,18 +134,18 @@ template <class T, bool ACOL, bool BCOL, bool GRAD, int TM, int TN, int WGM, int
 
 // Few rows: a work-group owns a tile of R x R of C and its waves split K between them, a step (64 k, fp32: 32, 128 bytes of every row) to a wave in turn; nothing is shared between
 // waves, so there is no barrier in the loop, and the waves' sums are added at the end, in fp32 and in ascending order (csrc/lcma_few_rows.hpp has the same for one product,
-// with the reasons and measurements).  S steps of a wave in flight.  Bound by memory: bf16, 2 rows of 8 experts, 28672 x 4096: 77 us, 6.1 TB/s, which is what a large read reaches; weights K x N
+// with the reasons and measurements).  Two steps of a wave in flight.  Bound by memory: bf16, 2 rows of 8 experts, 28672 x 4096: 77 us, 6.1 TB/s, which is what a large read reaches; weights K x N
 // 113 (32 columns are half a line; 64 x 64 takes 164).
-template <class T, bool BCOL, int R, int WK, int S> struct ExpFewRows {
-    static constexpr int F = R == 16 ? 16 : 32, NF = R / F, KF = 64 / (512 / F), KS = 128 / T::ES; // 16x16x32 or 32x32x16 instructions; fragments of a step along K
-    static constexpr int LOADS = R / 8, HALF = R * 128, STAGE = 2 * HALF, PITCH = R + 4, SUMS = WK * R * PITCH * 4, STAGES = WK * S * STAGE, LDS_BYTES = SUMS > STAGES ? SUMS : STAGES;
-    static_assert((R >= 32 || (!BCOL && T::ES == 2)) && LDS_BYTES <= 160 * 1024 && (S == 2 || S == 4) && 2 * LOADS * S <= 63, "LDS budget of one CU; counter of loads");
+template <class T, bool BCOL, int R, int WK> struct ExpFewRows {
+    static constexpr int KF = 64 / (512 / R), KS = 128 / T::ES; // 16x16x32 or 32x32x16 instructions; fragments of a step along K
+    static constexpr int LOADS = R / 8, HALF = R * 128, STAGE = 2 * HALF, PITCH = R + 4, SUMS = WK * R * PITCH * 4, STAGES = WK * 2 * STAGE, LDS_BYTES = SUMS > STAGES ? SUMS : STAGES;
+    static_assert((R == 32 || (R == 16 && !BCOL && T::ES == 2)) && LDS_BYTES <= 160 * 1024 && 4 * LOADS <= 63, "LDS budget of one CU; counter of loads");
     using Frag = typename Mma<T>::frag;
-    using Acc = std::conditional_t<F == 16, f32x4, f32x16>;
+    using Acc = std::conditional_t<R == 16, f32x4, f32x16>;
     static constexpr uint32_t NONE = 1u << 30;
 
     static LCMA_DEV void run(const ExpertsGemmParams &p, LCMA_LDS char *lds) {
-        const int lane = threadIdx.x & 63, fr = lane & (F - 1), fk = lane / F, wk = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const int lane = threadIdx.x & 63, fr = lane & (R - 1), fk = lane / R, wk = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         const I8Rows<R, ExpertsGemmParams> groups(p);
         exp_zero_behind<T, 64 * WK>(p, groups.behind);
         const int nx = groups.within(p), jobs = nx * p.nz, per = (jobs + 7) / 8;
@@ -161,24 +154,16 @@ template <class T, bool BCOL, int R, int WK, int S> struct ExpFewRows {
         int x, z;
         i8_tile_of_job(nx, p.nz, p.panel, job, x, z);
         const ExpJob j = product_job<T, BCOL, R, R>(p, groups.place(p, x), z * R);
-        Acc acc[NF][NF];
+        Acc acc;
 #pragma unroll
-        for (int i = 0; i < NF; ++i)
-#pragma unroll
-            for (int n = 0; n < NF; ++n)
-#pragma unroll
-                for (int v = 0; v < F * F / 64; ++v) acc[i][n][v] = 0.f;
-        LCMA_LDS char *st = lds + wk * (S * STAGE);
-        steps_of_wave(p, j, wk, acc, st, st + STAGE, st + (S == 4 ? 2 * STAGE : 0), st + (S == 4 ? 3 * STAGE : 0));
+        for (int v = 0; v < R * R / 64; ++v) acc[v] = 0.f;
+        LCMA_LDS char *st = lds + wk * (2 * STAGE);
+        steps_of_wave(p, j, wk, acc, st, st + STAGE);
         __syncthreads(); // no load is in flight and every wave has read its last step: the sums take the place of the stages
         LCMA_LDS float *mine = (LCMA_LDS float *)lds + wk * (R * PITCH);
 #pragma unroll
-        for (int i = 0; i < NF; ++i)
-#pragma unroll
-            for (int n = 0; n < NF; ++n)
-#pragma unroll
-                for (int g = 0; g < F * F / 256; ++g) // four neighbouring columns of row fr
-                    *(LCMA_LDS f32x4 *)(mine + (i * F + fr) * PITCH + n * F + g * 8 + fk * 4) = f32x4{acc[i][n][g * 4], acc[i][n][g * 4 + 1], acc[i][n][g * 4 + 2], acc[i][n][g * 4 + 3]};
+        for (int g = 0; g < R * R / 256; ++g) // four neighbouring columns of row fr
+            *(LCMA_LDS f32x4 *)(mine + fr * PITCH + g * 8 + fk * 4) = f32x4{acc[g * 4], acc[g * 4 + 1], acc[g * 4 + 2], acc[g * 4 + 3]};
         __syncthreads();
         for (int t = threadIdx.x; t < R * R / 4; t += 64 * WK) {
             const int row = t / (R / 4), n = t % (R / 4) * 4;
@@ -191,10 +176,9 @@ template <class T, bool BCOL, int R, int WK, int S> struct ExpFewRows {
         }
     }
     // Steps `y`, y + WK, ...
-    static LCMA_DEV void steps_of_wave(const ExpertsGemmParams &p, const ExpJob &j, int y, Acc (&acc)[NF][NF], LCMA_LDS char *__restrict__ s0, LCMA_LDS char *__restrict__ s1,
-                                       LCMA_LDS char *__restrict__ s2, LCMA_LDS char *__restrict__ s3) {
+    static LCMA_DEV void steps_of_wave(const ExpertsGemmParams &p, const ExpJob &j, int y, Acc &acc, LCMA_LDS char *__restrict__ s0, LCMA_LDS char *__restrict__ s1) {
         constexpr int CPR = R * T::ES / 16, RPL = 64 / CPR; // the other form: 16-byte chunks of a row, rows of a load
-        const int lane = threadIdx.x & 63, fr = lane & (F - 1), fk = lane / F, steps = (int)(((uint32_t)j.k + (KS - 1)) / KS), in_last = (j.k - 1) % KS + 1;
+        const int lane = threadIdx.x & 63, fr = lane & (R - 1), fk = lane / R, steps = (int)(((uint32_t)j.k + (KS - 1)) / KS), in_last = (j.k - 1) % KS + 1;
         const uint32_t lda = (uint32_t)p.lda_b, ldb = (uint32_t)p.ldb_b;
         const auto ra = exp_rows_of<T>(j.a, j.am, j.k, lda), rows_b = exp_rows_of<T>(j.b, j.bn, j.k, ldb);
         // a load brings 8 rows of 128 bytes, lanes 8 i to 8 i + 7 one row; `last`: what is past K from past the extents
@@ -221,24 +205,21 @@ template <class T, bool BCOL, int R, int WK, int S> struct ExpFewRows {
         };
         uint32_t frag[KF]; // of this lane's 16 bytes in k-contiguous rows
 #pragma unroll
-        for (int k = 0; k < KF; ++k) frag[k] = fr * 128 + ((k * (64 / F) + fk) ^ (fr >> 1 & 7)) * 16;
+        for (int k = 0; k < KF; ++k) frag[k] = fr * 128 + ((k * (64 / R) + fk) ^ (fr >> 1 & 7)) * 16;
         auto step = [&](LCMA_LDS char *st, int y) {
-            u32x4 a[NF][KF], b[NF][KF];
-            wait_loads<2 * LOADS *(S - 1)>();
+            u32x4 a[1][KF], b[1][KF];
+            wait_loads<2 * LOADS>();
+            if constexpr (BCOL) exp_fragments<T, true, R>(st + HALF, 0, b[0]);
 #pragma unroll
-            for (int i = 0; i < NF; ++i) {
-                if constexpr (BCOL) exp_fragments<T, true, R>(st + HALF, i, b[i]);
-#pragma unroll
-                for (int k = 0; k < KF; ++k) {
-                    a[i][k] = *(const LCMA_LDS u32x4 *)(st + frag[k] + i * F * 128);
-                    if constexpr (!BCOL) b[i][k] = *(const LCMA_LDS u32x4 *)(st + HALF + frag[k] + i * F * 128);
-                }
+            for (int k = 0; k < KF; ++k) {
+                a[0][k] = *(const LCMA_LDS u32x4 *)(st + frag[k]);
+                if constexpr (!BCOL) b[0][k] = *(const LCMA_LDS u32x4 *)(st + HALF + frag[k]);
             }
             __builtin_amdgcn_sched_barrier(0);
             __builtin_amdgcn_s_waitcnt(0xC07F); // lgkmcnt(0): what was read has left LDS, so its place may be loaded anew
             asm volatile("" ::: "memory");
             __builtin_amdgcn_sched_barrier(0);
-            load(st, y + S * WK);
+            load(st, y + 2 * WK);
             __builtin_amdgcn_sched_barrier(0);
             if constexpr (T::ES == 4)
                 if (y == steps - 1) {
@@ -246,33 +227,18 @@ template <class T, bool BCOL, int R, int WK, int S> struct ExpFewRows {
                     if constexpr (!BCOL) exp_end_of_k(b, in_last);
                 }
 #pragma unroll
-            for (int k = 0; k < KF; ++k)
-#pragma unroll
-                for (int i = 0; i < NF; ++i)
-#pragma unroll
-                    for (int n = 0; n < NF; ++n) {
-                        const Frag fa = __builtin_bit_cast(Frag, a[i][k]), fb = __builtin_bit_cast(Frag, b[n][k]);
-                        if constexpr (F == 16) acc[i][n] = Mma16<T>::run(fb, fa, acc[i][n]);
-                        else Mma<T>::run(fb, fa, acc[i][n]);
-                    }
+            for (int k = 0; k < KF; ++k) {
+                const Frag fa = __builtin_bit_cast(Frag, a[0][k]), fb = __builtin_bit_cast(Frag, b[0][k]);
+                if constexpr (R == 16) acc = Mma16<T>::run(fb, fa, acc);
+                else Mma<T>::run(fb, fa, acc);
+            }
         };
         load(s0, y);
         load(s1, y + WK);
-        if constexpr (S == 4) {
-            load(s2, y + 2 * WK);
-            load(s3, y + 3 * WK);
-        }
-        while (y < steps) {
+        for (; y < steps; y += WK) {
             step(s0, y);
             if ((y += WK) >= steps) break;
             step(s1, y);
-            if constexpr (S == 4) {
-                if ((y += WK) >= steps) break;
-                step(s2, y);
-                if ((y += WK) >= steps) break;
-                step(s3, y);
-            }
-            y += WK;
         }
         wait_loads<0>();
     }

@@ -85,8 +85,8 @@ template <class T, bool CODES> __global__ __launch_bounds__(256) void i4_prepare
     }
 }
 
-template <class T, int G, int MT, int NB, int WN, int WK, int D, int XB> __global__ __launch_bounds__(64 * WN * WK) void i4_gemm(const I4GemmParams p) {
-    using K = I4Gemm<T, G, MT, NB, WN, WK, D, XB>;
+template <class T, int G, int MT, int WN, int WK, int D, int XB> __global__ __launch_bounds__(64 * WN * WK) void i4_gemm(const I4GemmParams p) {
+    using K = I4Gemm<T, G, MT, WN, WK, D, XB>;
     __shared__ __attribute__((aligned(16))) char smem[K::LDS_BYTES];
     K::run(p, (LCMA_LDS char *)smem);
 }
@@ -110,18 +110,18 @@ extern "C" int lcma_launch_i4_gemm(const lcma::I4GemmParams *p, int kernel, int 
     else if (group == 64) i4_gemm<T, 64, __VA_ARGS__><<<dim3(grid), dim3(THREADS), 0, s>>>(*p);     \
     else i4_gemm<T, 128, __VA_ARGS__><<<dim3(grid), dim3(THREADS), 0, s>>>(*p);
 // (fp32: three parts of X in LDS)
-#define LCMA_I4(MT, NB, WN, WK, D, XB, D32, XB32)                                      \
-    if (dtype == 0) { LCMA_I4_G(F32, 64 * WN * WK, MT, NB, WN, WK, D32, XB32) }        \
-    else if (dtype == 1) { LCMA_I4_G(BF16, 64 * WN * WK, MT, NB, WN, WK, D, XB) }      \
-    else { LCMA_I4_G(F16, 64 * WN * WK, MT, NB, WN, WK, D, XB) }                       \
+#define LCMA_I4(MT, WN, WK, D, XB, D32, XB32)                                          \
+    if (dtype == 0) { LCMA_I4_G(F32, 64 * WN * WK, MT, WN, WK, D32, XB32) }            \
+    else if (dtype == 1) { LCMA_I4_G(BF16, 64 * WN * WK, MT, WN, WK, D, XB) }          \
+    else { LCMA_I4_G(F16, 64 * WN * WK, MT, WN, WK, D, XB) }                           \
     break;
     switch (kernel) {
-    case kI4Rows16K8: LCMA_I4(1, 1, 1, 8, 2, 66048, 1, 99072)
-    case kI4Rows16K4: LCMA_I4(1, 1, 2, 4, 4, 66048, 1, 50048)
-    case kI4Rows16: LCMA_I4(1, 1, 4, 1, 4, 33024, 2, 50048)
+    case kI4Rows16K8: LCMA_I4(1, 1, 8, 2, 66048, 1, 99072)
+    case kI4Rows16K4: LCMA_I4(1, 2, 4, 4, 66048, 1, 50048)
+    case kI4Rows16: LCMA_I4(1, 4, 1, 4, 33024, 2, 50048)
     default: // (16 bit: three parts of 64 rows do not stay in registers)
-        if (dtype == 1) { LCMA_I4_G(BF16, 512, 4, 1, 4, 2, 2, 66560) }
-        else { LCMA_I4_G(F16, 512, 4, 1, 4, 2, 2, 66560) }
+        if (dtype == 1) { LCMA_I4_G(BF16, 512, 4, 4, 2, 2, 66560) }
+        else { LCMA_I4_G(F16, 512, 4, 4, 2, 2, 66560) }
     }
 #undef LCMA_I4
 #undef LCMA_I4_G

@@ -37,17 +37,17 @@ template <class T> LCMA_DEV u32x4 i4_widened(uint32_t v) {
     return r;
 }
 
-// WN x WK waves: the first along N, NB blocks of rows (of the weights) each, the others along K, a block of columns to a wave in turn; the weights of D of a wave's blocks are in
+// WN x WK waves: the first along N, a block of rows (of the weights) each, the others along K, a block of columns to a wave in turn; the weights of D of a wave's blocks are in
 // flight.  MT x 16 rows of X; as many blocks of columns of them are in LDS at a time as XB bytes hold.
 // bf16, groups of 128: a row, 14336 x 4096: 9.1 us (31 MB at 3.4 TB/s, 6.6 without the 2.5 of an empty launch: 448 tiles of 16 x 32, all at once, no second round to hide a start behind);
 // 16 rows over 8 experts, 28672 x 4096: 80 us, 5.6 TB/s; fp16, groups of 64, 366 rows over 64 experts, 2816 x 2048: 48 us, 4.3 TB/s.
 // What bounds it is the latency of the weights' way from memory, not the arithmetic: a block takes a wave about 60 vector instructions, 240 of the 420 clocks in which a CU's fourth of the
 // memory's rate brings it.
-template <class T, int G, int MT, int NB, int WN, int WK, int D, int XB> struct I4Gemm {
+template <class T, int G, int MT, int WN, int WK, int D, int XB> struct I4Gemm {
     using I = I4Type<T>;
     using Mul = typename I::Mul;
     using Frag = typename Mma16<Mul>::frag;
-    static constexpr int NT = 64 * WN * WK, TM = 16 * MT, TN = 16 * NB * WN, GROUPS = 128 / G, BLOCK = 1024 + GROUPS * 64, PER = 4 / GROUPS; // PER: instructions of a group
+    static constexpr int NT = 64 * WN * WK, TM = 16 * MT, TN = 16 * WN, GROUPS = 128 / G, BLOCK = 1024 + GROUPS * 64, PER = 4 / GROUPS; // PER: instructions of a group
     static constexpr int PITCH = TN + 4, SUMS = WK * TM * PITCH * 4, LDS_BYTES = SUMS > XB ? SUMS : XB;
     static_assert(LDS_BYTES <= 160 * 1024 && I::PARTS * TM * (WK * D * 256 + 16) <= XB, "LDS budget of one CU; a turn of all waves");
 
@@ -114,12 +114,12 @@ template <class T, int G, int MT, int NB, int WN, int WK, int D, int XB> struct 
     }
 
     // A block of columns: x, this lane's row of X in LDS (`row` of every 16), at the block's columns.
-    static LCMA_DEV void multiply(const LCMA_LDS char *(&x)[MT], int at, int part_bytes, const Block (&blk)[NB], f32x4 (&acc)[NB][MT]) {
+    static LCMA_DEV void multiply(const LCMA_LDS char *(&x)[MT], int at, int part_bytes, const Block &blk, f32x4 (&acc)[MT]) {
         const Frag minus = __builtin_bit_cast(Frag, u32x4{I::MINUS, I::MINUS, I::MINUS, I::MINUS});
 #pragma unroll
         for (int g = 0; g < GROUPS; ++g) {
             Frag xf[PER][MT][I::PARTS];
-            f32x4 off[MT];
+            f32x4 sum[MT];
 #pragma unroll
             for (int j = 0; j < PER; ++j)
 #pragma unroll
@@ -128,30 +128,24 @@ template <class T, int G, int MT, int NB, int WN, int WK, int D, int XB> struct 
                     for (int part = 0; part < I::PARTS; ++part) xf[j][i][part] = __builtin_bit_cast(Frag, *(const LCMA_LDS u32x4 *)(x[i] + at + part * part_bytes + (g * PER + j) * 64));
 #pragma unroll
             for (int i = 0; i < MT; ++i) {
-                off[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+                sum[i] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int j = 0; j < PER; ++j)
 #pragma unroll
-                    for (int part = 0; part < I::PARTS; ++part) off[i] = Mma16<Mul>::run(xf[j][i][part], minus, off[i]);
+                    for (int part = 0; part < I::PARTS; ++part) sum[i] = Mma16<Mul>::run(xf[j][i][part], minus, sum[i]);
             }
 #pragma unroll
-            for (int b = 0; b < NB; ++b) {
-                f32x4 sum[MT];
-#pragma unroll
-                for (int i = 0; i < MT; ++i) sum[i] = off[i];
-#pragma unroll
-                for (int j = 0; j < PER; ++j) {
-                    const Frag wf = __builtin_bit_cast(Frag, i4_widened<T>(blk[b].codes[g * PER + j]));
-#pragma unroll
-                    for (int i = 0; i < MT; ++i)
-#pragma unroll
-                        for (int part = 0; part < I::PARTS; ++part) sum[i] = Mma16<Mul>::run(xf[j][i][part], wf, sum[i]);
-                }
+            for (int j = 0; j < PER; ++j) {
+                const Frag wf = __builtin_bit_cast(Frag, i4_widened<T>(blk.codes[g * PER + j]));
 #pragma unroll
                 for (int i = 0; i < MT; ++i)
 #pragma unroll
-                    for (int v = 0; v < 4; ++v) acc[b][i][v] = __builtin_fmaf(sum[i][v], blk[b].scales[g], acc[b][i][v]);
+                    for (int part = 0; part < I::PARTS; ++part) sum[i] = Mma16<Mul>::run(xf[j][i][part], wf, sum[i]);
             }
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int v = 0; v < 4; ++v) acc[i][v] = __builtin_fmaf(sum[i][v], blk.scales[g], acc[i][v]);
         }
     }
 
@@ -165,22 +159,14 @@ template <class T, int G, int MT, int NB, int WN, int WK, int D, int XB> struct 
         i8_tile_of_job(nx, p.nz, p.panel, job, tile, z);
         const I8Place at = groups.place(p, tile);
         const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wk = w / WN, wn = w % WN;
-        const int first = (z * WN + wn) * NB, all = (p.N + 15) / 16, blocks = p.blocks; // blocks of rows; of columns
-        const char *q[NB];
+        const int first = z * WN + wn, all = (p.N + 15) / 16, blocks = p.blocks; // blocks of rows; of columns
+        const char *q = p.Q + at.expert * p.expert_q + (int64_t)(first < all ? first : all - 1) * blocks * BLOCK; // (past the last: the last again, dropped)
+        auto fetch_from = [&](int y, Block &blk) { fetch(q + (int64_t)(y < blocks ? y : blocks - 1) * BLOCK, blk); }; // (past the last: the last again, not used)
+        f32x4 acc[MT];
 #pragma unroll
-        for (int b = 0; b < NB; ++b) q[b] = p.Q + at.expert * p.expert_q + (int64_t)(first + b < all ? first + b : all - 1) * blocks * BLOCK; // (past the last: the last again, dropped)
-        auto fetch_from = [&](int y, Block (&blk)[NB]) { // (past the last: the last again, not used)
-            const int64_t off = (int64_t)(y < blocks ? y : blocks - 1) * BLOCK;
-#pragma unroll
-            for (int b = 0; b < NB; ++b) fetch(q[b] + off, blk[b]);
-        };
-        f32x4 acc[NB][MT];
-#pragma unroll
-        for (int b = 0; b < NB; ++b)
-#pragma unroll
-            for (int i = 0; i < MT; ++i) acc[b][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int i = 0; i < MT; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
         if (blocks) {
-            Block now[D][NB], next[D][NB];
+            Block now[D], next[D];
             int y = wk;
 #pragma unroll
             for (int d = 0; d < D; ++d) fetch_from(y + d * WK, next[d]);
@@ -200,9 +186,7 @@ template <class T, int G, int MT, int NB, int WN, int WK, int D, int XB> struct 
                 __syncthreads();
                 for (; y < end; y += WK * D) {
 #pragma unroll
-                    for (int d = 0; d < D; ++d)
-#pragma unroll
-                        for (int b = 0; b < NB; ++b) now[d][b] = next[d][b];
+                    for (int d = 0; d < D; ++d) now[d] = next[d];
                     if (y + WK * D < blocks)
 #pragma unroll
                         for (int d = 0; d < D; ++d) fetch_from(y + (D + d) * WK, next[d]);
@@ -214,13 +198,11 @@ template <class T, int G, int MT, int NB, int WN, int WK, int D, int XB> struct 
             __syncthreads(); // the sums take the place of X
         }
         // lane: column lane % 16 of rows 4 (lane / 16) .. + 3
-        LCMA_LDS float *mine = (LCMA_LDS float *)lds + wk * (TM * PITCH) + (lane >> 4) * 4 * PITCH + wn * NB * 16 + (lane & 15);
+        LCMA_LDS float *mine = (LCMA_LDS float *)lds + wk * (TM * PITCH) + (lane >> 4) * 4 * PITCH + wn * 16 + (lane & 15);
 #pragma unroll
-        for (int b = 0; b < NB; ++b)
+        for (int i = 0; i < MT; ++i)
 #pragma unroll
-            for (int i = 0; i < MT; ++i)
-#pragma unroll
-                for (int v = 0; v < 4; ++v) mine[(i * 16 + v) * PITCH + b * 16] = acc[b][i][v];
+            for (int v = 0; v < 4; ++v) mine[(i * 16 + v) * PITCH] = acc[i][v];
         __syncthreads();
         for (int t = threadIdx.x; t < TM * TN / 4; t += NT) { // four neighbouring columns of a row; the waves along K in ascending order
             const int row = t / (TN / 4), n = t % (TN / 4) * 4, col = z * TN + n;
