@@ -190,8 +190,10 @@ extern "C" lcma_status lcma_gemm_experts_grad(int64_t rows, int64_t N, int64_t K
     if (kernel < 0) return fail(LCMA_ERR_SHAPE, "%s: 2^31 tiles or more", who);
     p.nx = (int32_t)tiles(N, kTile[kernel][0]);
     p.nz = (int32_t)tiles(K, kTile[kernel][1]);
-    // (the kernels deal out eighths of an expert's tiles, exp_gradient_tile)
-    if (const int err = launch(p, kGrad, kernel, dtype, gradient_tiles(kernel, N, K, experts), ((int64_t)p.nx * p.nz + 7) / 8 * 8, stream))
+    // (how the kernels deal out tiles, and what it measured: exp_gradient_tile)
+    const int64_t of = (int64_t)p.nx * p.nz, all = gradient_tiles(kernel, N, K, experts), few = p.nx < p.nz ? p.nx : p.nz, many = p.nx < p.nz ? p.nz : p.nx;
+    p.by_expert = es == 2 && (kernel == kExpRing64 || kernel == kExpRing64x128) && of < 64 && few >= 3 && many <= 4 * few;
+    if (const int err = launch(p, kGrad, kernel, dtype, all, ((p.by_expert ? all : of) + 7) / 8 * 8, stream))
         return fail(LCMA_ERR_HIP, "%s: launch failed with HIP error %d", who, err);
     return LCMA_OK;
 }

@@ -46,12 +46,15 @@ template <class T, int TM, int TN> LCMA_DEV ExpJob gradient_job(const ExpertsGem
     return j;
 }
 
-// Tiles of the gradient to work-groups, one each: eighths of an expert's tiles to the XCDs in turn (work-groups go to the eight in turn), so that each of them has a share of every
-// expert: an expert's tiles take as long as it has rows, and an XCD that had whole experts would be done long before another (fp32, 2331 rows spread
-// unequally over 12 experts, 1001 x 515: 41 us so, 37 now).  -1: none.  The launch holds whole eights of such eighths.
+// Tiles of the gradient to work-groups, one each (work-groups go to the eight XCDs in turn); -1: none.  An expert's tiles take as long as it has rows, so an XCD that had whole experts would
+// be done long before another: eighths of each expert's tiles to every XCD, in turn (the launch holds whole eights of them).  fp32, 2331 rows spread unequally over 12 experts, 1001 x 515: 41 us by experts, 37 by
+// eighths; 120 narrow matrices with a router's counts 16 % less by eighths on average.
+// But then an expert's rows, which one L2 would hold, go to eight.  `by_expert` (16 bit, matrices of a few tiles along both sides, where every eighth reads most of the rows): by experts, one behind the other.  bf16, 42342 rows
+// over 8, 304 x 1104: 100.7 us by eighths, 70.3 by experts, 39392 rows in equal shares, 384 x 1152: 88.6 and 46.3; 59 such matrices with a router's counts 13 % less on average by experts and 1.2 times at worst (15574 x 4 of 8, 752 x 320: 97.8 and 117), in equal shares
+// 27 % less.  Where it is left at eighths, 16 bit: 1 to 5 % less by eighths with a router's counts (0.55 to 1.3 times), 5 to 15 % more in equal shares.
 LCMA_DEV int exp_gradient_tile(const ExpertsGemmParams &p) {
-    const int of = p.nx * p.nz, q = (of + 7) >> 3, i = p.from + (int)(blockIdx.x >> 3), job = (i / q * 8 + (int)(blockIdx.x & 7)) * q + i % q;
-    return job < p.experts * of ? job : -1;
+    const int of = p.nx * p.nz, jobs = p.experts * of, q = p.by_expert ? (jobs + 7) >> 3 : (of + 7) >> 3, i = p.from + (int)(blockIdx.x >> 3), job = (i / q * 8 + (int)(blockIdx.x & 7)) * q + i % q;
+    return job < jobs ? job : -1;
 }
 
 // Where 16-byte chunk c of a row lies in LDS.  k-contiguous rows of 128 bytes: 16 rows at one chunk column meet all banks once.  Rows of columns, 16 bit: the four

@@ -80,6 +80,7 @@ struct ExpertsGemmParams {
     int32_t rows, M, N, K, experts; // M: rows of an expert's C (gradient); K: what a product sums over
     int32_t nx, nz, panel;          // tiles along M (gradient) and N; width of a column panel of the tile order (product)
     int32_t stream, lines;          // the gradient passes the caches by; the 256 x 256 tiles' waves write whole lines of it
+    int32_t by_expert;              // the gradient's tiles are dealt to the XCDs by experts, not by eighths of each
     int32_t from;                   // kernels with a work-group for each tile: the launch's first tile of each eighth of them
 };
 
