@@ -499,7 +499,7 @@ lcma_status lcma_gemm_experts_grad(int64_t rows, int64_t N, int64_t K, int exper
 /* The gate between an experts' layer's products, and its gradient.  A row of X is 2 F long, gates and then the linear part:
  *   lcma_gated_silu       Y[f] = silu(X[f]) * X[F + f],  silu(g) = g s(g),  s(g) = 1 / (1 + exp(-g))
  *   lcma_gated_silu_grad  dX[f] = dY[f] * X[F + f] * s(g) (1 + g (1 - s(g))),  dX[F + f] = dY[f] * silu(g),  g = X[f]
- * All in fp32 (gates below -174 may give zero, an infinite one NaN), one rounding.  F32, BF16 and F16, alignment of an element, F below 2^26, rows below 2^31, leading
+ * All in fp32 (gates below -174 may give zero, an infinite one NaN; a dX[f] whose dY[f] * X[F + f] is beyond fp32 may be infinite), one rounding.  F32, BF16 and F16, alignment of an element, F below 2^26, rows below 2^31, leading
  * dimensions that hold a row, below 2^29 (SHAPE).  Outputs must not overlap inputs (ARG). */
 lcma_status lcma_gated_silu(int64_t rows, int64_t F, const void *X, int64_t ldx, void *Y, int64_t ldy, lcma_dtype dtype, void *stream);
 lcma_status lcma_gated_silu_grad(int64_t rows, int64_t F, const void *dY, int64_t lddy, const void *X, int64_t ldx, void *dX, int64_t lddx, lcma_dtype dtype,
@@ -518,7 +518,8 @@ lcma_status lcma_gated_silu_grad(int64_t rows, int64_t F, const void *dY, int64_
  *   lcma_i4_prepare    from codes (int8, experts x N x K, -8 .. 7; others count as the nearest of these) and scales (fp32, experts x N x ceil(K / group))
  * Any sizes: N and K below 2^29, N * K (N * ldw) up to 2^44, rows below 2^31 (SHAPE), alignment of an element; leading dimensions that hold a row, below 2^29 (SHAPE).  bias (fp32, N, or experts x N) may be null.
  * K = 0: C = bias, or zeros.  Outputs must not overlap inputs (ARG).  Calls run on `stream`, allocate nothing and do not synchronise.
- *   lcma_i4_gemm_nt       any number of rows M: up to a few hundred the weights' bytes decide, for long prompts lcma_gemm_nt with 16-bit weights is faster
+ *   lcma_i4_gemm_nt       any number of rows M; made for the few rows of single tokens, up to about 16 of which the weights' bytes decide.  lcma_gemm_nt with bf16 weights, where a program keeps those too, is as
+ *                         fast at 40 to 60 rows and faster from there on (14336 x 4096, groups of 128, against bf16: 1 row 9.4 us and 25, 32 rows 22 and 27, 64 rows 34 and 29, 256 rows 97 and 45, 2048 rows 810 and 187)
  *   lcma_i4_gemm_experts  rows offsets[e] .. offsets[e + 1] - 1 of X times the weights of expert e, as lcma_i8_gemm_experts; rows of C from offsets[experts] on are set to zero
  */
 int64_t lcma_i4_prepared_bytes(int64_t N, int64_t K, int group);

@@ -45,6 +45,7 @@ bool whole_vectors(int es, const void *A, int64_t lda_b, const void *B, int64_t 
 // are no whole lines of 128 bytes a step takes `off` of its time more and the bytes half of that.  start 0: not taken.  Fitted to 164 layers in 16 bit, 94 in fp32 and 130 of sizes
 // that are no whole 16 bytes, of 1 to 8192 tokens and 8 to 128 experts, timed on every kernel: a single time is predicted within 10 to 31 % (root mean square); the kernel with the smallest
 // prediction is 1.2 to 2.4 % slower than the fastest one on average in whole 16 bytes (31 % at worst, of the gradient 65 %), 0.2 to 0.6 % in fp32 (18 %), 1.5 to 3 % in other sizes (52 %, one gradient 2.2 times).
+// (The fp32 gradient's 64 x 64 came out as a line through the number of tiles, `slots` and `step` near nothing: it tells large ones apart, and nothing of less than a round of tiles.)
 struct Cost {
     double start, end, step, rate, slots, off;
 };
@@ -182,7 +183,7 @@ extern "C" lcma_status lcma_gemm_experts_grad(int64_t rows, int64_t N, int64_t K
     p.N = (int32_t)K;
     p.experts = experts;
     p.panel = 8;
-    p.stream = !(((uintptr_t)dW | (uint64_t)p.ldc_b) & 127); // (rows of whole lines: every store writes some; parts of them to memory cost up to twice the time instead)
+    p.stream = !(((uintptr_t)dW | (uint64_t)p.ldc_b) & 127); // (rows of whole lines, which a wave's store, or two waves' at the same time, fill; lines filled part by part cost up to twice the time instead)
     p.lines = rows <= (int64_t)512 * experts; // (512 rows an expert: 88 -> 82 us at 2048 x 4096, 1024: 141 -> 145)
     const bool short_rows = p.lda_b <= kShortRow && p.ldb_b <= kShortRow, vectors = short_rows && whole_vectors(es, dC, p.lda_b, A, p.ldb_b, 0);
     int kernel = tuning_experts_kernel();

@@ -141,8 +141,9 @@ template <class T, bool COL, int R> LCMA_DEV void exp_fragments(const LCMA_LDS c
 // A wave's part of a tile of C (NMI x NNI blocks of 32 x 32; rows, cols: of C from its first element on) rounded and stored: through SR rows of 128 bytes of LDS that are the
 // wave's own, so that it leaves as whole lines, 16 bytes a lane.  The right operand is the left one of the matrix instruction: a lane holds four neighbouring columns.
 // Blocks of rows follow each other, or, TWO, the second pair of them is 128 rows on; the blocks of columns are GAP columns apart.
-// FULL: all of it lies inside C.  STREAM: and passes the caches by, in whole lines (64 x 128 tiles, gradient of 1021 x 6 of 64, 2816 x 2048: 355 -> 292 us;
-// half lines a store were 340 -> 540 at 2 rows of 8 experts, 28672 x 4096).
+// FULL: all of it lies inside C.  STREAM: and passes the caches by, in rows that are whole lines in memory (64 x 128 tiles, gradient of 1021 x 6 of 64, 2816 x 2048: 355 -> 292 us).  A wave's store is whole
+// lines of it, or, with one block of columns in 16 bit (64 x 64 tiles), halves that the wave beside it completes at about the same time: through the caches these took 1.07 times as long on average over 57 gradients
+// (1.33 at most, 0.98 at least), off 16 bytes 1.04 (1.2, 0.99).  Halves that nothing completes soon (256 x 256 tiles whose waves' columns lie apart) were 340 -> 540 past the caches, at 2 rows of 8 experts, 28672 x 4096.
 template <class T, int NMI, int NNI, bool TWO, int GAP, int SR, bool FULL, bool STREAM>
 LCMA_DEV void exp_store_rows(LCMA_LDS char *strip, char *c, int64_t ldc_b, int rows, int cols, const f32x16 (&acc)[NMI][NNI]) {
     constexpr int ES = T::ES, BLOCKS = ES == 4 ? 1 : NNI == 1 ? 1 : 2, L = BLOCKS * 32 * ES / 16, RPS = 64 / L; // 32-column blocks of a pass; lanes of a row, rows of a store

@@ -53,7 +53,7 @@ LCMA_DEV float gated_far(float g, float u) {
     return g * s * p.r * u * s;
 }
 // dy times d silu(g) u / d g = s (1 + g (1 - s)) u and times d / d u = s g, s = 1 / (1 + exp(-g)).  Below zero one h is multiplied in first and one last, so that
-// no factor leaves fp32 before the value does.
+// no factor is lost below fp32 before the value is.  (Above it: where dy u itself is beyond fp32 a product on the way may be, and the result an infinity, whatever the value.)
 LCMA_DEV void gated_back(float g, float u, float dy, float &dg, float &du) {
 #pragma clang fp contract(off)
     const GateParts p = gate_parts(g);

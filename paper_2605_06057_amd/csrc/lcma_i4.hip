@@ -7,7 +7,8 @@ using namespace lcma;
 namespace {
 
 // A work-group: the blocks of 16 rows; a wave: a block in turn.  Lane: row lane % 16 and, of every 32 columns, the eight from 8 (lane / 16) on.  Codes from their values: rint(x / S),
-// S = max |x| / 7 of the group, in fp32, held to -7 .. 7; a group whose S is zero, infinite or NaN has codes of zero.  Runs once for a matrix of weights: bound by nothing that matters.
+// S = max |x| / 7 of the group, in fp32, held to -7 .. 7; a group whose S is zero, infinite or NaN has codes of zero.  Runs once for a matrix of weights, and is plain: values come 16 bytes a load,
+// codes one by one.  Groups of 128, 14336 x 4096: 53 us from bf16 values (2.8 TB/s), 118 from codes (0.8); eight experts of 28672 x 4096: 625 (3.8 TB/s) and 1754 (0.84), as long as 20 single tokens' products with them.
 template <class T, bool CODES> __global__ __launch_bounds__(256) void i4_prepare(const I4PrepareParams p) {
 #pragma clang fp contract(off)
     const int lane = threadIdx.x & 63, groups = 128 / p.group, blocks = (p.K + 127) / 128, per_row = (p.K + p.group - 1) / p.group;
